@@ -11,7 +11,8 @@
  *      (the "suffix"), and
  *   2. temperature sampling of the next token from the logits.
  *
- * This library provides exactly those two operations.  The attention is computed
+ * This library provides those two operations, and what stands before them: page tables, the prompts'
+ * own attention and KV writes, penalties on the logits.  The decode attention is computed
  * as a cascade: one pass treats all samples' queries of a KV head as a dense tile
  * against the shared prefix (so the prefix is read once, not once per sample), a
  * second pass streams each sample's private suffix, and the two partial softmax
@@ -373,6 +374,165 @@ SPD_API int decode_step_advance(int64_t *step_state, int64_t num_steps,
                         const int32_t *last_tokens, int32_t end_token, int32_t *finished,
                         int32_t *lens_record,
                         void *stream);
+
+/* ---- from a request to its first token ----------------------------------------------------------
+ *
+ * Before samples can be decoded from a prompt (Alg. 1, "parallel sampling"; Sec. "Adaptive
+ * self-improvement learning": base prompt, demonstrations and task text in front of every sample), the
+ * prompt's own tokens have to be in the KV cache and attended to.  build_page_tables deals pages to
+ * requests, write_prompt_kv stores the new tokens' keys and values in them, prompt_attn is the
+ * attention of the new tokens over the cache.  What each writes is what the next reads:
+ * new_indptr is prompt_attn's query_indptr, lens_out its kv_lens, page_indptr / page_indices its KV table
+ * (and prefix_lens, prefix_indptr, prefix_page_indices of the decode call); slot_map is write_prompt_kv's.
+ */
+
+/*
+ * Description of a batch of prompts (host memory, read during the call only).  Query head h reads KV
+ * head h / (num_q_heads / num_kv_heads).  Supported: dtype bf16 or f32, head_dim a multiple of 8 up to
+ * 256, page_size 0 (contiguous KV) or 16.  Strides are in elements and a multiple of 16 bytes.
+ */
+typedef struct spd_prompt_desc {
+    int32_t dtype;        /* spd_dtype of q, k, v and the output */
+    int32_t num_q_heads;  /* Hq (write_prompt_kv ignores it) */
+    int32_t num_kv_heads; /* Hkv, divides Hq */
+    int32_t head_dim;     /* D */
+    int32_t num_prompts;  /* B >= 1 */
+    int32_t page_size;    /* 0 = contiguous KV, 16 = paged */
+    int32_t causal;       /* nonzero: a token sees itself and what stands before it; 0: the whole prompt */
+    float sm_scale;       /* score scale; <= 0 selects 1/sqrt(D) */
+    int64_t q_stride;     /* between consecutive tokens of q; 0 = Hq * D */
+    int64_t kv_stride;    /* between consecutive tokens of contiguous k and v; 0 = Hkv * D */
+} spd_prompt_desc;
+
+/* Bytes of workspace prompt_attn needs for these bounds (0 on an invalid desc). */
+SPD_API size_t prompt_attn_workspace_size(const spd_prompt_desc *desc, int64_t total_queries,
+                                          int64_t max_query_len, int64_t max_kv_len);
+
+/*
+ * Attention of a batch of prompts' new tokens.  Prompt b has kv_lens[b] tokens of KV, of which the
+ * last n_b = query_indptr[b+1] - query_indptr[b] are the new ones with a query each: query i of prompt b
+ * stands at position kv_lens[b] - n_b + i, and
+ *   out = softmax(q K^T * scale) V over the tokens up to and including its position (causal), or over
+ * all kv_lens[b] tokens.  A query that sees no token (n_b > kv_lens[b]) gets zeros, and -inf as its
+ * log-sum-exp.  Nothing that a query does not see, whatever its value, enters its result.
+ *
+ *   q              [total_queries, Hq, D], tokens q_stride apart; prompt b's start at query_indptr[b]
+ *   contiguous KV  k, v [tokens, Hkv, D], tokens kv_stride apart; prompt b's start at kv_indptr[b]
+ *   paged KV       k, v [num_pages, Hkv, 16, D]; prompt b's pages are
+ *                  kv_page_indices[kv_indptr[b] .. kv_indptr[b+1]) (prompts may share pages)
+ *   query_indptr, kv_indptr  int32 [B+1]; kv_lens int32 [B]
+ *   total_queries  rows of q, out and lse_out (>= query_indptr[B]; rows past it are not written)
+ *   max_query_len / max_kv_len  host-known upper bounds on n_b and kv_lens[b] that size the launch
+ *   out            [total_queries, Hq, D], desc->dtype
+ *   lse_out        float [total_queries, Hq], natural log, or NULL
+ *
+ * total_queries 0 is a call that does nothing.  Data pointers 16-byte aligned.  Returns spd_status.
+ */
+SPD_API int prompt_attn(const spd_prompt_desc *desc, const void *q, const void *k, const void *v,
+                        const int32_t *query_indptr, const int32_t *kv_lens,
+                        const int32_t *kv_indptr, const int32_t *kv_page_indices,
+                        int64_t total_queries, int64_t max_query_len, int64_t max_kv_len,
+                        void *out, float *lse_out,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of workspace build_page_tables needs (0 on an invalid count). */
+SPD_API size_t build_page_tables_workspace_size(int64_t num_requests);
+
+/*
+ * Page tables of requests that have to hold lens[i] tokens, on the device.  Request i holds
+ * held_lens[i] tokens already, in the pages held_pages[held_indptr[i] .. held_indptr[i+1]); the pages it
+ * lacks are dealt from free_pages[begin ..num_free) in order of the requests, begin = *free_begin (0 where
+ * free_begin is NULL).  A request whose pages no longer fit gets none, nor does any later one that
+ * needs some; a refused request keeps what it holds and lens_out[i] = held_lens[i].  Otherwise
+ * lens_out[i] = max(lens[i], held_lens[i]) (negative lens count as 0).
+ *
+ *   held_lens, held_indptr, held_pages  all NULL: nobody holds anything
+ *   page_indptr    int32 [num_requests+1], page_indices int32 [max_pages]: the tables (a request's held
+ *                  pages first); entries past the last are -1.  Entries beyond max_pages are not written.
+ *   new_indptr     int32 [num_requests+1]: running count of new tokens, lens_out[i] - held_lens[i] each
+ *   slot_map       int64 [max_tokens] or NULL: page * page_size + place in the page of every new token in
+ *                  order; entries past the last are -1.  Entries beyond max_tokens are not written.
+ *   free_end       int32 [1]: index of the first page of free_pages not dealt; may be the next call's
+ *                  free_begin, not this one's
+ *   page_size      1 .. 65536
+ *
+ * Outputs must not overlap inputs.  Returns spd_status.
+ */
+SPD_API int build_page_tables(int64_t num_requests, int32_t page_size, const int32_t *lens,
+                              const int32_t *held_lens, const int32_t *held_indptr,
+                              const int32_t *held_pages, const int32_t *free_pages,
+                              int64_t num_free, const int32_t *free_begin,
+                              int64_t max_pages, int64_t max_tokens,
+                              int32_t *page_indptr, int32_t *page_indices, int32_t *lens_out,
+                              int32_t *new_indptr, int64_t *slot_map, int32_t *free_end,
+                              void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Stores num_tokens rows of keys and values in the cache: token t goes to slot slot_map[t] (device,
+ * int64).  Slots outside the pool are skipped; two tokens of one slot leave either's row.
+ *   k, v            [num_tokens, Hkv, D], tokens desc->kv_stride apart
+ *   k_pool, v_pool  page_size 16: [num_pages, Hkv, 16, D]; page_size 0: [num_pages, Hkv, D], a slot each
+ * desc: dtype, num_kv_heads, head_dim, page_size, kv_stride.  Pointers 16-byte aligned.
+ * num_tokens 0 is a call that does nothing.  Returns spd_status.
+ */
+SPD_API int write_prompt_kv(const spd_prompt_desc *desc, const void *k, const void *v,
+                            const int64_t *slot_map, int64_t num_tokens, int64_t num_pages,
+                            void *k_pool, void *v_pool, void *stream);
+
+/* ---- between the logits and the sampler ----------------------------------------------------------- */
+
+/*
+ * Which tokens of the vocabulary occur in each prompt: bit i % 32 of word i / 32 of row b is set where
+ * token i is among tokens[indptr[b] .. indptr[b+1]) (ids outside 0 .. vocab - 1 are ignored).
+ *   bits    uint32 [num_prompts, >= ceil(vocab / 32)], rows bits_stride words apart
+ *   accumulate  nonzero: bits that are set stay set; 0: the rows' ceil(vocab / 32) words are written whole
+ * vocab up to 1048576.  Returns spd_status.
+ */
+SPD_API int mark_prompt_tokens(const int32_t *tokens, const int32_t *indptr, int64_t num_prompts,
+                               int64_t vocab, uint32_t *bits, int64_t bits_stride,
+                               int32_t accumulate, void *stream);
+
+/*
+ * What shapes the logits of a row r (host memory, read during the call; all pointers device pointers).
+ * Every part may be left out (NULL).
+ */
+typedef struct spd_penalties {
+    const float *repetition;       /* [rows], > 0; NULL = 1 */
+    const float *frequency;        /* [rows]; NULL = 0 */
+    const float *presence;         /* [rows]; NULL = 0 */
+    const uint32_t *prompt_bits;   /* which tokens occur in the prompts (mark_prompt_tokens) */
+    int64_t prompt_bits_stride;    /* words between its rows */
+    const int32_t *prompt_of_row;  /* [rows]: row of prompt_bits; negative: none; NULL: row r reads row r */
+    const int32_t *tokens;         /* generated tokens: token t of row r at tokens[r * token_row_stride + t * token_step_stride] */
+    int64_t token_row_stride, token_step_stride;
+    const int32_t *token_lens;     /* [rows]: how many of them (needed with tokens) */
+    int64_t max_tokens;            /* host-known upper bound on token_lens */
+    const int32_t *bias_indptr;    /* [rows+1] (needed with bias_tokens) */
+    const int32_t *bias_tokens;    /* tokens bias_tokens[bias_indptr[r] ..  bias_indptr[r+1]), different ones */
+    const float *bias_values;
+    const uint32_t *allowed_bits;  /* grammar states: bit set = token allowed */
+    int64_t allowed_stride;        /* words between its rows */
+    const int32_t *allowed_of_row; /* [rows]: row of allowed_bits; negative: all allowed; NULL: row r reads row r */
+} spd_penalties;
+
+/*
+ * The logits a sampler gets, with c the number of times token i occurs among the row's generated tokens
+ * and seen = c > 0 or i occurs in the row's prompt:
+ *   x1 = seen ? (x > 0 ? x / repetition : x * repetition) : x
+ *   x2 = x1 - frequency * c - presence * (c > 0)
+ *   x3 = x2 + bias of i
+ *   out = allowed ? x3 : -inf
+ * in fp32.  Token ids outside 0 .. vocab - 1 are ignored.  A token listed twice among a row's biases gets
+ * one of the two.
+ *   logits     [rows, vocab] fp32 or bf16 (logits_dtype), rows row_stride elements apart
+ *   out        float [rows, vocab], rows out_stride apart; may be logits itself (fp32, equal strides), else
+ *              must not overlap it
+ *   penalties  max_tokens up to 2^24; vocab up to 2^30
+ * rows 0 is a call that does nothing.  Returns spd_status.
+ */
+SPD_API int penalize_logits(const void *logits, int32_t logits_dtype, int64_t rows, int64_t vocab,
+                            int64_t row_stride, const spd_penalties *penalties,
+                            float *out, int64_t out_stride, void *stream);
 
 /* Short description of a status code (static storage). */
 SPD_API const char *spd_status_string(int status);

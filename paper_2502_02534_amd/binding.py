@@ -48,6 +48,23 @@ class RowCopy(ctypes.Structure):
     _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("row_bytes", ctypes.c_int64)]
 
 
+class PromptDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("num_prompts", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("sm_scale", ctypes.c_float), ("q_stride", ctypes.c_int64),
+                ("kv_stride", ctypes.c_int64)]
+
+
+class Penalties(ctypes.Structure):
+    _fields_ = [("repetition", ctypes.c_void_p), ("frequency", ctypes.c_void_p), ("presence", ctypes.c_void_p),
+                ("prompt_bits", ctypes.c_void_p), ("prompt_bits_stride", ctypes.c_int64),
+                ("prompt_of_row", ctypes.c_void_p), ("tokens", ctypes.c_void_p), ("token_row_stride", ctypes.c_int64),
+                ("token_step_stride", ctypes.c_int64), ("token_lens", ctypes.c_void_p), ("max_tokens", ctypes.c_int64),
+                ("bias_indptr", ctypes.c_void_p), ("bias_tokens", ctypes.c_void_p), ("bias_values", ctypes.c_void_p),
+                ("allowed_bits", ctypes.c_void_p), ("allowed_stride", ctypes.c_int64),
+                ("allowed_of_row", ctypes.c_void_p)]
+
+
 def load() -> ctypes.CDLL:
     """Load the HIP library.  Raises if it has not been built."""
     global _lib
@@ -89,6 +106,21 @@ def load() -> ctypes.CDLL:
     lib.decode_step_advance.argtypes = ([vp, i64, ctypes.c_int32, ctypes.POINTER(RowCopy), ctypes.c_int32,
                                          ctypes.POINTER(RowCopy), dp] + [vp] * 7 +
                                         [i64, vp, ctypes.c_int32, vp, vp, vp])
+    pp = ctypes.POINTER(PromptDesc)
+    lib.prompt_attn_workspace_size.restype = sz
+    lib.prompt_attn_workspace_size.argtypes = [pp, i64, i64, i64]
+    lib.prompt_attn.restype = ctypes.c_int
+    lib.prompt_attn.argtypes = [pp] + [vp] * 7 + [i64, i64, i64, vp, vp, vp, sz, vp]
+    lib.build_page_tables_workspace_size.restype = sz
+    lib.build_page_tables_workspace_size.argtypes = [i64]
+    lib.build_page_tables.restype = ctypes.c_int
+    lib.build_page_tables.argtypes = ([i64, ctypes.c_int32] + [vp] * 5 + [i64, vp, i64, i64] + [vp] * 7 + [sz, vp])
+    lib.write_prompt_kv.restype = ctypes.c_int
+    lib.write_prompt_kv.argtypes = [pp, vp, vp, vp, i64, i64, vp, vp, vp]
+    lib.mark_prompt_tokens.restype = ctypes.c_int
+    lib.mark_prompt_tokens.argtypes = [vp, vp, i64, i64, vp, i64, ctypes.c_int32, vp]
+    lib.penalize_logits.restype = ctypes.c_int
+    lib.penalize_logits.argtypes = [vp, ctypes.c_int32, i64, i64, i64, ctypes.POINTER(Penalties), vp, i64, vp]
     _lib = lib
     return lib
 
@@ -252,3 +284,77 @@ def sample_tokens_filtered(logits, logits_dtype: int, rows: int, vocab: int, row
         _bytes(workspace), _stream(stream))
     if rc != SPD_OK:
         raise SpdError(rc, "sample_tokens_filtered")
+
+
+def make_prompt_desc(*, dtype: int, num_q_heads: int, num_kv_heads: int, head_dim: int, num_prompts: int,
+                     page_size: int = 0, causal: bool = True, sm_scale: float = 0.0, q_stride: int = 0,
+                     kv_stride: int = 0) -> PromptDesc:
+    return PromptDesc(dtype, num_q_heads, num_kv_heads, head_dim, num_prompts, page_size, 1 if causal else 0, sm_scale,
+                      q_stride, kv_stride)
+
+
+def prompt_attn_workspace_size(desc: PromptDesc, total_queries: int, max_query_len: int, max_kv_len: int) -> int:
+    return int(load().prompt_attn_workspace_size(ctypes.byref(desc), int(total_queries), int(max_query_len),
+                                                 int(max_kv_len)))
+
+
+def prompt_attn(desc: PromptDesc, q, k, v, query_indptr, kv_lens, kv_indptr, kv_page_indices, total_queries: int,
+                max_query_len: int, max_kv_len: int, out, lse_out, workspace, stream=None) -> None:
+    rc = load().prompt_attn(
+        ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(query_indptr), _ptr(kv_lens), _ptr(kv_indptr),
+        _ptr(kv_page_indices), int(total_queries), int(max_query_len), int(max_kv_len), _ptr(out), _ptr(lse_out),
+        _ptr(workspace), _bytes(workspace), _stream(stream))
+    if rc != SPD_OK:
+        raise SpdError(rc, "prompt_attn")
+
+
+def build_page_tables_workspace_size(num_requests: int) -> int:
+    return int(load().build_page_tables_workspace_size(int(num_requests)))
+
+
+def build_page_tables(num_requests: int, page_size: int, lens, held_lens, held_indptr, held_pages, free_pages,
+                      num_free: int, free_begin, max_pages: int, max_tokens: int, page_indptr, page_indices, lens_out,
+                      new_indptr, slot_map, free_end, workspace, stream=None) -> None:
+    rc = load().build_page_tables(
+        int(num_requests), int(page_size), _ptr(lens), _ptr(held_lens), _ptr(held_indptr), _ptr(held_pages),
+        _ptr(free_pages), int(num_free), _ptr(free_begin), int(max_pages), int(max_tokens), _ptr(page_indptr),
+        _ptr(page_indices), _ptr(lens_out), _ptr(new_indptr), _ptr(slot_map), _ptr(free_end), _ptr(workspace),
+        _bytes(workspace), _stream(stream))
+    if rc != SPD_OK:
+        raise SpdError(rc, "build_page_tables")
+
+
+def write_prompt_kv(desc: PromptDesc, k, v, slot_map, num_tokens: int, num_pages: int, k_pool, v_pool,
+                    stream=None) -> None:
+    rc = load().write_prompt_kv(ctypes.byref(desc), _ptr(k), _ptr(v), _ptr(slot_map), int(num_tokens), int(num_pages),
+                                _ptr(k_pool), _ptr(v_pool), _stream(stream))
+    if rc != SPD_OK:
+        raise SpdError(rc, "write_prompt_kv")
+
+
+def mark_prompt_tokens(tokens, indptr, num_prompts: int, vocab: int, bits, bits_stride: int, accumulate: bool = False,
+                       stream=None) -> None:
+    rc = load().mark_prompt_tokens(_ptr(tokens), _ptr(indptr), int(num_prompts), int(vocab), _ptr(bits),
+                                   int(bits_stride), 1 if accumulate else 0, _stream(stream))
+    if rc != SPD_OK:
+        raise SpdError(rc, "mark_prompt_tokens")
+
+
+def make_penalties(*, repetition=None, frequency=None, presence=None, prompt_bits=None, prompt_of_row=None,
+                   tokens=None, token_lens=None, bias_indptr=None, bias_tokens=None, bias_values=None,
+                   allowed_bits=None, allowed_of_row=None) -> Penalties:
+    """Penalties from tensors, strides included: `tokens` is [rows, steps] with any strides (a loop's
+    [steps, rows] record is passed as its transposed view).  The tensors have to outlive the record."""
+    row = lambda t: 0 if t is None else t.stride(0)
+    return Penalties(_ptr(repetition), _ptr(frequency), _ptr(presence), _ptr(prompt_bits), row(prompt_bits),
+                     _ptr(prompt_of_row), _ptr(tokens), row(tokens), 0 if tokens is None else tokens.stride(1),
+                     _ptr(token_lens), 0 if tokens is None else tokens.shape[1], _ptr(bias_indptr), _ptr(bias_tokens),
+                     _ptr(bias_values), _ptr(allowed_bits), row(allowed_bits), _ptr(allowed_of_row))
+
+
+def penalize_logits(logits, logits_dtype: int, rows: int, vocab: int, row_stride: int, penalties: Penalties, out,
+                    out_stride: int, stream=None) -> None:
+    rc = load().penalize_logits(_ptr(logits), int(logits_dtype), int(rows), int(vocab), int(row_stride),
+                                ctypes.byref(penalties), _ptr(out), int(out_stride), _stream(stream))
+    if rc != SPD_OK:
+        raise SpdError(rc, "penalize_logits")

@@ -1,0 +1,78 @@
+// Launch planning of prompt_attn: host arithmetic only (no HIP, no allocation), so that it can also be
+// compiled and exercised on a machine without a GPU.
+#pragma once
+
+#include "../../include/spdecode.h"
+
+#include <stddef.h>
+#include <stdint.h>
+
+namespace spd {
+namespace plan {
+
+struct PromptPlan {
+    int tiles;       // upper bound on the row tiles of all prompts, one KV head
+    int num_splits;  // parts of a tile's tokens
+    size_t acc_bytes, ml_bytes;
+};
+
+constexpr int kPromptRows = 128;       // (token, head of the group) rows per workgroup
+constexpr int kPromptMaxSplits = 32;
+constexpr int kPromptMinTokens = 128;  // per split
+
+inline int check_prompt_desc(const spd_prompt_desc* d, bool queries)
+{
+    if (!d || d->num_kv_heads <= 0 || d->head_dim <= 0 || d->num_prompts <= 0 || d->q_stride < 0 || d->kv_stride < 0)
+        return SPD_EINVAL;
+    if (queries && (d->num_q_heads <= 0 || d->num_q_heads % d->num_kv_heads != 0))
+        return SPD_EINVAL;
+    if (d->dtype != SPD_F32 && d->dtype != SPD_BF16)
+        return SPD_EUNSUPPORTED;
+    if (d->page_size != 0 && d->page_size != 16)
+        return SPD_EUNSUPPORTED;
+    if (d->head_dim > 256 || d->head_dim % 8 != 0 || d->num_kv_heads > 65536 || d->num_q_heads > 65536)
+        return SPD_EUNSUPPORTED;
+    const int per_piece = d->dtype == SPD_BF16 ? 8 : 4;  // elements of 16 bytes
+    if (d->q_stride % per_piece != 0 || d->kv_stride % per_piece != 0)
+        return SPD_EINVAL;
+    if ((queries && d->q_stride != 0 && d->q_stride < (int64_t)d->num_q_heads * d->head_dim) ||
+        (d->kv_stride != 0 && d->kv_stride < (int64_t)d->num_kv_heads * d->head_dim))
+        return SPD_EINVAL;
+    return SPD_OK;
+}
+
+inline int make_prompt_plan(const spd_prompt_desc* d, int64_t total, int64_t max_query, int64_t max_kv, PromptPlan* out)
+{
+    const int rc = check_prompt_desc(d, true);
+    if (rc != SPD_OK)
+        return rc;
+    const int64_t most = 0x7fffffff;
+    if (total < 0 || max_query < 0 || max_kv < 0)
+        return SPD_EINVAL;
+    // row and token numbers are 32-bit; so is the grid
+    if (total > most / d->num_q_heads || max_query > (1ll << 30) || max_kv > (1ll << 30))
+        return SPD_EUNSUPPORTED;
+    const int64_t group = d->num_q_heads / d->num_kv_heads;
+    // a prompt's last tile may be partly filled, and no prompt has more tiles than its longest
+    const int64_t per_prompt = (max_query * group + kPromptRows - 1) / kPromptRows;
+    int64_t tiles = total * group / kPromptRows + d->num_prompts;
+    if (per_prompt < tiles / d->num_prompts + 1 && per_prompt * d->num_prompts < tiles)
+        tiles = per_prompt * d->num_prompts;
+    const int64_t units = tiles * d->num_kv_heads;
+    int64_t splits = units > 0 ? (512 + units - 1) / units : 1;
+    const int64_t whole = max_kv / kPromptMinTokens;
+    splits = splits < whole ? splits : whole;
+    splits = splits < kPromptMaxSplits ? splits : kPromptMaxSplits;
+    splits = splits > 1 ? splits : 1;
+    if (units > most / splits)
+        return SPD_EUNSUPPORTED;
+    out->tiles = (int)tiles;
+    out->num_splits = (int)splits;
+    const size_t states = splits > 1 ? (size_t)total * d->num_q_heads * splits : 0;
+    out->acc_bytes = (states * d->head_dim * sizeof(float) + 255) / 256 * 256;
+    out->ml_bytes = (states * 2 * sizeof(float) + 255) / 256 * 256;
+    return SPD_OK;
+}
+
+}  // namespace plan
+}  // namespace spd

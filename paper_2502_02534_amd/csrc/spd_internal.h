@@ -131,6 +131,80 @@ struct SamplerParams {
     const float* min_p;  // per row, 0 = off; may be null
 };
 
+// A batch of prompts' new tokens over their KV (see prompt_attn.hip).
+struct PromptParams {
+    int dtype, Hq, Hkv, D, G, B, page_size, causal;
+    float scale_log2;  // sm_scale * log2(e)
+    const void* q;
+    const void* k;
+    const void* v;
+    long long q_stride, kv_stride;  // elements between tokens
+    const int* query_indptr;
+    const int* kv_lens;
+    const int* kv_indptr;
+    const int* pages;
+    int tiles;       // upper bound on the row tiles of all prompts
+    int num_splits;  // parts a tile's tokens are cut into
+    long long rows;  // total_queries * Hq
+    float* part_acc;   // [rows][splits][D], unnormalised sums; null with one split
+    float2* part_ml;   // [rows][splits] (m, l)
+    void* out;
+    float* lse;        // may be null
+};
+
+struct PageTableParams {
+    long long n;
+    int page_size;
+    const int* lens;
+    const int* held_lens;  // null: nothing held
+    const int* held_indptr;
+    const int* held_pages;
+    const int* free_pages;
+    long long num_free;
+    const int* free_begin;  // may be null
+    long long max_pages, max_tokens;
+    int* page_indptr;
+    int* page_indices;
+    int* lens_out;
+    int* new_indptr;
+    long long* slot_map;  // may be null
+    int* free_end;
+    int* first_free;  // workspace: [n] index in free_pages of a request's first new page
+};
+
+struct KvWriteParams {
+    const void* k;
+    const void* v;
+    const long long* slots;
+    void* k_pool;
+    void* v_pool;
+    long long tokens, num_slots;
+    long long stride_u4;  // 16-byte pieces between tokens of k and v
+    int Hkv, head_u4;     // pieces of one head's row
+    int page_size;        // 0: slots are rows
+};
+
+struct LogitsParams {
+    const void* logits;
+    int bf16;
+    long long rows, vocab, stride, out_stride;
+    float* out;
+    const float *repetition, *frequency, *presence;
+    const uint32_t* prompt_bits;
+    long long prompt_stride;
+    const int* prompt_of_row;
+    const int* tokens;
+    long long token_row_stride, token_step_stride;
+    const int* token_lens;
+    const int* bias_indptr;
+    const int* bias_tokens;
+    const float* bias_values;
+    const uint32_t* allowed_bits;
+    long long allowed_stride;
+    const int* allowed_of_row;
+    int max_tokens;
+};
+
 // Index of the partial state of output row `row` (= n * Hq + h) in slot `slot`.
 __device__ __forceinline__ long long part_index(const AttnParams& p, long long row, int slot)
 {
@@ -169,6 +243,12 @@ long long step_rows_blocks(long long row_bytes);
 hipError_t launch_step_rows(const StepRowsParams& a, bool record, hipStream_t s);
 hipError_t launch_step_advance(const StepAdvanceParams& a, hipStream_t s);
 size_t sampler_workspace_bytes(long long rows, long long vocab);
+hipError_t launch_prompt_attn(const PromptParams& p, hipStream_t s);
+hipError_t launch_page_tables(const PageTableParams& p, hipStream_t s);
+hipError_t launch_kv_write(const KvWriteParams& p, hipStream_t s);
+hipError_t launch_mark_tokens(const int* tokens, const int* indptr, long long prompts, long long vocab, uint32_t* bits,
+                              long long stride, bool accumulate, hipStream_t s);
+hipError_t launch_penalize_logits(const LogitsParams& p, hipStream_t s);
 hipError_t launch_sampler(const SamplerParams& p, void* workspace, hipStream_t s);
 
 }  // namespace spd
