@@ -66,6 +66,7 @@ int prompt_attn(const spd_prompt_desc* desc, const void* q, const void* k, const
     p.kv_lens = kv_lens;
     p.kv_indptr = kv_indptr;
     p.pages = kv_page_indices;
+    p.block_rows = pl.block_rows;
     p.tiles = pl.tiles;
     p.num_splits = pl.num_splits;
     p.rows = total_queries * p.Hq;

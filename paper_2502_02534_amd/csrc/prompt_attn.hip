@@ -56,7 +56,7 @@ __device__ __forceinline__ TileOf find_tile(const PromptParams& p, int item)
             const int x = __shfl_up(upto, o);
             upto += lane >= o ? x : 0;
         }
-        const int all = __shfl(upto, 63);
+        const int all = __builtin_amdgcn_readfirstlane(__shfl(upto, 63));
         if (item < base + all) {
             const int l = __ffsll((unsigned long long)__ballot(item < base + upto)) - 1;
             const int before = __shfl(upto - n, l), tiles = __shfl(n, l);
@@ -352,7 +352,7 @@ __global__ __launch_bounds__(kThreads) void prompt_attn_kernel(PromptParams p)
             }
         return;
     }
-    const bool none = m == -INFINITY && l == 0.f;
+    const bool none = l == 0.f;
     const float inv = none ? 0.f : 1.f / l;
     if (p.lse && h == 0)
         p.lse[row] = none ? -INFINITY : m * kLn2 + logf(l);
@@ -398,7 +398,7 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptParams p)
         acc.z = fmaf(w, a.z, acc.z);
         acc.w = fmaf(w, a.w, acc.w);
     }
-    const bool none = m == -INFINITY && l == 0.f;
+    const bool none = l == 0.f;
     const float inv = none ? 0.f : 1.f / l;
     if (p.lse && c == 0)
         p.lse[row] = none ? -INFINITY : m * kLn2 + logf(l);
@@ -414,7 +414,9 @@ template <typename T>
 hipError_t launch(const PromptParams& p, hipStream_t s)
 {
     const dim3 grid((unsigned)((long long)p.tiles * p.num_splits * p.Hkv)), block(kThreads);
-    if (p.D <= 64)
+    if (sizeof(T) == 2 && (p.D == 64 || p.D == 128))
+        launch_prompt_mfma(p, s);
+    else if (p.D <= 64)
         hipLaunchKernelGGL((prompt_attn_kernel<T, 64>), grid, block, 0, s, p);
     else if (p.D <= 128)
         hipLaunchKernelGGL((prompt_attn_kernel<T, 128>), grid, block, 0, s, p);

@@ -1,0 +1,536 @@
+// prompt_attn for bf16 with 64 or 128 channels: the tiled kernel (prompt_attn.hip holds the general one and the
+// definition of rows, tiles and splits).
+//
+// Workgroup = (tile of 32 WAVES rows, KV head, split); a wavefront owns 32 rows.  K and V tiles of 32 tokens go from
+// global memory straight into LDS (global_load_lds_dwordx4), kAhead tiles before their use, with the 16-byte pieces
+// of a row swizzled on the global side so that both operand reads are free of bank conflicts: K with
+// ds_read_b128, V with the transposing ds_read_b64_tr_b16.  The reads are issued by hand a few fragments ahead of
+// the product that takes them, with exact waits (the compiler would drain the copies before every LDS read).
+//
+// Tiles that every row of the workgroup sees whole run through a pipeline: one region of matrix products holds the
+// scores of tile t, the probabilities of tile t - 1 and P V of tile t - 2, interleaved instruction by instruction, with
+// one barrier a tile.  The others (the causal edge, a prompt's ragged end) follow one by one with the mask;
+// wavefronts whose rows see nothing of such a tile skip it.
+#include "attn_prefix_body.h"
+
+namespace spd {
+namespace {
+
+using prefix_impl::as_bf16x8;
+using prefix_impl::bf16x8;
+using prefix_impl::floatx16;
+using prefix_impl::for_each_index;
+using prefix_impl::pack_bf16_rne;
+using prefix_impl::u32x2;
+using prefix_impl::u32x4;
+using prefix_impl::wait_vmcnt;
+
+constexpr int kTileN = 32;
+constexpr int kAhead = 3;             // tiles under way
+constexpr int kRingK = kAhead + 1;    // and the one whose scores are taken
+constexpr int kRingV = kAhead + 3;    // and those of the three in work
+constexpr int kFragAhead = 4;         // LDS fragments in flight
+constexpr float kNever = -1e30f;      // reference maximum of a row that has seen nothing: finite, so that no exponent is inf - inf
+constexpr float kRaise = 1024.f;
+
+template <int D> struct Shape {
+    static constexpr int kRow = 2 * D, kTile = kTileN * kRow;  // bytes
+    static constexpr int kRowsPerCopy = 1024 / kRow, kCopies = kTile / 1024;
+    static constexpr int kQK = D / 16, kDB = D / 32, kPV = 2 * kDB;  // fragments
+    static constexpr int kLds = (kRingK + kRingV) * kTile;  // 80 KB with 128 channels: two workgroups per CU
+    // Piece p of a row lies in slot p ^ swz(row): sixteen rows' equal pieces take all 64 banks, and so do the four rows and
+    // 64 bytes that half a wavefront's transposing reads touch.
+    static __device__ __forceinline__ int swz(int row)
+    {
+        if (D == 128)
+            return ((row & 3) << 2) | ((row >> 2) & 3);
+        return (((row >> 1) & 1) << 2) | (((row >> 2) & 1) << 1) | ((row >> 3) & 1);
+    }
+};
+
+// Which prompt and tile: as in the general kernel, with ROWS rows a tile.
+struct TileOf {
+    int b, tile;
+};
+template <int ROWS> __device__ __forceinline__ TileOf find_tile(const PromptParams& p, int item)
+{
+    const int lane = threadIdx.x & 63;
+    int base = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        const int b = b0 + lane;
+        int n = 0;
+        if (b < p.B)
+            n = (max(p.query_indptr[b + 1] - p.query_indptr[b], 0) * p.G + ROWS - 1) / ROWS;
+        int upto = n;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(upto, o);
+            upto += lane >= o ? x : 0;
+        }
+        const int all = __builtin_amdgcn_readfirstlane(__shfl(upto, 63));
+        if (item < base + all) {
+            const int l = __ffsll((unsigned long long)__ballot(item < base + upto)) - 1;
+            const int before = __shfl(upto - n, l), tiles = __shfl(n, l);
+            return {__builtin_amdgcn_readfirstlane(b0 + l), __builtin_amdgcn_readfirstlane(tiles - 1 - (item - base - before))};
+        }
+        base += all;
+    }
+    return {-1, 0};
+}
+
+template <int D, int WAVES, bool PAGED>
+__global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(PromptParams p)
+{
+    using S = Shape<D>;
+    constexpr int kRows = 32 * WAVES, kIPW = 2 * S::kCopies / WAVES;
+    static_assert(kIPW >= 1, "a copy for every wavefront");
+    __shared__ __align__(16) char lds[S::kLds];
+
+    const int j = blockIdx.x % p.Hkv, unit = blockIdx.x / p.Hkv, split = unit % p.num_splits;
+    const TileOf at = find_tile<kRows>(p, unit / p.num_splits);
+    if (at.b < 0)
+        return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, h = lane >> 5;
+    const int q0 = p.query_indptr[at.b], n = p.query_indptr[at.b + 1] - q0, L = p.kv_lens[at.b];
+    const int rows = n * p.G, row0 = at.tile * kRows, rr = row0 + wave * 32 + col;
+    const bool row_ok = rr < rows;
+    const int token = (row_ok ? rr : 0) / p.G, head = j * p.G + (row_ok ? rr : 0) % p.G;
+    const long long out_row = (long long)(q0 + token) * p.Hq + head;
+    const int limit = !row_ok ? -1 : p.causal ? L - n + token : L - 1;  // the last token the row sees
+    const int least = p.causal ? L - n + row0 / p.G : L - 1;
+    const int most = p.causal ? L - n + (min(row0 + kRows, rows) - 1) / p.G : L - 1;
+    const int wave_last = min(row0 + wave * 32 + 32, rows) - 1;  // last row of this wavefront
+    const int wave_most = wave_last < row0 + wave * 32 ? -1 : p.causal ? L - n + wave_last / p.G : L - 1;
+
+    const int seen = max(most + 1, 0);
+    const int part = ((seen + p.num_splits - 1) / p.num_splits + kTileN - 1) / kTileN * kTileN;
+    const int t0 = min(split * part, seen), t1 = min(t0 + part, seen);
+    const int ntiles = (t1 - t0 + kTileN - 1) / kTileN;
+    int nfull = max(min(least + 1, t1) - t0, 0) / kTileN;  // tiles that every row sees whole
+    if (nfull < 3)
+        nfull = 0;
+
+    // ---- query fragments (B operand): column = this lane's row, channels 16 s + 8 h
+    bf16x8 qf[S::kQK];
+    {
+        const uint4* qg = (const uint4*)((const char*)p.q + ((long long)(q0 + token) * p.q_stride + (long long)head * D) * 2);
+#pragma unroll
+        for (int s = 0; s < S::kQK; ++s) {
+            uint4 v = qg[2 * s + h];
+            if (!row_ok)
+                v = make_uint4(0, 0, 0, 0);
+            qf[s] = as_bf16x8(v);
+        }
+    }
+
+    // ---- global -> LDS copies: the first half of the wavefronts copies K, the other half V, kIPW instructions a tile each
+    typedef const __attribute__((address_space(4))) int* const_int_ptr;
+    const const_int_ptr pages = PAGED ? (const_int_ptr)(p.pages + p.kv_indptr[at.b]) : nullptr;
+    const long long tok_stride = PAGED ? S::kRow : p.kv_stride * 2;
+    const long long head_base = PAGED ? (long long)j * 16 * S::kRow : (long long)p.kv_indptr[at.b] * p.kv_stride * 2 + (long long)j * S::kRow;
+    const long long page_stride = (long long)p.Hkv * 16 * S::kRow;
+    const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) void*)lds;
+    constexpr int kLanesPerRow = 64 / S::kRowsPerCopy;
+    const int lane_row = lane / kLanesPerRow, lane_piece = lane % kLanesPerRow;
+    const bool copies_v = wave >= WAVES / 2;
+    const int row_first = S::kRowsPerCopy * kIPW * (copies_v ? wave - WAVES / 2 : wave);
+    unsigned lane_off[kIPW];
+#pragma unroll
+    for (int i = 0; i < kIPW; ++i) {
+        const int tl = S::kRowsPerCopy * i + lane_row;
+        lane_off[i] = (unsigned)(tl * (unsigned)tok_stride + ((lane_piece ^ S::swz(row_first + tl)) << 4));
+    }
+    const char* const tensor = (const char*)(copies_v ? p.v : p.k);
+    char* const ring_lds = lds + (copies_v ? kRingK * S::kTile : 0) + row_first * S::kRow;
+    const int ring = copies_v ? kRingV : kRingK;
+    int next_page = 0;
+    auto fetch_page = [&](int tile) __attribute__((always_inline)) {
+        if (PAGED)
+            next_page = pages[min(t0 + tile * kTileN + row_first, t1 - 1) >> 4];
+    };
+    int slot_next = 0;  // ring slot of the next tile to be copied
+    auto issue_tile = [&](int tile) __attribute__((always_inline)) {
+        const int tb = t0 + tile * kTileN;
+        char* const dst = ring_lds + slot_next * S::kTile;
+        slot_next = slot_next + 1 == ring ? 0 : slot_next + 1;
+        const bool full = tb + kTileN <= t1;
+        const int tg = min(tb + row_first, t1 - 1);  // this wavefront's first row; rows past the end repeat the last token
+        const char* const src = PAGED ? tensor + (long long)next_page * page_stride + head_base + (tg & 15) * S::kRow
+                                      : tensor + head_base + (long long)tg * tok_stride;
+#pragma unroll
+        for (int i = 0; i < kIPW; ++i) {
+            unsigned off = lane_off[i];
+            if (!full) {
+                const int tl = S::kRowsPerCopy * i + lane_row, row = min(tb + row_first + tl, t1 - 1) - tg;
+                off = (unsigned)(max(row, 0) * (unsigned)tok_stride + ((lane_piece ^ S::swz(row_first + tl)) << 4));
+            }
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + off),
+                                             (__attribute__((address_space(3))) void*)(dst + i * 1024), 16, 0, 0);
+        }
+        fetch_page(tile + 1);
+    };
+    auto start_copies = [&](int tile) __attribute__((always_inline)) {
+        if (tile < ntiles)
+            issue_tile(tile);
+    };
+    // Waits until at most `tiles` later tiles of this wavefront's copies are under way, then for everybody.
+    auto wait_copies = [&](int tiles) __attribute__((always_inline)) {
+        if (tiles >= kAhead - 1)
+            wait_vmcnt<(kAhead - 1) * kIPW>();
+        else if (tiles == 1)
+            wait_vmcnt<kIPW>();
+        else
+            wait_vmcnt<0>();
+        __builtin_amdgcn_s_barrier();
+    };
+    static_assert(kAhead == 3, "wait_copies lists the counts below kAhead - 1");
+
+    // ---- per-lane LDS addresses of the operand fragments, relative to a tile
+    const unsigned k_row = (unsigned)(col * S::kRow), k_xor = (unsigned)((h ^ S::swz(col)) << 4);
+    unsigned v_off[S::kDB][2];
+    {
+        const int g16 = (lane >> 4) & 1, r = (lane & 15) >> 2, q4 = lane & 3;
+#pragma unroll
+        for (int db = 0; db < S::kDB; ++db)
+#pragma unroll
+            for (int part2 = 0; part2 < 2; ++part2) {
+                const int tok = 8 * part2 + 4 * h + r, piece = 4 * db + 2 * g16 + (q4 >> 1);
+                v_off[db][part2] = (unsigned)(tok * S::kRow + ((piece ^ S::swz(tok)) << 4) + (q4 & 1) * 8);
+            }
+    }
+
+    float m_run = kNever, l_run = 0.f;
+    floatx16 o[S::kDB];
+#pragma unroll
+    for (int db = 0; db < S::kDB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            o[db][i] = 0.f;
+
+    u32x4 ring_k[kFragAhead + 2];
+    u32x2 ring_lo[kFragAhead + 2], ring_hi[kFragAhead + 2];
+    // Fragment order of a region: the two products alternate where both are there.
+    // One region: scores of the tile in K slot `kslot` into `sn` (QK), P V of the tile in V slot `vslot` with
+    // probabilities `pp` (PV), and between the products the probabilities `pn` of the scores `so` (SM; their sum over the
+    // lane is returned).
+    auto region = [&](auto qk_tag, auto sm_tag, auto pv_tag, int kslot, int vslot, floatx16& sn, const floatx16& so,
+                      bf16x8 (&pn)[2], const bf16x8 (&pp)[2]) __attribute__((always_inline)) -> float {
+        constexpr bool QK = decltype(qk_tag)::value, SM = decltype(sm_tag)::value, PV = decltype(pv_tag)::value;
+        constexpr bool kBoth = QK && PV;
+        static_assert(S::kQK == S::kPV, "as many fragments of either product");
+        constexpr int NF = (QK ? S::kQK : 0) + (PV ? S::kPV : 0);
+        unsigned kbase = lds_base + (unsigned)kslot * S::kTile;
+        unsigned vbase = lds_base + (unsigned)(kRingK + vslot) * S::kTile;
+        asm("" : "+s"(kbase), "+s"(vbase));
+        if (QK) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                sn[i] = 0.f;
+        }
+        auto issue = [&](auto kc) __attribute__((always_inline)) {
+            constexpr int K = decltype(kc)::value;
+            if constexpr (K < NF) {
+                constexpr int idx = kBoth ? K >> 1 : K;
+                constexpr bool is_pv = kBoth ? (K & 1) != 0 : PV;
+                if constexpr (!is_pv) {
+                    const unsigned addr = kbase + k_row + ((32u * idx) ^ k_xor);
+                    u32x4& dst = ring_k[K % (kFragAhead + 2)];
+                    asm volatile("ds_read_b128 %0, %1" : "=v"(dst) : "v"(addr));
+                } else {
+                    constexpr int a = idx / S::kDB, b = idx % S::kDB;
+                    u32x2& lo = ring_lo[K % (kFragAhead + 2)];
+                    u32x2& hi = ring_hi[K % (kFragAhead + 2)];
+                    const unsigned a0 = vbase + v_off[b][0], a1 = vbase + v_off[b][1];
+                    asm volatile("ds_read_b64_tr_b16 %0, %2 offset:%4\n\tds_read_b64_tr_b16 %1, %3 offset:%4"
+                                 : "=&v"(lo), "=&v"(hi)
+                                 : "v"(a0), "v"(a1), "n"(a * 16 * S::kRow));
+                }
+            }
+        };
+        auto consume = [&](auto kc) __attribute__((always_inline)) {
+            constexpr int K = decltype(kc)::value;
+            constexpr int idx = kBoth ? K >> 1 : K;
+            constexpr bool is_pv = kBoth ? (K & 1) != 0 : PV;
+            // LDS instructions issued after fragment K
+            constexpr int last = K + kFragAhead < NF ? K + kFragAhead : NF - 1;
+            constexpr int later = last - K;
+            constexpr int after = kBoth ? later + (is_pv ? later / 2 : (later + 1) / 2) : PV ? 2 * later : later;
+            if constexpr (!is_pv) {
+                u32x4& f = ring_k[K % (kFragAhead + 2)];
+                asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(f) : "n"(after));
+                sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(f), qf[idx], sn, 0, 0, 0);
+            } else {
+                u32x2& lo = ring_lo[K % (kFragAhead + 2)];
+                u32x2& hi = ring_hi[K % (kFragAhead + 2)];
+                asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(lo), "+v"(hi) : "n"(after));
+                const u32x4 f = {lo[0], lo[1], hi[0], hi[1]};
+                constexpr int a = idx / S::kDB, b = idx % S::kDB;
+                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(f), pp[a], o[b], 0, 0, 0);
+            }
+        };
+        // Slot e of the softmax: the exponent of score e, the exponential of score e - 1, the sum of score e - 2.
+        float psum = 0.f, x[16], pv[16];
+        uint32_t w[8];
+        auto soft = [&](auto ec) __attribute__((always_inline)) {
+            constexpr int e = decltype(ec)::value;
+            if constexpr (SM && e >= 0 && e < 18) {
+                if constexpr (e < 16)
+                    x[e] = __builtin_fmaf(so[e], p.scale_log2, -m_run);
+                if constexpr (e >= 1 && e < 17)
+                    pv[e - 1] = __builtin_amdgcn_exp2f(x[e - 1]);
+                if constexpr (e >= 2) {
+                    psum += pv[e - 2];
+                    if constexpr ((e & 1) != 0)
+                        w[(e - 2) >> 1] = pack_bf16_rne(pv[e - 3], pv[e - 2]);
+                }
+            }
+        };
+        constexpr int kPer = (18 + NF - 1) / NF;                   // softmax slots per product
+        constexpr int kLead = kPer * NF >= 18 + 2 ? 0 : 18 > kPer * NF ? 18 - kPer * NF : 0;
+        for_each_index(issue, std::make_integer_sequence<int, kFragAhead + 1>{});
+        if constexpr (SM) {
+            for_each_index(soft, std::make_integer_sequence<int, kLead>{});
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        for_each_index(
+            [&](auto kc) __attribute__((always_inline)) {
+                constexpr int K = decltype(kc)::value;
+                consume(kc);
+                issue(std::integral_constant<int, K + kFragAhead + 1>{});
+                if constexpr (SM) {
+                    for_each_index([&](auto ic) __attribute__((always_inline)) {
+                        soft(std::integral_constant<int, K * kPer + decltype(ic)::value + kLead>{});
+                    }, std::make_integer_sequence<int, kPer>{});
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            },
+            std::make_integer_sequence<int, NF>{});
+        if constexpr (SM) {
+            const uint4 p0 = make_uint4(w[0], w[1], w[2], w[3]), p1 = make_uint4(w[4], w[5], w[6], w[7]);
+            pn[0] = as_bf16x8(p0);
+            pn[1] = as_bf16x8(p1);
+        }
+        return psum;
+    };
+
+    auto probabilities = [&](const floatx16& sc, bf16x8 (&pn)[2]) __attribute__((always_inline)) -> float {
+        float psum = 0.f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            float pv[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                pv[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[8 * u + e], p.scale_log2, -m_run));
+                psum += pv[e];
+            }
+            uint4 pu;
+            pu.x = pack_bf16_rne(pv[0], pv[1]);
+            pu.y = pack_bf16_rne(pv[2], pv[3]);
+            pu.z = pack_bf16_rne(pv[4], pv[5]);
+            pu.w = pack_bf16_rne(pv[6], pv[7]);
+            pn[u] = as_bf16x8(pu);
+        }
+        return psum;
+    };
+    // The reference maximum only has to bound the exponents: it is raised where a lane's 16 probabilities add up to more
+    // than kRaise (none is above that otherwise: exact in fp32 and bf16 alike).  O holds every earlier tile by then.
+    auto raise_maximum = [&](const floatx16& sc) __attribute__((always_inline)) -> float {
+        float tmax = kNever;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            tmax = fmaxf(tmax, sc[i] * p.scale_log2);
+        tmax = fmaxf(tmax, __shfl_xor(tmax, 32));
+        const float m_up = fmaxf(m_run, tmax);
+        const float corr = __builtin_amdgcn_exp2f(m_run - m_up);
+        m_run = m_up;
+        return corr;
+    };
+    auto take_sum = [&](float psum, const floatx16& sc, bf16x8 (&pn)[2]) __attribute__((always_inline)) {
+        if (__ballot(!(psum <= kRaise)) != 0) {
+            const float corr = raise_maximum(sc);
+            psum = probabilities(sc, pn);
+            l_run *= corr;
+#pragma unroll
+            for (int db = 0; db < S::kDB; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    o[db][i] *= corr;
+        }
+        l_run += psum;
+    };
+
+    // ---- the pipeline ---------------------------------------------------------------------------------------------------
+    // Step t starts the copies of tile t + kAhead (into slots that a barrier has freed: K of tile t - 1, V of tile t - 3), runs its
+    // region, and waits until K and V of tile t + 1 have landed for everybody.
+    const std::true_type yes{};
+    const std::false_type no{};
+    floatx16 sa, sb;
+    bf16x8 pa[2], pb[2];
+    auto end_of_step = [&](int t) __attribute__((always_inline)) { wait_copies(ntiles - 2 - t); };
+    if (ntiles > 0) {
+        fetch_page(0);
+#pragma unroll
+        for (int t = 0; t < kAhead; ++t)
+            start_copies(t);
+        // tile 0 has landed once at most the kAhead - 1 tiles after it are under way
+        wait_copies(ntiles - 1);
+    }
+    int t = 0;
+    if (nfull > 0) {
+        start_copies(kAhead);
+        region(yes, no, no, 0, 0, sb, sb, pa, pa);
+        end_of_step(0);
+        raise_maximum(sb);
+        start_copies(1 + kAhead);
+        take_sum(region(yes, yes, no, 1 % kRingK, 0, sa, sb, pb, pa), sb, pb);
+        end_of_step(1);
+        // scores of tile t - 1 are in sa, probabilities of tile t - 2 in pb
+        int ks = 2 % kRingK, vs = 0;
+        auto next = [&] __attribute__((always_inline)) {
+            ks = ks + 1 == kRingK ? 0 : ks + 1;
+            vs = vs + 1 == kRingV ? 0 : vs + 1;
+        };
+        for (t = 2; t + 1 < nfull; t += 2) {
+            start_copies(t + kAhead);
+            take_sum(region(yes, yes, yes, ks, vs, sb, sa, pa, pb), sa, pa);
+            end_of_step(t);
+            next();
+            start_copies(t + 1 + kAhead);
+            take_sum(region(yes, yes, yes, ks, vs, sa, sb, pb, pa), sb, pb);
+            end_of_step(t + 1);
+            next();
+        }
+        if (t < nfull) {
+            start_copies(t + kAhead);
+            take_sum(region(yes, yes, yes, ks, vs, sb, sa, pa, pb), sa, pa);
+            end_of_step(t);
+            next();
+            sa = sb;
+            pb[0] = pa[0];
+            pb[1] = pa[1];
+        }
+        t = nfull;
+        // drain: softmax of the last tile beside P V of the one before, then its own P V
+        take_sum(region(no, yes, yes, 0, vs, sb, sa, pa, pb), sa, pa);
+        next();
+        region(no, no, yes, 0, vs, sa, sa, pa, pa);
+        __builtin_amdgcn_s_barrier();  // the V slots of these two tiles are free for everybody
+    }
+
+    // ---- tiles that some row does not see whole ------------------------------------------------------------------------------
+    for (; t < ntiles; ++t) {
+        const int tb = t0 + t * kTileN, kslot = t % kRingK, vslot = t % kRingV;
+        // Does the tile hold values that are not finite (0 * inf is not 0)?  Its copies have landed; the flag lies in a V
+        // slot that is free here: of the six, tile t takes one and the copies under way three.
+        volatile uint32_t* const odd_flag = (volatile uint32_t*)(lds + (kRingK + (t + 4) % kRingV) * S::kTile);
+        if (tid == 0)
+            *odd_flag = 0u;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        start_copies(t + kAhead);  // (K of tile t - 1 and V of tile t - 3 are free for everybody from here on)
+        const bool some = tb <= wave_most;
+        {
+            bool any = false;
+            for (int i = tid; i < S::kTile / 16; i += WAVES * 64) {
+                u32x4 v;
+                const unsigned addr = lds_base + (unsigned)(kRingK + vslot) * S::kTile + i * 16;
+                asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=v"(v) : "v"(addr));
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    any = any || (v[e] & 0x7f80u) == 0x7f80u || (v[e] & 0x7f800000u) == 0x7f800000u;
+            }
+            if (any)
+                *odd_flag = 1u;
+        }
+        if (some) {
+            region(yes, no, no, kslot, 0, sa, sa, pa, pa);
+            const int end = min(limit, t1 - 1) - tb - 4 * h;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                sa[i] = 8 * (i >> 2) + (i & 3) <= end ? sa[i] : -INFINITY;
+            take_sum(probabilities(sa, pa), sa, pa);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        const bool odd = __builtin_amdgcn_readfirstlane(*odd_flag) != 0u;
+        if (some && !odd) {
+            region(no, no, yes, 0, vslot, sa, sa, pa, pa);
+        } else if (some) {
+            // token by token, to the rows (lanes) that see it
+            for (int x = 0; x < kTileN; ++x) {
+                const int slot = (x >> 3) * 4 + (x & 3);  // place among the lane's 16 probabilities
+                const bool own = h == ((x >> 2) & 1), sees = tb + x <= min(limit, t1 - 1);
+                uint32_t pw = 0u;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const u32x4 q = *reinterpret_cast<const u32x4*>(&pa[u >> 2]);
+                    pw = u == (slot >> 1) ? q[u & 3] : pw;
+                }
+                pw = own ? ((slot & 1) ? pw >> 16 : pw & 0xffffu) : 0u;
+                const u32x4 b = {pw, 0u, 0u, 0u};
+#pragma unroll
+                for (int db = 0; db < S::kDB; ++db) {
+                    const int c = 32 * db + col;  // channel
+                    const char* v = lds + (kRingK + vslot) * S::kTile + x * S::kRow + (((c >> 3) ^ S::swz(x)) << 4) + (c & 7) * 2;
+                    const u32x4 a = {own ? (uint32_t)*(volatile const uint16_t*)v : 0u, 0u, 0u, 0u};
+                    const floatx16 sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(b), o[db], 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        o[db][i] = sees ? sum[i] : o[db][i];
+                }
+            }
+        }
+        end_of_step(t);
+    }
+
+    // ---- results ---------------------------------------------------------------------------------------------------------
+    const float l = l_run + __shfl_xor(l_run, 32);
+    if (!row_ok)
+        return;
+    if (p.num_splits > 1) {
+        if (h == 0)
+            p.part_ml[out_row * p.num_splits + split] = make_float2(m_run, l);
+        float* dst = p.part_acc + (out_row * p.num_splits + split) * D;
+#pragma unroll
+        for (int db = 0; db < S::kDB; ++db)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4)
+                *reinterpret_cast<float4*>(dst + 32 * db + 8 * q4 + 4 * h) =
+                    make_float4(o[db][4 * q4], o[db][4 * q4 + 1], o[db][4 * q4 + 2], o[db][4 * q4 + 3]);
+        return;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (p.lse && h == 0)
+        p.lse[out_row] = l == 0.f ? -INFINITY : m_run * kLn2 + logf(l);
+    char* dst = (char*)p.out + out_row * S::kRow;
+#pragma unroll
+    for (int db = 0; db < S::kDB; ++db)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4)
+            *reinterpret_cast<uint2*>(dst + (32 * db + 8 * q4 + 4 * h) * 2) =
+                make_uint2(pack_bf16_rne(o[db][4 * q4] * inv, o[db][4 * q4 + 1] * inv),
+                           pack_bf16_rne(o[db][4 * q4 + 2] * inv, o[db][4 * q4 + 3] * inv));
+}
+
+template <int D, int WAVES> void launch(const PromptParams& p, hipStream_t s)
+{
+    const dim3 grid((unsigned)((long long)p.tiles * p.num_splits * p.Hkv)), block(WAVES * 64);
+    if (p.page_size != 0)
+        hipLaunchKernelGGL((prompt_mfma_kernel<D, WAVES, true>), grid, block, 0, s, p);
+    else
+        hipLaunchKernelGGL((prompt_mfma_kernel<D, WAVES, false>), grid, block, 0, s, p);
+}
+
+}  // namespace
+
+hipError_t launch_prompt_mfma(const PromptParams& p, hipStream_t s)
+{
+    if (p.D == 128)
+        p.block_rows == 256 ? launch<128, 8>(p, s) : launch<128, 4>(p, s);
+    else
+        p.block_rows == 256 ? launch<64, 8>(p, s) : launch<64, 4>(p, s);
+    return hipGetLastError();
+}
+
+}  // namespace spd

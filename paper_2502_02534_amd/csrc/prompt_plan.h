@@ -11,12 +11,12 @@ namespace spd {
 namespace plan {
 
 struct PromptPlan {
+    int block_rows;  // (token, head of the group) rows per workgroup
     int tiles;       // upper bound on the row tiles of all prompts, one KV head
     int num_splits;  // parts of a tile's tokens
     size_t acc_bytes, ml_bytes;
 };
 
-constexpr int kPromptRows = 128;       // (token, head of the group) rows per workgroup
 constexpr int kPromptMaxSplits = 32;
 constexpr int kPromptMinTokens = 128;  // per split
 
@@ -41,6 +41,9 @@ inline int check_prompt_desc(const spd_prompt_desc* d, bool queries)
     return SPD_OK;
 }
 
+// bf16 with 64 or 128 channels runs on the tiled kernel.
+inline bool prompt_tiled(const spd_prompt_desc* d) { return d->dtype == SPD_BF16 && (d->head_dim == 64 || d->head_dim == 128); }
+
 inline int make_prompt_plan(const spd_prompt_desc* d, int64_t total, int64_t max_query, int64_t max_kv, PromptPlan* out)
 {
     const int rc = check_prompt_desc(d, true);
@@ -54,18 +57,23 @@ inline int make_prompt_plan(const spd_prompt_desc* d, int64_t total, int64_t max
         return SPD_EUNSUPPORTED;
     const int64_t group = d->num_q_heads / d->num_kv_heads;
     // a prompt's last tile may be partly filled, and no prompt has more tiles than its longest
-    const int64_t per_prompt = (max_query * group + kPromptRows - 1) / kPromptRows;
-    int64_t tiles = total * group / kPromptRows + d->num_prompts;
-    if (per_prompt < tiles / d->num_prompts + 1 && per_prompt * d->num_prompts < tiles)
-        tiles = per_prompt * d->num_prompts;
-    const int64_t units = tiles * d->num_kv_heads;
+    auto tiles_of = [&](int64_t rows) {
+        const int64_t per_prompt = (max_query * group + rows - 1) / rows, all = total * group / rows + d->num_prompts;
+        return per_prompt <= all / d->num_prompts ? per_prompt * d->num_prompts : all;
+    };
+    const bool tiled = prompt_tiled(d);
+    const int rows = tiled && tiles_of(256) * d->num_kv_heads >= 256 ? 256 : 128;
+    const int64_t tiles = tiles_of(rows), units = tiles * d->num_kv_heads;
     int64_t splits = units > 0 ? (512 + units - 1) / units : 1;
     const int64_t whole = max_kv / kPromptMinTokens;
     splits = splits < whole ? splits : whole;
     splits = splits < kPromptMaxSplits ? splits : kPromptMaxSplits;
     splits = splits > 1 ? splits : 1;
+    if (rows == 256)
+        splits = 1;
     if (units > most / splits)
         return SPD_EUNSUPPORTED;
+    out->block_rows = rows;
     out->tiles = (int)tiles;
     out->num_splits = (int)splits;
     const size_t states = splits > 1 ? (size_t)total * d->num_q_heads * splits : 0;

@@ -143,6 +143,7 @@ struct PromptParams {
     const int* kv_lens;
     const int* kv_indptr;
     const int* pages;
+    int block_rows;  // rows per workgroup
     int tiles;       // upper bound on the row tiles of all prompts
     int num_splits;  // parts a tile's tokens are cut into
     long long rows;  // total_queries * Hq
@@ -243,6 +244,7 @@ long long step_rows_blocks(long long row_bytes);
 hipError_t launch_step_rows(const StepRowsParams& a, bool record, hipStream_t s);
 hipError_t launch_step_advance(const StepAdvanceParams& a, hipStream_t s);
 size_t sampler_workspace_bytes(long long rows, long long vocab);
+hipError_t launch_prompt_mfma(const PromptParams& p, hipStream_t s);
 hipError_t launch_prompt_attn(const PromptParams& p, hipStream_t s);
 hipError_t launch_page_tables(const PageTableParams& p, hipStream_t s);
 hipError_t launch_kv_write(const KvWriteParams& p, hipStream_t s);
