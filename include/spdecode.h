@@ -486,7 +486,7 @@ SPD_API int write_prompt_kv(const spd_prompt_desc *desc, const void *k, const vo
  * token i is among tokens[indptr[b] .. indptr[b+1]) (ids outside 0 .. vocab - 1 are ignored).
  *   bits    uint32 [num_prompts, >= ceil(vocab / 32)], rows bits_stride words apart
  *   accumulate  nonzero: bits that are set stay set; 0: the rows' ceil(vocab / 32) words are written whole
- * vocab up to 1048576.  Returns spd_status.
+ * vocab up to 1048576, num_prompts below 2^22.  Returns spd_status.
  */
 SPD_API int mark_prompt_tokens(const int32_t *tokens, const int32_t *indptr, int64_t num_prompts,
                                int64_t vocab, uint32_t *bits, int64_t bits_stride,
@@ -527,7 +527,8 @@ typedef struct spd_penalties {
  *   logits     [rows, vocab] fp32 or bf16 (logits_dtype), rows row_stride elements apart
  *   out        float [rows, vocab], rows out_stride apart; may be logits itself (fp32, equal strides), else
  *              must not overlap it
- *   penalties  max_tokens up to 2^24; vocab up to 2^30
+ *   penalties  max_tokens up to 2^24
+ *   vocab      up to 2^30; rows + 8 times ceil(vocab / 16384) up to 2^22
  * rows 0 is a call that does nothing.  Returns spd_status.
  */
 SPD_API int penalize_logits(const void *logits, int32_t logits_dtype, int64_t rows, int64_t vocab,

@@ -2,6 +2,8 @@
 // and the logits shaped by penalties, biases and a grammar mask.
 #include "spd_internal.h"
 
+#include <type_traits>
+
 namespace spd {
 namespace {
 
@@ -32,58 +34,238 @@ __global__ __launch_bounds__(kMarkThreads) void mark_tokens_kernel(const int* to
 }
 
 // ---- penalties, biases, grammar mask -----------------------------------------------------------------------
-// One workgroup per row and slice of the vocabulary.  The row's generated tokens that lie in the slice are
-// counted in LDS, then the slice's logits pass through once; biases, few, are added in LDS beforehand.
-constexpr int kThreads = 256;
-constexpr int kSlice = 4096;
+// One workgroup per row and slice of the vocabulary.  The tokens of the slice that occur in the row's history or biases
+// ("listed", few) get a bit each and, by the number of bits before it, a place in a table of counts and biases; the logits
+// then pass through once, four a thread, and only those whose bit is set look into the table.  A slice with more
+// listed tokens than the table holds is taken in stretches as long as the table.  A wavefront has the logits of its
+// tokens on their way before the table is begun, and takes a word of every bit row per lane, handed round with shuffles.
+constexpr int kThreads = 512;
+constexpr int kTable = 2048;         // places
+constexpr int kEntries = 4;          // of the history, a thread: a history of kEntries * kThreads is read once
+constexpr int kMaxSlice = 16384;     // tokens: a bit each
+constexpr int kWords = kMaxSlice / 32;
+static_assert(kWords <= kThreads, "one word a thread");
+// Tokens of a slice with ROUNDS rounds of four tokens a lane.
+constexpr int slice_tokens(int rounds) { return rounds * 4 * kThreads; }
 
+// Four logits as they lie in memory, from a place that is aligned to its element only (the hardware takes any).
+template <bool BF16> struct Four {
+    uint32_t w[BF16 ? 2 : 4];
+    __device__ __forceinline__ void load(const char* at, int m)  // m of them: up to four
+    {
+        typedef uint32_t __attribute__((ext_vector_type(2), aligned(2))) any2;
+        typedef uint32_t __attribute__((ext_vector_type(4), aligned(4))) any4;
+        if (m == 4) {
+            if constexpr (BF16) {
+                const any2 v = *reinterpret_cast<const any2*>(at);
+                w[0] = v[0];
+                w[1] = v[1];
+            } else {
+                const any4 v = *reinterpret_cast<const any4*>(at);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    w[i] = v[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < (BF16 ? 2 : 4); ++i)
+                w[i] = 0u;
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (e < m) {
+                    if constexpr (BF16)
+                        w[e >> 1] |= (uint32_t)((const uint16_t*)at)[e] << (16 * (e & 1));
+                    else
+                        w[e] = ((const uint32_t*)at)[e];
+                }
+        }
+    }
+    __device__ __forceinline__ float get(int e) const
+    {
+        if constexpr (BF16)
+            return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+        else
+            return __uint_as_float(w[e]);
+    }
+};
+
+template <bool BF16, int ROUNDS>
 __global__ __launch_bounds__(kThreads) void penalize_kernel(LogitsParams p, int slices)
 {
-    __shared__ uint32_t counts[kSlice];
-    __shared__ float bias[kSlice];
-    const long long r = blockIdx.x / slices;
-    const long long i0 = (long long)(blockIdx.x % slices) * kSlice;
-    const int len = (int)min((long long)kSlice, p.vocab - i0);
-    for (int i = threadIdx.x; i < kSlice; i += kThreads) {
-        counts[i] = 0u;
-        bias[i] = 0.f;
-    }
-    __syncthreads();
-    if (p.tokens) {
-        const int n = min(p.token_lens[r], p.max_tokens);
-        const int* mine = p.tokens + r * p.token_row_stride;
-        for (int t = threadIdx.x; t < n; t += kThreads) {
-            const long long id = mine[t * p.token_step_stride] - i0;
-            if (id >= 0 && id < len)
-                atomicAdd(&counts[id], 1u);
-        }
-    }
-    if (p.bias_tokens)
-        for (int b = p.bias_indptr[r] + (int)threadIdx.x, end = p.bias_indptr[r + 1]; b < end; b += kThreads) {
-            const long long id = p.bias_tokens[b] - i0;
-            if (id >= 0 && id < len)
-                bias[id] = p.bias_values[b];
-        }
-    __syncthreads();
-    const float rep = p.repetition ? p.repetition[r] : 1.f;
+    constexpr int slice_len = slice_tokens(ROUNDS), kTile = 256 * ROUNDS;
+    static_assert(slice_len <= kMaxSlice, "a bit for every token");
+    __shared__ uint32_t listed[kWords];
+    __shared__ uint16_t before[kWords];  // listed tokens in the words before
+    __shared__ uint32_t counts[kTable];
+    __shared__ float bias[kTable];
+    __shared__ int wave_sums[kThreads / 64];
+    const int tid = threadIdx.x;
+    // the rows of an XCD follow one another: they read the same lines of a step-major history and the same prompts' bits
+    const long long unit = blockIdx.x >> 3, rows8 = (p.rows + 7) / 8;
+    const long long r = (blockIdx.x & 7) * rows8 + unit / slices;
+    if (r >= p.rows)
+        return;
+    const long long lo = unit % slices * slice_len, hi = min(p.vocab, lo + slice_len);
+
+    const float rep = p.repetition ? p.repetition[r] : 1.f, inv_rep = 1.f / rep;  // (a product for the quotient: half an ulp more)
     const float freq = p.frequency ? p.frequency[r] : 0.f, pres = p.presence ? p.presence[r] : 0.f;
     const long long prompt = !p.prompt_bits ? -1 : p.prompt_of_row ? p.prompt_of_row[r] : r;
     const long long grammar = !p.allowed_bits ? -1 : p.allowed_of_row ? p.allowed_of_row[r] : r;
-    const uint32_t* seen_words = p.prompt_bits + (prompt < 0 ? 0 : prompt) * p.prompt_stride;
-    const uint32_t* allowed_words = p.allowed_bits + (grammar < 0 ? 0 : grammar) * p.allowed_stride;
-    for (int k = threadIdx.x; k < len; k += kThreads) {
-        const long long i = i0 + k;
-        float x = p.bf16 ? __uint_as_float((uint32_t)((const uint16_t*)p.logits)[r * p.stride + i] << 16)
-                         : ((const float*)p.logits)[r * p.stride + i];
-        const uint32_t c = counts[k];
-        if (c != 0u || (prompt >= 0 && ((seen_words[i >> 5] >> (i & 31)) & 1u)))
-            x = x > 0.f ? x / rep : x * rep;
-        if (c != 0u)
-            x = x - freq * (float)c - pres;
-        x += bias[k];
-        if (grammar >= 0 && !((allowed_words[i >> 5] >> (i & 31)) & 1u))
-            x = -INFINITY;
-        p.out[r * p.out_stride + i] = x;
+    const uint32_t* seen_bits = p.prompt_bits + (prompt < 0 ? 0 : prompt) * p.prompt_stride;
+    const uint32_t* allowed_bits = p.allowed_bits + (grammar < 0 ? 0 : grammar) * p.allowed_stride;
+    const int n = p.tokens ? min(p.token_lens[r], p.max_tokens) : 0;
+    const int* mine = p.tokens + r * p.token_row_stride;
+    const int b0 = p.bias_tokens ? p.bias_indptr[r] : 0, b1 = p.bias_tokens ? p.bias_indptr[r + 1] : 0;
+    const char* in = (const char*)p.logits + r * p.stride * (BF16 ? 2 : 4);
+    float* out = p.out + r * p.out_stride;
+
+    const bool any = n > 0 || b1 > b0;
+    int ids[kEntries];
+    auto read_history = [&](int q0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < kEntries; ++u) {
+            const int q = q0 + tid + u * kThreads;
+            const int id = mine[min(q, n - 1) * p.token_step_stride];
+            ids[u] = q < n ? id : -1;
+        }
+    };
+    if (n > 0)
+        read_history(0);
+    int step = slice_len;
+    for (long long s0 = lo; s0 < hi;) {
+        const int len = (int)min((long long)step, hi - s0), words = (len + 31) / 32;
+        // k = place in the stretch.  The wavefront's tile and the words of its bits, all at once
+        const int lane = tid & 63, tile0 = (tid >> 6) * kTile, tile_len = min(len - tile0, kTile);
+        Four<BF16> raw[ROUNDS];
+        uint32_t seen_words = 0u, allowed_words = 0xffffffffu;
+#pragma unroll
+        for (int u = 0; u < ROUNDS; ++u) {
+            const int k = tile0 + 256 * u + 4 * lane;
+            if (k < len)
+                raw[u].load(in + (s0 + k) * (BF16 ? 2 : 4), min(4, len - k));
+        }
+        if (32 * lane < tile_len) {
+            const long long w = (s0 + tile0) / 32 + lane;
+            if (prompt >= 0)
+                seen_words = seen_bits[w];
+            if (grammar >= 0)
+                allowed_words = allowed_bits[w];
+        }
+        if (any) {
+            // every history entry of this stretch, and every bias entry
+            auto each_token = [&](auto f) __attribute__((always_inline)) {
+                for (int q0 = 0; q0 < n; q0 += kEntries * kThreads) {
+                    if (n > kEntries * kThreads)
+                        read_history(q0);
+#pragma unroll
+                    for (int u = 0; u < kEntries; ++u) {
+                        const long long id = ids[u] - s0;
+                        if (ids[u] >= 0 && id >= 0 && id < len)
+                            f((int)id);
+                    }
+                }
+            };
+            auto each_bias = [&](auto f) __attribute__((always_inline)) {
+                for (int k = b0 + tid; k < b1; k += kThreads) {
+                    const long long id = p.bias_tokens[k] - s0;
+                    if (id >= 0 && id < len)
+                        f((int)id, k);
+                }
+            };
+            auto place = [&](int id) __attribute__((always_inline)) -> int {
+                return before[id >> 5] + __popc(listed[id >> 5] & ((1u << (id & 31)) - 1u));
+            };
+            __syncthreads();  // the stretch before has been read
+            if (tid < words)
+                listed[tid] = 0u;
+            for (int i = tid; i < kTable; i += kThreads) {
+                counts[i] = 0u;
+                bias[i] = 0.f;
+            }
+            __syncthreads();
+            each_token([&](int id) __attribute__((always_inline)) { atomicOr(&listed[id >> 5], 1u << (id & 31)); });
+            each_bias([&](int id, int) __attribute__((always_inline)) { atomicOr(&listed[id >> 5], 1u << (id & 31)); });
+            __syncthreads();
+            const int bits = tid < words ? __popc(listed[tid]) : 0;
+            int upto = bits;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int x = __shfl_up(upto, o);
+                upto += (tid & 63) >= o ? x : 0;
+            }
+            if ((tid & 63) == 63)
+                wave_sums[tid >> 6] = upto;
+            __syncthreads();
+            int first = upto - bits, total = 0;
+#pragma unroll
+            for (int w = 0; w < kThreads / 64; ++w) {
+                first += w < (tid >> 6) ? wave_sums[w] : 0;
+                total += wave_sums[w];
+            }
+            if (total > kTable) {  // (for everybody alike)
+                step = kTable;
+                continue;
+            }
+            if (tid < words)
+                before[tid] = (uint16_t)first;
+            __syncthreads();
+            each_token([&](int id) __attribute__((always_inline)) { atomicAdd(&counts[place(id)], 1u); });
+            each_bias([&](int id, int k) __attribute__((always_inline)) { bias[place(id)] = p.bias_values[k]; });
+            __syncthreads();
+        }
+        // one that is listed: its count and bias
+        auto shape = [&](float x, bool seen, int k) __attribute__((always_inline)) -> float {
+            const int at = before[k >> 5] + __popc(listed[k >> 5] & ((1u << (k & 31)) - 1u));
+            const uint32_t c = counts[at];
+            if (c != 0u && !seen)
+                x *= x > 0.f ? inv_rep : rep;
+            if (c != 0u)
+                x = x - freq * (float)c - pres;
+            return x + bias[at];
+        };
+        const uint32_t listed_words = any && 32 * lane < tile_len ? listed[tile0 / 32 + lane] : 0u;
+#pragma unroll
+        for (int u = 0; u < ROUNDS; ++u) {
+            // the lane's four bits: of word 8 u + lane / 8, from bit 4 (lane % 8) on
+            const int from = 8 * u + (lane >> 3), shift = 4 * (lane & 7);
+            const uint32_t bits = (uint32_t)__shfl((int)listed_words, from) >> shift & 0xfu;
+            const uint32_t seen = (uint32_t)__shfl((int)seen_words, from) >> shift & 0xfu;
+            const uint32_t allowed = (uint32_t)__shfl((int)allowed_words, from) >> shift & 0xfu;
+            const int k = tile0 + 256 * u + 4 * lane;
+            if (k < len) {
+                float x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    x[e] = raw[u].get(e);
+                if (seen != 0u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float y = x[e] * (x[e] > 0.f ? inv_rep : rep);
+                        x[e] = (seen >> e) & 1u ? y : x[e];
+                    }
+                if (bits != 0u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if ((bits >> e) & 1u)
+                            x[e] = shape(x[e], (seen >> e) & 1u, k + e);
+                if (allowed != 0xfu)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        x[e] = (allowed >> e) & 1u ? x[e] : -INFINITY;
+                if (len - k >= 4) {
+                    typedef float __attribute__((ext_vector_type(4), aligned(4))) any4;
+                    const any4 y = {x[0], x[1], x[2], x[3]};
+                    *reinterpret_cast<any4*>(out + s0 + k) = y;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 3; ++e)
+                        if (e < len - k)
+                            out[s0 + k + e] = x[e];
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);  // (the rounds' shuffles would otherwise all be kept in registers)
+        }
+        s0 += len;
     }
 }
 
@@ -100,8 +282,23 @@ hipError_t launch_mark_tokens(const int* tokens, const int* indptr, long long pr
 
 hipError_t launch_penalize_logits(const LogitsParams& p, hipStream_t s)
 {
-    const long long slices = (p.vocab + kSlice - 1) / kSlice;
-    hipLaunchKernelGGL(penalize_kernel, dim3((unsigned)(p.rows * slices)), dim3(kThreads), 0, s, p, (int)slices);
+    // Short slices fill the chip where rows are few, long ones read a row's history fewer times.
+    auto go = [&](auto rounds) {
+        constexpr int R = decltype(rounds)::value;
+        const long long slices = (p.vocab + slice_tokens(R) - 1) / slice_tokens(R);
+        const dim3 grid((unsigned)((p.rows + 7) / 8 * 8 * slices));
+        if (p.bf16)
+            hipLaunchKernelGGL((penalize_kernel<true, R>), grid, dim3(kThreads), 0, s, p, (int)slices);
+        else
+            hipLaunchKernelGGL((penalize_kernel<false, R>), grid, dim3(kThreads), 0, s, p, (int)slices);
+    };
+    const long long tokens = p.rows * p.vocab;
+    if (tokens >= 4096ll * slice_tokens(8))
+        go(std::integral_constant<int, 8>{});
+    else if (tokens >= 1024ll * slice_tokens(2))
+        go(std::integral_constant<int, 4>{});
+    else
+        go(std::integral_constant<int, 1>{});
     return hipGetLastError();
 }
 

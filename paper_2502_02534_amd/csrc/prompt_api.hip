@@ -13,6 +13,7 @@ using namespace spd::plan;
 inline bool misaligned(const void* p, size_t a) { return ((uintptr_t)p % a) != 0; }
 
 constexpr int64_t kMostInt = 0x7fffffff;
+constexpr int64_t kMostBlocks = 1ll << 22;  // workgroups of up to 1024 threads: a launch counts its threads in 32 bits
 
 }  // namespace
 
@@ -157,7 +158,7 @@ int write_prompt_kv(const spd_prompt_desc* desc, const void* k, const void* v, c
     p.head_u4 = desc->head_dim * elt / 16;
     p.stride_u4 = desc->kv_stride != 0 ? desc->kv_stride * elt / 16 : (long long)p.Hkv * p.head_u4;
     p.page_size = desc->page_size;
-    if (num_tokens > kMostInt * 256ll / ((long long)p.Hkv * p.head_u4))
+    if (num_tokens > kMostBlocks * 1024 / ((long long)p.Hkv * p.head_u4))
         return SPD_EUNSUPPORTED;
     return spd::launch_kv_write(p, (hipStream_t)stream) == hipSuccess ? SPD_OK : SPD_ELAUNCH;
 }
@@ -169,7 +170,7 @@ int mark_prompt_tokens(const int32_t* tokens, const int32_t* indptr, int64_t num
         return SPD_EINVAL;
     if (misaligned(tokens, 4) || misaligned(indptr, 4) || misaligned(bits, 4))
         return SPD_EINVAL;
-    if (vocab > (1 << 20) || num_prompts > kMostInt)
+    if (vocab > (1 << 20) || num_prompts >= kMostBlocks)
         return SPD_EUNSUPPORTED;
     return spd::launch_mark_tokens(tokens, indptr, num_prompts, vocab, bits, bits_stride, accumulate != 0,
                                    (hipStream_t)stream) == hipSuccess ? SPD_OK : SPD_ELAUNCH;
@@ -182,7 +183,7 @@ int penalize_logits(const void* logits, int32_t logits_dtype, int64_t rows, int6
         return SPD_EINVAL;
     if (logits_dtype != SPD_F32 && logits_dtype != SPD_BF16)
         return SPD_EUNSUPPORTED;
-    if (vocab > (1ll << 30) || rows > kMostInt || pen->max_tokens > (1ll << 24))
+    if (vocab > (1ll << 30) || rows > kMostBlocks / ((vocab + 16383) / 16384) - 8 || pen->max_tokens > (1ll << 24))
         return SPD_EUNSUPPORTED;
     if (misaligned(logits, logits_dtype == SPD_BF16 ? 2 : 4) || misaligned(out, 4))
         return SPD_EINVAL;

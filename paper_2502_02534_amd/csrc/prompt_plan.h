@@ -71,7 +71,7 @@ inline int make_prompt_plan(const spd_prompt_desc* d, int64_t total, int64_t max
     splits = splits > 1 ? splits : 1;
     if (rows == 256)
         splits = 1;
-    if (units > most / splits)
+    if (units > (1ll << 23) / splits)  // a launch counts its threads in 32 bits
         return SPD_EUNSUPPORTED;
     out->block_rows = rows;
     out->tiles = (int)tiles;
