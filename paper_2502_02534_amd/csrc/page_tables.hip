@@ -2,8 +2,12 @@
 // step needs no round trip to the host between admitting requests and running them.
 //
 // need_i = pages request i lacks; a request is served while the running sum of need fits the free list (and
-// always when it needs nothing).  Three running sums follow: pages, free pages and new tokens.  One workgroup
-// takes the sums, then every entry of the page list and of the slot map is found by bisection.
+// always when it needs nothing).  Three running sums follow: pages, free pages and new tokens.  Every entry of the page
+// list and of the slot map is then found by bisection in the sums.
+//
+// Up to kFew requests are one launch: every workgroup takes the sums of all requests by itself, into LDS, and fills
+// its share of the entries (a second launch that waits for the first costs more than the sums).  More requests are
+// two launches: one workgroup leaves the sums in memory, the others bisect there.
 #include "spd_internal.h"
 
 namespace spd {
@@ -137,10 +141,179 @@ __global__ __launch_bounds__(kThreads) void page_fill_kernel(PageTableParams p, 
     }
 }
 
+// ---- one launch ------------------------------------------------------------------------------------------------
+constexpr int kFew = 2048;
+constexpr int kFewThreads = 512;
+constexpr int kEach = kFew / kFewThreads;  // requests a thread
+constexpr int kFill = 2;                   // entries a thread
+
+// Sums over the wavefronts before this one, of one value a wavefront in `lds`.
+template <typename T, typename F> __device__ __forceinline__ T earlier(const T* lds, F add)
+{
+    T x = 0;
+#pragma unroll
+    for (int w = 0; w < kFewThreads / 64 - 1; ++w)
+        x = add(x, w < (int)(threadIdx.x >> 6) ? lds[w] : (T)0);
+    return x;
+}
+
+template <bool HELD>
+__global__ __launch_bounds__(kFewThreads) void page_tables_kernel(PageTableParams p, unsigned page_blocks)
+{
+    __shared__ int page_starts[kFew + 1], new_starts[kFew + 1], free_starts[kFew];
+    __shared__ int held_first[HELD ? kFew + 1 : 1], had_tokens[HELD ? kFew : 1];
+    __shared__ uint32_t wave_need[kFewThreads / 64];
+    __shared__ int wave_pages[kFewThreads / 64], wave_taken[kFewThreads / 64], wave_fresh[kFewThreads / 64];
+    const int n = (int)p.n, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int begin = p.free_begin ? *p.free_begin : 0;
+    const uint32_t room = (uint32_t)max(p.num_free - begin, 0ll);
+    const auto sat = [](uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); };
+    const auto add = [](int a, int b) { return a + b; };
+    int held[kEach], had[kEach], want[kEach];
+    uint32_t need[kEach], mine = 0u;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int i = tid * kEach + k;
+        held[k] = had[k] = want[k] = 0;
+        if (i < n) {
+            if constexpr (HELD) {
+                const int first = p.held_indptr[i];
+                held_first[i] = first;
+                held[k] = p.held_indptr[i + 1] - first;
+                had[k] = p.held_lens[i];
+                had_tokens[i] = had[k];
+                if (i == n - 1)
+                    held_first[n] = first + held[k];
+            }
+            want[k] = max(p.lens[i], max(had[k], 0));
+        }
+        const unsigned pages = ((unsigned)want[k] + (unsigned)p.page_size - 1u) / (unsigned)p.page_size;
+        need[k] = (uint32_t)max((int)pages - held[k], 0);
+        mine = sat(mine, need[k]);
+    }
+    uint32_t upto = mine;  // saturating: a sum past 2^32 fits no free list either
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t x = (uint32_t)__shfl_up((int)upto, o);
+        upto = lane >= o ? sat(upto, x) : upto;
+    }
+    uint32_t before = (uint32_t)__shfl_up((int)upto, 1);
+    before = lane == 0 ? 0u : before;
+    if (lane == 63)
+        wave_need[wave] = upto;
+    __syncthreads();
+    before = sat(before, earlier(wave_need, sat));
+    int pages[kEach], taken[kEach], fresh[kEach];  // running sums within the thread
+    int sum_pages = 0, sum_taken = 0, sum_fresh = 0;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        before = sat(before, need[k]);
+        const bool granted = need[k] == 0u || before <= room;
+        const int get = granted ? (int)need[k] : 0;
+        want[k] = granted ? want[k] : had[k];
+        pages[k] = sum_pages;
+        taken[k] = sum_taken;
+        fresh[k] = sum_fresh;
+        sum_pages += held[k] + get;
+        sum_taken += get;
+        sum_fresh += want[k] - had[k];
+    }
+    int up_pages = sum_pages, up_taken = sum_taken, up_fresh = sum_fresh;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int a = __shfl_up(up_pages, o), b = __shfl_up(up_taken, o), c = __shfl_up(up_fresh, o);
+        up_pages += lane >= o ? a : 0;
+        up_taken += lane >= o ? b : 0;
+        up_fresh += lane >= o ? c : 0;
+    }
+    if (lane == 63) {
+        wave_pages[wave] = up_pages;
+        wave_taken[wave] = up_taken;
+        wave_fresh[wave] = up_fresh;
+    }
+    __syncthreads();
+    const int base_pages = up_pages - sum_pages + earlier(wave_pages, add);
+    const int base_taken = begin + up_taken - sum_taken + earlier(wave_taken, add);
+    const int base_fresh = up_fresh - sum_fresh + earlier(wave_fresh, add);
+    const bool writes = blockIdx.x == 0;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int i = tid * kEach + k;
+        if (i <= n) {  // (request n holds nothing: its starts are the totals)
+            page_starts[i] = base_pages + pages[k];
+            new_starts[i] = base_fresh + fresh[k];
+            if (writes) {
+                p.page_indptr[i] = base_pages + pages[k];
+                p.new_indptr[i] = base_fresh + fresh[k];
+            }
+        }
+        if (i < n) {
+            free_starts[i] = base_taken + taken[k];
+            if (writes)
+                p.lens_out[i] = want[k];
+        }
+    }
+    if (tid == kFewThreads - 1) {
+        const int all = base_taken + sum_taken;
+        if (n == kFew) {
+            page_starts[n] = base_pages + sum_pages;
+            new_starts[n] = base_fresh + sum_fresh;
+            if (writes) {
+                p.page_indptr[n] = base_pages + sum_pages;
+                p.new_indptr[n] = base_fresh + sum_fresh;
+            }
+        }
+        if (writes)
+            *p.free_end = all;
+    }
+    __syncthreads();
+    const auto page_at = [&](int i, int k) -> int {
+        const int first = HELD ? held_first[i] : 0, mine_held = HELD ? held_first[i + 1] - first : 0;
+        return HELD && k < mine_held ? p.held_pages[first + k] : p.free_pages[free_starts[i] + k - mine_held];
+    };
+    const bool slots = blockIdx.x >= page_blocks;
+    const long long first = (long long)(blockIdx.x - (slots ? page_blocks : 0u)) * kFewThreads * kFill + tid;
+    const int* starts = slots ? new_starts : page_starts;
+    const long long total = starts[n], most = slots ? p.max_tokens : p.max_pages;
+#pragma unroll
+    for (int u = 0; u < kFill; ++u) {
+        const long long t = first + u * kFewThreads;
+        if (t >= most)
+            return;
+        long long got = -1;
+        if (t < total) {
+            const int i = range_of(starts, n, t), k = (int)(t - starts[i]);
+            if (slots) {
+                const unsigned at = (unsigned)((HELD ? had_tokens[i] : 0) + k), page = at / (unsigned)p.page_size;
+                got = (long long)page_at(i, (int)page) * p.page_size + (at - page * (unsigned)p.page_size);
+            } else {
+                got = page_at(i, k);
+            }
+        }
+        if (slots)
+            p.slot_map[t] = got;
+        else
+            p.page_indices[t] = (int)got;
+    }
+}
+
 }  // namespace
 
 hipError_t launch_page_tables(const PageTableParams& p, hipStream_t s)
 {
+    if (p.n <= kFew) {
+        const long long per_block = (long long)kFewThreads * kFill;
+        const long long page_blocks = (p.max_pages + per_block - 1) / per_block;
+        const long long slot_blocks = p.slot_map ? (p.max_tokens + per_block - 1) / per_block : 0;
+        const long long blocks = page_blocks + slot_blocks > 0 ? page_blocks + slot_blocks : 1;
+        const dim3 grid((unsigned)blocks), block(kFewThreads);
+        // (with no page entries at all the one workgroup there is fills none)
+        if (p.held_lens)
+            hipLaunchKernelGGL(page_tables_kernel<true>, grid, block, 0, s, p, (unsigned)(slot_blocks > 0 ? page_blocks : blocks));
+        else
+            hipLaunchKernelGGL(page_tables_kernel<false>, grid, block, 0, s, p, (unsigned)(slot_blocks > 0 ? page_blocks : blocks));
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL(page_sums_kernel, dim3(1), dim3(kScanThreads), 0, s, p);
     const long long per_block = (long long)kThreads * kPerThread;
     const long long page_blocks = (p.max_pages + per_block - 1) / per_block;
