@@ -67,12 +67,12 @@ int prompt_attn(const spd_prompt_desc* desc, const void* q, const void* k, const
     p.kv_lens = kv_lens;
     p.kv_indptr = kv_indptr;
     p.pages = kv_page_indices;
-    p.block_rows = pl.block_rows;
     p.tiles = pl.tiles;
     p.num_splits = pl.num_splits;
+    p.split_tokens = pl.split_tokens;
     p.rows = total_queries * p.Hq;
-    p.part_acc = (float*)workspace;
-    p.part_ml = (float2*)((char*)workspace + pl.acc_bytes);
+    p.part_acc = workspace;
+    p.part_ml = (float4*)((char*)workspace + pl.acc_bytes);
     p.out = out;
     p.lse = lse_out;
     return spd::launch_prompt_attn(p, (hipStream_t)stream) == hipSuccess ? SPD_OK : SPD_ELAUNCH;

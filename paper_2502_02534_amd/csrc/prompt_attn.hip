@@ -13,10 +13,16 @@
 // What a row must not see enters nowhere: scores are replaced, not added to, and where a tile holds tokens that
 // some of its rows do not see and values that are not finite (0 * inf is not 0), its tokens are added one by
 // one, each to the rows that see it.
-#include "spd_internal.h"
+#include "prompt_units.h"
+
+#include <hip/hip_fp16.h>
 
 namespace spd {
 namespace {
+
+using prompt_impl::find_unit;
+using prompt_impl::kRows;
+using prompt_impl::Unit;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -27,7 +33,6 @@ typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTileN = 32;      // tokens per tile
-constexpr int kBlockRows = 128;
 constexpr int kThreads = 256;
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
@@ -35,36 +40,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
     const f32x2 v = {lo, hi};
     const bf16x2 r = __builtin_convertvector(v, bf16x2);
     return *reinterpret_cast<const uint32_t*>(&r);
-}
-
-// The prompt and row tile of tile number `item`: prompts in order, each one's longest tiles (its last) first.
-struct TileOf {
-    int b, tile;
-};
-__device__ __forceinline__ TileOf find_tile(const PromptParams& p, int item)
-{
-    const int lane = threadIdx.x & 63;
-    int base = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-        const int b = b0 + lane;
-        int n = 0;
-        if (b < p.B)
-            n = (max(p.query_indptr[b + 1] - p.query_indptr[b], 0) * p.G + kBlockRows - 1) / kBlockRows;
-        int upto = n;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int x = __shfl_up(upto, o);
-            upto += lane >= o ? x : 0;
-        }
-        const int all = __builtin_amdgcn_readfirstlane(__shfl(upto, 63));
-        if (item < base + all) {
-            const int l = __ffsll((unsigned long long)__ballot(item < base + upto)) - 1;
-            const int before = __shfl(upto - n, l), tiles = __shfl(n, l);
-            return {__builtin_amdgcn_readfirstlane(b0 + l), __builtin_amdgcn_readfirstlane(tiles - 1 - (item - base - before))};
-        }
-        base += all;
-    }
-    return {-1, 0};
 }
 
 // Operands of the two products for an element type; a piece is 16 bytes.
@@ -225,30 +200,30 @@ __global__ __launch_bounds__(kThreads) void prompt_attn_kernel(PromptParams p)
     __shared__ __align__(16) char lds_v[kTileN * M::kStrideV];
     __shared__ uint32_t lds_odd[2];  // whether a tile holds values that are not finite
 
-    const int j = blockIdx.x % p.Hkv, unit = blockIdx.x / p.Hkv, split = unit % p.num_splits;
-    const TileOf at = find_tile(p, unit / p.num_splits);
-    if (at.b < 0)
+    const int j = blockIdx.x % p.Hkv;
+    const Unit at = find_unit(p, blockIdx.x / p.Hkv);
+    if (!at.any)
         return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, h = lane >> 5;
-    const int q0 = p.query_indptr[at.b], n = p.query_indptr[at.b + 1] - q0, L = p.kv_lens[at.b];
-    const int row0 = at.tile * kBlockRows, rr = row0 + wave * 32 + col;
+    const int q0 = at.q0, n = at.n, L = at.L;
+    const int row0 = at.tile * kRows, rr = row0 + wave * 32 + col;
     const bool row_ok = rr < n * p.G;
     const int token = (row_ok ? rr : 0) / p.G, head = j * p.G + (row_ok ? rr : 0) % p.G;
     // the last token a row sees, and the first and last row's
     const int limit = !row_ok ? -1 : p.causal ? L - n + token : L - 1;
-    const int last_row = min(row0 + kBlockRows, n * p.G) - 1;
+    const int last_row = min(row0 + kRows, n * p.G) - 1;
     const int least = p.causal ? L - n + row0 / p.G : L - 1, most = p.causal ? L - n + last_row / p.G : L - 1;
 
-    // this split's tokens
+    // this part's tokens
     const int seen = max(most + 1, 0);
-    const int part = ((seen + p.num_splits - 1) / p.num_splits + kTileN - 1) / kTileN * kTileN;
-    const int t0 = min(split * part, seen), t1 = min(t0 + part, seen);
+    const int t0 = p.num_splits > 1 ? min(at.split * at.split_tokens, seen) : 0;
+    const int t1 = p.num_splits > 1 ? min(t0 + at.split_tokens, seen) : seen;
 
     M mat;
     mat.load_q((const char*)p.q + ((long long)(q0 + token) * p.q_stride + (long long)head * p.D) * E, p.D, h, row_ok);
 
-    const int first = p.kv_indptr[at.b];
+    const int first = at.kv0;
     auto offset = [&](int t) -> long long {  // of token t's row of this KV head, in bytes
         if (p.page_size != 0)
             return (((long long)p.pages[first + (t >> 4)] * p.Hkv + j) * 16 + (t & 15)) * p.D * E;
@@ -339,9 +314,15 @@ __global__ __launch_bounds__(kThreads) void prompt_attn_kernel(PromptParams p)
         return;
     const long long row = (long long)(q0 + token) * p.Hq + head;
     if (p.num_splits > 1) {
-        if (h == 0)
-            p.part_ml[row * p.num_splits + split] = make_float2(m, l);
-        float* dst = p.part_acc + (row * p.num_splits + split) * p.D;
+        if (h == 0) {
+            p.part_ml[row * p.num_splits + at.split] = make_float4(m, l, 1.f, 0.f);
+            if (at.split == 0)  // and the parts that this prompt does not have
+                for (int s = at.splits; s < p.num_splits; ++s)
+                    p.part_ml[row * p.num_splits + s] = make_float4(-INFINITY, 0.f, 1.f, 0.f);
+        }
+        if (t0 >= t1)
+            return;
+        float* dst = (float*)p.part_acc + (row * p.num_splits + at.split) * p.D;
 #pragma unroll
         for (int db = 0; db < DP / 32; ++db)
 #pragma unroll
@@ -372,59 +353,120 @@ __global__ __launch_bounds__(kThreads) void prompt_attn_kernel(PromptParams p)
         }
 }
 
-// Joins the splits of a row: with states (m_i, l_i, acc_i), m = max m_i and w_i = 2^(m_i - m),
-// out = sum w_i acc_i / sum w_i l_i.  One thread per four channels of a row.
-template <typename T>
+// Joins the parts of a row: with states (m_i, l_i, acc_i), m = max m_i and w_i = 2^(m_i - m),
+// out = sum w_i acc_i / sum w_i l_i.  LANES lanes take a row, 16 bytes of a part each; they also take its parts' (m, l, scale)
+// and hand their weights round.  Bound by the partial states, all of whose loads a lane has in flight kBatch at a time.
+template <typename T, bool HALF, int LANES>
 __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptParams p)
 {
-    const int quads = p.D / 4;
-    const long long i = (long long)blockIdx.x * kThreads + threadIdx.x, row = i / quads;
-    const int c = (int)(i % quads) * 4;
-    if (row >= (long long)p.query_indptr[p.B] * p.Hq)
-        return;
-    const float2* ml = p.part_ml + row * p.num_splits;
+    constexpr int kRowsPerBlock = kThreads / LANES, kBatch = 8, kCh = HALF ? 8 : 4;
+    const int lane = threadIdx.x % LANES, first_lane = (threadIdx.x & 63) - lane, c = lane * kCh;
+    const long long row = (long long)blockIdx.x * kRowsPerBlock + threadIdx.x / LANES;
+    const bool row_ok = row < (long long)p.query_indptr[p.B] * p.Hq && row < p.rows;
+    const int S = p.num_splits;
+    const float4* ml = p.part_ml + (row_ok ? row : 0) * S;
+    const char* parts = (const char*)p.part_acc + ((row_ok ? row : 0) * S * p.D + (c < p.D ? c : 0)) * (HALF ? 2 : 4);
+    const long long part_bytes = (long long)p.D * (HALF ? 2 : 4);
     float m = -INFINITY;
-    for (int s = 0; s < p.num_splits; ++s)
-        m = fmaxf(m, ml[s].x);
-    const float ref = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s = 0; s < p.num_splits; ++s) {
-        const float w = __builtin_amdgcn_exp2f(ml[s].x - ref);
-        const float4 a = *reinterpret_cast<const float4*>(p.part_acc + (row * p.num_splits + s) * p.D + c);
-        l = fmaf(w, ml[s].y, l);
-        acc.x = fmaf(w, a.x, acc.x);
-        acc.y = fmaf(w, a.y, acc.y);
-        acc.z = fmaf(w, a.z, acc.z);
-        acc.w = fmaf(w, a.w, acc.w);
+    for (int s = lane; s < S; s += LANES) {
+        const float4 x = ml[s];
+        m = x.y != 0.f ? fmaxf(m, x.x) : m;
     }
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1)
+        m = fmaxf(m, __shfl_xor(m, o));
+    float l = 0.f, acc[kCh];
+#pragma unroll
+    for (int e = 0; e < kCh; ++e)
+        acc[e] = 0.f;
+    for (int s0 = 0; s0 < S; s0 += LANES) {  // LANES weights at a time
+        float w = 0.f;
+        if (s0 + lane < S) {
+            const float4 x = ml[s0 + lane];
+            if (x.y != 0.f) {  // (a sum that is not a number stays one)
+                const float u = __builtin_amdgcn_exp2f(x.x - m);
+                l = fmaf(u, x.y, l);
+                w = HALF ? u * x.y * x.z : u;
+            }
+        }
+        const int here = min(LANES, S - s0);
+        for (int k0 = 0; k0 < here; k0 += kBatch) {
+            uint4 a[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k)
+                a[k] = *reinterpret_cast<const uint4*>(parts + min(s0 + k0 + k, S - 1) * part_bytes);
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const float ws = __shfl(w, first_lane + min(k0 + k, LANES - 1));
+                if (ws != 0.f && k0 + k < here) {  // (a part that holds nothing was not written)
+                    const uint32_t v[4] = {a[k].x, a[k].y, a[k].z, a[k].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if constexpr (HALF) {
+                            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v[e]));
+                            acc[2 * e] = fmaf(ws, f.x, acc[2 * e]);
+                            acc[2 * e + 1] = fmaf(ws, f.y, acc[2 * e + 1]);
+                        } else {
+                            acc[e] = fmaf(ws, __uint_as_float(v[e]), acc[e]);
+                        }
+                    }
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1)
+        l += __shfl_xor(l, o);
+    if (!row_ok)
+        return;
     const bool none = l == 0.f;
     const float inv = none ? 0.f : 1.f / l;
-    if (p.lse && c == 0)
+    if (p.lse && lane == 0)
         p.lse[row] = none ? -INFINITY : m * kLn2 + logf(l);
-    if constexpr (sizeof(T) == 2)
-        *reinterpret_cast<uint2*>((char*)p.out + (row * p.D + c) * 2) =
-            make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-    else
-        *reinterpret_cast<float4*>((char*)p.out + (row * p.D + c) * 4) =
-            make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    if (c >= p.D)
+        return;
+    char* dst = (char*)p.out + (row * p.D + c) * (long long)sizeof(T);
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int e = 0; e < kCh; e += 4)
+            *reinterpret_cast<uint2*>(dst + 2 * e) =
+                make_uint2(pack_bf16(acc[e] * inv, acc[e + 1] * inv), pack_bf16(acc[e + 2] * inv, acc[e + 3] * inv));
+    } else {
+        *reinterpret_cast<float4*>(dst) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+    }
+}
+
+template <typename T, bool HALF, int LANES> void launch_merge(const PromptParams& p, hipStream_t s)
+{
+    constexpr int kRowsPerBlock = kThreads / LANES;
+    hipLaunchKernelGGL((prompt_merge_kernel<T, HALF, LANES>), dim3((unsigned)((p.rows + kRowsPerBlock - 1) / kRowsPerBlock)),
+                       dim3(kThreads), 0, s, p);
 }
 
 template <typename T>
 hipError_t launch(const PromptParams& p, hipStream_t s)
 {
     const dim3 grid((unsigned)((long long)p.tiles * p.num_splits * p.Hkv)), block(kThreads);
-    if (sizeof(T) == 2 && (p.D == 64 || p.D == 128))
-        launch_prompt_mfma(p, s);
-    else if (p.D <= 64)
+    if (sizeof(T) == 2 && (p.D == 64 || p.D == 128)) {
+        const hipError_t e = launch_prompt_mfma(p, s);
+        if (e != hipSuccess)
+            return e;
+        if (p.num_splits > 1)
+            p.D == 64 ? launch_merge<T, true, 8>(p, s) : launch_merge<T, true, 16>(p, s);
+        return hipGetLastError();
+    }
+    if (p.D <= 64) {
         hipLaunchKernelGGL((prompt_attn_kernel<T, 64>), grid, block, 0, s, p);
-    else if (p.D <= 128)
+        if (p.num_splits > 1)
+            launch_merge<T, false, 16>(p, s);
+    } else if (p.D <= 128) {
         hipLaunchKernelGGL((prompt_attn_kernel<T, 128>), grid, block, 0, s, p);
-    else
+        if (p.num_splits > 1)
+            launch_merge<T, false, 32>(p, s);
+    } else {
         hipLaunchKernelGGL((prompt_attn_kernel<T, 256>), grid, block, 0, s, p);
-    if (p.num_splits > 1) {
-        const long long items = p.rows * (p.D / 4);
-        hipLaunchKernelGGL(prompt_merge_kernel<T>, dim3((unsigned)((items + kThreads - 1) / kThreads)), block, 0, s, p);
+        if (p.num_splits > 1)
+            launch_merge<T, false, 64>(p, s);
     }
     return hipGetLastError();
 }

@@ -1,7 +1,7 @@
 // prompt_attn for bf16 with 64 or 128 channels: the tiled kernel (prompt_attn.hip holds the general one and the
 // definition of rows, tiles and splits).
 //
-// Workgroup = (tile of 32 WAVES rows, KV head, split); a wavefront owns 32 rows.  K and V tiles of 32 tokens go from
+// Workgroup = (unit, KV head), four wavefronts that own 32 rows each.  K and V tiles of 32 tokens go from
 // global memory straight into LDS (global_load_lds_dwordx4), kAhead tiles before their use, with the 16-byte pieces
 // of a row swizzled on the global side so that both operand reads are free of bank conflicts: K with
 // ds_read_b128, V with the transposing ds_read_b64_tr_b16.  The reads are issued by hand a few fragments ahead of
@@ -12,6 +12,7 @@
 // one barrier a tile.  The others (the causal edge, a prompt's ragged end) follow one by one with the mask;
 // wavefronts whose rows see nothing of such a tile skip it.
 #include "attn_prefix_body.h"
+#include "prompt_units.h"
 
 namespace spd {
 namespace {
@@ -24,8 +25,12 @@ using prefix_impl::pack_bf16_rne;
 using prefix_impl::u32x2;
 using prefix_impl::u32x4;
 using prefix_impl::wait_vmcnt;
+using prompt_impl::find_unit;
+using prompt_impl::kRows;
+using prompt_impl::Unit;
 
 constexpr int kTileN = 32;
+constexpr int kWaves = 4;
 constexpr int kAhead = 3;             // tiles under way
 constexpr int kRingK = kAhead + 1;    // and the one whose scores are taken
 constexpr int kRingV = kAhead + 3;    // and those of the three in work
@@ -48,51 +53,21 @@ template <int D> struct Shape {
     }
 };
 
-// Which prompt and tile: as in the general kernel, with ROWS rows a tile.
-struct TileOf {
-    int b, tile;
-};
-template <int ROWS> __device__ __forceinline__ TileOf find_tile(const PromptParams& p, int item)
-{
-    const int lane = threadIdx.x & 63;
-    int base = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-        const int b = b0 + lane;
-        int n = 0;
-        if (b < p.B)
-            n = (max(p.query_indptr[b + 1] - p.query_indptr[b], 0) * p.G + ROWS - 1) / ROWS;
-        int upto = n;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int x = __shfl_up(upto, o);
-            upto += lane >= o ? x : 0;
-        }
-        const int all = __builtin_amdgcn_readfirstlane(__shfl(upto, 63));
-        if (item < base + all) {
-            const int l = __ffsll((unsigned long long)__ballot(item < base + upto)) - 1;
-            const int before = __shfl(upto - n, l), tiles = __shfl(n, l);
-            return {__builtin_amdgcn_readfirstlane(b0 + l), __builtin_amdgcn_readfirstlane(tiles - 1 - (item - base - before))};
-        }
-        base += all;
-    }
-    return {-1, 0};
-}
-
-template <int D, int WAVES, bool PAGED>
-__global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(PromptParams p)
+template <int D, bool PAGED>
+__global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParams p)
 {
     using S = Shape<D>;
-    constexpr int kRows = 32 * WAVES, kIPW = 2 * S::kCopies / WAVES;
-    static_assert(kIPW >= 1, "a copy for every wavefront");
+    constexpr int kIPW = 2 * S::kCopies / kWaves;
+    static_assert(kIPW >= 1 && kRows == 32 * kWaves, "a copy for every wavefront");
     __shared__ __align__(16) char lds[S::kLds];
 
-    const int j = blockIdx.x % p.Hkv, unit = blockIdx.x / p.Hkv, split = unit % p.num_splits;
-    const TileOf at = find_tile<kRows>(p, unit / p.num_splits);
-    if (at.b < 0)
+    const int j = blockIdx.x % p.Hkv;
+    const Unit at = find_unit(p, blockIdx.x / p.Hkv);
+    if (!at.any)
         return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, h = lane >> 5;
-    const int q0 = p.query_indptr[at.b], n = p.query_indptr[at.b + 1] - q0, L = p.kv_lens[at.b];
+    const int q0 = at.q0, n = at.n, L = at.L;
     const int rows = n * p.G, row0 = at.tile * kRows, rr = row0 + wave * 32 + col;
     const bool row_ok = rr < rows;
     const int token = (row_ok ? rr : 0) / p.G, head = j * p.G + (row_ok ? rr : 0) % p.G;
@@ -104,8 +79,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(PromptParams
     const int wave_most = wave_last < row0 + wave * 32 ? -1 : p.causal ? L - n + wave_last / p.G : L - 1;
 
     const int seen = max(most + 1, 0);
-    const int part = ((seen + p.num_splits - 1) / p.num_splits + kTileN - 1) / kTileN * kTileN;
-    const int t0 = min(split * part, seen), t1 = min(t0 + part, seen);
+    const int t0 = p.num_splits > 1 ? min(at.split * at.split_tokens, seen) : 0;
+    const int t1 = p.num_splits > 1 ? min(t0 + at.split_tokens, seen) : seen;
     const int ntiles = (t1 - t0 + kTileN - 1) / kTileN;
     int nfull = max(min(least + 1, t1) - t0, 0) / kTileN;  // tiles that every row sees whole
     if (nfull < 3)
@@ -126,15 +101,15 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(PromptParams
 
     // ---- global -> LDS copies: the first half of the wavefronts copies K, the other half V, kIPW instructions a tile each
     typedef const __attribute__((address_space(4))) int* const_int_ptr;
-    const const_int_ptr pages = PAGED ? (const_int_ptr)(p.pages + p.kv_indptr[at.b]) : nullptr;
+    const const_int_ptr pages = PAGED ? (const_int_ptr)(p.pages + at.kv0) : nullptr;
     const long long tok_stride = PAGED ? S::kRow : p.kv_stride * 2;
-    const long long head_base = PAGED ? (long long)j * 16 * S::kRow : (long long)p.kv_indptr[at.b] * p.kv_stride * 2 + (long long)j * S::kRow;
+    const long long head_base = PAGED ? (long long)j * 16 * S::kRow : (long long)at.kv0 * p.kv_stride * 2 + (long long)j * S::kRow;
     const long long page_stride = (long long)p.Hkv * 16 * S::kRow;
     const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) void*)lds;
     constexpr int kLanesPerRow = 64 / S::kRowsPerCopy;
     const int lane_row = lane / kLanesPerRow, lane_piece = lane % kLanesPerRow;
-    const bool copies_v = wave >= WAVES / 2;
-    const int row_first = S::kRowsPerCopy * kIPW * (copies_v ? wave - WAVES / 2 : wave);
+    const bool copies_v = wave >= kWaves / 2;
+    const int row_first = S::kRowsPerCopy * kIPW * (copies_v ? wave - kWaves / 2 : wave);
     unsigned lane_off[kIPW];
 #pragma unroll
     for (int i = 0; i < kIPW; ++i) {
@@ -432,7 +407,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(PromptParams
         const bool some = tb <= wave_most;
         {
             bool any = false;
-            for (int i = tid; i < S::kTile / 16; i += WAVES * 64) {
+            for (int i = tid; i < S::kTile / 16; i += kWaves * 64) {
                 u32x4 v;
                 const unsigned addr = lds_base + (unsigned)(kRingK + vslot) * S::kTile + i * 16;
                 asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=v"(v) : "v"(addr));
@@ -486,20 +461,44 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(PromptParams
 
     // ---- results ---------------------------------------------------------------------------------------------------------
     const float l = l_run + __shfl_xor(l_run, 32);
-    if (!row_ok)
-        return;
     if (p.num_splits > 1) {
-        if (h == 0)
-            p.part_ml[out_row * p.num_splits + split] = make_float2(m_run, l);
-        float* dst = p.part_acc + (out_row * p.num_splits + split) * D;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        float top = 0.f;
 #pragma unroll
         for (int db = 0; db < S::kDB; ++db)
 #pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4)
-                *reinterpret_cast<float4*>(dst + 32 * db + 8 * q4 + 4 * h) =
-                    make_float4(o[db][4 * q4], o[db][4 * q4 + 1], o[db][4 * q4 + 2], o[db][4 * q4 + 3]);
+            for (int i = 0; i < 16; ++i) {
+                o[db][i] *= inv;
+                const float x = fabsf(o[db][i]);
+                top = x < INFINITY ? fmaxf(top, x) : top;
+            }
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (!row_ok)
+            return;
+        // the power of two in [top, 2 top)'s place, but none so small that its inverse overflows
+        const float scale = __uint_as_float(max(__float_as_uint(top) & 0x7f800000u, 0x01000000u)), unscale = 1.f / scale;
+        if (h == 0) {
+            p.part_ml[out_row * p.num_splits + at.split] = make_float4(m_run, l, scale, 0.f);
+            if (at.split == 0)  // and the parts that this prompt does not have
+                for (int s = at.splits; s < p.num_splits; ++s)
+                    p.part_ml[out_row * p.num_splits + s] = make_float4(kNever, 0.f, 1.f, 0.f);
+        }
+        if (t0 >= t1)
+            return;
+        __half* dst = (__half*)p.part_acc + (out_row * p.num_splits + at.split) * D;
+#pragma unroll
+        for (int db = 0; db < S::kDB; ++db)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+                const __half2 lo = __floats2half2_rn(o[db][4 * q4] * unscale, o[db][4 * q4 + 1] * unscale);
+                const __half2 hi = __floats2half2_rn(o[db][4 * q4 + 2] * unscale, o[db][4 * q4 + 3] * unscale);
+                *reinterpret_cast<uint2*>(dst + 32 * db + 8 * q4 + 4 * h) =
+                    make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+            }
         return;
     }
+    if (!row_ok)
+        return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     if (p.lse && h == 0)
         p.lse[out_row] = l == 0.f ? -INFINITY : m_run * kLn2 + logf(l);
@@ -513,23 +512,20 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(PromptParams
                            pack_bf16_rne(o[db][4 * q4 + 2] * inv, o[db][4 * q4 + 3] * inv));
 }
 
-template <int D, int WAVES> void launch(const PromptParams& p, hipStream_t s)
+template <int D> void launch(const PromptParams& p, hipStream_t s)
 {
-    const dim3 grid((unsigned)((long long)p.tiles * p.num_splits * p.Hkv)), block(WAVES * 64);
+    const dim3 grid((unsigned)((long long)p.tiles * p.num_splits * p.Hkv)), block(kWaves * 64);
     if (p.page_size != 0)
-        hipLaunchKernelGGL((prompt_mfma_kernel<D, WAVES, true>), grid, block, 0, s, p);
+        hipLaunchKernelGGL((prompt_mfma_kernel<D, true>), grid, block, 0, s, p);
     else
-        hipLaunchKernelGGL((prompt_mfma_kernel<D, WAVES, false>), grid, block, 0, s, p);
+        hipLaunchKernelGGL((prompt_mfma_kernel<D, false>), grid, block, 0, s, p);
 }
 
 }  // namespace
 
 hipError_t launch_prompt_mfma(const PromptParams& p, hipStream_t s)
 {
-    if (p.D == 128)
-        p.block_rows == 256 ? launch<128, 8>(p, s) : launch<128, 4>(p, s);
-    else
-        p.block_rows == 256 ? launch<64, 8>(p, s) : launch<64, 4>(p, s);
+    p.D == 128 ? launch<128>(p, s) : launch<64>(p, s);
     return hipGetLastError();
 }
 

@@ -11,13 +11,15 @@ namespace spd {
 namespace plan {
 
 struct PromptPlan {
-    int block_rows;  // (token, head of the group) rows per workgroup
-    int tiles;       // upper bound on the row tiles of all prompts, one KV head
-    int num_splits;  // parts of a tile's tokens
+    int tiles;         // upper bound on the row tiles of all prompts, one KV head
+    int num_splits;    // most parts of a prompt's tokens
+    int split_tokens;  // fewest tokens of a part (the device knows the lengths, and how many tokens make the parts few enough)
     size_t acc_bytes, ml_bytes;
 };
 
-constexpr int kPromptMaxSplits = 32;
+constexpr int kPromptRows = 128;       // (token, head of the group) rows per workgroup
+constexpr int kPromptPlaces = 512;     // workgroups that run at once
+constexpr int kPromptMaxSplits = 64;
 constexpr int kPromptMinTokens = 128;  // per split
 
 inline int check_prompt_desc(const spd_prompt_desc* d, bool queries)
@@ -41,8 +43,8 @@ inline int check_prompt_desc(const spd_prompt_desc* d, bool queries)
     return SPD_OK;
 }
 
-// bf16 with 64 or 128 channels runs on the tiled kernel.
-inline bool prompt_tiled(const spd_prompt_desc* d) { return d->dtype == SPD_BF16 && (d->head_dim == 64 || d->head_dim == 128); }
+// bf16 with 64 or 128 channels runs on the tiled kernel, which leaves its partial states in fp16.
+inline bool prompt_half_states(const spd_prompt_desc* d) { return d->dtype == SPD_BF16 && (d->head_dim == 64 || d->head_dim == 128); }
 
 inline int make_prompt_plan(const spd_prompt_desc* d, int64_t total, int64_t max_query, int64_t max_kv, PromptPlan* out)
 {
@@ -57,28 +59,29 @@ inline int make_prompt_plan(const spd_prompt_desc* d, int64_t total, int64_t max
         return SPD_EUNSUPPORTED;
     const int64_t group = d->num_q_heads / d->num_kv_heads;
     // a prompt's last tile may be partly filled, and no prompt has more tiles than its longest
-    auto tiles_of = [&](int64_t rows) {
-        const int64_t per_prompt = (max_query * group + rows - 1) / rows, all = total * group / rows + d->num_prompts;
-        return per_prompt <= all / d->num_prompts ? per_prompt * d->num_prompts : all;
-    };
-    const bool tiled = prompt_tiled(d);
-    const int rows = tiled && tiles_of(256) * d->num_kv_heads >= 256 ? 256 : 128;
-    const int64_t tiles = tiles_of(rows), units = tiles * d->num_kv_heads;
-    int64_t splits = units > 0 ? (512 + units - 1) / units : 1;
-    const int64_t whole = max_kv / kPromptMinTokens;
-    splits = splits < whole ? splits : whole;
-    splits = splits < kPromptMaxSplits ? splits : kPromptMaxSplits;
+    const int64_t per_prompt = (max_query * group + kPromptRows - 1) / kPromptRows;
+    int64_t tiles = total * group / kPromptRows + d->num_prompts;
+    if (per_prompt <= tiles / d->num_prompts)
+        tiles = per_prompt * d->num_prompts;
+    // Where the tiles alone do not fill the chip, the tokens are cut into parts, which another launch joins.
+    const int64_t units = tiles * d->num_kv_heads;
+    int64_t tokens = max_kv;
+    if (units > 0 && units < kPromptPlaces) {
+        tokens = units * max_kv / (2 * kPromptPlaces);
+        const int64_t least = max_kv / kPromptMaxSplits > kPromptMinTokens ? max_kv / kPromptMaxSplits : kPromptMinTokens;
+        tokens = tokens > least ? tokens : least;
+    }
+    tokens = (tokens + 31) / 32 * 32;
+    int64_t splits = tokens > 0 ? (max_kv + tokens - 1) / tokens : 1;
     splits = splits > 1 ? splits : 1;
-    if (rows == 256)
-        splits = 1;
     if (units > (1ll << 23) / splits)  // a launch counts its threads in 32 bits
         return SPD_EUNSUPPORTED;
-    out->block_rows = rows;
     out->tiles = (int)tiles;
     out->num_splits = (int)splits;
+    out->split_tokens = (int)tokens;
     const size_t states = splits > 1 ? (size_t)total * d->num_q_heads * splits : 0;
-    out->acc_bytes = (states * d->head_dim * sizeof(float) + 255) / 256 * 256;
-    out->ml_bytes = (states * 2 * sizeof(float) + 255) / 256 * 256;
+    out->acc_bytes = (states * d->head_dim * (prompt_half_states(d) ? 2 : 4) + 255) / 256 * 256;
+    out->ml_bytes = states * 4 * sizeof(float);
     return SPD_OK;
 }
 

@@ -1,0 +1,94 @@
+// Which piece of a prompt_attn call a workgroup takes, shared by its kernels.
+//
+// Work is cut into units: (prompt, tile of kPromptRows rows, part of split_tokens tokens), times the KV heads.  The
+// host knows only bounds on the lengths, so the units of each prompt are counted on the device, by every wavefront
+// for itself: 64 prompts at a time, a lane each, with everything about the prompt that the workgroup needs.
+//
+// Parts.  A part costs its rows' partial states (written once, read once by the launch that joins them) besides a workgroup's
+// start, so there are no more than run at once: with W = sum of tiles * tokens and T = number of tiles, over all KV heads,
+// parts of W / (kPlaces - T) tokens are at most kPlaces, because a prompt's last part is the only one that is not full.
+#pragma once
+
+#include "spd_internal.h"
+
+namespace spd {
+namespace prompt_impl {
+
+constexpr int kRows = 128;   // (new token, head of the group) rows per workgroup
+constexpr int kPlaces = 512; // workgroups that run at once: two a CU
+
+struct Unit {
+    bool any;           // false: past the last unit
+    int q0, n, L, kv0;  // the prompt's first query and their number, its tokens, its place in the KV table
+    int tile;           // the prompt's last tiles, which see most, come first
+    int split, splits;  // of the prompt's tokens
+    int split_tokens;
+};
+
+__device__ __forceinline__ int row_tiles(const PromptParams& p, int n) { return (n * p.G + kRows - 1) / kRows; }
+
+// Tokens of a part: the same in every lane of every wavefront.
+__device__ __forceinline__ int part_tokens(const PromptParams& p)
+{
+    const int lane = threadIdx.x & 63;
+    float work = 0.f, tiles = 0.f;
+    for (int b = lane; b < p.B; b += 64) {
+        const float t = (float)row_tiles(p, max(p.query_indptr[b + 1] - p.query_indptr[b], 0));
+        tiles += t;
+        work += t * (float)max(p.kv_lens[b], 0);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        work += __shfl_xor(work, o);
+        tiles += __shfl_xor(tiles, o);
+    }
+    const float parts = fmaxf((float)kPlaces - tiles * (float)p.Hkv, 1.f);
+    const float even = fminf(work * (float)p.Hkv / parts, 1e9f);
+    const int tokens = ((int)even + 32) & ~31;
+    return __builtin_amdgcn_readfirstlane(max(tokens, p.split_tokens));
+}
+
+__device__ __forceinline__ Unit find_unit(const PromptParams& p, int item)
+{
+    const int lane = threadIdx.x & 63;
+    Unit u;
+    u.any = false;
+    u.q0 = u.n = u.L = u.kv0 = u.tile = u.split = 0;
+    u.splits = 1;
+    u.split_tokens = p.num_splits > 1 ? part_tokens(p) : 0;
+    int base = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        const int b = min(b0 + lane, p.B - 1);
+        const int q0 = p.query_indptr[b], n = max(p.query_indptr[b + 1] - q0, 0), L = p.kv_lens[b], kv0 = p.kv_indptr[b];
+        const int tiles = b0 + lane < p.B ? row_tiles(p, n) : 0;
+        const int splits = p.num_splits > 1 ? min(max((L + u.split_tokens - 1) / u.split_tokens, 1), p.num_splits) : 1;
+        const int units = tiles * splits;
+        int upto = units;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(upto, o);
+            upto += lane >= o ? x : 0;
+        }
+        const int all = __builtin_amdgcn_readfirstlane(__shfl(upto, 63));
+        if (item < base + all) {
+            const int l = __ffsll((unsigned long long)__ballot(item < base + upto)) - 1;
+            const auto of = [&](int x) { return __builtin_amdgcn_readfirstlane(__shfl(x, l)); };
+            u.any = true;
+            u.q0 = of(q0);
+            u.n = of(n);
+            u.L = of(L);
+            u.kv0 = of(kv0);
+            u.splits = of(splits);
+            // the tiles of a part follow one another: they read the same tokens
+            const int local = item - base - of(upto - units), t = of(tiles);
+            u.split = local / t;
+            u.tile = t - 1 - local % t;
+            break;
+        }
+        base += all;
+    }
+    return u;
+}
+
+}  // namespace prompt_impl
+}  // namespace spd

@@ -143,12 +143,14 @@ struct PromptParams {
     const int* kv_lens;
     const int* kv_indptr;
     const int* pages;
-    int block_rows;  // rows per workgroup
-    int tiles;       // upper bound on the row tiles of all prompts
-    int num_splits;  // parts a tile's tokens are cut into
-    long long rows;  // total_queries * Hq
-    float* part_acc;   // [rows][splits][D], unnormalised sums; null with one split
-    float2* part_ml;   // [rows][splits] (m, l)
+    int tiles;         // upper bound on the row tiles of all prompts
+    int num_splits;    // most parts that a prompt's tokens are cut into
+    int split_tokens;  // fewest tokens of a part
+    long long rows;    // total_queries * Hq
+    // Partial states, [rows][num_splits]: (m, l, scale), l = 0 where a part holds nothing, and the sums: fp32 as they are
+    // (scale 1), or (bf16) divided by l and by the scale, a power of two that brings the row into the range of fp16.
+    void* part_acc;
+    float4* part_ml;
     void* out;
     float* lse;        // may be null
 };
