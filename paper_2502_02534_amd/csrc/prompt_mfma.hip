@@ -86,15 +86,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
     if (nfull < 3)
         nfull = 0;
 
-    // ---- query fragments (B operand): column = this lane's row, channels 16 s + 8 h
+    // ---- query fragments (B operand): column = this lane's row, channels 16 s + 8 h (a lane without a row of its own takes
+    // the first token's: nothing of it is stored)
     bf16x8 qf[S::kQK];
     {
         const uint4* qg = (const uint4*)((const char*)p.q + ((long long)(q0 + token) * p.q_stride + (long long)head * D) * 2);
 #pragma unroll
         for (int s = 0; s < S::kQK; ++s) {
-            uint4 v = qg[2 * s + h];
-            if (!row_ok)
-                v = make_uint4(0, 0, 0, 0);
+            const uint4 v = qg[2 * s + h];
             qf[s] = as_bf16x8(v);
         }
     }
@@ -261,8 +260,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
                 }
             }
         };
-        constexpr int kPer = (18 + NF - 1) / NF;                   // softmax slots per product
-        constexpr int kLead = kPer * NF >= 18 + 2 ? 0 : 18 > kPer * NF ? 18 - kPer * NF : 0;
+        constexpr int kPer = 18 / NF > 0 ? 18 / NF : 1, kLead = 18 - kPer * NF;  // slots per product, and before the first
+        static_assert(!SM || kLead >= 0, "every score gets its slot");
         for_each_index(issue, std::make_integer_sequence<int, kFragAhead + 1>{});
         if constexpr (SM) {
             for_each_index(soft, std::make_integer_sequence<int, kLead>{});
