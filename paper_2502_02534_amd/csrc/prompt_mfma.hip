@@ -458,57 +458,58 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
         end_of_step(t);
     }
 
-    // ---- results ---------------------------------------------------------------------------------------------------------
+    // ---- results: through LDS (the rings are free), so that a row leaves in whole lines ------------------------------------
     const float l = l_run + __shfl_xor(l_run, 32);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    __builtin_amdgcn_s_barrier();
+    char* const mine = lds + wave * 32 * S::kRow;
+    auto place = [&](int row, int piece) __attribute__((always_inline)) -> char* {
+        return mine + row * S::kRow + ((piece ^ (row & (S::kRow / 16 - 1))) << 4);
+    };
+    // Rows 0 .. 31 of the wavefront to `first` + out_row * `pitch`, two halves of a pair from `pack`.
+    auto store_rows = [&](auto pack, char* first, long long pitch) __attribute__((always_inline)) {
+#pragma unroll
+        for (int db = 0; db < S::kDB; ++db)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4)  // registers 4 q4 .. + 3 are channels 32 db + 8 q4 + 4 h .. + 3
+                *reinterpret_cast<uint2*>(place(col, 4 * db + q4) + 8 * h) =
+                    make_uint2(pack(o[db][4 * q4], o[db][4 * q4 + 1]), pack(o[db][4 * q4 + 2], o[db][4 * q4 + 3]));
+        const int to = row_ok ? (int)out_row : -1;
+#pragma unroll
+        for (int i = 0; i < S::kCopies; ++i) {
+            const int row = S::kRowsPerCopy * i + lane_row, dst = __shfl(to, row);
+            if (dst >= 0)
+                *reinterpret_cast<uint4*>(first + dst * pitch + lane_piece * 16) = *reinterpret_cast<const uint4*>(place(row, lane_piece));
+        }
+    };
     if (p.num_splits > 1) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
         float top = 0.f;
 #pragma unroll
         for (int db = 0; db < S::kDB; ++db)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                o[db][i] *= inv;
-                const float x = fabsf(o[db][i]);
+                const float x = fabsf(o[db][i] * inv);
                 top = x < INFINITY ? fmaxf(top, x) : top;
             }
         top = fmaxf(top, __shfl_xor(top, 32));
-        if (!row_ok)
-            return;
-        // the power of two in [top, 2 top)'s place, but none so small that its inverse overflows
+        // the largest power of two up to it, but none whose inverse overflows
         const float scale = __uint_as_float(max(__float_as_uint(top) & 0x7f800000u, 0x01000000u)), unscale = 1.f / scale;
-        if (h == 0) {
+        if (h == 0 && row_ok) {
             p.part_ml[out_row * p.num_splits + at.split] = make_float4(m_run, l, scale, 0.f);
             if (at.split == 0)  // and the parts that this prompt does not have
                 for (int s = at.splits; s < p.num_splits; ++s)
                     p.part_ml[out_row * p.num_splits + s] = make_float4(kNever, 0.f, 1.f, 0.f);
         }
-        if (t0 >= t1)
-            return;
-        __half* dst = (__half*)p.part_acc + (out_row * p.num_splits + at.split) * D;
-#pragma unroll
-        for (int db = 0; db < S::kDB; ++db)
-#pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4) {
-                const __half2 lo = __floats2half2_rn(o[db][4 * q4] * unscale, o[db][4 * q4 + 1] * unscale);
-                const __half2 hi = __floats2half2_rn(o[db][4 * q4 + 2] * unscale, o[db][4 * q4 + 3] * unscale);
-                *reinterpret_cast<uint2*>(dst + 32 * db + 8 * q4 + 4 * h) =
-                    make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-            }
+        if (t0 < t1)
+            store_rows([&](float x, float y) __attribute__((always_inline)) {
+                const __half2 v = __floats2half2_rn(x * inv * unscale, y * inv * unscale);
+                return *reinterpret_cast<const uint32_t*>(&v);
+            }, (char*)p.part_acc + at.split * S::kRow, (long long)p.num_splits * S::kRow);
         return;
     }
-    if (!row_ok)
-        return;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    if (p.lse && h == 0)
+    if (p.lse && h == 0 && row_ok)
         p.lse[out_row] = l == 0.f ? -INFINITY : m_run * kLn2 + logf(l);
-    char* dst = (char*)p.out + out_row * S::kRow;
-#pragma unroll
-    for (int db = 0; db < S::kDB; ++db)
-#pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4)
-            *reinterpret_cast<uint2*>(dst + (32 * db + 8 * q4 + 4 * h) * 2) =
-                make_uint2(pack_bf16_rne(o[db][4 * q4] * inv, o[db][4 * q4 + 1] * inv),
-                           pack_bf16_rne(o[db][4 * q4 + 2] * inv, o[db][4 * q4 + 3] * inv));
+    store_rows([&](float x, float y) __attribute__((always_inline)) { return pack_bf16_rne(x * inv, y * inv); }, (char*)p.out, S::kRow);
 }
 
 template <int D> void launch(const PromptParams& p, hipStream_t s)
