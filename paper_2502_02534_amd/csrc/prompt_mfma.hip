@@ -2,7 +2,7 @@
 // definition of rows, tiles and splits).
 //
 // Workgroup = (unit, KV head), four wavefronts that own 32 rows each.  K and V tiles of 32 tokens go from
-// global memory straight into LDS (global_load_lds_dwordx4), kAhead tiles before their use, with the 16-byte pieces
+// global memory straight into LDS (global_load_lds_dwordx4), two or three tiles before their use, with the 16-byte pieces
 // of a row swizzled on the global side so that both operand reads are free of bank conflicts: K with
 // ds_read_b128, V with the transposing ds_read_b64_tr_b16.  The reads are issued by hand a few fragments ahead of
 // the product that takes them, with exact waits (the compiler would drain the copies before every LDS read).
@@ -31,9 +31,7 @@ using prompt_impl::Unit;
 
 constexpr int kTileN = 32;
 constexpr int kWaves = 4;
-constexpr int kAhead = 3;             // tiles under way
-constexpr int kRingK = kAhead + 1;    // and the one whose scores are taken
-constexpr int kRingV = kAhead + 3;    // and those of the three in work
+constexpr int kRing = 4;              // slots of K and of V: the tile in use and up to three under way
 constexpr int kFragAhead = 4;         // LDS fragments in flight
 constexpr float kNever = -1e30f;      // reference maximum of a row that has seen nothing: finite, so that no exponent is inf - inf
 constexpr float kRaise = 1024.f;
@@ -42,7 +40,7 @@ template <int D> struct Shape {
     static constexpr int kRow = 2 * D, kTile = kTileN * kRow;  // bytes
     static constexpr int kRowsPerCopy = 1024 / kRow, kCopies = kTile / 1024;
     static constexpr int kQK = D / 16, kDB = D / 32, kPV = 2 * kDB;  // fragments
-    static constexpr int kLds = (kRingK + kRingV) * kTile;  // 80 KB with 128 channels: two workgroups per CU
+    static constexpr int kLds = 2 * kRing * kTile + 16;  // K, V, a flag; 64 KB with 128 channels: two workgroups per CU
     // Piece p of a row lies in slot p ^ swz(row): sixteen rows' equal pieces take all 64 banks, and so do the four rows and
     // 64 bytes that half a wavefront's transposing reads touch.
     static __device__ __forceinline__ int swz(int row)
@@ -53,6 +51,10 @@ template <int D> struct Shape {
     }
 };
 
+// A ring slot that is known at compile time, 0 for one that is a number.
+constexpr int slot_constant(int) { return 0; }
+template <int N> constexpr int slot_constant(std::integral_constant<int, N>) { return N; }
+
 template <int D, bool PAGED>
 __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParams p)
 {
@@ -60,6 +62,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
     constexpr int kIPW = 2 * S::kCopies / kWaves;
     static_assert(kIPW >= 1 && kRows == 32 * kWaves, "a copy for every wavefront");
     __shared__ __align__(16) char lds[S::kLds];
+    volatile uint32_t* const odd_flag = (volatile uint32_t*)(lds + 2 * kRing * S::kTile);
 
     const int j = blockIdx.x % p.Hkv;
     const Unit at = find_unit(p, blockIdx.x / p.Hkv);
@@ -116,18 +119,16 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
         lane_off[i] = (unsigned)(tl * (unsigned)tok_stride + ((lane_piece ^ S::swz(row_first + tl)) << 4));
     }
     const char* const tensor = (const char*)(copies_v ? p.v : p.k);
-    char* const ring_lds = lds + (copies_v ? kRingK * S::kTile : 0) + row_first * S::kRow;
-    const int ring = copies_v ? kRingV : kRingK;
+    char* const ring_lds = lds + (copies_v ? kRing * S::kTile : 0) + row_first * S::kRow;
     int next_page = 0;
     auto fetch_page = [&](int tile) __attribute__((always_inline)) {
         if (PAGED)
             next_page = pages[min(t0 + tile * kTileN + row_first, t1 - 1) >> 4];
     };
-    int slot_next = 0;  // ring slot of the next tile to be copied
-    auto issue_tile = [&](int tile) __attribute__((always_inline)) {
-        const int tb = t0 + tile * kTileN;
-        char* const dst = ring_lds + slot_next * S::kTile;
-        slot_next = slot_next + 1 == ring ? 0 : slot_next + 1;
+    int issued = -1;  // last tile whose copies this wavefront has started
+    auto issue_next = [&]() __attribute__((always_inline)) {
+        const int tile = ++issued, tb = t0 + tile * kTileN;
+        char* const dst = ring_lds + (tile % kRing) * S::kTile;
         const bool full = tb + kTileN <= t1;
         const int tg = min(tb + row_first, t1 - 1);  // this wavefront's first row; rows past the end repeat the last token
         const char* const src = PAGED ? tensor + (long long)next_page * page_stride + head_base + (tg & 15) * S::kRow
@@ -144,25 +145,28 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
         }
         fetch_page(tile + 1);
     };
-    auto start_copies = [&](int tile) __attribute__((always_inline)) {
-        if (tile < ntiles)
-            issue_tile(tile);
+    auto copies_up_to = [&](int tile) __attribute__((always_inline)) {
+#pragma unroll 1
+        while (issued < min(tile, ntiles - 1))
+            issue_next();
     };
-    // Waits until at most `tiles` later tiles of this wavefront's copies are under way, then for everybody.
-    auto wait_copies = [&](int tiles) __attribute__((always_inline)) {
-        if (tiles >= kAhead - 1)
-            wait_vmcnt<(kAhead - 1) * kIPW>();
-        else if (tiles == 1)
+    // Waits until this wavefront's copies of `tile` have landed (later ones may be under way), then for everybody.
+    auto landed = [&](int tile) __attribute__((always_inline)) {
+        const int later = issued - tile;
+        if (later >= 2)
+            wait_vmcnt<2 * kIPW>();
+        else if (later == 1)
             wait_vmcnt<kIPW>();
         else
             wait_vmcnt<0>();
         __builtin_amdgcn_s_barrier();
     };
-    static_assert(kAhead == 3, "wait_copies lists the counts below kAhead - 1");
 
-    // ---- per-lane LDS addresses of the operand fragments, relative to a tile
-    const unsigned k_row = (unsigned)(col * S::kRow), k_xor = (unsigned)((h ^ S::swz(col)) << 4);
-    unsigned v_off[S::kDB][2];
+    // ---- per-lane LDS addresses of the operand fragments in slot 0; the slot goes into the instruction's offset
+    unsigned k_addr[S::kQK], v_addr[S::kDB][2];
+#pragma unroll
+    for (int s = 0; s < S::kQK; ++s)
+        k_addr[s] = lds_base + (unsigned)(col * S::kRow) + ((32u * s) ^ (unsigned)((h ^ S::swz(col)) << 4));
     {
         const int g16 = (lane >> 4) & 1, r = (lane & 15) >> 2, q4 = lane & 3;
 #pragma unroll
@@ -170,7 +174,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
 #pragma unroll
             for (int part2 = 0; part2 < 2; ++part2) {
                 const int tok = 8 * part2 + 4 * h + r, piece = 4 * db + 2 * g16 + (q4 >> 1);
-                v_off[db][part2] = (unsigned)(tok * S::kRow + ((piece ^ S::swz(tok)) << 4) + (q4 & 1) * 8);
+                v_addr[db][part2] = lds_base + (unsigned)(kRing * S::kTile + tok * S::kRow + ((piece ^ S::swz(tok)) << 4) + (q4 & 1) * 8);
             }
     }
 
@@ -184,19 +188,15 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
 
     u32x4 ring_k[kFragAhead + 2];
     u32x2 ring_lo[kFragAhead + 2], ring_hi[kFragAhead + 2];
-    // Fragment order of a region: the two products alternate where both are there.
     // One region: scores of the tile in K slot `kslot` into `sn` (QK), P V of the tile in V slot `vslot` with
-    // probabilities `pp` (PV), and between the products the probabilities `pn` of the scores `so` (SM; their sum over the
+    // probabilities `pp` (PV; the two products alternate; slots are constants or numbers), and between the products the probabilities `pn` of the scores `so` (SM; their sum over the
     // lane is returned).
-    auto region = [&](auto qk_tag, auto sm_tag, auto pv_tag, int kslot, int vslot, floatx16& sn, const floatx16& so,
+    auto region = [&](auto qk_tag, auto sm_tag, auto pv_tag, auto kslot, auto vslot, floatx16& sn, const floatx16& so,
                       bf16x8 (&pn)[2], const bf16x8 (&pp)[2]) __attribute__((always_inline)) -> float {
         constexpr bool QK = decltype(qk_tag)::value, SM = decltype(sm_tag)::value, PV = decltype(pv_tag)::value;
         constexpr bool kBoth = QK && PV;
         static_assert(S::kQK == S::kPV, "as many fragments of either product");
         constexpr int NF = (QK ? S::kQK : 0) + (PV ? S::kPV : 0);
-        unsigned kbase = lds_base + (unsigned)kslot * S::kTile;
-        unsigned vbase = lds_base + (unsigned)(kRingK + vslot) * S::kTile;
-        asm("" : "+s"(kbase), "+s"(vbase));
         if (QK) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
@@ -207,18 +207,27 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
             if constexpr (K < NF) {
                 constexpr int idx = kBoth ? K >> 1 : K;
                 constexpr bool is_pv = kBoth ? (K & 1) != 0 : PV;
+                constexpr bool fixed = !std::is_same<decltype(kslot), int>::value;
                 if constexpr (!is_pv) {
-                    const unsigned addr = kbase + k_row + ((32u * idx) ^ k_xor);
                     u32x4& dst = ring_k[K % (kFragAhead + 2)];
-                    asm volatile("ds_read_b128 %0, %1" : "=v"(dst) : "v"(addr));
+                    unsigned addr = k_addr[idx];
+                    constexpr int kSlot = slot_constant(decltype(kslot){}) * S::kTile;
+                    if constexpr (!fixed)
+                        addr += (unsigned)kslot * S::kTile;
+                    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(dst) : "v"(addr), "n"(kSlot));
                 } else {
                     constexpr int a = idx / S::kDB, b = idx % S::kDB;
                     u32x2& lo = ring_lo[K % (kFragAhead + 2)];
                     u32x2& hi = ring_hi[K % (kFragAhead + 2)];
-                    const unsigned a0 = vbase + v_off[b][0], a1 = vbase + v_off[b][1];
+                    unsigned a0 = v_addr[b][0], a1 = v_addr[b][1];
+                    constexpr int kSlot = slot_constant(decltype(vslot){}) * S::kTile;
+                    if constexpr (!fixed) {
+                        a0 += (unsigned)vslot * S::kTile;
+                        a1 += (unsigned)vslot * S::kTile;
+                    }
                     asm volatile("ds_read_b64_tr_b16 %0, %2 offset:%4\n\tds_read_b64_tr_b16 %1, %3 offset:%4"
                                  : "=&v"(lo), "=&v"(hi)
-                                 : "v"(a0), "v"(a1), "n"(a * 16 * S::kRow));
+                                 : "v"(a0), "v"(a1), "n"(kSlot + a * 16 * S::kRow));
                 }
             }
         };
@@ -335,80 +344,85 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
     };
 
     // ---- the pipeline ---------------------------------------------------------------------------------------------------
-    // Step t starts the copies of tile t + kAhead (into slots that a barrier has freed: K of tile t - 1, V of tile t - 3), runs its
-    // region, and waits until K and V of tile t + 1 have landed for everybody.
+    // Step t starts the copies of K of tile t + 3 and V of tile t + 1 (into slots that a barrier has freed: K of tile t - 1, V of
+    // tile t - 3), runs its region (scores of tile t, P V of tile t - 2), and waits until K of tile t + 1 and V of tile t - 1 have
+    // landed for everybody.  The four slots make four steps one round of the loop.
     const std::true_type yes{};
     const std::false_type no{};
     floatx16 sa, sb;
     bf16x8 pa[2], pb[2];
-    auto end_of_step = [&](int t) __attribute__((always_inline)) { wait_copies(ntiles - 2 - t); };
+    const int lead = copies_v && nfull > 0 ? 1 : 3, lag = copies_v ? 1 : -1;
     if (ntiles > 0) {
         fetch_page(0);
-#pragma unroll
-        for (int t = 0; t < kAhead; ++t)
-            start_copies(t);
-        // tile 0 has landed once at most the kAhead - 1 tiles after it are under way
-        wait_copies(ntiles - 1);
+        copies_up_to(lead - 1);
+        landed(0);
     }
     int t = 0;
     if (nfull > 0) {
-        start_copies(kAhead);
-        region(yes, no, no, 0, 0, sb, sb, pa, pa);
-        end_of_step(0);
-        raise_maximum(sb);
-        start_copies(1 + kAhead);
-        take_sum(region(yes, yes, no, 1 % kRingK, 0, sa, sb, pb, pa), sb, pb);
-        end_of_step(1);
-        // scores of tile t - 1 are in sa, probabilities of tile t - 2 in pb
-        int ks = 2 % kRingK, vs = 0;
-        auto next = [&] __attribute__((always_inline)) {
-            ks = ks + 1 == kRingK ? 0 : ks + 1;
-            vs = vs + 1 == kRingV ? 0 : vs + 1;
+        // One step with its slots as constants: the scores of even tiles are in sa, those of odd ones in sb.
+        auto step = [&](auto tc) __attribute__((always_inline)) {
+            constexpr int T = decltype(tc)::value;
+            const std::integral_constant<int, T % kRing> kslot;
+            const std::integral_constant<int, (T + 2) % kRing> vslot;
+            copies_up_to(t + lead);
+            if constexpr (T % 2 == 0)
+                take_sum(region(yes, yes, yes, kslot, vslot, sa, sb, pb, pa), sb, pb);
+            else
+                take_sum(region(yes, yes, yes, kslot, vslot, sb, sa, pa, pb), sa, pa);
+            landed(t - lag);
+            ++t;
         };
-        for (t = 2; t + 1 < nfull; t += 2) {
-            start_copies(t + kAhead);
-            take_sum(region(yes, yes, yes, ks, vs, sb, sa, pa, pb), sa, pa);
-            end_of_step(t);
-            next();
-            start_copies(t + 1 + kAhead);
-            take_sum(region(yes, yes, yes, ks, vs, sa, sb, pb, pa), sb, pb);
-            end_of_step(t + 1);
-            next();
+        copies_up_to(lead);
+        region(yes, no, no, std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{}, sa, sa, pa, pa);
+        landed(copies_v ? 0 : 1);
+        raise_maximum(sa);
+        copies_up_to(1 + lead);
+        take_sum(region(yes, yes, no, std::integral_constant<int, 1>{}, std::integral_constant<int, 0>{}, sb, sa, pa, pb), sa, pa);
+        landed(1 - lag);
+        t = 2;
+        while (true) {  // (nfull > 2)
+            step(std::integral_constant<int, 2>{});
+            if (t >= nfull)
+                break;
+            step(std::integral_constant<int, 3>{});
+            if (t >= nfull)
+                break;
+            step(std::integral_constant<int, 0>{});
+            if (t >= nfull)
+                break;
+            step(std::integral_constant<int, 1>{});
+            if (t >= nfull)
+                break;
         }
-        if (t < nfull) {
-            start_copies(t + kAhead);
-            take_sum(region(yes, yes, yes, ks, vs, sb, sa, pa, pb), sa, pa);
-            end_of_step(t);
-            next();
-            sa = sb;
-            pb[0] = pa[0];
-            pb[1] = pa[1];
+        // The scores of tile t - 1 and the probabilities of tile t - 2 are left; V of tile t - 2 has landed.
+        if (t & 1) {
+            sb = sa;
+            pa[0] = pb[0];
+            pa[1] = pb[1];
         }
-        t = nfull;
-        // drain: softmax of the last tile beside P V of the one before, then its own P V
-        take_sum(region(no, yes, yes, 0, vs, sb, sa, pa, pb), sa, pa);
-        next();
-        region(no, no, yes, 0, vs, sa, sa, pa, pa);
-        __builtin_amdgcn_s_barrier();  // the V slots of these two tiles are free for everybody
+        copies_up_to(t + (copies_v ? 1 : 2));
+        take_sum(region(no, yes, yes, 0, (t - 2) % kRing, sa, sb, pb, pa), sb, pb);
+        landed(copies_v ? t - 1 : min(t, ntiles - 1));
+        copies_up_to(t + 2);
+        region(no, no, yes, 0, (t - 1) % kRing, sa, sa, pa, pb);
+        landed(min(t, ntiles - 1));
     }
 
     // ---- tiles that some row does not see whole ------------------------------------------------------------------------------
     for (; t < ntiles; ++t) {
-        const int tb = t0 + t * kTileN, kslot = t % kRingK, vslot = t % kRingV;
-        // Does the tile hold values that are not finite (0 * inf is not 0)?  Its copies have landed; the flag lies in a V
-        // slot that is free here: of the six, tile t takes one and the copies under way three.
-        volatile uint32_t* const odd_flag = (volatile uint32_t*)(lds + (kRingK + (t + 4) % kRingV) * S::kTile);
+        const int tb = t0 + t * kTileN, slot = t % kRing;
+        // Does the tile hold values that are not finite (0 * inf is not 0)?  Its copies have landed.
         if (tid == 0)
             *odd_flag = 0u;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
-        start_copies(t + kAhead);  // (K of tile t - 1 and V of tile t - 3 are free for everybody from here on)
+        copies_up_to(t + 3);  // (the slots of tile t - 1 are free for everybody from here on)
         const bool some = tb <= wave_most;
         {
             bool any = false;
             for (int i = tid; i < S::kTile / 16; i += kWaves * 64) {
                 u32x4 v;
-                const unsigned addr = lds_base + (unsigned)(kRingK + vslot) * S::kTile + i * 16;
+                const unsigned addr = lds_base + (unsigned)(kRing + slot) * S::kTile + i * 16;
                 asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=v"(v) : "v"(addr));
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
@@ -418,7 +432,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
                 *odd_flag = 1u;
         }
         if (some) {
-            region(yes, no, no, kslot, 0, sa, sa, pa, pa);
+            region(yes, no, no, slot, 0, sa, sa, pa, pa);
             const int end = min(limit, t1 - 1) - tb - 4 * h;
 #pragma unroll
             for (int i = 0; i < 16; ++i)
@@ -429,24 +443,24 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
         __builtin_amdgcn_s_barrier();
         const bool odd = __builtin_amdgcn_readfirstlane(*odd_flag) != 0u;
         if (some && !odd) {
-            region(no, no, yes, 0, vslot, sa, sa, pa, pa);
+            region(no, no, yes, 0, slot, sa, sa, pa, pa);
         } else if (some) {
             // token by token, to the rows (lanes) that see it
             for (int x = 0; x < kTileN; ++x) {
-                const int slot = (x >> 3) * 4 + (x & 3);  // place among the lane's 16 probabilities
+                const int nth = (x >> 3) * 4 + (x & 3);  // among the lane's 16 probabilities
                 const bool own = h == ((x >> 2) & 1), sees = tb + x <= min(limit, t1 - 1);
                 uint32_t pw = 0u;
 #pragma unroll
                 for (int u = 0; u < 8; ++u) {
                     const u32x4 q = *reinterpret_cast<const u32x4*>(&pa[u >> 2]);
-                    pw = u == (slot >> 1) ? q[u & 3] : pw;
+                    pw = u == (nth >> 1) ? q[u & 3] : pw;
                 }
-                pw = own ? ((slot & 1) ? pw >> 16 : pw & 0xffffu) : 0u;
+                pw = own ? ((nth & 1) ? pw >> 16 : pw & 0xffffu) : 0u;
                 const u32x4 b = {pw, 0u, 0u, 0u};
 #pragma unroll
                 for (int db = 0; db < S::kDB; ++db) {
                     const int c = 32 * db + col;  // channel
-                    const char* v = lds + (kRingK + vslot) * S::kTile + x * S::kRow + (((c >> 3) ^ S::swz(x)) << 4) + (c & 7) * 2;
+                    const char* v = lds + (kRing + slot) * S::kTile + x * S::kRow + (((c >> 3) ^ S::swz(x)) << 4) + (c & 7) * 2;
                     const u32x4 a = {own ? (uint32_t)*(volatile const uint16_t*)v : 0u, 0u, 0u, 0u};
                     const floatx16 sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(b), o[db], 0, 0, 0);
 #pragma unroll
@@ -455,7 +469,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
                 }
             }
         }
-        end_of_step(t);
+        if (t + 1 < ntiles)
+            landed(t + 1);
     }
 
     // ---- results: through LDS (the rings are free), so that a row leaves in whole lines ------------------------------------
