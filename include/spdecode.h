@@ -389,7 +389,7 @@ SPD_API int decode_step_advance(int64_t *step_state, int64_t num_steps,
 /*
  * Description of a batch of prompts (host memory, read during the call only).  Query head h reads KV
  * head h / (num_q_heads / num_kv_heads).  Supported: dtype bf16 or f32, head_dim a multiple of 8 up to
- * 256, page_size 0 (contiguous KV) or 16.  Strides are in elements and a multiple of 16 bytes.
+ * 256, page_size 0 (contiguous KV) or 16.  Strides are in elements, a multiple of 16 bytes, up to 2^24.
  */
 typedef struct spd_prompt_desc {
     int32_t dtype;        /* spd_dtype of q, k, v and the output */

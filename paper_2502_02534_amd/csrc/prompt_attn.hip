@@ -1,18 +1,21 @@
-// Attention of a batch of prompts' new tokens over their KV, causal or not.
+// Attention of a batch of prompts' new tokens over their KV, causal or not: the kernel for fp32 (prompt_mfma.hip holds
+// the one for bf16) and the joining of parts.
 //
 // The rows of a prompt and KV head are its (new token, query head of the group) pairs, token by token, so
-// that the heads that share K and V share a tile.  Workgroup = (tile of 128 rows, KV head, split of the tokens
-// the tile sees); a wavefront owns 32 rows and walks the tokens in tiles of 32 with the online softmax of the
-// paper's attention tasks (App., attn task 2: running maximum, running sum, deferred division).
+// that the heads that share K and V share a tile.  Workgroup = (unit, KV head), a unit being 128 rows and a part of the
+// tokens they see (prompt_units.h); a wavefront owns 32 rows and walks the tokens in tiles of 32 with the online softmax
+// of the paper's attention tasks (App., attn task 2: running maximum, running sum, deferred division).
 //
 // Both products run on the matrix pipe in the transposed form S^T = K Q^T, O^T += V^T P^T, so that a lane
 // owns one row in both: the softmax statistics are the lane's own (two lanes share a row's tokens) and P is the
-// S^T accumulator itself.  bf16: v_mfma_f32_32x32x16_bf16, P rounded to bf16 (its 2^-9 is that of the
-// result's own rounding; the sum l takes the unrounded values).  fp32: v_mfma_f32_32x32x2_f32, nothing rounded.
+// S^T accumulator itself (v_mfma_f32_32x32x2_f32: nothing is rounded to fewer bits).
 //
 // What a row must not see enters nowhere: scores are replaced, not added to, and where a tile holds tokens that
-// some of its rows do not see and values that are not finite (0 * inf is not 0), its tokens are added one by
-// one, each to the rows that see it.
+// some of its rows do not see and values that are not finite (0 * inf is not 0), these are taken out of the tile and
+// added at the end to the rows that see them.
+//
+// Bound: the matrix pipe, 155 TFLOP/s for fp32 products.  The tile after the present one is on its way into registers
+// while its products run, and goes to the other half of LDS after them: one barrier a tile.
 #include "prompt_units.h"
 
 #include <hip/hip_fp16.h>
@@ -24,16 +27,16 @@ using prompt_impl::find_unit;
 using prompt_impl::kRows;
 using prompt_impl::Unit;
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
-typedef short shortx4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTileN = 32;      // tokens per tile
 constexpr int kThreads = 256;
+// Tiles that some row of a workgroup does not see whole: its 128 rows end at up to 128 tokens, and a prompt's end may be ragged.
+constexpr int kOddWords = 8;
+constexpr float kNever = -1e30f;  // reference maximum of a row that has seen nothing: finite, so that no exponent is inf - inf
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 {
@@ -42,163 +45,30 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
     return *reinterpret_cast<const uint32_t*>(&r);
 }
 
-// Operands of the two products for an element type; a piece is 16 bytes.
-template <typename T, int DP> struct Mat;
-
-template <int DP> struct Mat<__bf16, DP> {
-    static constexpr int kStrideK = DP * 2 + 16, kStrideV = DP * 2 + 16;  // bytes between token rows in LDS
-    bf16x8 qf[DP / 16];  // channels 16 s + 8 h .. + 7 of the lane's row
-    __device__ __forceinline__ void load_q(const char* row, int d, int h, bool ok)
-    {
-#pragma unroll
-        for (int s = 0; s < DP / 16; ++s) {
-            uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (ok && 16 * s + 8 * h < d)
-                v = *reinterpret_cast<const uint4*>(row + (16 * s + 8 * h) * 2);
-            qf[s] = *reinterpret_cast<bf16x8*>(&v);
-        }
-    }
-    __device__ __forceinline__ floatx16 scores(const char* k, int col, int h) const
-    {
-        floatx16 s = {};
-#pragma unroll
-        for (int u = 0; u < DP / 16; ++u) {
-            const bf16x8 a = *reinterpret_cast<const bf16x8*>(k + col * kStrideK + (16 * u + 8 * h) * 2);
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[u], s, 0, 0, 0);
-        }
-        return s;
-    }
-    __device__ __forceinline__ void add_values(const char* v, const floatx16& pr, floatx16 (&o)[DP / 32], int lane) const
-    {
-        const int h = lane >> 5, g16 = (lane >> 4) & 1, r = (lane & 15) >> 2, q4 = lane & 3;
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            const uint4 w = make_uint4(pack_bf16(pr[8 * ks], pr[8 * ks + 1]), pack_bf16(pr[8 * ks + 2], pr[8 * ks + 3]),
-                                       pack_bf16(pr[8 * ks + 4], pr[8 * ks + 5]), pack_bf16(pr[8 * ks + 6], pr[8 * ks + 7]));
-            const bf16x8 b = *reinterpret_cast<const bf16x8*>(&w);
-#pragma unroll
-            for (int db = 0; db < DP / 32; ++db) {
-                // the transposing read hands each lane four tokens of one channel
-                union {
-                    shortx4 part[2];
-                    bf16x8 all;
-                } a;
-#pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    const char* at = v + (16 * ks + 8 * part + 4 * h + r) * kStrideV + (32 * db + 16 * g16 + 4 * q4) * 2;
-                    a.part[part] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (__attribute__((address_space(3))) shortx4*)(size_t)(__attribute__((address_space(3))) const void*)at);
-                }
-                o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.all, b, o[db], 0, 0, 0);
-            }
-        }
-    }
-    // Whether a piece holds values that are not finite.
-    static __device__ __forceinline__ bool odd(const uint4& v)
-    {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-        bool any = false;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            any = any || (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
-        return any;
-    }
-    // Token x of the tile alone, to the rows (lanes) that see it.
-    __device__ __forceinline__ void add_token(const char* v, const floatx16& pr, floatx16 (&o)[DP / 32], int lane, int x, bool seen) const
-    {
-        const int h = lane >> 5, col = lane & 31, slot = (x >> 3) * 4 + (x & 3);  // accumulator register of the token
-        float mine = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            mine = i == slot ? pr[i] : mine;
-        const bool own = h == ((x >> 2) & 1);
-        const uint4 w = make_uint4(own ? pack_bf16(mine, 0.f) : 0u, 0u, 0u, 0u);
-#pragma unroll
-        for (int db = 0; db < DP / 32; ++db) {
-            const uint4 a = make_uint4(own ? *reinterpret_cast<const uint16_t*>(v + x * kStrideV + (32 * db + col) * 2) : 0u, 0u, 0u, 0u);
-            const floatx16 t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(&a),
-                                                                       *reinterpret_cast<const bf16x8*>(&w), o[db], 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                o[db][i] = seen ? t[i] : o[db][i];
-        }
-    }
-};
-
-template <int DP> struct Mat<float, DP> {
-    static constexpr int kStrideK = DP * 4 + 16, kStrideV = DP * 4 + 32;
-    floatx4 qf[DP / 8];  // channels 8 u + 4 h .. + 3
-    __device__ __forceinline__ void load_q(const char* row, int d, int h, bool ok)
-    {
-#pragma unroll
-        for (int u = 0; u < DP / 8; ++u) {
-            floatx4 v = {0.f, 0.f, 0.f, 0.f};
-            if (ok && 8 * u + 4 * h < d)
-                v = *reinterpret_cast<const floatx4*>(row + (8 * u + 4 * h) * 4);
-            qf[u] = v;
-        }
-    }
-    __device__ __forceinline__ floatx16 scores(const char* k, int col, int h) const
-    {
-        floatx16 s = {};
-#pragma unroll
-        for (int u = 0; u < DP / 8; ++u) {
-            const floatx4 a = *reinterpret_cast<const floatx4*>(k + col * kStrideK + (8 * u + 4 * h) * 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                s = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], qf[u][i], s, 0, 0, 0);
-        }
-        return s;
-    }
-    __device__ __forceinline__ void add_values(const char* v, const floatx16& pr, floatx16 (&o)[DP / 32], int lane) const
-    {
-        const int h = lane >> 5, col = lane & 31;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const char* row = v + (8 * (i >> 2) + 4 * h + (i & 3)) * kStrideV + col * 4;
-#pragma unroll
-            for (int db = 0; db < DP / 32; ++db)
-                o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(row + 128 * db), pr[i], o[db], 0, 0, 0);
-        }
-    }
-    static __device__ __forceinline__ bool odd(const uint4& v)
-    {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-        bool any = false;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            any = any || (w[i] & 0x7f800000u) == 0x7f800000u;
-        return any;
-    }
-    __device__ __forceinline__ void add_token(const char* v, const floatx16& pr, floatx16 (&o)[DP / 32], int lane, int x, bool seen) const
-    {
-        const int h = lane >> 5, col = lane & 31, slot = (x >> 3) * 4 + (x & 3);
-        float mine = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            mine = i == slot ? pr[i] : mine;
-        const bool own = h == ((x >> 2) & 1);
-        mine = own ? mine : 0.f;
-#pragma unroll
-        for (int db = 0; db < DP / 32; ++db) {
-            const float a = own ? *reinterpret_cast<const float*>(v + x * kStrideV + (32 * db + col) * 4) : 0.f;
-            const floatx16 t = __builtin_amdgcn_mfma_f32_32x32x2f32(a, mine, o[db], 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                o[db][i] = seen ? t[i] : o[db][i];
-        }
-    }
-};
-
-template <typename T, int DP>
-__global__ __launch_bounds__(kThreads) void prompt_attn_kernel(PromptParams p)
+// Zeroes the values of a piece that are not finite; whether there were any.
+__device__ __forceinline__ bool take_odd(uint4& v)
 {
-    using M = Mat<T, DP>;
-    constexpr int E = sizeof(T), kRowPieces = DP * E / 16, kPieces = kTileN * kRowPieces / kThreads;
+    uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bool odd = (w[i] & 0x7f800000u) == 0x7f800000u;
+        w[i] = odd ? 0u : w[i];
+        any = any || odd;
+    }
+    return any;
+}
+
+template <int DP>  // channels, padded with zeros
+__global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void prompt_attn_f32_kernel(PromptParams p)
+{
+    constexpr int kRowPieces = DP / 4, kPieces = kTileN * kRowPieces / kThreads;
     static_assert(kPieces * kThreads == kTileN * kRowPieces, "whole pieces per thread");
-    __shared__ __align__(16) char lds_k[kTileN * M::kStrideK];
-    __shared__ __align__(16) char lds_v[kTileN * M::kStrideV];
-    __shared__ uint32_t lds_odd[2];  // whether a tile holds values that are not finite
+    // bytes between token rows: 16 lanes' equal pieces of K, and rows four apart of V, lie in different banks
+    constexpr int kStrideK = DP * 4 + 16, kStrideV = DP * 4 + 32;
+    __shared__ __align__(16) char lds_k[2][kTileN * kStrideK];
+    __shared__ __align__(16) char lds_v[2][kTileN * kStrideV];
+    __shared__ uint32_t lds_odd[kOddWords];  // tokens whose values are not all finite, a word per tile that some row does not see whole
 
     const int j = blockIdx.x % p.Hkv;
     const Unit at = find_unit(p, blockIdx.x / p.Hkv);
@@ -214,36 +84,59 @@ __global__ __launch_bounds__(kThreads) void prompt_attn_kernel(PromptParams p)
     const int limit = !row_ok ? -1 : p.causal ? L - n + token : L - 1;
     const int last_row = min(row0 + kRows, n * p.G) - 1;
     const int least = p.causal ? L - n + row0 / p.G : L - 1, most = p.causal ? L - n + last_row / p.G : L - 1;
+    const int wave_last = min(row0 + wave * 32 + 32, n * p.G) - 1;
+    const int wave_most = wave_last < row0 + wave * 32 ? -1 : p.causal ? L - n + wave_last / p.G : L - 1;
 
     // this part's tokens
     const int seen = max(most + 1, 0);
     const int t0 = p.num_splits > 1 ? min(at.split * at.split_tokens, seen) : 0;
     const int t1 = p.num_splits > 1 ? min(t0 + at.split_tokens, seen) : seen;
 
-    M mat;
-    mat.load_q((const char*)p.q + ((long long)(q0 + token) * p.q_stride + (long long)head * p.D) * E, p.D, h, row_ok);
-
     const int first = at.kv0;
     auto offset = [&](int t) -> long long {  // of token t's row of this KV head, in bytes
         if (p.page_size != 0)
-            return (((long long)p.pages[first + (t >> 4)] * p.Hkv + j) * 16 + (t & 15)) * p.D * E;
-        return ((long long)(first + t) * p.kv_stride + (long long)j * p.D) * E;
+            return (((long long)p.pages[first + (t >> 4)] * p.Hkv + j) * 16 + (t & 15)) * p.D * 4;
+        return ((long long)(first + t) * p.kv_stride + (long long)j * p.D) * 4;
     };
     uint4 kreg[kPieces], vreg[kPieces];
-    auto request = [&](int tb) {
+    auto request = [&](int tb) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
             const int piece = tid + i * kThreads, row = piece / kRowPieces, c = piece % kRowPieces;
             kreg[i] = vreg[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (tb + row < t1 && c * 16 < p.D * E) {
+            if (tb + row < t1 && c * 4 < p.D) {
                 const long long o = offset(tb + row) + c * 16;
                 kreg[i] = *reinterpret_cast<const uint4*>((const char*)p.k + o);
                 vreg[i] = *reinterpret_cast<const uint4*>((const char*)p.v + o);
             }
         }
     };
+    const int whole = max(min(least + 1, t1) - t0, 0) / kTileN;  // tiles that every row sees whole
+    auto put = [&](int nth) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int piece = tid + i * kThreads, row = piece / kRowPieces, c = piece % kRowPieces;
+            if (nth >= whole && take_odd(vreg[i]))
+                atomicOr(&lds_odd[min(nth - whole, kOddWords - 1)], 1u << row);
+            *reinterpret_cast<uint4*>(lds_k[nth & 1] + row * kStrideK + c * 16) = kreg[i];
+            *reinterpret_cast<uint4*>(lds_v[nth & 1] + row * kStrideV + c * 16) = vreg[i];
+        }
+    };
+    if (t0 < t1)
+        request(t0);
+    floatx4 qf[DP / 8];  // channels 8 u + 4 h .. + 3 of the lane's row
+    {
+        const float* q = (const float*)p.q + (long long)(q0 + token) * p.q_stride + (long long)head * p.D;
+#pragma unroll
+        for (int u = 0; u < DP / 8; ++u) {
+            floatx4 v = {0.f, 0.f, 0.f, 0.f};
+            if (8 * u + 4 * h < p.D)
+                v = *reinterpret_cast<const floatx4*>(q + 8 * u + 4 * h);
+            qf[u] = v;
+        }
+    }
 
-    float m = -INFINITY, l = 0.f;
+    float m = kNever, l = 0.f;
     floatx16 o[DP / 32];
 #pragma unroll
     for (int db = 0; db < DP / 32; ++db)
@@ -251,114 +144,129 @@ __global__ __launch_bounds__(kThreads) void prompt_attn_kernel(PromptParams p)
         for (int i = 0; i < 16; ++i)
             o[db][i] = 0.f;
 
-    if (tid < 2)
+    if (tid < kOddWords)
         lds_odd[tid] = 0u;
+    __syncthreads();
     if (t0 < t1)
-        request(t0);
-    int stage = 0;
-    for (int tb = t0; tb < t1; tb += kTileN, stage ^= 1) {
-        const bool masked = tb + kTileN - 1 > least;  // some row does not see all of the tile
-        __syncthreads();  // everybody is done with the tile before
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int piece = tid + i * kThreads, row = piece / kRowPieces, c = piece % kRowPieces;
-            if (masked && M::odd(vreg[i]))
-                lds_odd[stage] = 1u;
-            *reinterpret_cast<uint4*>(lds_k + row * M::kStrideK + c * 16) = kreg[i];
-            *reinterpret_cast<uint4*>(lds_v + row * M::kStrideV + c * 16) = vreg[i];
-        }
-        __syncthreads();
+        put(0);
+    __syncthreads();
+    int nth = 0;
+    for (int tb = t0; tb < t1; tb += kTileN, ++nth) {
         if (tb + kTileN < t1)
             request(tb + kTileN);
-        if (tid == 0)
-            lds_odd[stage ^ 1] = 0u;
-        floatx16 s = mat.scores(lds_k, col, h);
-        // accumulator register i of lane-half h is token 8 (i/4) + 4 h + i%4 of the tile
-        if (masked || tb + kTileN > t1) {
-            const int end = min(limit, t1 - 1) - tb - 4 * h;
+        if (tb <= wave_most) {
+            const char* const k = lds_k[nth & 1] + col * kStrideK + 16 * h;
+            const char* const v = lds_v[nth & 1] + 4 * h * kStrideV + col * 4;
+            floatx16 s = {};
+            floatx4 a = *reinterpret_cast<const floatx4*>(k);
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                s[i] = 8 * (i >> 2) + (i & 3) <= end ? s[i] : -INFINITY;
+            for (int u = 0; u < DP / 8; ++u) {
+                const floatx4 now = a;
+                if (u + 1 < DP / 8)
+                    a = *reinterpret_cast<const floatx4*>(k + (u + 1) * 32);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    s = __builtin_amdgcn_mfma_f32_32x32x2f32(now[i], qf[u][i], s, 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);  // (all the reads ahead of all the products would not fit the registers)
+            }
+            // accumulator register i of lane-half h is token 8 (i/4) + 4 h + i%4 of the tile
+            if (nth >= whole) {  // some row does not see all of the tile
+                const int end = min(limit, t1 - 1) - tb - 4 * h;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    s[i] = 8 * (i >> 2) + (i & 3) <= end ? s[i] : -INFINITY;
+            }
+            float top = s[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i)
+                top = fmaxf(top, s[i]);
+            top = fmaxf(top, __shfl_xor(top, 32)) * p.scale_log2;
+            // the reference maximum only has to bound the exponents: raised where the tile's is well above it
+            if (__ballot(top > m + 10.f) != 0) {
+                const float m_new = fmaxf(m, top), corr = __builtin_amdgcn_exp2f(m - m_new);
+                m = m_new;
+                l *= corr;
+#pragma unroll
+                for (int db = 0; db < DP / 32; ++db) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        o[db][i] *= corr;
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], p.scale_log2, -m));
+                sum += s[i];
+            }
+            l += sum;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const char* row = v + (8 * (i >> 2) + (i & 3)) * kStrideV;
+#pragma unroll
+                for (int db = 0; db < DP / 32; ++db)
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(row + 128 * db), s[i], o[db], 0, 0, 0);
+                if (DP > 128 && (i & 1))
+                    __builtin_amdgcn_sched_barrier(0);
+            }
         }
-        float most_s = s[0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i)
-            most_s = fmaxf(most_s, s[i]);
-        most_s = fmaxf(most_s, __shfl_xor(most_s, 32));
-        const float m_new = fmaxf(m, most_s * p.scale_log2);
-        const float ref = m_new == -INFINITY ? 0.f : m_new;  // nothing seen yet: every exponent is -inf
-        const float corr = __builtin_amdgcn_exp2f(m - ref);
-        m = m_new;
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], p.scale_log2, -ref));
-            sum += s[i];
-        }
-        l = l * corr + sum;
-#pragma unroll
-        for (int db = 0; db < DP / 32; ++db)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                o[db][i] *= corr;
-        if (masked && lds_odd[stage] != 0u) {
-            for (int x = 0; x < kTileN; ++x)
-                mat.add_token(lds_v, s, o, lane, x, tb + x <= limit);
-        } else {
-            mat.add_values(lds_v, s, o, lane);
-        }
+        if (tb + kTileN < t1)
+            put(nth + 1);
+        __syncthreads();
     }
 
     l += __shfl_xor(l, 32);
     if (!row_ok)
         return;
     const long long row = (long long)(q0 + token) * p.Hq + head;
+    float inv = 1.f;
+    float* dst = (float*)p.out + row * p.D;
     if (p.num_splits > 1) {
         if (h == 0) {
             p.part_ml[row * p.num_splits + at.split] = make_float4(m, l, 1.f, 0.f);
             if (at.split == 0)  // and the parts that this prompt does not have
                 for (int s = at.splits; s < p.num_splits; ++s)
-                    p.part_ml[row * p.num_splits + s] = make_float4(-INFINITY, 0.f, 1.f, 0.f);
+                    p.part_ml[row * p.num_splits + s] = make_float4(kNever, 0.f, 1.f, 0.f);
         }
         if (t0 >= t1)
             return;
-        float* dst = (float*)p.part_acc + (row * p.num_splits + at.split) * p.D;
-#pragma unroll
-        for (int db = 0; db < DP / 32; ++db)
-#pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4) {
-                const int c = 32 * db + 8 * q4 + 4 * h;
-                if (c < p.D)
-                    *reinterpret_cast<float4*>(dst + c) = make_float4(o[db][4 * q4], o[db][4 * q4 + 1], o[db][4 * q4 + 2], o[db][4 * q4 + 3]);
-            }
-        return;
+        dst = (float*)p.part_acc + (row * p.num_splits + at.split) * p.D;
+    } else {
+        inv = l == 0.f ? 0.f : 1.f / l;
+        if (p.lse && h == 0)
+            p.lse[row] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
     }
-    const bool none = l == 0.f;
-    const float inv = none ? 0.f : 1.f / l;
-    if (p.lse && h == 0)
-        p.lse[row] = none ? -INFINITY : m * kLn2 + logf(l);
-    char* dst = (char*)p.out + row * p.D * E;
 #pragma unroll
     for (int db = 0; db < DP / 32; ++db)
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {
             const int c = 32 * db + 8 * q4 + 4 * h;
-            if (c >= p.D)
+            if (c < p.D)
+                *reinterpret_cast<float4*>(dst + c) =
+                    make_float4(o[db][4 * q4] * inv, o[db][4 * q4 + 1] * inv, o[db][4 * q4 + 2] * inv, o[db][4 * q4 + 3] * inv);
+        }
+    // rare: the values that were taken out of the tiles, to the rows that see them (a lane's own channels, as stored above)
+    for (int w = 0; w < kOddWords; ++w)
+        for (uint32_t bits = lds_odd[w]; bits != 0u; bits &= bits - 1u) {
+            const int x = t0 + (whole + w) * kTileN + __ffs(bits) - 1;
+            if (x >= t1 || x > limit)
                 continue;
-            const float x0 = o[db][4 * q4] * inv, x1 = o[db][4 * q4 + 1] * inv, x2 = o[db][4 * q4 + 2] * inv, x3 = o[db][4 * q4 + 3] * inv;
-            if constexpr (E == 2)
-                *reinterpret_cast<uint2*>(dst + c * 2) = make_uint2(pack_bf16(x0, x1), pack_bf16(x2, x3));
-            else
-                *reinterpret_cast<float4*>(dst + c * 4) = make_float4(x0, x1, x2, x3);
+            const float* v = (const float*)((const char*)p.v + offset(x));
+            for (int c0 = 4 * h; c0 < p.D; c0 += 8)
+                for (int c = c0; c < c0 + 4; ++c)
+                    if (!(fabsf(v[c]) < INFINITY))
+                        dst[c] += v[c];
         }
 }
 
 // Joins the parts of a row: with states (m_i, l_i, acc_i), m = max m_i and w_i = 2^(m_i - m),
 // out = sum w_i acc_i / sum w_i l_i.  LANES lanes take a row, 16 bytes of a part each; they also take its parts' (m, l, scale)
 // and hand their weights round.  Bound by the partial states, all of whose loads a lane has in flight kBatch at a time.
-template <typename T, bool HALF, int LANES>
+template <typename T, int LANES>
 __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptParams p)
 {
+    constexpr bool HALF = sizeof(T) == 2;
     constexpr int kRowsPerBlock = kThreads / LANES, kBatch = 8, kCh = HALF ? 8 : 4;
     const int lane = threadIdx.x % LANES, first_lane = (threadIdx.x & 63) - lane, c = lane * kCh;
     const long long row = (long long)blockIdx.x * kRowsPerBlock + threadIdx.x / LANES;
@@ -436,46 +344,35 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptParams p)
     }
 }
 
-template <typename T, bool HALF, int LANES> void launch_merge(const PromptParams& p, hipStream_t s)
+template <typename T, int LANES> void launch_merge(const PromptParams& p, hipStream_t s)
 {
     constexpr int kRowsPerBlock = kThreads / LANES;
-    hipLaunchKernelGGL((prompt_merge_kernel<T, HALF, LANES>), dim3((unsigned)((p.rows + kRowsPerBlock - 1) / kRowsPerBlock)),
+    hipLaunchKernelGGL((prompt_merge_kernel<T, LANES>), dim3((unsigned)((p.rows + kRowsPerBlock - 1) / kRowsPerBlock)),
                        dim3(kThreads), 0, s, p);
 }
 
-template <typename T>
-hipError_t launch(const PromptParams& p, hipStream_t s)
+template <int DP, int LANES> void launch_f32(const PromptParams& p, hipStream_t s)
 {
     const dim3 grid((unsigned)((long long)p.tiles * p.num_splits * p.Hkv)), block(kThreads);
-    if (sizeof(T) == 2 && (p.D == 64 || p.D == 128)) {
-        const hipError_t e = launch_prompt_mfma(p, s);
-        if (e != hipSuccess)
-            return e;
-        if (p.num_splits > 1)
-            p.D == 64 ? launch_merge<T, true, 8>(p, s) : launch_merge<T, true, 16>(p, s);
-        return hipGetLastError();
-    }
-    if (p.D <= 64) {
-        hipLaunchKernelGGL((prompt_attn_kernel<T, 64>), grid, block, 0, s, p);
-        if (p.num_splits > 1)
-            launch_merge<T, false, 16>(p, s);
-    } else if (p.D <= 128) {
-        hipLaunchKernelGGL((prompt_attn_kernel<T, 128>), grid, block, 0, s, p);
-        if (p.num_splits > 1)
-            launch_merge<T, false, 32>(p, s);
-    } else {
-        hipLaunchKernelGGL((prompt_attn_kernel<T, 256>), grid, block, 0, s, p);
-        if (p.num_splits > 1)
-            launch_merge<T, false, 64>(p, s);
-    }
-    return hipGetLastError();
+    hipLaunchKernelGGL(prompt_attn_f32_kernel<DP>, grid, block, 0, s, p);
+    if (p.num_splits > 1)
+        launch_merge<float, LANES>(p, s);
 }
 
 }  // namespace
 
 hipError_t launch_prompt_attn(const PromptParams& p, hipStream_t s)
 {
-    return p.dtype == 1 ? launch<__bf16>(p, s) : launch<float>(p, s);
+    if (p.dtype == 1) {
+        const hipError_t e = launch_prompt_mfma(p, s);
+        if (e != hipSuccess)
+            return e;
+        if (p.num_splits > 1)
+            p.D <= 64 ? launch_merge<__bf16, 8>(p, s) : p.D <= 128 ? launch_merge<__bf16, 16>(p, s) : launch_merge<__bf16, 32>(p, s);
+    } else {
+        p.D <= 64 ? launch_f32<64, 16>(p, s) : p.D <= 128 ? launch_f32<128, 32>(p, s) : launch_f32<256, 64>(p, s);
+    }
+    return hipGetLastError();
 }
 
 }  // namespace spd

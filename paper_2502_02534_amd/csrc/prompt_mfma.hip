@@ -1,5 +1,6 @@
-// prompt_attn for bf16 with 64 or 128 channels: the tiled kernel (prompt_attn.hip holds the general one and the
-// definition of rows, tiles and splits).
+// prompt_attn for bf16: the tiled kernel (prompt_attn.hip holds that for fp32 and the definition of rows and parts).
+// Heads of 64, 128 and 256 channels fill a tile's rows; other dimensions run in the next larger of these, their missing
+// channels zeros that are put into LDS once and never overwritten.
 //
 // Workgroup = (unit, KV head), four wavefronts that own 32 rows each.  K and V tiles of 32 tokens go from
 // global memory straight into LDS (global_load_lds_dwordx4), two or three tiles before their use, with the 16-byte pieces
@@ -33,19 +34,21 @@ constexpr int kTileN = 32;
 constexpr int kWaves = 4;
 constexpr int kRing = 4;              // slots of K and of V: the tile in use and up to three under way
 constexpr int kFragAhead = 4;         // LDS fragments in flight
+// Tiles that some row of a workgroup does not see whole: its 128 rows end at up to 128 tokens, and a prompt's end may be ragged.
+constexpr int kOddWords = 8;
 constexpr float kNever = -1e30f;      // reference maximum of a row that has seen nothing: finite, so that no exponent is inf - inf
 constexpr float kRaise = 1024.f;
 
-template <int D> struct Shape {
+template <int D> struct Shape {  // D: channels of a tile row
     static constexpr int kRow = 2 * D, kTile = kTileN * kRow;  // bytes
     static constexpr int kRowsPerCopy = 1024 / kRow, kCopies = kTile / 1024;
     static constexpr int kQK = D / 16, kDB = D / 32, kPV = 2 * kDB;  // fragments
-    static constexpr int kLds = 2 * kRing * kTile + 16;  // K, V, a flag; 64 KB with 128 channels: two workgroups per CU
+    static constexpr int kLds = 2 * kRing * kTile + 4 * kOddWords;  // K, V, flags; 64 KB with 128 channels: two workgroups per CU
     // Piece p of a row lies in slot p ^ swz(row): sixteen rows' equal pieces take all 64 banks, and so do the four rows and
     // 64 bytes that half a wavefront's transposing reads touch.
     static __device__ __forceinline__ int swz(int row)
     {
-        if (D == 128)
+        if (D >= 128)
             return ((row & 3) << 2) | ((row >> 2) & 3);
         return (((row >> 1) & 1) << 2) | (((row >> 2) & 1) << 1) | ((row >> 3) & 1);
     }
@@ -55,14 +58,15 @@ template <int D> struct Shape {
 constexpr int slot_constant(int) { return 0; }
 template <int N> constexpr int slot_constant(std::integral_constant<int, N>) { return N; }
 
-template <int D, bool PAGED>
-__global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParams p)
+template <int D, bool FULL, bool PAGED>  // FULL: the heads have D channels, not fewer
+__global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void prompt_mfma_kernel(PromptParams p)
 {
     using S = Shape<D>;
+    const int head_bytes = FULL ? S::kRow : p.D * 2, head_pieces = head_bytes / 16;
     constexpr int kIPW = 2 * S::kCopies / kWaves;
     static_assert(kIPW >= 1 && kRows == 32 * kWaves, "a copy for every wavefront");
     __shared__ __align__(16) char lds[S::kLds];
-    volatile uint32_t* const odd_flag = (volatile uint32_t*)(lds + 2 * kRing * S::kTile);
+    uint32_t* const odd_words = (uint32_t*)(lds + 2 * kRing * S::kTile);  // tokens whose values are not all finite, a word per such tile
 
     const int j = blockIdx.x % p.Hkv;
     const Unit at = find_unit(p, blockIdx.x / p.Hkv);
@@ -85,18 +89,19 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
     const int t0 = p.num_splits > 1 ? min(at.split * at.split_tokens, seen) : 0;
     const int t1 = p.num_splits > 1 ? min(t0 + at.split_tokens, seen) : seen;
     const int ntiles = (t1 - t0 + kTileN - 1) / kTileN;
-    int nfull = max(min(least + 1, t1) - t0, 0) / kTileN;  // tiles that every row sees whole
-    if (nfull < 3)
-        nfull = 0;
+    const int whole = max(min(least + 1, t1) - t0, 0) / kTileN;  // tiles that every row sees whole
+    const int nfull = whole < 3 ? 0 : whole;                      // those that run through the pipeline
 
     // ---- query fragments (B operand): column = this lane's row, channels 16 s + 8 h (a lane without a row of its own takes
     // the first token's: nothing of it is stored)
     bf16x8 qf[S::kQK];
     {
-        const uint4* qg = (const uint4*)((const char*)p.q + ((long long)(q0 + token) * p.q_stride + (long long)head * D) * 2);
+        const uint4* qg = (const uint4*)((const char*)p.q + ((long long)(q0 + token) * p.q_stride + (long long)head * (head_bytes / 2)) * 2);
 #pragma unroll
         for (int s = 0; s < S::kQK; ++s) {
-            const uint4 v = qg[2 * s + h];
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if (FULL || 2 * s + h < head_pieces)
+                v = qg[2 * s + h];
             qf[s] = as_bf16x8(v);
         }
     }
@@ -104,20 +109,20 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
     // ---- global -> LDS copies: the first half of the wavefronts copies K, the other half V, kIPW instructions a tile each
     typedef const __attribute__((address_space(4))) int* const_int_ptr;
     const const_int_ptr pages = PAGED ? (const_int_ptr)(p.pages + at.kv0) : nullptr;
-    const long long tok_stride = PAGED ? S::kRow : p.kv_stride * 2;
-    const long long head_base = PAGED ? (long long)j * 16 * S::kRow : (long long)at.kv0 * p.kv_stride * 2 + (long long)j * S::kRow;
-    const long long page_stride = (long long)p.Hkv * 16 * S::kRow;
+    const long long tok_stride = PAGED ? head_bytes : p.kv_stride * 2;
+    const long long head_base = PAGED ? (long long)j * 16 * head_bytes : (long long)at.kv0 * p.kv_stride * 2 + (long long)j * head_bytes;
+    const long long page_stride = (long long)p.Hkv * 16 * head_bytes;
     const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) void*)lds;
     constexpr int kLanesPerRow = 64 / S::kRowsPerCopy;
     const int lane_row = lane / kLanesPerRow, lane_piece = lane % kLanesPerRow;
     const bool copies_v = wave >= kWaves / 2;
     const int row_first = S::kRowsPerCopy * kIPW * (copies_v ? wave - kWaves / 2 : wave);
+    // piece of its row that this lane fetches with instruction i
+    auto piece_of = [&](int i) __attribute__((always_inline)) { return lane_piece ^ S::swz(row_first + S::kRowsPerCopy * i + lane_row); };
     unsigned lane_off[kIPW];
 #pragma unroll
-    for (int i = 0; i < kIPW; ++i) {
-        const int tl = S::kRowsPerCopy * i + lane_row;
-        lane_off[i] = (unsigned)(tl * (unsigned)tok_stride + ((lane_piece ^ S::swz(row_first + tl)) << 4));
-    }
+    for (int i = 0; i < kIPW; ++i)
+        lane_off[i] = (unsigned)((S::kRowsPerCopy * i + lane_row) * (unsigned)tok_stride + (piece_of(i) << 4));
     const char* const tensor = (const char*)(copies_v ? p.v : p.k);
     char* const ring_lds = lds + (copies_v ? kRing * S::kTile : 0) + row_first * S::kRow;
     int next_page = 0;
@@ -131,16 +136,17 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
         char* const dst = ring_lds + (tile % kRing) * S::kTile;
         const bool full = tb + kTileN <= t1;
         const int tg = min(tb + row_first, t1 - 1);  // this wavefront's first row; rows past the end repeat the last token
-        const char* const src = PAGED ? tensor + (long long)next_page * page_stride + head_base + (tg & 15) * S::kRow
+        const char* const src = PAGED ? tensor + (long long)next_page * page_stride + head_base + (tg & 15) * head_bytes
                                       : tensor + head_base + (long long)tg * tok_stride;
 #pragma unroll
         for (int i = 0; i < kIPW; ++i) {
             unsigned off = lane_off[i];
             if (!full) {
                 const int tl = S::kRowsPerCopy * i + lane_row, row = min(tb + row_first + tl, t1 - 1) - tg;
-                off = (unsigned)(max(row, 0) * (unsigned)tok_stride + ((lane_piece ^ S::swz(row_first + tl)) << 4));
+                off = (unsigned)(max(row, 0) * (unsigned)tok_stride + (piece_of(i) << 4));
             }
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + off),
+            if (FULL || piece_of(i) < head_pieces)  // (every instruction has lanes that copy)
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + off),
                                              (__attribute__((address_space(3))) void*)(dst + i * 1024), 16, 0, 0);
         }
         fetch_page(tile + 1);
@@ -162,15 +168,17 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
         __builtin_amdgcn_s_barrier();
     };
 
-    // ---- per-lane LDS addresses of the operand fragments in slot 0; the slot goes into the instruction's offset
-    unsigned k_addr[S::kQK], v_addr[S::kDB][2];
+    // ---- per-lane LDS addresses of the operand fragments in slot 0; the slot goes into the instruction's offset, and so do
+    // the second 256 bytes of a row, whose swizzle is the first's
+    constexpr int kAddrK = S::kQK < 8 ? S::kQK : 8, kAddrV = S::kDB < 4 ? S::kDB : 4;
+    unsigned k_addr[kAddrK], v_addr[kAddrV][2];
 #pragma unroll
-    for (int s = 0; s < S::kQK; ++s)
+    for (int s = 0; s < kAddrK; ++s)
         k_addr[s] = lds_base + (unsigned)(col * S::kRow) + ((32u * s) ^ (unsigned)((h ^ S::swz(col)) << 4));
     {
         const int g16 = (lane >> 4) & 1, r = (lane & 15) >> 2, q4 = lane & 3;
 #pragma unroll
-        for (int db = 0; db < S::kDB; ++db)
+        for (int db = 0; db < kAddrV; ++db)
 #pragma unroll
             for (int part2 = 0; part2 < 2; ++part2) {
                 const int tok = 8 * part2 + 4 * h + r, piece = 4 * db + 2 * g16 + (q4 >> 1);
@@ -210,16 +218,16 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
                 constexpr bool fixed = !std::is_same<decltype(kslot), int>::value;
                 if constexpr (!is_pv) {
                     u32x4& dst = ring_k[K % (kFragAhead + 2)];
-                    unsigned addr = k_addr[idx];
+                    unsigned addr = k_addr[idx % kAddrK];
                     constexpr int kSlot = slot_constant(decltype(kslot){}) * S::kTile;
                     if constexpr (!fixed)
                         addr += (unsigned)kslot * S::kTile;
-                    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(dst) : "v"(addr), "n"(kSlot));
+                    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(dst) : "v"(addr), "n"(kSlot + idx / kAddrK * 256));
                 } else {
                     constexpr int a = idx / S::kDB, b = idx % S::kDB;
                     u32x2& lo = ring_lo[K % (kFragAhead + 2)];
                     u32x2& hi = ring_hi[K % (kFragAhead + 2)];
-                    unsigned a0 = v_addr[b][0], a1 = v_addr[b][1];
+                    unsigned a0 = v_addr[b % kAddrV][0], a1 = v_addr[b % kAddrV][1];
                     constexpr int kSlot = slot_constant(decltype(vslot){}) * S::kTile;
                     if constexpr (!fixed) {
                         a0 += (unsigned)vslot * S::kTile;
@@ -227,7 +235,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
                     }
                     asm volatile("ds_read_b64_tr_b16 %0, %2 offset:%4\n\tds_read_b64_tr_b16 %1, %3 offset:%4"
                                  : "=&v"(lo), "=&v"(hi)
-                                 : "v"(a0), "v"(a1), "n"(kSlot + a * 16 * S::kRow));
+                                 : "v"(a0), "v"(a1), "n"(kSlot + a * 16 * S::kRow + b / kAddrV * 256));
                 }
             }
         };
@@ -269,8 +277,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
                 }
             }
         };
-        constexpr int kPer = 18 / NF > 0 ? 18 / NF : 1, kLead = 18 - kPer * NF;  // slots per product, and before the first
-        static_assert(!SM || kLead >= 0, "every score gets its slot");
+        constexpr int kPer = 18 / NF > 0 ? 18 / NF : 1, kLead = kPer * NF < 18 ? 18 - kPer * NF : 0;  // slots per product, and before the first
         for_each_index(issue, std::make_integer_sequence<int, kFragAhead + 1>{});
         if constexpr (SM) {
             for_each_index(soft, std::make_integer_sequence<int, kLead>{});
@@ -335,10 +342,13 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
             psum = probabilities(sc, pn);
             l_run *= corr;
 #pragma unroll
-            for (int db = 0; db < S::kDB; ++db)
+            for (int db = 0; db < S::kDB; ++db) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     o[db][i] *= corr;
+                if (D > 128)
+                    __builtin_amdgcn_sched_barrier(0);  // (one block at a time out of the accumulation registers)
+            }
         }
         l_run += psum;
     };
@@ -353,6 +363,13 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
     bf16x8 pa[2], pb[2];
     const int lead = copies_v && nfull > 0 ? 1 : 3, lag = copies_v ? 1 : -1;
     if (ntiles > 0) {
+        if (tid < kOddWords)
+            odd_words[tid] = 0u;  // (a barrier follows before any is set)
+        if (!FULL) {
+            for (int i = tid; i < 2 * kRing * S::kTile / 16; i += kWaves * 64)
+                reinterpret_cast<uint4*>(lds)[i] = make_uint4(0u, 0u, 0u, 0u);
+            __syncthreads();
+        }
         fetch_page(0);
         copies_up_to(lead - 1);
         landed(0);
@@ -411,64 +428,51 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
     // ---- tiles that some row does not see whole ------------------------------------------------------------------------------
     for (; t < ntiles; ++t) {
         const int tb = t0 + t * kTileN, slot = t % kRing;
-        // Does the tile hold values that are not finite (0 * inf is not 0)?  Its copies have landed.
-        if (tid == 0)
-            *odd_flag = 0u;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         copies_up_to(t + 3);  // (the slots of tile t - 1 are free for everybody from here on)
         const bool some = tb <= wave_most;
-        {
-            bool any = false;
+        const bool masked = t >= whole;
+        if (masked) {
+            // 0 * inf is not 0: values that are not finite are noted, taken out of the tile, and added at the end to the rows that
+            // see them.  (The tile's copies have landed.)
             for (int i = tid; i < S::kTile / 16; i += kWaves * 64) {
-                u32x4 v;
+                uint4* const at_piece = reinterpret_cast<uint4*>(lds + (kRing + slot) * S::kTile) + i;
+                uint4 v;
                 const unsigned addr = lds_base + (unsigned)(kRing + slot) * S::kTile + i * 16;
-                asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=v"(v) : "v"(addr));
+                u32x4 raw;
+                asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=v"(raw) : "v"(addr));
+                uint32_t w[4];
+                bool any = false;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    any = any || (v[e] & 0x7f80u) == 0x7f80u || (v[e] & 0x7f800000u) == 0x7f800000u;
+                for (int e = 0; e < 4; ++e) {
+                    const bool lo = (raw[e] & 0x7f80u) == 0x7f80u, hi = (raw[e] & 0x7f800000u) == 0x7f800000u;
+                    w[e] = raw[e] & (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0x0000ffffu : 0xffffffffu);
+                    any = any || lo || hi;
+                }
+                if (any) {
+                    atomicOr(&odd_words[min(t - whole, kOddWords - 1)], 1u << (i / (S::kRow / 16)));
+                    v = make_uint4(w[0], w[1], w[2], w[3]);
+                    *at_piece = v;
+                }
             }
-            if (any)
-                *odd_flag = 1u;
         }
         if (some) {
             region(yes, no, no, slot, 0, sa, sa, pa, pa);
-            const int end = min(limit, t1 - 1) - tb - 4 * h;
+            if (masked) {
+                const int end = min(limit, t1 - 1) - tb - 4 * h;
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                sa[i] = 8 * (i >> 2) + (i & 3) <= end ? sa[i] : -INFINITY;
+                for (int i = 0; i < 16; ++i)
+                    sa[i] = 8 * (i >> 2) + (i & 3) <= end ? sa[i] : -INFINITY;
+            }
             take_sum(probabilities(sa, pa), sa, pa);
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        const bool odd = __builtin_amdgcn_readfirstlane(*odd_flag) != 0u;
-        if (some && !odd) {
-            region(no, no, yes, 0, slot, sa, sa, pa, pa);
-        } else if (some) {
-            // token by token, to the rows (lanes) that see it
-            for (int x = 0; x < kTileN; ++x) {
-                const int nth = (x >> 3) * 4 + (x & 3);  // among the lane's 16 probabilities
-                const bool own = h == ((x >> 2) & 1), sees = tb + x <= min(limit, t1 - 1);
-                uint32_t pw = 0u;
-#pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    const u32x4 q = *reinterpret_cast<const u32x4*>(&pa[u >> 2]);
-                    pw = u == (nth >> 1) ? q[u & 3] : pw;
-                }
-                pw = own ? ((nth & 1) ? pw >> 16 : pw & 0xffffu) : 0u;
-                const u32x4 b = {pw, 0u, 0u, 0u};
-#pragma unroll
-                for (int db = 0; db < S::kDB; ++db) {
-                    const int c = 32 * db + col;  // channel
-                    const char* v = lds + (kRing + slot) * S::kTile + x * S::kRow + (((c >> 3) ^ S::swz(x)) << 4) + (c & 7) * 2;
-                    const u32x4 a = {own ? (uint32_t)*(volatile const uint16_t*)v : 0u, 0u, 0u, 0u};
-                    const floatx16 sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(b), o[db], 0, 0, 0);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        o[db][i] = sees ? sum[i] : o[db][i];
-                }
-            }
+        if (masked) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
         }
+        if (some)
+            region(no, no, yes, 0, slot, sa, sa, pa, pa);
         if (t + 1 < ntiles)
             landed(t + 1);
     }
@@ -481,19 +485,39 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
     auto place = [&](int row, int piece) __attribute__((always_inline)) -> char* {
         return mine + row * S::kRow + ((piece ^ (row & (S::kRow / 16 - 1))) << 4);
     };
-    // Rows 0 .. 31 of the wavefront to `first` + out_row * `pitch`, two halves of a pair from `pack`.
-    auto store_rows = [&](auto pack, char* first, long long pitch) __attribute__((always_inline)) {
+    // Rows 0 .. 31 of the wavefront to `first` + out_row * `pitch`; `pack` makes two 16-bit values, of sums or as they are, `unpack`
+    // reads one.
+    auto store_rows = [&](auto pack, auto unpack, char* first, long long pitch) __attribute__((always_inline)) {
 #pragma unroll
         for (int db = 0; db < S::kDB; ++db)
 #pragma unroll
             for (int q4 = 0; q4 < 4; ++q4)  // registers 4 q4 .. + 3 are channels 32 db + 8 q4 + 4 h .. + 3
                 *reinterpret_cast<uint2*>(place(col, 4 * db + q4) + 8 * h) =
-                    make_uint2(pack(o[db][4 * q4], o[db][4 * q4 + 1]), pack(o[db][4 * q4 + 2], o[db][4 * q4 + 3]));
+                    make_uint2(pack(o[db][4 * q4], o[db][4 * q4 + 1], true), pack(o[db][4 * q4 + 2], o[db][4 * q4 + 3], true));
+        // rare: the values that were taken out of the tiles, to the rows that see them
+        for (int w = 0; w < kOddWords; ++w)
+            for (uint32_t bits = ntiles > 0 ? __builtin_amdgcn_readfirstlane(odd_words[w]) : 0u; bits != 0u; bits &= bits - 1u) {
+                const int x = t0 + (whole + w) * kTileN + __ffs(bits) - 1;
+                if (x >= t1)
+                    continue;
+                const uint16_t* v = (const uint16_t*)((const char*)p.v + head_base + (PAGED ? (long long)pages[x >> 4] * page_stride + (x & 15) * head_bytes
+                                                                                              : (long long)x * tok_stride));
+                for (int row = 0; row < 32; ++row) {
+                    if (x > __builtin_amdgcn_readfirstlane(__shfl(limit, row)))
+                        continue;
+                    for (int c = lane; c < head_bytes / 2; c += 64) {
+                        const float value = __uint_as_float((uint32_t)v[c] << 16);
+                        uint16_t* const mine_at = reinterpret_cast<uint16_t*>(place(row, c >> 3)) + (c & 7);
+                        if (!(fabsf(value) < INFINITY))
+                            *mine_at = (uint16_t)pack(unpack(*mine_at) + value, 0.f, false);
+                    }
+                }
+            }
         const int to = row_ok ? (int)out_row : -1;
 #pragma unroll
         for (int i = 0; i < S::kCopies; ++i) {
             const int row = S::kRowsPerCopy * i + lane_row, dst = __shfl(to, row);
-            if (dst >= 0)
+            if (dst >= 0 && (FULL || lane_piece < head_pieces))
                 *reinterpret_cast<uint4*>(first + dst * pitch + lane_piece * 16) = *reinterpret_cast<const uint4*>(place(row, lane_piece));
         }
     };
@@ -516,31 +540,38 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_mfma_kernel(PromptParam
                     p.part_ml[out_row * p.num_splits + s] = make_float4(kNever, 0.f, 1.f, 0.f);
         }
         if (t0 < t1)
-            store_rows([&](float x, float y) __attribute__((always_inline)) {
-                const __half2 v = __floats2half2_rn(x * inv * unscale, y * inv * unscale);
+            store_rows([&](float x, float y, bool sums) __attribute__((always_inline)) {
+                const float f = sums ? inv * unscale : 1.f;
+                const __half2 v = __floats2half2_rn(x * f, y * f);
                 return *reinterpret_cast<const uint32_t*>(&v);
-            }, (char*)p.part_acc + at.split * S::kRow, (long long)p.num_splits * S::kRow);
+            }, [](uint16_t x) __attribute__((always_inline)) { return __half2float(*reinterpret_cast<const __half*>(&x)); }, (char*)p.part_acc + (long long)at.split * head_bytes, (long long)p.num_splits * head_bytes);
         return;
     }
     if (p.lse && h == 0 && row_ok)
         p.lse[out_row] = l == 0.f ? -INFINITY : m_run * kLn2 + logf(l);
-    store_rows([&](float x, float y) __attribute__((always_inline)) { return pack_bf16_rne(x * inv, y * inv); }, (char*)p.out, S::kRow);
+    store_rows([&](float x, float y, bool sums) __attribute__((always_inline)) { return sums ? pack_bf16_rne(x * inv, y * inv) : pack_bf16_rne(x, y); },
+               [](uint16_t x) __attribute__((always_inline)) { return __uint_as_float((uint32_t)x << 16); }, (char*)p.out, head_bytes);
+}
+
+template <int D, bool FULL> void launch(const PromptParams& p, hipStream_t s)
+{
+    const dim3 grid((unsigned)((long long)p.tiles * p.num_splits * p.Hkv)), block(kWaves * 64);
+    if (p.page_size != 0)
+        hipLaunchKernelGGL((prompt_mfma_kernel<D, FULL, true>), grid, block, 0, s, p);
+    else
+        hipLaunchKernelGGL((prompt_mfma_kernel<D, FULL, false>), grid, block, 0, s, p);
 }
 
 template <int D> void launch(const PromptParams& p, hipStream_t s)
 {
-    const dim3 grid((unsigned)((long long)p.tiles * p.num_splits * p.Hkv)), block(kWaves * 64);
-    if (p.page_size != 0)
-        hipLaunchKernelGGL((prompt_mfma_kernel<D, true>), grid, block, 0, s, p);
-    else
-        hipLaunchKernelGGL((prompt_mfma_kernel<D, false>), grid, block, 0, s, p);
+    p.D == D ? launch<D, true>(p, s) : launch<D, false>(p, s);
 }
 
 }  // namespace
 
 hipError_t launch_prompt_mfma(const PromptParams& p, hipStream_t s)
 {
-    p.D == 128 ? launch<128>(p, s) : launch<64>(p, s);
+    p.D <= 64 ? launch<64>(p, s) : p.D <= 128 ? launch<128>(p, s) : launch<256>(p, s);
     return hipGetLastError();
 }
 

@@ -12,6 +12,7 @@ namespace plan {
 
 struct PromptPlan {
     int tiles;         // upper bound on the row tiles of all prompts, one KV head
+    int paired;        // all units run at once, two a CU
     int num_splits;    // most parts of a prompt's tokens
     int split_tokens;  // fewest tokens of a part (the device knows the lengths, and how many tokens make the parts few enough)
     size_t acc_bytes, ml_bytes;
@@ -32,7 +33,8 @@ inline int check_prompt_desc(const spd_prompt_desc* d, bool queries)
         return SPD_EUNSUPPORTED;
     if (d->page_size != 0 && d->page_size != 16)
         return SPD_EUNSUPPORTED;
-    if (d->head_dim > 256 || d->head_dim % 8 != 0 || d->num_kv_heads > 65536 || d->num_q_heads > 65536)
+    if (d->head_dim > 256 || d->head_dim % 8 != 0 || d->num_kv_heads > 65536 || d->num_q_heads > 65536 ||
+        d->q_stride > (1 << 24) || d->kv_stride > (1 << 24))
         return SPD_EUNSUPPORTED;
     const int per_piece = d->dtype == SPD_BF16 ? 8 : 4;  // elements of 16 bytes
     if (d->q_stride % per_piece != 0 || d->kv_stride % per_piece != 0)
@@ -42,9 +44,6 @@ inline int check_prompt_desc(const spd_prompt_desc* d, bool queries)
         return SPD_EINVAL;
     return SPD_OK;
 }
-
-// bf16 with 64 or 128 channels runs on the tiled kernel, which leaves its partial states in fp16.
-inline bool prompt_half_states(const spd_prompt_desc* d) { return d->dtype == SPD_BF16 && (d->head_dim == 64 || d->head_dim == 128); }
 
 inline int make_prompt_plan(const spd_prompt_desc* d, int64_t total, int64_t max_query, int64_t max_kv, PromptPlan* out)
 {
@@ -63,10 +62,10 @@ inline int make_prompt_plan(const spd_prompt_desc* d, int64_t total, int64_t max
     int64_t tiles = total * group / kPromptRows + d->num_prompts;
     if (per_prompt <= tiles / d->num_prompts)
         tiles = per_prompt * d->num_prompts;
-    // Where the tiles alone do not fill the chip, the tokens are cut into parts, which another launch joins.
+    // Where the tiles alone leave CUs idle, the tokens are cut into parts, which another launch joins.
     const int64_t units = tiles * d->num_kv_heads;
     int64_t tokens = max_kv;
-    if (units > 0 && units < kPromptPlaces) {
+    if (units > 0 && units <= kPromptPlaces / 2) {
         tokens = units * max_kv / (2 * kPromptPlaces);
         const int64_t least = max_kv / kPromptMaxSplits > kPromptMinTokens ? max_kv / kPromptMaxSplits : kPromptMinTokens;
         tokens = tokens > least ? tokens : least;
@@ -77,10 +76,11 @@ inline int make_prompt_plan(const spd_prompt_desc* d, int64_t total, int64_t max
     if (units > (1ll << 23) / splits)  // a launch counts its threads in 32 bits
         return SPD_EUNSUPPORTED;
     out->tiles = (int)tiles;
+    out->paired = splits == 1 && d->causal != 0 && units > kPromptPlaces / 2 && units <= kPromptPlaces;
     out->num_splits = (int)splits;
     out->split_tokens = (int)tokens;
     const size_t states = splits > 1 ? (size_t)total * d->num_q_heads * splits : 0;
-    out->acc_bytes = (states * d->head_dim * (prompt_half_states(d) ? 2 : 4) + 255) / 256 * 256;
+    out->acc_bytes = (states * d->head_dim * (d->dtype == SPD_BF16 ? 2 : 4) + 255) / 256 * 256;
     out->ml_bytes = states * 4 * sizeof(float);
     return SPD_OK;
 }

@@ -20,7 +20,8 @@ constexpr int kPlaces = 512; // workgroups that run at once: two a CU
 struct Unit {
     bool any;           // false: past the last unit
     int q0, n, L, kv0;  // the prompt's first query and their number, its tokens, its place in the KV table
-    int tile;           // the prompt's last tiles, which see most, come first
+    int tile;           // the prompt's last tiles, which see most, come first; where all units run at once, two a CU (unit i and unit
+                        // i + half of them), those of the second half come last, so that pairs are even
     int split, splits;  // of the prompt's tokens
     int split_tokens;
 };
@@ -80,9 +81,17 @@ __device__ __forceinline__ Unit find_unit(const PromptParams& p, int item)
             u.kv0 = of(kv0);
             u.splits = of(splits);
             // the tiles of a part follow one another: they read the same tokens
-            const int local = item - base - of(upto - units), t = of(tiles);
+            const int start = base + of(upto - units), local = item - start, t = of(tiles);
+            const int i = local % t;
             u.split = local / t;
-            u.tile = t - 1 - local % t;
+            u.tile = t - 1 - i;
+            if (p.paired) {
+                const int half = p.tiles / 2;
+                if (start >= half)
+                    u.tile = i;
+                else if (start + t > half && i >= half - start)
+                    u.tile = i - (half - start);
+            }
             break;
         }
         base += all;

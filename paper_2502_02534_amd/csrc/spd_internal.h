@@ -144,6 +144,7 @@ struct PromptParams {
     const int* kv_indptr;
     const int* pages;
     int tiles;         // upper bound on the row tiles of all prompts
+    int paired;        // all units run at once, two a CU
     int num_splits;    // most parts that a prompt's tokens are cut into
     int split_tokens;  // fewest tokens of a part
     long long rows;    // total_queries * Hq
