@@ -159,7 +159,7 @@ int write_prompt_kv(const spd_prompt_desc* desc, const void* k, const void* v, c
     p.head_u4 = desc->head_dim * elt / 16;
     p.stride_u4 = desc->kv_stride != 0 ? desc->kv_stride * elt / 16 : (long long)p.Hkv * p.head_u4;
     p.page_size = desc->page_size;
-    if (num_tokens > kMostBlocks * 1024 / ((long long)p.Hkv * p.head_u4))
+    if (num_tokens > 4 * kMostBlocks * 255 / ((long long)p.Hkv * p.head_u4))
         return SPD_EUNSUPPORTED;
     return spd::launch_kv_write(p, (hipStream_t)stream) == hipSuccess ? SPD_OK : SPD_ELAUNCH;
 }

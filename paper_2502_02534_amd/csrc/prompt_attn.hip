@@ -275,6 +275,13 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptParams p)
     const float4* ml = p.part_ml + (row_ok ? row : 0) * S;
     const char* parts = (const char*)p.part_acc + ((row_ok ? row : 0) * S * p.D + (c < p.D ? c : 0)) * (HALF ? 2 : 4);
     const long long part_bytes = (long long)p.D * (HALF ? 2 : 4);
+    uint4 a[kBatch];
+    auto request = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+            a[k] = *reinterpret_cast<const uint4*>(parts + min(s0 + k, S - 1) * part_bytes);
+    };
+    request(0);  // the first parts need not wait for their weights
     float m = -INFINITY;
     for (int s = lane; s < S; s += LANES) {
         const float4 x = ml[s];
@@ -299,10 +306,8 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptParams p)
         }
         const int here = min(LANES, S - s0);
         for (int k0 = 0; k0 < here; k0 += kBatch) {
-            uint4 a[kBatch];
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k)
-                a[k] = *reinterpret_cast<const uint4*>(parts + min(s0 + k0 + k, S - 1) * part_bytes);
+            if (s0 + k0 > 0)
+                request(s0 + k0);
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
                 const float ws = __shfl(w, first_lane + min(k0 + k, LANES - 1));

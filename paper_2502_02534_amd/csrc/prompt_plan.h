@@ -21,7 +21,10 @@ struct PromptPlan {
 constexpr int kPromptRows = 128;       // (token, head of the group) rows per workgroup
 constexpr int kPromptPlaces = 512;     // workgroups that run at once
 constexpr int kPromptMaxSplits = 64;
-constexpr int kPromptMinTokens = 128;  // per split
+// Fewest tokens of a part: a tile of fp32 takes two to eight us, one of bf16 less than one, and a part costs its rows' states.
+// 256 tokens of 4 / 1 fp32 heads of 64 channels, at least 32 / 64 / 128 tokens: 14.2 / 16.5 / 20.9 us; 32 new tokens over 1024 of 32 / 8
+// bf16 heads 20.4 / 18.0 / 16.6, over 2048 26.2 / 21.5 / 19.1.
+inline int prompt_min_tokens(const spd_prompt_desc* d) { return d->dtype == SPD_BF16 ? 128 : 32; }
 
 inline int check_prompt_desc(const spd_prompt_desc* d, bool queries)
 {
@@ -67,7 +70,7 @@ inline int make_prompt_plan(const spd_prompt_desc* d, int64_t total, int64_t max
     int64_t tokens = max_kv;
     if (units > 0 && units <= kPromptPlaces / 2) {
         tokens = units * max_kv / (2 * kPromptPlaces);
-        const int64_t least = max_kv / kPromptMaxSplits > kPromptMinTokens ? max_kv / kPromptMaxSplits : kPromptMinTokens;
+        const int64_t least = max_kv / kPromptMaxSplits > prompt_min_tokens(d) ? max_kv / kPromptMaxSplits : prompt_min_tokens(d);
         tokens = tokens > least ? tokens : least;
     }
     tokens = (tokens + 31) / 32 * 32;
