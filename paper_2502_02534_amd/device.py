@@ -108,11 +108,69 @@ def upload_sampler(inp, device="cuda:0", row_stride=None, pad_value=float("nan")
                          _dev(inp.uniforms, device), torch.empty(rows, dtype=torch.int32, device=device), ws)
 
 
+@dataclasses.dataclass
+class PageTables:
+    """What `build_page_tables` leaves for a batch of requests (all on the device)."""
+    page_indptr: torch.Tensor
+    page_indices: torch.Tensor
+    lens: torch.Tensor        # tokens each request may hold now
+    new_indptr: torch.Tensor  # running count of new tokens
+    slots: Optional[torch.Tensor]
+    free_end: torch.Tensor    # first page of the free list not dealt
+
+
+def build_tables(lens, free_pages, max_pages: int, max_tokens: int = 0, page_size: int = 16, held: Optional[PageTables] = None,
+                 free_begin=None, stream=None) -> PageTables:
+    """Page tables of requests that have to hold `lens` tokens (device int32), dealt from `free_pages`.  `held`: the
+    tables the same requests have so far; `free_begin`: another call's `free_end`.  max_tokens 0: no slot map.
+    The tables and the workspace are allocated here; with `stream` the caller keeps them alive until it is done."""
+    n, dev = lens.numel(), lens.device
+    empty = lambda k, t=torch.int32: torch.empty(k, dtype=t, device=dev)
+    out = PageTables(empty(n + 1), empty(max_pages), empty(n), empty(n + 1), empty(max_tokens, torch.int64) if max_tokens else None,
+                     empty(1))
+    ws = empty(B.build_page_tables_workspace_size(n), torch.uint8)
+    B.build_page_tables(n, page_size, lens, held and held.lens, held and held.page_indptr, held and held.page_indices, free_pages,
+                        free_pages.numel(), free_begin, max_pages, max_tokens, out.page_indptr, out.page_indices, out.lens,
+                        out.new_indptr, out.slots, out.free_end, ws, stream)
+    return out
+
+
+class DevicePrompts:
+    """One layer's prompt pass on the GPU: stores the new tokens' keys and values in the pages that `tables` name, then
+    the attention of the new tokens over everything their prompts hold.  q, k, v: [tokens, heads, head_dim], rows of a
+    projection (their token stride may be larger than their heads); k_pool, v_pool: [pages, kv_heads, 16, head_dim]."""
+
+    def __init__(self, tables: PageTables, q, k, v, k_pool, v_pool, max_query_len: int, max_kv_len: int, causal: bool = True,
+                 sm_scale: float = 0.0):
+        tokens, hq, d = q.shape
+        hkv = k.shape[1]
+        self.tables, self.q, self.k, self.v, self.k_pool, self.v_pool = tables, q, k, v, k_pool, v_pool
+        self.max_query_len, self.max_kv_len = max_query_len, max_kv_len
+        self.desc = B.make_prompt_desc(dtype=B.SPD_BF16 if q.dtype == torch.bfloat16 else B.SPD_F32, num_q_heads=hq, num_kv_heads=hkv,
+                                       head_dim=d, num_prompts=tables.lens.numel(), page_size=16, causal=causal, sm_scale=sm_scale,
+                                       q_stride=q.stride(0), kv_stride=k.stride(0))
+        self.out = torch.empty((tokens, hq, d), dtype=q.dtype, device=q.device)
+        self.lse = torch.empty((tokens, hq), dtype=torch.float32, device=q.device)
+        size = B.prompt_attn_workspace_size(self.desc, tokens, max_query_len, max_kv_len)
+        self.workspace = torch.empty(max(size, 256), dtype=torch.uint8, device=q.device)
+
+    def run(self, stream=None) -> None:
+        t, tokens = self.tables, self.q.shape[0]
+        B.write_prompt_kv(self.desc, self.k, self.v, t.slots, tokens, self.k_pool.shape[0], self.k_pool, self.v_pool, stream)
+        B.prompt_attn(self.desc, self.q, self.k_pool, self.v_pool, t.new_indptr, t.lens, t.page_indptr, t.page_indices, tokens,
+                      self.max_query_len, self.max_kv_len, self.out, self.lse, self.workspace, stream)
+
+
 class DecodeLoop:
     """A loop of decode steps on the device: append the step's K/V (synthetic: there are no
     weights), attention, sampling; lengths, finished flags and the step counter live on the
     device, so the steps can be replayed from a captured graph without host synchronisation.
     Every kernel of a step is one of the library's own launches.
+
+    With `raw_logits` ([rows, vocab], fp32 or bf16) and `penalties` (arguments of `make_penalties` other than
+    `tokens` and `token_lens`) every step shapes the raw logits by what the loop has drawn so far, into the
+    sampler's own logits, before it samples (needs `one_launch`: the step's first launch records the tokens
+    drawn before it; steps still to come hold -1, which is no token).
 
     Per-step inputs are rows of tensors indexed by the device-side step counter:
       q_steps [steps, N, Hq, D], k_steps / v_steps [steps, N, Hkv, D], u_steps [steps, rows].
@@ -120,7 +178,7 @@ class DecodeLoop:
     and `lens_steps` record every step's results for checking."""
 
     def __init__(self, attn: DeviceAttn, sampler: DeviceSampler, q_steps, k_steps, v_steps, u_steps,
-                 end_token: int = -1, one_launch: bool = True):
+                 end_token: int = -1, one_launch: bool = True, raw_logits=None, penalties: Optional[dict] = None):
         self.attn, self.sampler = attn, sampler
         self.one_launch = one_launch
         self.q_steps, self.k_steps, self.v_steps, self.u_steps = q_steps, k_steps, v_steps, u_steps
@@ -149,6 +207,18 @@ class DecodeLoop:
                                              (u_steps, sampler.uniforms, nbytes(sampler.uniforms))])
         self._record_to = B.make_row_copies([(sampler.tokens, self.tokens_steps, nbytes(sampler.tokens)),
                                              (attn.out, self.out_steps, nbytes(attn.out))])
+        if (raw_logits is None) != (penalties is None) or (penalties is not None and not one_launch):
+            raise ValueError("raw_logits and penalties go together, and need one_launch")
+        self.raw_logits, self.penalties = raw_logits, None
+        if penalties is not None:
+            self._steps_drawn = torch.full((self.tokens_steps.shape[1],), self.steps, dtype=torch.int32, device=dev)
+            self._penalty_tensors = dict(penalties, tokens=self.tokens_steps.t(), token_lens=self._steps_drawn)
+            self.penalties = B.make_penalties(**self._penalty_tensors)
+
+    def _shape_logits(self) -> None:
+        raw, s = self.raw_logits, self.sampler
+        B.penalize_logits(raw, B.SPD_BF16 if raw.dtype == torch.bfloat16 else B.SPD_F32, raw.shape[0], raw.shape[1], raw.stride(0),
+                          self.penalties, s.logits, s.logits.stride(0))
 
     def one_step(self) -> None:
         """Enqueues one decode step on the current stream (capturable: kernel launches only).  With
@@ -161,6 +231,8 @@ class DecodeLoop:
                                   a.suffix_page_indices, a.max_suffix_len, s.tokens, self.end_token, self.finished,
                                   self.lens_steps)
             a.run()
+            if self.penalties is not None:
+                self._shape_logits()
             s.run()
             return
         B.decode_step_select(self.step, self.steps, self._select)
