@@ -105,7 +105,7 @@ __global__ __launch_bounds__(kThreads) void penalize_kernel(LogitsParams p, int 
     const long long r = (blockIdx.x & 7) * rows8 + unit / slices;
     if (r >= p.rows)
         return;
-    const long long lo = unit % slices * slice_len, hi = min(p.vocab, lo + slice_len);
+    const int lo = (int)(unit % slices) * slice_len, hi = min((int)p.vocab, lo + slice_len);
 
     const float rep = p.repetition ? p.repetition[r] : 1.f, inv_rep = 1.f / rep;  // (a product for the quotient: half an ulp more)
     const float freq = p.frequency ? p.frequency[r] : 0.f, pres = p.presence ? p.presence[r] : 0.f;
@@ -132,8 +132,8 @@ __global__ __launch_bounds__(kThreads) void penalize_kernel(LogitsParams p, int 
     if (n > 0)
         read_history(0);
     int step = slice_len;
-    for (long long s0 = lo; s0 < hi;) {
-        const int len = (int)min((long long)step, hi - s0), words = (len + 31) / 32;
+    for (int s0 = lo; s0 < hi;) {
+        const int len = min(step, hi - s0), words = (len + 31) / 32;
         // k = place in the stretch.  The wavefront's tile and the words of its bits, all at once
         const int lane = tid & 63, tile0 = (tid >> 6) * kTile, tile_len = min(len - tile0, kTile);
         Four<BF16> raw[ROUNDS];
@@ -142,10 +142,10 @@ __global__ __launch_bounds__(kThreads) void penalize_kernel(LogitsParams p, int 
         for (int u = 0; u < ROUNDS; ++u) {
             const int k = tile0 + 256 * u + 4 * lane;
             if (k < len)
-                raw[u].load(in + (s0 + k) * (BF16 ? 2 : 4), min(4, len - k));
+                raw[u].load(in + (long long)s0 * (BF16 ? 2 : 4) + (unsigned)(k * (BF16 ? 2 : 4)), min(4, len - k));
         }
         if (32 * lane < tile_len) {
-            const long long w = (s0 + tile0) / 32 + lane;
+            const int w = (s0 + tile0) / 32 + lane;
             if (prompt >= 0)
                 seen_words = seen_bits[w];
             if (grammar >= 0)
@@ -159,16 +159,17 @@ __global__ __launch_bounds__(kThreads) void penalize_kernel(LogitsParams p, int 
                         read_history(q0);
 #pragma unroll
                     for (int u = 0; u < kEntries; ++u) {
-                        const long long id = ids[u] - s0;
-                        if (ids[u] >= 0 && id >= 0 && id < len)
+                        const unsigned id = (unsigned)ids[u] - (unsigned)s0;  // (a negative token's is past any length)
+                        if (ids[u] >= 0 && id < (unsigned)len)
                             f((int)id);
                     }
                 }
             };
             auto each_bias = [&](auto f) __attribute__((always_inline)) {
                 for (int k = b0 + tid; k < b1; k += kThreads) {
-                    const long long id = p.bias_tokens[k] - s0;
-                    if (id >= 0 && id < len)
+                    const int token = p.bias_tokens[k];
+                    const unsigned id = (unsigned)token - (unsigned)s0;
+                    if (token >= 0 && id < (unsigned)len)
                         f((int)id, k);
                 }
             };
@@ -255,7 +256,7 @@ __global__ __launch_bounds__(kThreads) void penalize_kernel(LogitsParams p, int 
                 if (len - k >= 4) {
                     typedef float __attribute__((ext_vector_type(4), aligned(4))) any4;
                     const any4 y = {x[0], x[1], x[2], x[3]};
-                    *reinterpret_cast<any4*>(out + s0 + k) = y;
+                    *reinterpret_cast<any4*>(out + s0 + (unsigned)k) = y;
                 } else {
 #pragma unroll
                     for (int e = 0; e < 3; ++e)

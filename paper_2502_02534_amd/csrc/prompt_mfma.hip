@@ -83,7 +83,8 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void prompt_mfma_ker
     const int least = p.causal ? L - n + row0 / p.G : L - 1;
     const int most = p.causal ? L - n + (min(row0 + kRows, rows) - 1) / p.G : L - 1;
     const int wave_last = min(row0 + wave * 32 + 32, rows) - 1;  // last row of this wavefront
-    const int wave_most = wave_last < row0 + wave * 32 ? -1 : p.causal ? L - n + wave_last / p.G : L - 1;
+    const bool works = row0 + wave * 32 < rows;                     // the others copy, and wait at the barriers
+    const int wave_most = !works ? -1 : p.causal ? L - n + wave_last / p.G : L - 1;
 
     const int seen = max(most + 1, 0);
     const int t0 = p.num_splits > 1 ? min(at.split * at.split_tokens, seen) : 0;
@@ -382,7 +383,8 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void prompt_mfma_ker
             const std::integral_constant<int, T % kRing> kslot;
             const std::integral_constant<int, (T + 2) % kRing> vslot;
             copies_up_to(t + lead);
-            if constexpr (T % 2 == 0)
+            if (!works) {
+            } else if constexpr (T % 2 == 0)
                 take_sum(region(yes, yes, yes, kslot, vslot, sa, sb, pb, pa), sb, pb);
             else
                 take_sum(region(yes, yes, yes, kslot, vslot, sb, sa, pa, pb), sa, pa);
