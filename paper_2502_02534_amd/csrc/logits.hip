@@ -138,11 +138,16 @@ __global__ __launch_bounds__(kThreads) void penalize_kernel(LogitsParams p, int 
         const int lane = tid & 63, tile0 = (tid >> 6) * kTile, tile_len = min(len - tile0, kTile);
         Four<BF16> raw[ROUNDS];
         uint32_t seen_words = 0u, allowed_words = 0xffffffffu;
+        const char* const from = in + (long long)(s0 + tile0) * (BF16 ? 2 : 4);
+        if (tile_len == kTile) {
 #pragma unroll
-        for (int u = 0; u < ROUNDS; ++u) {
-            const int k = tile0 + 256 * u + 4 * lane;
-            if (k < len)
-                raw[u].load(in + (long long)s0 * (BF16 ? 2 : 4) + (unsigned)(k * (BF16 ? 2 : 4)), min(4, len - k));
+            for (int u = 0; u < ROUNDS; ++u)
+                raw[u].load(from + (256 * u + 4 * lane) * (BF16 ? 2 : 4), 4);
+        } else {
+#pragma unroll
+            for (int u = 0; u < ROUNDS; ++u)
+                if (256 * u + 4 * lane < tile_len)
+                    raw[u].load(from + (256 * u + 4 * lane) * (BF16 ? 2 : 4), min(4, tile_len - (256 * u + 4 * lane)));
         }
         if (32 * lane < tile_len) {
             const int w = (s0 + tile0) / 32 + lane;
