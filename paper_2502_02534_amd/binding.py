@@ -139,9 +139,15 @@ def _bytes(t: Optional[torch.Tensor]) -> int:
     return 0 if t is None else t.numel() * t.element_size()
 
 
+_cuda_ready = False
+
+
 def _stream(stream) -> int:
     if stream is None:
-        torch.cuda.init()
+        global _cuda_ready
+        if not _cuda_ready:
+            torch.cuda.init()
+            _cuda_ready = True
         return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 

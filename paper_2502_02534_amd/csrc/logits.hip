@@ -8,25 +8,41 @@ namespace spd {
 namespace {
 
 // ---- which tokens occur in a prompt ----------------------------------------------------------------------
-// One workgroup per prompt and stretch of the vocabulary: the stretch's bits are collected in LDS.
+// One workgroup per prompt and stretch of the vocabulary: the stretch's bits are collected in LDS.  Bound: latency (the
+// launch, one round trip for the prompt's range, one for kBatch tokens a thread at a time).
 constexpr int kMarkThreads = 1024;
 constexpr int kMarkWords = 4096;  // of a stretch (131072 tokens)
+constexpr int kBatch = 8;
 
 __global__ __launch_bounds__(kMarkThreads) void mark_tokens_kernel(const int* tokens, const int* indptr, long long vocab,
                                                                    uint32_t* bits, long long stride, int accumulate)
 {
     __shared__ uint32_t lds[kMarkWords];
+    const int first = indptr[blockIdx.x], end = indptr[blockIdx.x + 1];
     const long long all_words = (vocab + 31) / 32, word0 = (long long)blockIdx.y * kMarkWords;
     const int words = (int)min(all_words - word0, (long long)kMarkWords);
     uint32_t* row = bits + (long long)blockIdx.x * stride + word0;
     for (int w = threadIdx.x; w < words; w += kMarkThreads)
         lds[w] = accumulate ? row[w] : 0u;
+    const int lo = (int)word0 * 32, len = (int)min(vocab - lo, (long long)words * 32);
+    int id[kBatch];
+    auto request = [&](int t0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+            id[u] = tokens[min(t0 + (int)threadIdx.x + u * kMarkThreads, end - 1)];
+    };
+    if (first < end)
+        request(first);
     __syncthreads();
-    const long long lo = word0 * 32, hi = min(vocab, lo + (long long)words * 32);
-    for (int t = indptr[blockIdx.x] + (int)threadIdx.x, end = indptr[blockIdx.x + 1]; t < end; t += kMarkThreads) {
-        const int id = tokens[t];
-        if (id >= lo && id < hi)
-            atomicOr(&lds[(id - lo) >> 5], 1u << (id & 31));
+    for (int t0 = first; t0 < end; t0 += kBatch * kMarkThreads) {
+        if (t0 > first)
+            request(t0);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const unsigned at = (unsigned)id[u] - (unsigned)lo;
+            if (t0 + (int)threadIdx.x + u * kMarkThreads < end && id[u] >= 0 && at < (unsigned)len)
+                atomicOr(&lds[at >> 5], 1u << (at & 31));
+        }
     }
     __syncthreads();
     for (int w = threadIdx.x; w < words; w += kMarkThreads)
@@ -101,11 +117,11 @@ __global__ __launch_bounds__(kThreads) void penalize_kernel(LogitsParams p, int 
     __shared__ int wave_sums[kThreads / 64];
     const int tid = threadIdx.x;
     // the rows of an XCD follow one another: they read the same lines of a step-major history and the same prompts' bits
-    const long long unit = blockIdx.x >> 3, rows8 = (p.rows + 7) / 8;
-    const long long r = (blockIdx.x & 7) * rows8 + unit / slices;
+    const unsigned unit = blockIdx.x >> 3, rows8 = (unsigned)((p.rows + 7) / 8);
+    const long long r = (unsigned)__builtin_amdgcn_readfirstlane((blockIdx.x & 7) * rows8 + unit / (unsigned)slices);
     if (r >= p.rows)
         return;
-    const int lo = (int)(unit % slices) * slice_len, hi = min((int)p.vocab, lo + slice_len);
+    const int lo = __builtin_amdgcn_readfirstlane((int)(unit % (unsigned)slices)) * slice_len, hi = min((int)p.vocab, lo + slice_len);
 
     const float rep = p.repetition ? p.repetition[r] : 1.f, inv_rep = 1.f / rep;  // (a product for the quotient: half an ulp more)
     const float freq = p.frequency ? p.frequency[r] : 0.f, pres = p.presence ? p.presence[r] : 0.f;
@@ -133,9 +149,12 @@ __global__ __launch_bounds__(kThreads) void penalize_kernel(LogitsParams p, int 
         read_history(0);
     int step = slice_len;
     for (int s0 = lo; s0 < hi;) {
+        // (opaque, here and in the rounds below, so that no place's address is worked out ahead and kept in registers)
+        int me = tid;
+        asm volatile("" : "+v"(me));
         const int len = min(step, hi - s0), words = (len + 31) / 32;
         // k = place in the stretch.  The wavefront's tile and the words of its bits, all at once
-        const int lane = tid & 63, tile0 = (tid >> 6) * kTile, tile_len = min(len - tile0, kTile);
+        const int lane = me & 63, tile0 = (me >> 6) * kTile, tile_len = min(len - tile0, kTile);
         Four<BF16> raw[ROUNDS];
         uint32_t seen_words = 0u, allowed_words = 0xffffffffu;
         const char* const from = in + (long long)(s0 + tile0) * (BF16 ? 2 : 4);
@@ -171,7 +190,7 @@ __global__ __launch_bounds__(kThreads) void penalize_kernel(LogitsParams p, int 
                 }
             };
             auto each_bias = [&](auto f) __attribute__((always_inline)) {
-                for (int k = b0 + tid; k < b1; k += kThreads) {
+                for (int k = b0 + me; k < b1; k += kThreads) {
                     const int token = p.bias_tokens[k];
                     const unsigned id = (unsigned)token - (unsigned)s0;
                     if (token >= 0 && id < (unsigned)len)
@@ -182,9 +201,9 @@ __global__ __launch_bounds__(kThreads) void penalize_kernel(LogitsParams p, int 
                 return before[id >> 5] + __popc(listed[id >> 5] & ((1u << (id & 31)) - 1u));
             };
             __syncthreads();  // the stretch before has been read
-            if (tid < words)
-                listed[tid] = 0u;
-            for (int i = tid; i < kTable; i += kThreads) {
+            if (me < words)
+                listed[me] = 0u;
+            for (int i = me; i < kTable; i += kThreads) {
                 counts[i] = 0u;
                 bias[i] = 0.f;
             }
@@ -192,28 +211,28 @@ __global__ __launch_bounds__(kThreads) void penalize_kernel(LogitsParams p, int 
             each_token([&](int id) __attribute__((always_inline)) { atomicOr(&listed[id >> 5], 1u << (id & 31)); });
             each_bias([&](int id, int) __attribute__((always_inline)) { atomicOr(&listed[id >> 5], 1u << (id & 31)); });
             __syncthreads();
-            const int bits = tid < words ? __popc(listed[tid]) : 0;
+            const int bits = me < words ? __popc(listed[me]) : 0;
             int upto = bits;
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1) {
                 const int x = __shfl_up(upto, o);
-                upto += (tid & 63) >= o ? x : 0;
+                upto += (me & 63) >= o ? x : 0;
             }
-            if ((tid & 63) == 63)
-                wave_sums[tid >> 6] = upto;
+            if ((me & 63) == 63)
+                wave_sums[me >> 6] = upto;
             __syncthreads();
             int first = upto - bits, total = 0;
 #pragma unroll
             for (int w = 0; w < kThreads / 64; ++w) {
-                first += w < (tid >> 6) ? wave_sums[w] : 0;
+                first += w < (me >> 6) ? wave_sums[w] : 0;
                 total += wave_sums[w];
             }
             if (total > kTable) {  // (for everybody alike)
                 step = kTable;
                 continue;
             }
-            if (tid < words)
-                before[tid] = (uint16_t)first;
+            if (me < words)
+                before[me] = (uint16_t)first;
             __syncthreads();
             each_token([&](int id) __attribute__((always_inline)) { atomicAdd(&counts[place(id)], 1u); });
             each_bias([&](int id, int k) __attribute__((always_inline)) { bias[place(id)] = p.bias_values[k]; });
@@ -229,48 +248,56 @@ __global__ __launch_bounds__(kThreads) void penalize_kernel(LogitsParams p, int 
                 x = x - freq * (float)c - pres;
             return x + bias[at];
         };
-        const uint32_t listed_words = any && 32 * lane < tile_len ? listed[tile0 / 32 + lane] : 0u;
+        uint32_t listed_words = any && 32 * lane < tile_len ? listed[tile0 / 32 + lane] : 0u;
+        float* const to = out + s0 + tile0;
+        auto rounds = [&](auto full) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < ROUNDS; ++u) {
-            // the lane's four bits: of word 8 u + lane / 8, from bit 4 (lane % 8) on
-            const int from = 8 * u + (lane >> 3), shift = 4 * (lane & 7);
-            const uint32_t bits = (uint32_t)__shfl((int)listed_words, from) >> shift & 0xfu;
-            const uint32_t seen = (uint32_t)__shfl((int)seen_words, from) >> shift & 0xfu;
-            const uint32_t allowed = (uint32_t)__shfl((int)allowed_words, from) >> shift & 0xfu;
-            const int k = tile0 + 256 * u + 4 * lane;
-            if (k < len) {
-                float x[4];
+            for (int u = 0; u < ROUNDS; ++u) {
+                int at_lane = lane;
+                asm volatile("" : "+v"(at_lane), "+v"(listed_words), "+v"(seen_words), "+v"(allowed_words));
+                // the lane's four bits: of word 8 u + lane / 8, from bit 4 (lane % 8) on
+                const int from_lane = 8 * u + (at_lane >> 3), shift = 4 * (at_lane & 7), k = 256 * u + 4 * at_lane;
+                const uint32_t bits = any ? (uint32_t)__shfl((int)listed_words, from_lane) >> shift & 0xfu : 0u;
+                const uint32_t seen = prompt >= 0 ? (uint32_t)__shfl((int)seen_words, from_lane) >> shift & 0xfu : 0u;
+                const uint32_t allowed = grammar >= 0 ? (uint32_t)__shfl((int)allowed_words, from_lane) >> shift & 0xfu : 0xfu;
+                if (full || k < tile_len) {
+                    float x[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    x[e] = raw[u].get(e);
-                if (seen != 0u)
+                    for (int e = 0; e < 4; ++e)
+                        x[e] = raw[u].get(e);
+                    if (seen != 0u)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float y = x[e] * (x[e] > 0.f ? inv_rep : rep);
-                        x[e] = (seen >> e) & 1u ? y : x[e];
+                        for (int e = 0; e < 4; ++e) {
+                            const float y = x[e] * (x[e] > 0.f ? inv_rep : rep);
+                            x[e] = (seen >> e) & 1u ? y : x[e];
+                        }
+                    if (bits != 0u)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if ((bits >> e) & 1u)
+                                x[e] = shape(x[e], (seen >> e) & 1u, tile0 + k + e);
+                    if (allowed != 0xfu)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            x[e] = (allowed >> e) & 1u ? x[e] : -INFINITY;
+                    if (full || tile_len - k >= 4) {
+                        typedef float __attribute__((ext_vector_type(4), aligned(4))) any4;
+                        const any4 y = {x[0], x[1], x[2], x[3]};
+                        *reinterpret_cast<any4*>(to + k) = y;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 3; ++e)
+                            if (e < tile_len - k)
+                                to[k + e] = x[e];
                     }
-                if (bits != 0u)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if ((bits >> e) & 1u)
-                            x[e] = shape(x[e], (seen >> e) & 1u, k + e);
-                if (allowed != 0xfu)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        x[e] = (allowed >> e) & 1u ? x[e] : -INFINITY;
-                if (len - k >= 4) {
-                    typedef float __attribute__((ext_vector_type(4), aligned(4))) any4;
-                    const any4 y = {x[0], x[1], x[2], x[3]};
-                    *reinterpret_cast<any4*>(out + s0 + (unsigned)k) = y;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 3; ++e)
-                        if (e < len - k)
-                            out[s0 + k + e] = x[e];
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
-            __builtin_amdgcn_sched_barrier(0);  // (the rounds' shuffles would otherwise all be kept in registers)
-        }
+        };
+        if (tile_len == kTile)
+            rounds(std::true_type{});
+        else
+            rounds(std::false_type{});
         s0 += len;
     }
 }
@@ -298,11 +325,11 @@ hipError_t launch_penalize_logits(const LogitsParams& p, hipStream_t s)
         else
             hipLaunchKernelGGL((penalize_kernel<false, R>), grid, dim3(kThreads), 0, s, p, (int)slices);
     };
-    // fp32 rows of 128256 tokens, histories of 128 to 1024, slices of 2 / 4 / 8 rounds: 1 row 7.7 / 9.4 / 11.6 us, 16 rows
-    // 9.6 / 10.4 / 12.9, 32 rows 16.6 / 14.3 / 16.5, 64 rows 23.8 / 20.9 / 19.6; 256 rows 101 / 77 / 81; 1024 rows of bf16
-    // and histories up to 2048 - / 256 / 207
+    // Rows of 128256 tokens, slices of 2 / 4 / 8 rounds.  fp32, histories of 128 to 1024: 1 row 8.4 / 8.4 / 11.6 us, 16 rows
+    // 9.5 / 10.4 / 12.8, 32 rows 16.6 / 14.4 / 16.2, 64 rows 20.7 / 19.1 / 19.9, 128 rows 34.7 / 31.6 / 29.1, 256 rows
+    // 80 / 62 / 65; bf16, histories up to 2048: 1024 rows 339 / 225 / 176.
     const long long tokens = p.rows * p.vocab;
-    if (tokens >= 6000000)
+    if (tokens >= 12000000)
         go(std::integral_constant<int, 8>{});
     else if (tokens >= 3000000)
         go(std::integral_constant<int, 4>{});
