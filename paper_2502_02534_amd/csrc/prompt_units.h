@@ -28,27 +28,6 @@ struct Unit {
 
 __device__ __forceinline__ int row_tiles(const PromptParams& p, int n) { return (n * p.G + kRows - 1) / kRows; }
 
-// Tokens of a part: the same in every lane of every wavefront.
-__device__ __forceinline__ int part_tokens(const PromptParams& p)
-{
-    const int lane = threadIdx.x & 63;
-    float work = 0.f, tiles = 0.f;
-    for (int b = lane; b < p.B; b += 64) {
-        const float t = (float)row_tiles(p, max(p.query_indptr[b + 1] - p.query_indptr[b], 0));
-        tiles += t;
-        work += t * (float)max(p.kv_lens[b], 0);
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        work += __shfl_xor(work, o);
-        tiles += __shfl_xor(tiles, o);
-    }
-    const float parts = fmaxf((float)kPlaces - tiles * (float)p.Hkv, 1.f);
-    const float even = fminf(work * (float)p.Hkv / parts, 1e9f);
-    const int tokens = ((int)even + 32) & ~31;
-    return __builtin_amdgcn_readfirstlane(max(tokens, p.split_tokens));
-}
-
 __device__ __forceinline__ Unit find_unit(const PromptParams& p, int item)
 {
     const int lane = threadIdx.x & 63;
@@ -56,12 +35,39 @@ __device__ __forceinline__ Unit find_unit(const PromptParams& p, int item)
     u.any = false;
     u.q0 = u.n = u.L = u.kv0 = u.tile = u.split = 0;
     u.splits = 1;
-    u.split_tokens = p.num_splits > 1 ? part_tokens(p) : 0;
+    u.split_tokens = 0;
+    int q0, n, L, kv0, tiles;  // of the lane's prompt
+    auto load = [&](int b0) __attribute__((always_inline)) {
+        const int b = min(b0 + lane, p.B - 1);
+        q0 = p.query_indptr[b];
+        const int q1 = p.query_indptr[b + 1];
+        L = p.kv_lens[b];
+        kv0 = p.kv_indptr[b];
+        n = max(q1 - q0, 0);
+        tiles = b0 + lane < p.B ? row_tiles(p, n) : 0;
+    };
+    load(0);
+    if (p.num_splits > 1) {
+        // tokens of a part: the same in every lane of every wavefront
+        float work = (float)tiles * (float)max(L, 0), all = (float)tiles;
+        for (int b0 = 64; b0 < p.B; b0 += 64) {
+            load(b0);
+            work += (float)tiles * (float)max(L, 0);
+            all += (float)tiles;
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            work += __shfl_xor(work, o);
+            all += __shfl_xor(all, o);
+        }
+        const float parts = fmaxf((float)kPlaces - all * (float)p.Hkv, 1.f);
+        const int tokens = ((int)fminf(work * (float)p.Hkv / parts, 1e9f) + 32) & ~31;
+        u.split_tokens = __builtin_amdgcn_readfirstlane(max(tokens, p.split_tokens));
+    }
     int base = 0;
     for (int b0 = 0; b0 < p.B; b0 += 64) {
-        const int b = min(b0 + lane, p.B - 1);
-        const int q0 = p.query_indptr[b], n = max(p.query_indptr[b + 1] - q0, 0), L = p.kv_lens[b], kv0 = p.kv_indptr[b];
-        const int tiles = b0 + lane < p.B ? row_tiles(p, n) : 0;
+        if (p.B > 64)
+            load(b0);
         const int splits = p.num_splits > 1 ? min(max((L + u.split_tokens - 1) / u.split_tokens, 1), p.num_splits) : 1;
         const int units = tiles * splits;
         int upto = units;
