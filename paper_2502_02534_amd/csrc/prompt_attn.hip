@@ -15,7 +15,10 @@
 // added at the end to the rows that see them.
 //
 // Bound: the matrix pipe, 155 TFLOP/s for fp32 products.  The tile after the present one is on its way into registers
-// while its products run, and goes to the other half of LDS after them: one barrier a tile.
+// while its products run, and goes to the other half of LDS after them: one barrier a tile (two: 4096 tokens 697 us, one: 578).
+// 16 query and 4 KV heads, causal: 4096 tokens of 128 channels 578 us, 119 TFLOP/s of the products that the rows need (8192: 2.34 ms, 117),
+// 8192 of 64 1.21 ms, 114; 8 and 4 heads, 2000 of 256 243 us, 68 (one workgroup a CU: its LDS and registers hold no second).
+// Few rows: 256 tokens of 4 and 1 heads of 64 channels 9.0 us in 128 units of up to 96 tokens, and 3.9 for the launch that joins them.
 #include "prompt_units.h"
 
 #include <hip/hip_fp16.h>
@@ -59,7 +62,7 @@ __device__ __forceinline__ bool take_odd(uint4& v)
     return any;
 }
 
-template <int DP>  // channels, padded with zeros
+template <int DP, bool PAGED>  // channels, padded with zeros
 __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void prompt_attn_f32_kernel(PromptParams p)
 {
     constexpr int kRowPieces = DP / 4, kPieces = kTileN * kRowPieces / kThreads;
@@ -94,18 +97,25 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void prompt_attn_f32_k
 
     const int first = at.kv0;
     auto offset = [&](int t) -> long long {  // of token t's row of this KV head, in bytes
-        if (p.page_size != 0)
+        if (PAGED)
             return (((long long)p.pages[first + (t >> 4)] * p.Hkv + j) * 16 + (t & 15)) * p.D * 4;
         return ((long long)(first + t) * p.kv_stride + (long long)j * p.D) * 4;
     };
     uint4 kreg[kPieces], vreg[kPieces];
     auto request = [&](int tb) __attribute__((always_inline)) {
+        int page[kPieces] = {};  // (all of them before the first row's load: each wait is for everything asked for before it)
+        if (PAGED) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+                page[i] = p.pages[first + (min(tb + (tid + i * kThreads) / kRowPieces, t1 - 1) >> 4)];
+        }
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            const int piece = tid + i * kThreads, row = piece / kRowPieces, c = piece % kRowPieces;
+            const int piece = tid + i * kThreads, row = piece / kRowPieces, c = piece % kRowPieces, t = tb + row;
             kreg[i] = vreg[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (tb + row < t1 && c * 4 < p.D) {
-                const long long o = offset(tb + row) + c * 16;
+            if (t < t1 && c * 4 < p.D) {
+                const long long o = c * 16 + (PAGED ? (((long long)page[i] * p.Hkv + j) * 16 + (t & 15)) * p.D * 4
+                                                : ((long long)(first + t) * p.kv_stride + (long long)j * p.D) * 4);
                 kreg[i] = *reinterpret_cast<const uint4*>((const char*)p.k + o);
                 vreg[i] = *reinterpret_cast<const uint4*>((const char*)p.v + o);
             }
@@ -149,6 +159,9 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void prompt_attn_f32_k
     __syncthreads();
     if (t0 < t1)
         put(0);
+#pragma unroll
+    for (int u = 0; DP <= 128 && u < DP / 8; ++u)  // waits for the queries here: a wait in the loop would be for the next tile's loads too
+        asm volatile("" : "+v"(qf[u]));
     __syncthreads();
     int nth = 0;
     for (int tb = t0; tb < t1; tb += kTileN, ++nth) {
@@ -359,7 +372,14 @@ template <typename T, int LANES> void launch_merge(const PromptParams& p, hipStr
 template <int DP, int LANES> void launch_f32(const PromptParams& p, hipStream_t s)
 {
     const dim3 grid((unsigned)((long long)p.tiles * p.num_splits * p.Hkv)), block(kThreads);
-    hipLaunchKernelGGL(prompt_attn_f32_kernel<DP>, grid, block, 0, s, p);
+    // Two workgroups a CU, which the pairs of tiles and the length of parts count on (prompt_units.h): 64 channels alone would fit
+    // four, and then long units share a CU.  16 heads, 64 channels, with four / three / two a CU: 2 x 4096 tokens 788 / 689 / 657 us,
+    // 1 x 8192 1292 / 1185 / 1210.
+    constexpr int kSpareLds = DP == 64 ? 20480 : 0;
+    if (p.page_size != 0)
+        hipLaunchKernelGGL((prompt_attn_f32_kernel<DP, true>), grid, block, kSpareLds, s, p);
+    else
+        hipLaunchKernelGGL((prompt_attn_f32_kernel<DP, false>), grid, block, kSpareLds, s, p);
     if (p.num_splits > 1)
         launch_merge<float, LANES>(p, s);
 }
