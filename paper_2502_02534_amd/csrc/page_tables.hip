@@ -38,6 +38,7 @@ __device__ __forceinline__ void block_sums(T (&x)[N], T (&all)[N], T* lds)
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         T before = 0, sum = 0;
+#pragma unroll 4
         for (int w = 0; w < kScanThreads / 64; ++w) {
             const T y = lds[k * (kScanThreads / 64) + w];
             before += w < wave ? y : (T)0;
