@@ -69,6 +69,7 @@ int prompt_attn(const spd_prompt_desc* desc, const void* q, const void* k, const
     p.pages = kv_page_indices;
     p.tiles = pl.tiles;
     p.paired = pl.paired;
+    p.by_length = pl.by_length;
     p.num_splits = pl.num_splits;
     p.split_tokens = pl.split_tokens;
     p.rows = total_queries * p.Hq;

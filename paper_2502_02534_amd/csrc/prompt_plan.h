@@ -13,6 +13,7 @@ namespace plan {
 struct PromptPlan {
     int tiles;         // upper bound on the row tiles of all prompts, one KV head
     int paired;        // all units run at once, two a CU
+    int by_length;     // units in the order of the tokens that they see, across prompts
     int num_splits;    // most parts of a prompt's tokens
     int split_tokens;  // fewest tokens of a part (the device knows the lengths, and how many tokens make the parts few enough)
     size_t acc_bytes, ml_bytes;
@@ -21,6 +22,11 @@ struct PromptPlan {
 constexpr int kPromptRows = 128;       // (token, head of the group) rows per workgroup
 constexpr int kPromptPlaces = 512;     // workgroups that run at once
 constexpr int kPromptMaxSplits = 64;
+// Up to so many prompts, the units of all of them run in the order of their tokens, so that a launch ends with its shortest; with more,
+// prompt by prompt, so that those that run together read the same K and V.  Prompt by prompt / by length: 2 x 4096 fp32 tokens of 16 heads
+// of 64 channels 656 / 612 us; 32 and 8 bf16 heads of 64 channels, 3 x 500..4001 114.7 / 110.6, 3 x 2000 73.3 / 69.5, 24 x 300..1000 90.7 / 92.2;
+// of 128, 4 x 1000..4000 271 / 265, 8 x 2048 323 / 327, 26 x 300..512 85.7 / 98.8.
+constexpr int kPromptsByLength = 4;
 // Fewest tokens of a part: a tile of fp32 takes two to eight us, one of bf16 less than one, and a part costs its rows' states.
 // 256 tokens of 4 / 1 fp32 heads of 64 channels, at least 32 / 64 / 128 tokens: 14.2 / 16.5 / 20.9 us; 32 new tokens over 1024 of 32 / 8
 // bf16 heads 20.4 / 18.0 / 16.6, over 2048 26.2 / 21.5 / 19.1.
@@ -80,6 +86,7 @@ inline int make_prompt_plan(const spd_prompt_desc* d, int64_t total, int64_t max
         return SPD_EUNSUPPORTED;
     out->tiles = (int)tiles;
     out->paired = splits == 1 && d->causal != 0 && units > kPromptPlaces / 2 && units <= kPromptPlaces;
+    out->by_length = splits == 1 && d->causal != 0 && !out->paired && d->num_prompts > 1 && d->num_prompts <= kPromptsByLength;
     out->num_splits = (int)splits;
     out->split_tokens = (int)tokens;
     const size_t states = splits > 1 ? (size_t)total * d->num_q_heads * splits : 0;

@@ -2,7 +2,8 @@
 //
 // Work is cut into units: (prompt, tile of kPromptRows rows, part of split_tokens tokens), times the KV heads.  The
 // host knows only bounds on the lengths, so the units of each prompt are counted on the device, by every wavefront
-// for itself: 64 prompts at a time, a lane each, with everything about the prompt that the workgroup needs.
+// for itself: 64 prompts at a time, a lane each, with everything about the prompt that the workgroup needs.  They follow
+// one another prompt by prompt, or (a few causal prompts) by the number of their tile, last tiles first.
 //
 // Parts.  A part costs its rows' partial states (written once, read once by the launch that joins them) besides a workgroup's
 // start, so there are no more than run at once: with W = sum of tiles * tokens and T = number of tiles, over all KV heads,
@@ -47,6 +48,37 @@ __device__ __forceinline__ Unit find_unit(const PromptParams& p, int item)
         tiles = b0 + lane < p.B ? row_tiles(p, n) : 0;
     };
     load(0);
+    const auto of = [](int x, int l) { return __builtin_amdgcn_readlane(x, l); };
+    const auto take = [&](int l) __attribute__((always_inline)) {
+        u.any = true;
+        u.q0 = of(q0, l);
+        u.n = of(n, l);
+        u.L = of(L, l);
+        u.kv0 = of(kv0, l);
+    };
+    if (p.by_length) {
+        // with `ahead(t)` the units of tiles t and later, the largest t with ahead(t) > item, 64 candidates at a time
+        int lo = 0, width = p.tiles + 1, ahead = 0;
+        while (width > 1) {
+            const int step = (width + 63) >> 6, t = lo + lane * step;
+            int here = 0;
+            for (int b = 0; b < p.B; ++b)
+                here += max(of(tiles, b) - t, 0);
+            const unsigned long long fits = __ballot(here > item);
+            if (fits == 0ull)
+                return u;  // past the last unit (the first candidate counts them all)
+            const int l = 63 - __clzll((long long)fits);
+            ahead = of(here, l);
+            lo += l * step;
+            width = step;
+        }
+        const unsigned long long have = __ballot(tiles > lo);
+        const int nth = item - (ahead - __popcll(have));  // among the prompts that have this tile
+        const int rank = __builtin_amdgcn_mbcnt_hi((unsigned)(have >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)have, 0u));
+        take(__ffsll(__ballot(tiles > lo && rank == nth)) - 1);
+        u.tile = lo;
+        return u;
+    }
     if (p.num_splits > 1) {
         // tokens of a part: the same in every lane of every wavefront
         float work = (float)tiles * (float)max(L, 0), all = (float)tiles;
@@ -79,15 +111,10 @@ __device__ __forceinline__ Unit find_unit(const PromptParams& p, int item)
         const int all = __builtin_amdgcn_readfirstlane(__shfl(upto, 63));
         if (item < base + all) {
             const int l = __ffsll((unsigned long long)__ballot(item < base + upto)) - 1;
-            const auto of = [&](int x) { return __builtin_amdgcn_readfirstlane(__shfl(x, l)); };
-            u.any = true;
-            u.q0 = of(q0);
-            u.n = of(n);
-            u.L = of(L);
-            u.kv0 = of(kv0);
-            u.splits = of(splits);
+            take(l);
+            u.splits = of(splits, l);
             // the tiles of a part follow one another: they read the same tokens
-            const int start = base + of(upto - units), local = item - start, t = of(tiles);
+            const int start = base + of(upto - units, l), local = item - start, t = of(tiles, l);
             const int i = local % t;
             u.split = local / t;
             u.tile = t - 1 - i;

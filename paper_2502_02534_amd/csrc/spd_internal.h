@@ -145,6 +145,7 @@ struct PromptParams {
     const int* pages;
     int tiles;         // upper bound on the row tiles of all prompts
     int paired;        // all units run at once, two a CU
+    int by_length;     // units in the order of the tokens that they see, most first, across prompts
     int num_splits;    // most parts that a prompt's tokens are cut into
     int split_tokens;  // fewest tokens of a part
     long long rows;    // total_queries * Hq

@@ -50,6 +50,8 @@ int main()
                                             return fail("parts where the tiles are enough, or too short", units, p.split_tokens);
                                         if (p.paired && (p.num_splits > 1 || !causal || units <= kPromptPlaces / 2 || units > kPromptPlaces))
                                             return fail("pairs", units, p.num_splits);
+                                        if (p.by_length && (p.num_splits > 1 || !causal || p.paired || prompts < 2 || prompts > 64))
+                                            return fail("order", prompts, p.num_splits);
                                         const size_t states = p.num_splits > 1 ? (size_t)total * d.num_q_heads * p.num_splits : 0;
                                         if (p.ml_bytes != states * 16 || p.acc_bytes < states * dim * (dtype == SPD_BF16 ? 2 : 4) || p.acc_bytes % 256 != 0)
                                             return fail("workspace", (long long)p.acc_bytes, (long long)states);

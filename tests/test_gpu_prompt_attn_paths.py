@@ -54,6 +54,19 @@ def test_pairs_of_several_prompts(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new,past", [([1300, 1217], [0, 0]), ([900, 0, 1100, 1], [0, 0, 200, 5]), ([40, 2500, 130], [0, 0, 7]),
+                                      ([1, 1, 1, 2177], [0, 0, 0, 0])])
+def test_units_of_a_few_prompts_by_length(dtype, new, past):
+    # more units than run at once: tile by tile across the prompts, also where one has no tiles or one alone has many
+    Whole(dtype, 32, 32, 64, new, past, seed=sum(new)).check()
+
+
+def test_units_by_length_of_a_prompt_of_many_tiles():
+    """More tiles than lanes: 32 rows of a token, 4 tokens a tile."""
+    Whole("bf16", 32, 1, 64, [2100, 4, 300], [0, 60, 0], seed=53, page=PAGE).check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_parts_of_more_prompts_than_lanes(dtype):
     """Some prompts are one part, some several: their length is found from all the lengths, 64 prompts at a time."""
     new = [(3 * i) % 4 for i in range(100)]
