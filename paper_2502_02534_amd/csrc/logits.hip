@@ -9,7 +9,8 @@ namespace {
 
 // ---- which tokens occur in a prompt ----------------------------------------------------------------------
 // One workgroup per prompt and stretch of the vocabulary: the stretch's bits are collected in LDS.  Bound: latency (the
-// launch, one round trip for the prompt's range, one for kBatch tokens a thread at a time).
+// launch, one round trip for the prompt's range, one for kBatch tokens a thread at a time): one prompt of 8192 tokens 2.8 us, eight
+// of 1024 to 16384 over 128256 ids 4.2.
 constexpr int kMarkThreads = 1024;
 constexpr int kMarkWords = 4096;  // of a stretch (131072 tokens)
 constexpr int kBatch = 8;
@@ -55,6 +56,11 @@ __global__ __launch_bounds__(kMarkThreads) void mark_tokens_kernel(const int* to
 // then pass through once, four a thread, and only those whose bit is set look into the table.  A slice with more
 // listed tokens than the table holds is taken in stretches as long as the table.  A wavefront has the logits of its
 // tokens on their way before the table is begun, and takes a word of every bit row per lane, handed round with shuffles.
+//
+// Bound: HBM, logits read and written once.  1024 rows of 128256 bf16 logits, histories up to 2048 by steps, 8 prompts' bits, 16 biases and
+// a grammar row each: 173 us, 4.6 TB/s (a cast of the same logits to fp32 136; histories row by row 163, none 150); 64 fp32 rows
+// 17.8 us, 3.7 TB/s: reading the history, then the table, is a chain that the first slices wait for.  48 to 64 registers: four
+// workgroups a CU (with 108, two: 198 us).
 constexpr int kThreads = 512;
 constexpr int kTable = 2048;         // places
 constexpr int kEntries = 4;          // of the history, a thread: a history of kEntries * kThreads is read once

