@@ -528,7 +528,7 @@ typedef struct spd_penalties {
  *   out        float [rows, vocab], rows out_stride apart; may be logits itself (fp32, equal strides), else
  *              must not overlap it
  *   penalties  max_tokens up to 2^24
- *   vocab      up to 2^30; rows + 8 times ceil(vocab / 16384) up to 2^22
+ *   vocab      up to 2^30; (rows + 8) * ceil(vocab / 16384) up to 2^22
  * rows 0 is a call that does nothing.  Returns spd_status.
  */
 SPD_API int penalize_logits(const void *logits, int32_t logits_dtype, int64_t rows, int64_t vocab,

@@ -19,7 +19,8 @@ __global__ __launch_bounds__(kMarkThreads) void mark_tokens_kernel(const int* to
                                                                    uint32_t* bits, long long stride, int accumulate)
 {
     __shared__ uint32_t lds[kMarkWords];
-    const int first = indptr[blockIdx.x], end = indptr[blockIdx.x + 1];
+    // (unsigned: past the last of up to 2^31 tokens a thread's place still fits)
+    const unsigned first = (unsigned)max(indptr[blockIdx.x], 0), end = (unsigned)max(indptr[blockIdx.x + 1], 0);
     const long long all_words = (vocab + 31) / 32, word0 = (long long)blockIdx.y * kMarkWords;
     const int words = (int)min(all_words - word0, (long long)kMarkWords);
     uint32_t* row = bits + (long long)blockIdx.x * stride + word0;
@@ -27,21 +28,21 @@ __global__ __launch_bounds__(kMarkThreads) void mark_tokens_kernel(const int* to
         lds[w] = accumulate ? row[w] : 0u;
     const int lo = (int)word0 * 32, len = (int)min(vocab - lo, (long long)words * 32);
     int id[kBatch];
-    auto request = [&](int t0) __attribute__((always_inline)) {
+    auto request = [&](unsigned t0) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < kBatch; ++u)
-            id[u] = tokens[min(t0 + (int)threadIdx.x + u * kMarkThreads, end - 1)];
+            id[u] = tokens[min(t0 + threadIdx.x + u * kMarkThreads, end - 1)];
     };
     if (first < end)
         request(first);
     __syncthreads();
-    for (int t0 = first; t0 < end; t0 += kBatch * kMarkThreads) {
+    for (unsigned t0 = first; t0 < end; t0 += kBatch * kMarkThreads) {
         if (t0 > first)
             request(t0);
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
             const unsigned at = (unsigned)id[u] - (unsigned)lo;
-            if (t0 + (int)threadIdx.x + u * kMarkThreads < end && id[u] >= 0 && at < (unsigned)len)
+            if (t0 + threadIdx.x + u * kMarkThreads < end && id[u] >= 0 && at < (unsigned)len)
                 atomicOr(&lds[at >> 5], 1u << (at & 31));
         }
     }

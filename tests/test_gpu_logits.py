@@ -236,3 +236,22 @@ def test_a_captured_call_follows_the_tokens():
         for t in range(step + 1):
             counts[torch.arange(rows, device=DEV), tokens[t].long()] += 1
         want = torch.where(counts > 0, x - 0.5 * counts - 0.0, x)
+
+
+def test_marks_of_the_last_of_two_to_the_31_tokens():
+    """Places of tokens that a thread would reach past 2^31 are not read."""
+    from paper_2502_02534_amd import binding as B
+    if torch.cuda.get_device_properties(0).total_memory < (24 << 30):
+        pytest.skip("needs 9 GB of device memory")
+    n, vocab = (1 << 31) - 1, 3000
+    tokens = torch.empty(n, dtype=torch.int32, device=DEV)
+    tail = torch.arange(100, dtype=torch.int32, device=DEV) * 29
+    tokens[-100:] = tail
+    indptr = torch.tensor([n - 100, n], dtype=torch.int32, device=DEV)
+    bits = torch.zeros((1, 94), dtype=torch.int32, device=DEV)
+    B.mark_prompt_tokens(tokens, indptr, 1, vocab, bits, 94)
+    torch.cuda.synchronize()
+    want = torch.zeros(94 * 32, dtype=torch.int64)
+    want[tail.cpu().long()] = 1
+    words = (want.view(94, 32) << torch.arange(32)).sum(1)
+    assert torch.equal(bits[0].cpu().long() & 0xffffffff, words)
