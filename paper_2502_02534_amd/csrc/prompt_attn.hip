@@ -18,10 +18,11 @@
 // while its products run, and goes to the other half of LDS after them: one barrier a tile (two: 4096 tokens 697 us, one: 578).
 // 16 query and 4 KV heads, causal: 4096 tokens of 128 channels 578 us, 119 TFLOP/s of the products that the rows need (8192: 2.34 ms, 117),
 // 8192 of 64 1.21 ms, 114; 8 and 4 heads, 2000 of 256 243 us, 68 (one workgroup a CU: its LDS and registers hold no second).
-// Few rows: 256 tokens of 4 and 1 heads of 64 channels 9.0 us in 64 units of 32 tokens, and 3.9 for the launch that joins them.
+// Few rows: 256 tokens of 4 and 1 heads of 64 channels 9.0 us in 64 units of 32 tokens, and 3.6 for the launch that joins them.
 #include "prompt_units.h"
 
 #include <hip/hip_fp16.h>
+#include <type_traits>
 
 namespace spd {
 namespace {
@@ -282,16 +283,17 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void prompt_attn_f32_k
 }
 
 // Joins the parts of a row: with states (m_i, l_i, acc_i), m = max m_i and w_i = 2^(m_i - m),
-// out = sum w_i acc_i / sum w_i l_i.  LANES lanes take a row, 16 bytes of a part each; they also take its parts' (m, l, scale)
-// and hand their weights round.  Bound by latency, then by the partial states, whose loads a lane has in flight kBatch at a time:
-// 7200 rows in 3 to 9 parts of 128 channels 7.0 us (23 MB), 1024 fp32 rows in 8 parts of 64 channels 3.9.
-template <typename T, int LANES>
-__global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptParams p)
+// out = sum w_i acc_i / sum w_i l_i.  LANES lanes take a part of a row, 16 bytes each, and SUB such groups
+// every SUB-th part; each group also takes all its parts' (m, l, scale) and hands their weights round.  Bound by latency, then by the
+// partial states, whose loads a lane has in flight kBatch at a time:
+// 7200 rows in 3 to 9 parts of 128 channels 6.4 us, 1024 fp32 rows in 8 parts of 64 channels 3.6.
+template <typename T, int LANES, int SUB>
+__global__ __launch_bounds__(kThreads, 7) void prompt_merge_kernel(PromptParams p)
 {
     constexpr bool HALF = sizeof(T) == 2;
-    constexpr int kRowsPerBlock = kThreads / LANES, kBatch = 8, kCh = HALF ? 8 : 4;
-    const int lane = threadIdx.x % LANES, first_lane = (threadIdx.x & 63) - lane, c = lane * kCh;
-    const long long row = (long long)blockIdx.x * kRowsPerBlock + threadIdx.x / LANES;
+    constexpr int kRowsPerBlock = kThreads / (LANES * SUB), kBatch = SUB > 1 ? 4 : 8, kCh = HALF ? 8 : 4;
+    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES % SUB, first_lane = (threadIdx.x & 63) - lane, c = lane * kCh;
+    const long long row = (long long)blockIdx.x * kRowsPerBlock + threadIdx.x / (LANES * SUB);
     const bool row_ok = row < (long long)p.query_indptr[p.B] * p.Hq && row < p.rows;
     const int S = p.num_splits;
     const float4* ml = p.part_ml + (row_ok ? row : 0) * S;
@@ -300,8 +302,11 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptParams p)
     uint4 a[kBatch];
     auto request = [&](int s0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int k = 0; k < kBatch; ++k)
-            a[k] = *reinterpret_cast<const uint4*>(parts + min(s0 + k, S - 1) * part_bytes);
+        for (int k = 0; k < kBatch; ++k) {
+            a[k] = make_uint4(0u, 0u, 0u, 0u);
+            if (s0 + group + SUB * k < S)
+                a[k] = *reinterpret_cast<const uint4*>(parts + (s0 + group + SUB * k) * part_bytes);
+        }
     };
     request(0);  // the first parts need not wait for their weights
     float m = -INFINITY;
@@ -326,14 +331,17 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptParams p)
                 w = HALF ? u * x.y * x.z : u;
             }
         }
-        const int here = min(LANES, S - s0);
-        for (int k0 = 0; k0 < here; k0 += kBatch) {
+        // up to the last part that holds anything: a prompt may have fewer than the longest one
+        const unsigned long long holds = __ballot(w != 0.f) >> first_lane;
+        const int here = 64 - __clzll((long long)(LANES == 64 ? holds : holds & ((1ull << (LANES & 63)) - 1)));
+        for (int k0 = 0; k0 < here; k0 += SUB * kBatch) {
             if (s0 + k0 > 0)
                 request(s0 + k0);
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
-                const float ws = __shfl(w, first_lane + min(k0 + k, LANES - 1));
-                if (ws != 0.f && k0 + k < here) {  // (a part that holds nothing was not written)
+                const int at = k0 + group + SUB * k;
+                const float ws = __shfl(w, first_lane + min(at, LANES - 1));
+                if (ws != 0.f && at < here) {  // (a part that holds nothing was not written)
                     const uint32_t v[4] = {a[k].x, a[k].y, a[k].z, a[k].w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -352,7 +360,12 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptParams p)
 #pragma unroll
     for (int o = LANES / 2; o > 0; o >>= 1)
         l += __shfl_xor(l, o);
-    if (!row_ok)
+#pragma unroll
+    for (int o = LANES; o < LANES * SUB; o <<= 1)
+#pragma unroll
+        for (int e = 0; e < kCh; ++e)
+            acc[e] += __shfl_xor(acc[e], o);
+    if (!row_ok || group != 0)
         return;
     const bool none = l == 0.f;
     const float inv = none ? 0.f : 1.f / l;
@@ -373,9 +386,18 @@ __global__ __launch_bounds__(kThreads) void prompt_merge_kernel(PromptParams p)
 
 template <typename T, int LANES> void launch_merge(const PromptParams& p, hipStream_t s)
 {
-    constexpr int kRowsPerBlock = kThreads / LANES;
-    hipLaunchKernelGGL((prompt_merge_kernel<T, LANES>), dim3((unsigned)((p.rows + kRowsPerBlock - 1) / kRowsPerBlock)),
-                       dim3(kThreads), 0, s, p);
+    // Few rows: more lanes for each, so that all its parts are on their way at once.  One / four groups of 16 lanes: 1024 rows of 128 bf16 channels
+    // in 32 parts 7.9 / 4.2 us, 1024 of 64 fp32 in 8 parts 3.9 / 3.6, 7200 of 128 bf16 in 3 to 9 (of up to 12) parts 6.4 / 8.4.
+    constexpr int kSub = LANES <= 16 ? 4 : 1;
+    const auto go = [&](auto sub) {
+        constexpr int SUB = decltype(sub)::value, kRowsPerBlock = kThreads / (LANES * SUB);
+        hipLaunchKernelGGL((prompt_merge_kernel<T, LANES, SUB>), dim3((unsigned)((p.rows + kRowsPerBlock - 1) / kRowsPerBlock)),
+                           dim3(kThreads), 0, s, p);
+    };
+    if (kSub > 1 && p.rows <= 2048)
+        go(std::integral_constant<int, kSub>{});
+    else
+        go(std::integral_constant<int, 1>{});
 }
 
 template <int DP, int LANES> void launch_f32(const PromptParams& p, hipStream_t s)
