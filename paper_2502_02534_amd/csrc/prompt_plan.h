@@ -29,7 +29,7 @@ constexpr int kPromptMaxSplits = 64;
 constexpr int kPromptsByLength = 4;
 // Fewest tokens of a part: a tile of fp32 takes two to eight us, one of bf16 less than one, and a part costs its rows' states.
 // 256 tokens of 4 / 1 fp32 heads of 64 channels, at least 32 / 64 / 128 tokens: 14.2 / 16.5 / 20.9 us; 32 new tokens over 1024 of 32 / 8
-// bf16 heads 20.4 / 18.0 / 16.6, over 2048 26.2 / 21.5 / 19.1.
+// bf16 heads, at least 64 / 96 / 128: 15.1 / 15.4 / 15.7, over 2048 17.1 / 16.7 / 16.0, over 4096 22.1 / 22.1 / 19.5.
 inline int prompt_min_tokens(const spd_prompt_desc* d) { return d->dtype == SPD_BF16 ? 128 : 32; }
 
 inline int check_prompt_desc(const spd_prompt_desc* d, bool queries)
