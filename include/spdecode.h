@@ -421,7 +421,8 @@ SPD_API size_t prompt_attn_workspace_size(const spd_prompt_desc *desc, int64_t t
  *   paged KV       k, v [num_pages, Hkv, 16, D]; prompt b's pages are
  *                  kv_page_indices[kv_indptr[b] .. kv_indptr[b+1]) (prompts may share pages)
  *   query_indptr, kv_indptr  int32 [B+1]; kv_lens int32 [B]
- *   total_queries  rows of q, out and lse_out (>= query_indptr[B]; rows past it are not written)
+ *   total_queries  rows of q, out and lse_out (>= query_indptr[B]; rows before query_indptr[0] and from query_indptr[B]
+ *                  on are neither read nor written)
  *   max_query_len / max_kv_len  host-known upper bounds on n_b and kv_lens[b] that size the launch
  *   out            [total_queries, Hq, D], desc->dtype
  *   lse_out        float [total_queries, Hq], natural log, or NULL

@@ -294,7 +294,8 @@ __global__ __launch_bounds__(kThreads, 7) void prompt_merge_kernel(PromptParams 
     constexpr int kRowsPerBlock = kThreads / (LANES * SUB), kBatch = SUB > 1 ? 4 : 8, kCh = HALF ? 8 : 4;
     const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES % SUB, first_lane = (threadIdx.x & 63) - lane, c = lane * kCh;
     const long long row = (long long)blockIdx.x * kRowsPerBlock + threadIdx.x / (LANES * SUB);
-    const bool row_ok = row < (long long)p.query_indptr[p.B] * p.Hq && row < p.rows;
+    // (rows before the first prompt's and past the last one's have no states: they belong to nobody in this call)
+    const bool row_ok = row >= (long long)p.query_indptr[0] * p.Hq && row < (long long)p.query_indptr[p.B] * p.Hq && row < p.rows;
     const int S = p.num_splits;
     const float4* ml = p.part_ml + (row_ok ? row : 0) * S;
     const char* parts = (const char*)p.part_acc + ((row_ok ? row : 0) * S * p.D + (c < p.D ? c : 0)) * (HALF ? 2 : 4);
