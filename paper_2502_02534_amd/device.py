@@ -169,8 +169,9 @@ class DecodeLoop:
 
     With `raw_logits` ([rows, vocab], fp32 or bf16) and `penalties` (arguments of `make_penalties` other than
     `tokens` and `token_lens`) every step shapes the raw logits by what the loop has drawn so far, into the
-    sampler's own logits, before it samples (needs `one_launch`: the step's first launch records the tokens
-    drawn before it; steps still to come hold -1, which is no token).
+    sampler's own logits, before it samples (needs `one_launch`: the step's first launch records the token
+    drawn before it).  How many there are follows the step counter: a loop whose counter is set back starts
+    from none, whatever its record still holds.
 
     Per-step inputs are rows of tensors indexed by the device-side step counter:
       q_steps [steps, N, Hq, D], k_steps / v_steps [steps, N, Hkv, D], u_steps [steps, rows].
@@ -211,8 +212,15 @@ class DecodeLoop:
             raise ValueError("raw_logits and penalties go together, and need one_launch")
         self.raw_logits, self.penalties = raw_logits, None
         if penalties is not None:
-            self._steps_drawn = torch.full((self.tokens_steps.shape[1],), self.steps, dtype=torch.int32, device=dev)
-            self._penalty_tensors = dict(penalties, tokens=self.tokens_steps.t(), token_lens=self._steps_drawn)
+            # one more step input: step t's history is the record's first t rows (steps past the last repeat its inputs,
+            # this one too)
+            rows = self.tokens_steps.shape[1]
+            self._drawn = torch.zeros(rows, dtype=torch.int32, device=dev)
+            self._drawn_steps = torch.arange(self.steps, dtype=torch.int32, device=dev)[:, None].repeat(1, rows)
+            self._select_qu = B.make_row_copies([(q_steps, attn.q, nbytes(attn.q)),
+                                                 (u_steps, sampler.uniforms, nbytes(sampler.uniforms)),
+                                                 (self._drawn_steps, self._drawn, nbytes(self._drawn))])
+            self._penalty_tensors = dict(penalties, tokens=self.tokens_steps.t(), token_lens=self._drawn)
             self.penalties = B.make_penalties(**self._penalty_tensors)
 
     def _shape_logits(self) -> None:
