@@ -108,6 +108,15 @@ def upload_sampler(inp, device="cuda:0", row_stride=None, pad_value=float("nan")
                          _dev(inp.uniforms, device), torch.empty(rows, dtype=torch.int32, device=device), ws)
 
 
+def _require(ok: bool, message: str) -> None:
+    if not ok:
+        raise ValueError(message)
+
+
+def _on_one_gpu(*tensors) -> bool:
+    return all(t.is_cuda and t.device == tensors[0].device for t in tensors if t is not None)
+
+
 @dataclasses.dataclass
 class PageTables:
     """What `build_page_tables` leaves for a batch of requests (all on the device)."""
@@ -117,6 +126,7 @@ class PageTables:
     new_indptr: torch.Tensor  # running count of new tokens
     slots: Optional[torch.Tensor]
     free_end: torch.Tensor    # first page of the free list not dealt
+    page_size: int = 16
 
 
 def build_tables(lens, free_pages, max_pages: int, max_tokens: int = 0, page_size: int = 16, held: Optional[PageTables] = None,
@@ -127,7 +137,7 @@ def build_tables(lens, free_pages, max_pages: int, max_tokens: int = 0, page_siz
     n, dev = lens.numel(), lens.device
     empty = lambda k, t=torch.int32: torch.empty(k, dtype=t, device=dev)
     out = PageTables(empty(n + 1), empty(max_pages), empty(n), empty(n + 1), empty(max_tokens, torch.int64) if max_tokens else None,
-                     empty(1))
+                     empty(1), page_size)
     ws = empty(B.build_page_tables_workspace_size(n), torch.uint8)
     B.build_page_tables(n, page_size, lens, held and held.lens, held and held.page_indptr, held and held.page_indices, free_pages,
                         free_pages.numel(), free_begin, max_pages, max_tokens, out.page_indptr, out.page_indices, out.lens,
@@ -138,21 +148,47 @@ def build_tables(lens, free_pages, max_pages: int, max_tokens: int = 0, page_siz
 class DevicePrompts:
     """One layer's prompt pass on the GPU: stores the new tokens' keys and values in the pages that `tables` name, then
     the attention of the new tokens over everything their prompts hold.  q, k, v: [tokens, heads, head_dim], rows of a
-    projection (their token stride may be larger than their heads); k_pool, v_pool: [pages, kv_heads, 16, head_dim]."""
+    projection (their token stride may be larger than their heads, k's and v's alike); k_pool, v_pool:
+    [pages, kv_heads, 16, head_dim].  What the kernels could not read as it lies raises ValueError."""
 
     def __init__(self, tables: PageTables, q, k, v, k_pool, v_pool, max_query_len: int, max_kv_len: int, causal: bool = True,
                  sm_scale: float = 0.0):
+        self._check(tables, q, k, v, k_pool, v_pool)
         tokens, hq, d = q.shape
         hkv = k.shape[1]
         self.tables, self.q, self.k, self.v, self.k_pool, self.v_pool = tables, q, k, v, k_pool, v_pool
         self.max_query_len, self.max_kv_len = max_query_len, max_kv_len
         self.desc = B.make_prompt_desc(dtype=B.SPD_BF16 if q.dtype == torch.bfloat16 else B.SPD_F32, num_q_heads=hq, num_kv_heads=hkv,
                                        head_dim=d, num_prompts=tables.lens.numel(), page_size=16, causal=causal, sm_scale=sm_scale,
-                                       q_stride=q.stride(0), kv_stride=k.stride(0))
+                                       q_stride=q.stride(0) if tokens > 1 else 0, kv_stride=k.stride(0) if tokens > 1 else 0)
         self.out = torch.empty((tokens, hq, d), dtype=q.dtype, device=q.device)
         self.lse = torch.empty((tokens, hq), dtype=torch.float32, device=q.device)
         size = B.prompt_attn_workspace_size(self.desc, tokens, max_query_len, max_kv_len)
         self.workspace = torch.empty(max(size, 256), dtype=torch.uint8, device=q.device)
+
+    @staticmethod
+    def _check(tables: PageTables, q, k, v, k_pool, v_pool) -> None:
+        _require(q.dtype in (torch.bfloat16, torch.float32), "q has to be bfloat16 or float32")
+        _require(all(x.dtype == q.dtype for x in (k, v, k_pool, v_pool)), "k, v and the pools have to be of q's type")
+        _require(q.dim() == 3 and k.dim() == 3 and v.shape == k.shape and k.shape[0] == q.shape[0] and k.shape[2] == q.shape[2],
+                 "q is [tokens, heads, head_dim], k and v [tokens, kv_heads, head_dim]")
+        tokens, hkv, d = k.shape
+        for name, x in (("q", q), ("k", k), ("v", v)):
+            _require(x[:1].is_contiguous(), f"{name}'s heads have to follow one another within a token")
+            _require(tokens < 2 or x.stride(0) >= x.shape[1] * d, f"{name}'s tokens must not overlap")
+        _require(tokens < 2 or k.stride(0) == v.stride(0), "k and v have to have one token stride")
+        for x in (k_pool, v_pool):
+            _require(x.dim() == 4 and x.shape[1:] == (hkv, 16, d) and x.shape[0] == k_pool.shape[0] and x.is_contiguous(),
+                     "the pools are [pages, kv_heads, 16, head_dim], contiguous")
+        n = tables.lens.numel()
+        _require(tables.page_size == 16, "the tables' pages have to be of 16 tokens")
+        _require(tables.slots is not None and tables.slots.numel() >= tokens, "the tables need a slot for every token")
+        lists = {"lens": n, "new_indptr": n + 1, "page_indptr": n + 1, "page_indices": 0}
+        _require(all(getattr(tables, x).dtype == torch.int32 and getattr(tables, x).is_contiguous() and getattr(tables, x).numel() >= least
+                     for x, least in lists.items()) and tables.slots.dtype == torch.int64 and tables.slots.is_contiguous(),
+                 "the tables are int32, the slots int64, contiguous, with an entry for every request")
+        _require(_on_one_gpu(q, k, v, k_pool, v_pool, tables.slots, *(getattr(tables, x) for x in lists)),
+                 "everything has to be on one GPU")
 
     def run(self, stream=None) -> None:
         t, tokens = self.tables, self.q.shape[0]
