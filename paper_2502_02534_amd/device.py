@@ -197,6 +197,37 @@ class DevicePrompts:
                       self.max_query_len, self.max_kv_len, self.out, self.lse, self.workspace, stream)
 
 
+def _check_penalties(sampler: DeviceSampler, raw, penalties: dict) -> None:
+    """That `penalize_logits` reads and writes what it is given: types, shapes and strides."""
+    to = sampler.logits
+    _require(raw.dtype in (torch.bfloat16, torch.float32), "raw_logits have to be bfloat16 or float32")
+    _require(to.dtype == torch.float32 and raw.dim() == 2 and raw.shape == to.shape,
+             "raw_logits need the shape of the sampler's float32 logits")
+    rows, vocab = raw.shape
+    _require(all(x[:1].is_contiguous() and (rows < 2 or x.stride(0) >= vocab) for x in (raw, to)), "a row of logits has to be contiguous")
+    words = -(-vocab // 32)
+    # type, entries at least
+    lists = {"repetition": (torch.float32, rows), "frequency": (torch.float32, rows), "presence": (torch.float32, rows),
+             "prompt_of_row": (torch.int32, rows), "allowed_of_row": (torch.int32, rows), "bias_indptr": (torch.int32, rows + 1),
+             "bias_tokens": (torch.int32, 0), "bias_values": (torch.float32, 0)}
+    for name, x in penalties.items():
+        _require(name in lists or name in ("prompt_bits", "allowed_bits"), f"{name} is no penalty that a loop takes")
+        if x is None:
+            continue
+        if name in lists:
+            dtype, least = lists[name]
+            _require(x.dtype == dtype and x.is_contiguous() and x.numel() >= least,
+                     f"{name} has to be contiguous {dtype}, with an entry for every row")
+        else:
+            least = rows if penalties.get(name.replace("bits", "of_row")) is None else 0
+            _require(x.dtype == torch.int32 and x.dim() == 2 and x.shape[1] >= words and x[:1].is_contiguous() and x.shape[0] >= least and
+                     (x.shape[0] < 2 or x.stride(0) >= words), f"{name} is int32 [rows, {words} words at least]")
+    biases = [penalties.get(x) for x in ("bias_indptr", "bias_tokens", "bias_values")]
+    _require(all(x is None for x in biases) or (all(x is not None for x in biases) and biases[1].numel() == biases[2].numel()),
+             "bias_indptr, bias_tokens and bias_values go together, a value for every token")
+    _require(_on_one_gpu(raw, to, *penalties.values()), "everything has to be on one GPU")
+
+
 class DecodeLoop:
     """A loop of decode steps on the device: append the step's K/V (synthetic: there are no
     weights), attention, sampling; lengths, finished flags and the step counter live on the
@@ -216,6 +247,10 @@ class DecodeLoop:
 
     def __init__(self, attn: DeviceAttn, sampler: DeviceSampler, q_steps, k_steps, v_steps, u_steps,
                  end_token: int = -1, one_launch: bool = True, raw_logits=None, penalties: Optional[dict] = None):
+        if (raw_logits is None) != (penalties is None) or (penalties is not None and not one_launch):
+            raise ValueError("raw_logits and penalties go together, and need one_launch")
+        if penalties is not None:
+            _check_penalties(sampler, raw_logits, penalties)
         self.attn, self.sampler = attn, sampler
         self.one_launch = one_launch
         self.q_steps, self.k_steps, self.v_steps, self.u_steps = q_steps, k_steps, v_steps, u_steps
@@ -244,8 +279,6 @@ class DecodeLoop:
                                              (u_steps, sampler.uniforms, nbytes(sampler.uniforms))])
         self._record_to = B.make_row_copies([(sampler.tokens, self.tokens_steps, nbytes(sampler.tokens)),
                                              (attn.out, self.out_steps, nbytes(attn.out))])
-        if (raw_logits is None) != (penalties is None) or (penalties is not None and not one_launch):
-            raise ValueError("raw_logits and penalties go together, and need one_launch")
         self.raw_logits, self.penalties = raw_logits, None
         if penalties is not None:
             # one more step input: step t's history is the record's first t rows (steps past the last repeat its inputs,

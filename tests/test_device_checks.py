@@ -115,3 +115,75 @@ def test_tables_that_do_not_fit(dev):
                dict(new_indptr=torch.zeros(3, dtype=torch.int32)), dict(page_indptr=torch.zeros(8, dtype=torch.int32)[::2])):
         with pytest.raises(ValueError, match="int32"):
             _prompts(dev, tables=_tables(dev, **kw))
+
+
+ROWS, VOCAB = 3, 100
+WORDS = 4
+
+
+def _shape(dev, raw=None, to=None, **penalties):
+    logits = torch.zeros((ROWS, VOCAB)) if to is None else to
+    sampler = dev.DeviceSampler(logits, *(torch.zeros(ROWS) for _ in range(3)), torch.full((ROWS,), 5, dtype=torch.int32), torch.zeros(256))
+    q = torch.zeros((2, ROWS, 4, 8))
+    try:
+        # (refused before the rest of the loop is looked at)
+        dev.DecodeLoop(None, sampler, q, q, q, torch.zeros((2, ROWS)), raw_logits=torch.zeros((ROWS, VOCAB)) if raw is None else raw,
+                       penalties=penalties)
+    finally:
+        assert bool((sampler.tokens == 5).all())
+
+
+def test_penalties_that_are_sound_get_as_far_as_the_device(dev):
+    i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32)  # noqa: E731
+    with pytest.raises(ValueError, match="one GPU"):
+        _shape(dev)
+    with pytest.raises(ValueError, match="one GPU"):
+        _shape(dev, torch.zeros((ROWS, VOCAB + 7), dtype=torch.bfloat16)[:, :VOCAB], torch.zeros((ROWS, VOCAB + 3))[:, :VOCAB],
+               repetition=torch.ones(ROWS), frequency=None, prompt_bits=i32(2, WORDS + 1), prompt_of_row=i32(ROWS), allowed_bits=i32(ROWS, WORDS),
+               bias_indptr=i32(ROWS + 1), bias_tokens=i32(5), bias_values=torch.zeros(5))
+
+
+def test_raw_logits_that_are_not_the_sampler_s(dev):
+    for dtype in (torch.float16, torch.float64):
+        with pytest.raises(ValueError, match="bfloat16 or float32"):
+            _shape(dev, torch.zeros((ROWS, VOCAB), dtype=dtype))
+    for shape in ((ROWS + 1, VOCAB), (ROWS - 1, VOCAB), (ROWS, VOCAB + 1), (VOCAB,)):
+        with pytest.raises(ValueError, match="shape of the sampler"):
+            _shape(dev, torch.zeros(shape))
+    with pytest.raises(ValueError, match="shape of the sampler"):
+        _shape(dev, to=torch.zeros((ROWS, VOCAB), dtype=torch.bfloat16))
+    for bad in (torch.zeros((VOCAB, ROWS)).t(), torch.zeros((ROWS, 2 * VOCAB))[:, ::2], torch.zeros((1, VOCAB)).expand(ROWS, -1)):
+        with pytest.raises(ValueError, match="contiguous"):
+            _shape(dev, bad)
+        with pytest.raises(ValueError, match="contiguous"):
+            _shape(dev, to=bad)
+
+
+@pytest.mark.parametrize("name", ["repetition", "frequency", "presence", "prompt_of_row", "allowed_of_row", "bias_indptr"])
+def test_penalties_without_an_entry_for_every_row(dev, name):
+    dtype = torch.int32 if "row" in name or "indptr" in name else torch.float32
+    more = {"bias_tokens": torch.zeros(0, dtype=torch.int32), "bias_values": torch.zeros(0)} if "bias" in name else {}
+    n = ROWS + ("indptr" in name)
+    for bad in (torch.zeros(n - 1, dtype=dtype), torch.zeros(n, dtype=torch.int64), torch.zeros(2 * n, dtype=dtype)[::2],
+                torch.zeros(1, dtype=dtype).expand(n)):
+        with pytest.raises(ValueError, match=name):
+            _shape(dev, **{name: bad}, **more)
+
+
+@pytest.mark.parametrize("name", ["prompt_bits", "allowed_bits"])
+def test_bits_that_do_not_fit(dev, name):
+    i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32)  # noqa: E731
+    for bad in (i32(ROWS, WORDS - 1), i32(ROWS - 1, WORDS), i32(ROWS * WORDS), i32(WORDS, ROWS).t(), i32(ROWS, WORDS).long(),
+                i32(1, WORDS).expand(ROWS, -1)):
+        with pytest.raises(ValueError, match=name):
+            _shape(dev, **{name: bad})
+
+
+def test_penalties_that_a_loop_does_not_take(dev):
+    for name in ("tokens", "token_lens", "temperature"):
+        with pytest.raises(ValueError, match=name):
+            _shape(dev, **{name: torch.zeros(ROWS, dtype=torch.int32)})
+    for kw in (dict(bias_tokens=torch.zeros(2, dtype=torch.int32)), dict(bias_values=torch.zeros(2)),
+               dict(bias_indptr=torch.zeros(4, dtype=torch.int32), bias_tokens=torch.zeros(2, dtype=torch.int32), bias_values=torch.zeros(1))):
+        with pytest.raises(ValueError, match="go together"):
+            _shape(dev, **kw)
