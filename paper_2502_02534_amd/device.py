@@ -134,6 +134,15 @@ def build_tables(lens, free_pages, max_pages: int, max_tokens: int = 0, page_siz
     """Page tables of requests that have to hold `lens` tokens (device int32), dealt from `free_pages`.  `held`: the
     tables the same requests have so far; `free_begin`: another call's `free_end`.  max_tokens 0: no slot map.
     The tables and the workspace are allocated here; with `stream` the caller keeps them alive until it is done."""
+    ints = {"lens": (lens, 1), "free_pages": (free_pages, 0), "free_begin": (free_begin, 1)}
+    if held is not None:
+        _require(held.page_size == page_size and held.lens.numel() == lens.numel(), "held tables are of the same requests and page size")
+        ints.update({"held lens": (held.lens, 1), "held page_indptr": (held.page_indptr, lens.numel() + 1),
+                     "held page_indices": (held.page_indices, 0)})
+    for name, (x, least) in ints.items():
+        _require(x is None or (x.dtype == torch.int32 and x.is_contiguous() and x.numel() >= least),
+                 f"{name} has to be contiguous int32 of {least} or more")
+    _require(_on_one_gpu(*(x for x, _ in ints.values())), "everything has to be on one GPU")
     n, dev = lens.numel(), lens.device
     empty = lambda k, t=torch.int32: torch.empty(k, dtype=t, device=dev)
     out = PageTables(empty(n + 1), empty(max_pages), empty(n), empty(n + 1), empty(max_tokens, torch.int64) if max_tokens else None,

@@ -187,3 +187,27 @@ def test_penalties_that_a_loop_does_not_take(dev):
                dict(bias_indptr=torch.zeros(4, dtype=torch.int32), bias_tokens=torch.zeros(2, dtype=torch.int32), bias_values=torch.zeros(1))):
         with pytest.raises(ValueError, match="go together"):
             _shape(dev, **kw)
+
+
+def test_lists_of_requests_of_other_types(dev):
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32)  # noqa: E731
+    lens, free = i32(5, 40, 3), i32(*range(10))
+    held = dev.PageTables(i32(0, 1, 2, 3), i32(7, 8, 9), i32(4, 4, 1), i32(0, 0, 0, 0), None, i32(0))
+    with pytest.raises(ValueError, match="one GPU"):
+        dev.build_tables(lens, free, 8, 60)
+    with pytest.raises(ValueError, match="one GPU"):
+        dev.build_tables(lens, free, 8, 60, held=held, free_begin=i32(0))
+    for bad in (lens.long(), lens.float(), i32(5, 0, 40, 0, 3, 0)[::2], i32()):
+        with pytest.raises(ValueError, match="lens"):
+            dev.build_tables(bad, free, 8, 60)
+    with pytest.raises(ValueError, match="free_pages"):
+        dev.build_tables(lens, free.long(), 8, 60)
+    for bad in (i32(0).long(), i32()):
+        with pytest.raises(ValueError, match="free_begin"):
+            dev.build_tables(lens, free, 8, 60, free_begin=bad)
+    for kw in (dict(lens=i32(4, 4)), dict(page_size=64)):
+        with pytest.raises(ValueError, match="same requests"):
+            dev.build_tables(lens, free, 8, 60, held=dataclasses.replace(held, **kw))
+    for kw in (dict(lens=held.lens.long()), dict(page_indptr=i32(0, 1, 2)), dict(page_indices=held.page_indices.long())):
+        with pytest.raises(ValueError, match="held"):
+            dev.build_tables(lens, free, 8, 60, held=dataclasses.replace(held, **kw))
