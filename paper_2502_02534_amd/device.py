@@ -117,6 +117,14 @@ def _on_one_gpu(*tensors) -> bool:
     return all(t.is_cuda and t.device == tensors[0].device for t in tensors if t is not None)
 
 
+def _torch_stream(stream, device):
+    """`stream` as the allocator knows it: None, a torch stream, or one made elsewhere (an object with its handle, or that)."""
+    if stream is None or isinstance(stream, torch.cuda.Stream):
+        return stream
+    handle = B._stream(stream)
+    return torch.cuda.ExternalStream(handle, device) if handle else torch.cuda.default_stream(device)
+
+
 @dataclasses.dataclass
 class PageTables:
     """What `build_page_tables` leaves for a batch of requests (all on the device)."""
@@ -133,7 +141,8 @@ def build_tables(lens, free_pages, max_pages: int, max_tokens: int = 0, page_siz
                  free_begin=None, stream=None) -> PageTables:
     """Page tables of requests that have to hold `lens` tokens (device int32), dealt from `free_pages`.  `held`: the
     tables the same requests have so far; `free_begin`: another call's `free_end`.  max_tokens 0: no slot map.
-    The tables and the workspace are allocated here; with `stream` the caller keeps them alive until it is done."""
+    The tables and the workspace are allocated here, on `stream` where one is given, so that their memory is not handed
+    out again before it is done with them (nor, when the tables go, before what the current stream then holds)."""
     ints = {"lens": (lens, 1), "free_pages": (free_pages, 0), "free_begin": (free_begin, 1)}
     if held is not None:
         _require(held.page_size == page_size and held.lens.numel() == lens.numel(), "held tables are of the same requests and page size")
@@ -145,9 +154,14 @@ def build_tables(lens, free_pages, max_pages: int, max_tokens: int = 0, page_siz
     _require(_on_one_gpu(*(x for x, _ in ints.values())), "everything has to be on one GPU")
     n, dev = lens.numel(), lens.device
     empty = lambda k, t=torch.int32: torch.empty(k, dtype=t, device=dev)
-    out = PageTables(empty(n + 1), empty(max_pages), empty(n), empty(n + 1), empty(max_tokens, torch.int64) if max_tokens else None,
-                     empty(1), page_size)
-    ws = empty(B.build_page_tables_workspace_size(n), torch.uint8)
+    with torch.cuda.stream(_torch_stream(stream, dev)):  # (nothing where it is None)
+        out = PageTables(empty(n + 1), empty(max_pages), empty(n), empty(n + 1), empty(max_tokens, torch.int64) if max_tokens else None,
+                         empty(1), page_size)
+        ws = empty(B.build_page_tables_workspace_size(n), torch.uint8)
+    if stream is not None:
+        for x in (out.page_indptr, out.page_indices, out.lens, out.new_indptr, out.slots, out.free_end):
+            if x is not None and x.numel():
+                x.record_stream(torch.cuda.current_stream(dev))
     B.build_page_tables(n, page_size, lens, held and held.lens, held and held.page_indptr, held and held.page_indices, free_pages,
                         free_pages.numel(), free_begin, max_pages, max_tokens, out.page_indptr, out.page_indices, out.lens,
                         out.new_indptr, out.slots, out.free_end, ws, stream)
