@@ -55,7 +55,7 @@ def run(prompt_lens=(700, 1203, 64), samples_per_prompt=4, steps=16, vocab=32000
     prompt_tokens = torch.randint(0, vocab, (tokens,), generator=g, device=dev, dtype=torch.int32)
     words = -(-vocab // 32)
     prompt_bits = torch.empty((prompts, words), dtype=torch.int32, device=dev)
-    B.mark_prompt_tokens(prompt_tokens, prompt_tables.new_indptr, prompts, vocab, prompt_bits, words)
+    B.mark_prompt_tokens(prompt_tokens, prompt_tables.packed_indptr, prompts, vocab, prompt_bits, words)
 
     # 4. decode: attention over the prompt's pages and the sample's own, greedy sampling of shaped logits
     desc = B.make_desc(dtype=B.SPD_BF16, num_q_heads=HQ, num_kv_heads=HKV, head_dim=HEAD_DIM, num_prompts=prompts, num_samples=rows,

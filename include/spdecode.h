@@ -384,6 +384,8 @@ SPD_API int decode_step_advance(int64_t *step_state, int64_t num_steps,
  * attention of the new tokens over the cache.  What each writes is what the next reads:
  * new_indptr is prompt_attn's query_indptr, lens_out its kv_lens, page_indptr / page_indices its KV table
  * (and prefix_lens, prefix_indptr, prefix_page_indices of the decode call); slot_map is write_prompt_kv's.
+ * These go by the tokens that were granted.  Rows packed before that is known, by what the requests ask for, go with
+ * build_page_tables_packed, whose packed_indptr and packed_lens take the place of new_indptr and lens_out in prompt_attn.
  */
 
 /*
@@ -467,6 +469,27 @@ SPD_API int build_page_tables(int64_t num_requests, int32_t page_size, const int
                               int32_t *page_indptr, int32_t *page_indices, int32_t *lens_out,
                               int32_t *new_indptr, int64_t *slot_map, int32_t *free_end,
                               void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * build_page_tables where the new tokens' rows (queries, keys, values, token ids) are packed before it is known which
+ * requests are granted: request after request, max(lens[i], held_lens[i]) - held_lens[i] rows each, granted or not.  Refused
+ * requests' rows keep their places:
+ *   packed_indptr  int32 [num_requests+1]: running count of these rows (2^31 - 1 where there are more); prompt_attn's
+ *                  query_indptr and mark_prompt_tokens' indptr
+ *   packed_lens    int32 [num_requests]: lens_out[i], 0 where the request is refused; prompt_attn's kv_lens: a refused
+ *                  request's queries get zeros
+ *   slot_map       in the order of these rows, -1 for a refused request's (write_prompt_kv skips them)
+ * new_indptr counts the granted tokens, as above: rows that are packed by it need build_page_tables' slot_map.
+ */
+SPD_API int build_page_tables_packed(int64_t num_requests, int32_t page_size, const int32_t *lens,
+                                     const int32_t *held_lens, const int32_t *held_indptr,
+                                     const int32_t *held_pages, const int32_t *free_pages,
+                                     int64_t num_free, const int32_t *free_begin,
+                                     int64_t max_pages, int64_t max_tokens,
+                                     int32_t *page_indptr, int32_t *page_indices, int32_t *lens_out,
+                                     int32_t *new_indptr, int64_t *slot_map, int32_t *free_end,
+                                     int32_t *packed_indptr, int32_t *packed_lens,
+                                     void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Stores num_tokens rows of keys and values in the cache: token t goes to slot slot_map[t] (device,

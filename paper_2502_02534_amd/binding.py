@@ -115,6 +115,8 @@ def load() -> ctypes.CDLL:
     lib.build_page_tables_workspace_size.argtypes = [i64]
     lib.build_page_tables.restype = ctypes.c_int
     lib.build_page_tables.argtypes = ([i64, ctypes.c_int32] + [vp] * 5 + [i64, vp, i64, i64] + [vp] * 7 + [sz, vp])
+    lib.build_page_tables_packed.restype = ctypes.c_int
+    lib.build_page_tables_packed.argtypes = ([i64, ctypes.c_int32] + [vp] * 5 + [i64, vp, i64, i64] + [vp] * 9 + [sz, vp])
     lib.write_prompt_kv.restype = ctypes.c_int
     lib.write_prompt_kv.argtypes = [pp, vp, vp, vp, i64, i64, vp, vp, vp]
     lib.mark_prompt_tokens.restype = ctypes.c_int
@@ -341,6 +343,18 @@ def build_page_tables(num_requests: int, page_size: int, lens, held_lens, held_i
         0 if workspace is None else workspace.nbytes, _stream(stream))
     if rc != SPD_OK:
         raise SpdError(rc, "build_page_tables")
+
+
+def build_page_tables_packed(num_requests: int, page_size: int, lens, held_lens, held_indptr, held_pages, free_pages,
+                             num_free: int, free_begin, max_pages: int, max_tokens: int, page_indptr, page_indices, lens_out,
+                             new_indptr, slot_map, free_end, packed_indptr, packed_lens, workspace, stream=None) -> None:
+    rc = load().build_page_tables_packed(
+        int(num_requests), int(page_size), _ptr(lens), _ptr(held_lens), _ptr(held_indptr), _ptr(held_pages), _ptr(free_pages),
+        int(num_free), _ptr(free_begin), int(max_pages), int(max_tokens), _ptr(page_indptr), _ptr(page_indices), _ptr(lens_out),
+        _ptr(new_indptr), _ptr(slot_map), _ptr(free_end), _ptr(packed_indptr), _ptr(packed_lens), _ptr(workspace),
+        _bytes(workspace), _stream(stream))
+    if rc != SPD_OK:
+        raise SpdError(rc, "build_page_tables_packed")
 
 
 def write_prompt_kv(desc: PromptDesc, k, v, slot_map, num_tokens: int, num_pages: int, k_pool, v_pool,

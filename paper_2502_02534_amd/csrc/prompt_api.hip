@@ -15,6 +15,54 @@ inline bool misaligned(const void* p, size_t a) { return ((uintptr_t)p % a) != 0
 constexpr int64_t kMostInt = 0x7fffffff;
 constexpr int64_t kMostBlocks = 1ll << 22;  // workgroups of up to 1024 threads: a launch counts its threads in 32 bits
 
+int page_tables(int64_t num_requests, int32_t page_size, const int32_t* lens, const int32_t* held_lens,
+                const int32_t* held_indptr, const int32_t* held_pages, const int32_t* free_pages, int64_t num_free,
+                const int32_t* free_begin, int64_t max_pages, int64_t max_tokens, int32_t* page_indptr,
+                int32_t* page_indices, int32_t* lens_out, int32_t* new_indptr, int64_t* slot_map, int32_t* free_end,
+                int32_t* packed_indptr, int32_t* packed_lens, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (num_requests <= 0 || num_free < 0 || max_pages < 0 || max_tokens < 0 || page_size < 1)
+        return SPD_EINVAL;
+    if (page_size > 65536 || num_requests >= kMostInt || num_free > kMostInt || max_pages > kMostInt || max_tokens > kMostInt)
+        return SPD_EUNSUPPORTED;
+    if (!lens || !page_indptr || !lens_out || !new_indptr || !free_end || (num_free > 0 && !free_pages) ||
+        (max_pages > 0 && !page_indices))
+        return SPD_EINVAL;
+    if ((held_lens || held_indptr || held_pages) && (!held_lens || !held_indptr || !held_pages))
+        return SPD_EINVAL;
+    const void* ints[] = {lens, held_lens, held_indptr, held_pages, free_pages, free_begin, page_indptr, page_indices,
+                          lens_out, new_indptr, free_end, packed_indptr, packed_lens};
+    for (const void* x : ints)
+        if (misaligned(x, 4))
+            return SPD_EINVAL;
+    if (misaligned(slot_map, 8) || free_begin == free_end)
+        return SPD_EINVAL;
+    if (!workspace || misaligned(workspace, 256) || workspace_bytes < build_page_tables_workspace_size(num_requests))
+        return SPD_EWORKSPACE;
+    spd::PageTableParams p;
+    p.n = num_requests;
+    p.page_size = page_size;
+    p.lens = lens;
+    p.held_lens = held_lens;
+    p.held_indptr = held_indptr;
+    p.held_pages = held_pages;
+    p.free_pages = free_pages;
+    p.num_free = num_free;
+    p.free_begin = free_begin;
+    p.max_pages = max_pages;
+    p.max_tokens = max_tokens;
+    p.page_indptr = page_indptr;
+    p.page_indices = page_indices;
+    p.lens_out = lens_out;
+    p.new_indptr = new_indptr;
+    p.slot_map = (long long*)slot_map;
+    p.free_end = free_end;
+    p.packed_indptr = packed_indptr;
+    p.packed_lens = packed_lens;
+    p.first_free = (int*)workspace;
+    return spd::launch_page_tables(p, (hipStream_t)stream) == hipSuccess ? SPD_OK : SPD_ELAUNCH;
+}
+
 }  // namespace
 
 extern "C" {
@@ -93,44 +141,22 @@ int build_page_tables(int64_t num_requests, int32_t page_size, const int32_t* le
                       int32_t* page_indices, int32_t* lens_out, int32_t* new_indptr, int64_t* slot_map, int32_t* free_end,
                       void* workspace, size_t workspace_bytes, void* stream)
 {
-    if (num_requests <= 0 || num_free < 0 || max_pages < 0 || max_tokens < 0 || page_size < 1)
+    return page_tables(num_requests, page_size, lens, held_lens, held_indptr, held_pages, free_pages, num_free, free_begin, max_pages,
+                       max_tokens, page_indptr, page_indices, lens_out, new_indptr, slot_map, free_end, nullptr, nullptr, workspace,
+                       workspace_bytes, stream);
+}
+
+int build_page_tables_packed(int64_t num_requests, int32_t page_size, const int32_t* lens, const int32_t* held_lens,
+                             const int32_t* held_indptr, const int32_t* held_pages, const int32_t* free_pages, int64_t num_free,
+                             const int32_t* free_begin, int64_t max_pages, int64_t max_tokens, int32_t* page_indptr,
+                             int32_t* page_indices, int32_t* lens_out, int32_t* new_indptr, int64_t* slot_map, int32_t* free_end,
+                             int32_t* packed_indptr, int32_t* packed_lens, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!packed_indptr || !packed_lens)
         return SPD_EINVAL;
-    if (page_size > 65536 || num_requests >= kMostInt || num_free > kMostInt || max_pages > kMostInt || max_tokens > kMostInt)
-        return SPD_EUNSUPPORTED;
-    if (!lens || !page_indptr || !lens_out || !new_indptr || !free_end || (num_free > 0 && !free_pages) ||
-        (max_pages > 0 && !page_indices))
-        return SPD_EINVAL;
-    if ((held_lens || held_indptr || held_pages) && (!held_lens || !held_indptr || !held_pages))
-        return SPD_EINVAL;
-    const void* ints[] = {lens, held_lens, held_indptr, held_pages, free_pages, free_begin, page_indptr, page_indices,
-                          lens_out, new_indptr, free_end};
-    for (const void* x : ints)
-        if (misaligned(x, 4))
-            return SPD_EINVAL;
-    if (misaligned(slot_map, 8) || free_begin == free_end)
-        return SPD_EINVAL;
-    if (!workspace || misaligned(workspace, 256) || workspace_bytes < build_page_tables_workspace_size(num_requests))
-        return SPD_EWORKSPACE;
-    spd::PageTableParams p;
-    p.n = num_requests;
-    p.page_size = page_size;
-    p.lens = lens;
-    p.held_lens = held_lens;
-    p.held_indptr = held_indptr;
-    p.held_pages = held_pages;
-    p.free_pages = free_pages;
-    p.num_free = num_free;
-    p.free_begin = free_begin;
-    p.max_pages = max_pages;
-    p.max_tokens = max_tokens;
-    p.page_indptr = page_indptr;
-    p.page_indices = page_indices;
-    p.lens_out = lens_out;
-    p.new_indptr = new_indptr;
-    p.slot_map = (long long*)slot_map;
-    p.free_end = free_end;
-    p.first_free = (int*)workspace;
-    return spd::launch_page_tables(p, (hipStream_t)stream) == hipSuccess ? SPD_OK : SPD_ELAUNCH;
+    return page_tables(num_requests, page_size, lens, held_lens, held_indptr, held_pages, free_pages, num_free, free_begin, max_pages,
+                       max_tokens, page_indptr, page_indices, lens_out, new_indptr, slot_map, free_end, packed_indptr, packed_lens,
+                       workspace, workspace_bytes, stream);
 }
 
 int write_prompt_kv(const spd_prompt_desc* desc, const void* k, const void* v, const int64_t* slot_map, int64_t num_tokens,

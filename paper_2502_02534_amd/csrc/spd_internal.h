@@ -174,6 +174,8 @@ struct PageTableParams {
     int* new_indptr;
     long long* slot_map;  // may be null
     int* free_end;
+    int* packed_indptr;  // null: the slot map is that of the tokens granted; else of all that were asked for
+    int* packed_lens;
     int* first_free;  // workspace: [n] index in free_pages of a request's first new page
 };
 

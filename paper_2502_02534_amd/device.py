@@ -131,16 +131,19 @@ class PageTables:
     page_indptr: torch.Tensor
     page_indices: torch.Tensor
     lens: torch.Tensor        # tokens each request may hold now
-    new_indptr: torch.Tensor  # running count of new tokens
-    slots: Optional[torch.Tensor]
+    new_indptr: torch.Tensor  # running count of new tokens granted
+    slots: Optional[torch.Tensor]  # of the rows that packed_indptr counts
     free_end: torch.Tensor    # first page of the free list not dealt
     page_size: int = 16
+    packed_indptr: Optional[torch.Tensor] = None  # running count of new tokens asked for: rows are packed by it
+    packed_lens: Optional[torch.Tensor] = None    # `lens`, 0 for refused requests
 
 
 def build_tables(lens, free_pages, max_pages: int, max_tokens: int = 0, page_size: int = 16, held: Optional[PageTables] = None,
                  free_begin=None, stream=None) -> PageTables:
     """Page tables of requests that have to hold `lens` tokens (device int32), dealt from `free_pages`.  `held`: the
-    tables the same requests have so far; `free_begin`: another call's `free_end`.  max_tokens 0: no slot map.
+    tables the same requests have so far; `free_begin`: another call's `free_end`.  max_tokens 0: no slot map and no packed_*.
+    The rows of new tokens (q, k, v, ids) are packed by what `lens` asks for beyond `held`, granted or not.
     The tables and the workspace are allocated here, on `stream` where one is given, so that their memory is not handed
     out again before it is done with them (nor, when the tables go, before what the current stream then holds)."""
     ints = {"lens": (lens, 1), "free_pages": (free_pages, 0), "free_begin": (free_begin, 1)}
@@ -156,15 +159,19 @@ def build_tables(lens, free_pages, max_pages: int, max_tokens: int = 0, page_siz
     empty = lambda k, t=torch.int32: torch.empty(k, dtype=t, device=dev)
     with torch.cuda.stream(_torch_stream(stream, dev)):  # (nothing where it is None)
         out = PageTables(empty(n + 1), empty(max_pages), empty(n), empty(n + 1), empty(max_tokens, torch.int64) if max_tokens else None,
-                         empty(1), page_size)
+                         empty(1), page_size, *((empty(n + 1), empty(n)) if max_tokens else ()))
         ws = empty(B.build_page_tables_workspace_size(n), torch.uint8)
     if stream is not None:
-        for x in (out.page_indptr, out.page_indices, out.lens, out.new_indptr, out.slots, out.free_end):
+        for x in (out.page_indptr, out.page_indices, out.lens, out.new_indptr, out.slots, out.free_end, out.packed_indptr, out.packed_lens):
             if x is not None and x.numel():
                 x.record_stream(torch.cuda.current_stream(dev))
-    B.build_page_tables(n, page_size, lens, held and held.lens, held and held.page_indptr, held and held.page_indices, free_pages,
-                        free_pages.numel(), free_begin, max_pages, max_tokens, out.page_indptr, out.page_indices, out.lens,
-                        out.new_indptr, out.slots, out.free_end, ws, stream)
+    args = (n, page_size, lens, held and held.lens, held and held.page_indptr, held and held.page_indices, free_pages,
+            free_pages.numel(), free_begin, max_pages, max_tokens, out.page_indptr, out.page_indices, out.lens, out.new_indptr, out.slots,
+            out.free_end)
+    if max_tokens:
+        B.build_page_tables_packed(*args, out.packed_indptr, out.packed_lens, ws, stream)
+    else:
+        B.build_page_tables(*args, ws, stream)
     return out
 
 
@@ -172,7 +179,8 @@ class DevicePrompts:
     """One layer's prompt pass on the GPU: stores the new tokens' keys and values in the pages that `tables` name, then
     the attention of the new tokens over everything their prompts hold.  q, k, v: [tokens, heads, head_dim], rows of a
     projection (their token stride may be larger than their heads, k's and v's alike); k_pool, v_pool:
-    [pages, kv_heads, 16, head_dim].  What the kernels could not read as it lies raises ValueError."""
+    [pages, kv_heads, 16, head_dim].  The rows are packed as the tables were asked for: a refused request's keep their places,
+    are stored nowhere, and get zeros (and -inf).  What the kernels could not read as it lies raises ValueError."""
 
     def __init__(self, tables: PageTables, q, k, v, k_pool, v_pool, max_query_len: int, max_kv_len: int, causal: bool = True,
                  sm_scale: float = 0.0):
@@ -207,6 +215,9 @@ class DevicePrompts:
         _require(tables.page_size == 16, "the tables' pages have to be of 16 tokens")
         _require(tables.slots is not None and tables.slots.numel() >= tokens, "the tables need a slot for every token")
         lists = {"lens": n, "new_indptr": n + 1, "page_indptr": n + 1, "page_indices": 0}
+        if tables.packed_indptr is not None or tables.packed_lens is not None:
+            _require(tables.packed_indptr is not None and tables.packed_lens is not None, "packed_indptr and packed_lens go together")
+            lists.update(packed_indptr=n + 1, packed_lens=n)
         _require(all(getattr(tables, x).dtype == torch.int32 and getattr(tables, x).is_contiguous() and getattr(tables, x).numel() >= least
                      for x, least in lists.items()) and tables.slots.dtype == torch.int64 and tables.slots.is_contiguous(),
                  "the tables are int32, the slots int64, contiguous, with an entry for every request")
@@ -216,7 +227,8 @@ class DevicePrompts:
     def run(self, stream=None) -> None:
         t, tokens = self.tables, self.q.shape[0]
         B.write_prompt_kv(self.desc, self.k, self.v, t.slots, tokens, self.k_pool.shape[0], self.k_pool, self.v_pool, stream)
-        B.prompt_attn(self.desc, self.q, self.k_pool, self.v_pool, t.new_indptr, t.lens, t.page_indptr, t.page_indices, tokens,
+        starts, lens = (t.new_indptr, t.lens) if t.packed_indptr is None else (t.packed_indptr, t.packed_lens)
+        B.prompt_attn(self.desc, self.q, self.k_pool, self.v_pool, starts, lens, t.page_indptr, t.page_indices, tokens,
                       self.max_query_len, self.max_kv_len, self.out, self.lse, self.workspace, stream)
 
 

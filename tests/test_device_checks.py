@@ -211,3 +211,15 @@ def test_lists_of_requests_of_other_types(dev):
     for kw in (dict(lens=held.lens.long()), dict(page_indptr=i32(0, 1, 2)), dict(page_indices=held.page_indices.long())):
         with pytest.raises(ValueError, match="held"):
             dev.build_tables(lens, free, 8, 60, held=dataclasses.replace(held, **kw))
+
+
+def test_packed_counts_of_other_types_or_alone(dev):
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    with pytest.raises(ValueError, match="one GPU"):
+        _prompts(dev, tables=_tables(dev, packed_indptr=i32(4), packed_lens=i32(3)))
+    for kw in (dict(packed_indptr=i32(4)), dict(packed_lens=i32(3))):
+        with pytest.raises(ValueError, match="go together"):
+            _prompts(dev, tables=_tables(dev, **kw))
+    for kw in (dict(packed_indptr=i32(3), packed_lens=i32(3)), dict(packed_indptr=i32(4).long(), packed_lens=i32(3))):
+        with pytest.raises(ValueError, match="int32"):
+            _prompts(dev, tables=_tables(dev, **kw))

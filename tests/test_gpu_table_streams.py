@@ -30,8 +30,8 @@ def test_memory_of_a_call_on_another_stream(n, kind, monkeypatch):
     side = torch.cuda.Stream()
     torch.cuda.synchronize()
     seen = []
-    call = B.build_page_tables
-    monkeypatch.setattr(B, "build_page_tables", lambda *a: (seen.append(a[-2]), call(*a))[1])
+    for name in ("build_page_tables", "build_page_tables_packed"):
+        monkeypatch.setattr(B, name, lambda *a, call=getattr(B, name): (seen.append(a[-2]), call(*a))[1])
     x = torch.randn((2048, 2048), device=DEV)
     torch.cuda.synchronize()
     with torch.cuda.stream(side):
