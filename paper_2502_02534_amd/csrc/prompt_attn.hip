@@ -21,7 +21,6 @@
 // Few rows: 256 tokens of 4 and 1 heads of 64 channels 9.0 us in 64 units of 32 tokens, and 3.6 for the launch that joins them.
 #include "prompt_units.h"
 
-#include <hip/hip_fp16.h>
 #include <type_traits>
 
 namespace spd {
@@ -246,10 +245,10 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void prompt_attn_f32_k
     float* dst = (float*)p.out + row * p.D;
     if (p.num_splits > 1) {
         if (h == 0) {
-            p.part_ml[row * p.num_splits + at.split] = make_float4(m, l, 1.f, 0.f);
+            p.part_ml[row * p.num_splits + at.split] = make_float4(m, l, 0.f, 0.f);
             if (at.split == 0)  // and the parts that this prompt does not have
                 for (int s = at.splits; s < p.num_splits; ++s)
-                    p.part_ml[row * p.num_splits + s] = make_float4(kNever, 0.f, 1.f, 0.f);
+                    p.part_ml[row * p.num_splits + s] = make_float4(kNever, 0.f, 0.f, 0.f);
         }
         if (t0 >= t1)
             return;
@@ -284,22 +283,21 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void prompt_attn_f32_k
 
 // Joins the parts of a row: with states (m_i, l_i, acc_i), m = max m_i and w_i = 2^(m_i - m),
 // out = sum w_i acc_i / sum w_i l_i.  LANES lanes take a part of a row, 16 bytes each, and SUB such groups
-// every SUB-th part; each group also takes all its parts' (m, l, scale) and hands their weights round.  Bound by latency, then by the
+// every SUB-th part; each group also takes all its parts' (m, l) and hands their weights round.  Bound by latency, then by the
 // partial states, whose loads a lane has in flight kBatch at a time:
-// 7200 rows in 3 to 9 parts of 128 channels 6.4 us, 1024 fp32 rows in 8 parts of 64 channels 3.6.
+// 7200 rows in 3 to 9 parts of 128 channels 8.2 us, 1024 rows of 128 channels in 32 parts 9.3 (17 MB), of 64 in 8 parts 3.5.
 template <typename T, int LANES, int SUB>
 __global__ __launch_bounds__(kThreads, 7) void prompt_merge_kernel(PromptParams p)
 {
-    constexpr bool HALF = sizeof(T) == 2;
-    constexpr int kRowsPerBlock = kThreads / (LANES * SUB), kBatch = SUB > 1 ? 4 : 8, kCh = HALF ? 8 : 4;
+    constexpr int kRowsPerBlock = kThreads / (LANES * SUB), kBatch = SUB > 1 ? 4 : 8, kCh = 4;
     const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES % SUB, first_lane = (threadIdx.x & 63) - lane, c = lane * kCh;
     const long long row = (long long)blockIdx.x * kRowsPerBlock + threadIdx.x / (LANES * SUB);
     // (rows before the first prompt's and past the last one's have no states: they belong to nobody in this call)
     const bool row_ok = row >= (long long)p.query_indptr[0] * p.Hq && row < (long long)p.query_indptr[p.B] * p.Hq && row < p.rows;
     const int S = p.num_splits;
     const float4* ml = p.part_ml + (row_ok ? row : 0) * S;
-    const char* parts = (const char*)p.part_acc + ((row_ok ? row : 0) * S * p.D + (c < p.D ? c : 0)) * (HALF ? 2 : 4);
-    const long long part_bytes = (long long)p.D * (HALF ? 2 : 4);
+    const char* parts = (const char*)p.part_acc + ((row_ok ? row : 0) * S * p.D + (c < p.D ? c : 0)) * 4;
+    const long long part_bytes = (long long)p.D * 4;
     uint4 a[kBatch];
     auto request = [&](int s0) __attribute__((always_inline)) {
 #pragma unroll
@@ -329,12 +327,13 @@ __global__ __launch_bounds__(kThreads, 7) void prompt_merge_kernel(PromptParams 
             if (x.y != 0.f) {  // (a sum that is not a number stays one)
                 const float u = __builtin_amdgcn_exp2f(x.x - m);
                 l = fmaf(u, x.y, l);
-                w = HALF ? u * x.y * x.z : u;
+                w = u;
             }
         }
         // up to the last part that holds anything: a prompt may have fewer than the longest one
         const unsigned long long holds = __ballot(w != 0.f) >> first_lane;
         const int here = 64 - __clzll((long long)(LANES == 64 ? holds : holds & ((1ull << (LANES & 63)) - 1)));
+#pragma unroll 1  // (rounds side by side would not fit the registers)
         for (int k0 = 0; k0 < here; k0 += SUB * kBatch) {
             if (s0 + k0 > 0)
                 request(s0 + k0);
@@ -345,15 +344,8 @@ __global__ __launch_bounds__(kThreads, 7) void prompt_merge_kernel(PromptParams 
                 if (ws != 0.f && at < here) {  // (a part that holds nothing was not written)
                     const uint32_t v[4] = {a[k].x, a[k].y, a[k].z, a[k].w};
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if constexpr (HALF) {
-                            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v[e]));
-                            acc[2 * e] = fmaf(ws, f.x, acc[2 * e]);
-                            acc[2 * e + 1] = fmaf(ws, f.y, acc[2 * e + 1]);
-                        } else {
-                            acc[e] = fmaf(ws, __uint_as_float(v[e]), acc[e]);
-                        }
-                    }
+                    for (int e = 0; e < kCh; ++e)
+                        acc[e] = fmaf(ws, __uint_as_float(v[e]), acc[e]);
                 }
             }
         }
@@ -375,21 +367,18 @@ __global__ __launch_bounds__(kThreads, 7) void prompt_merge_kernel(PromptParams 
     if (c >= p.D)
         return;
     char* dst = (char*)p.out + (row * p.D + c) * (long long)sizeof(T);
-    if constexpr (sizeof(T) == 2) {
-#pragma unroll
-        for (int e = 0; e < kCh; e += 4)
-            *reinterpret_cast<uint2*>(dst + 2 * e) =
-                make_uint2(pack_bf16(acc[e] * inv, acc[e + 1] * inv), pack_bf16(acc[e + 2] * inv, acc[e + 3] * inv));
-    } else {
+    if constexpr (sizeof(T) == 2)
+        *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv));
+    else
         *reinterpret_cast<float4*>(dst) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
-    }
 }
 
 template <typename T, int LANES> void launch_merge(const PromptParams& p, hipStream_t s)
 {
-    // Few rows: more lanes for each, so that all its parts are on their way at once.  One / four groups of 16 lanes: 1024 rows of 128 bf16 channels
-    // in 32 parts 7.9 / 4.2 us, 1024 of 64 fp32 in 8 parts 3.9 / 3.6, 7200 of 128 bf16 in 3 to 9 (of up to 12) parts 6.4 / 8.4.
-    constexpr int kSub = LANES <= 16 ? 4 : 1;
+    // Few rows: a wavefront for each, so that all its parts are on their way at once.  One / several groups of lanes, whole calls: 32 new tokens of
+    // 32 bf16 heads of 128 channels (1024 rows) over 2048 tokens 20.5 / 17.3 us, over 16384 36.4 / 32.3; two such prompts over 4096 (2048 rows)
+    // 27.3 / 26.9, four (4096 rows) 34.4 / 34.2; 7200 rows in 3 to 9 (of up to 12) parts 46.3 / 47.1; 1024 fp32 rows of 64 in 8 parts 3.9 / 3.6 (the join alone).
+    constexpr int kSub = 64 / LANES;
     const auto go = [&](auto sub) {
         constexpr int SUB = decltype(sub)::value, kRowsPerBlock = kThreads / (LANES * SUB);
         hipLaunchKernelGGL((prompt_merge_kernel<T, LANES, SUB>), dim3((unsigned)((p.rows + kRowsPerBlock - 1) / kRowsPerBlock)),
@@ -425,7 +414,7 @@ hipError_t launch_prompt_attn(const PromptParams& p, hipStream_t s)
         if (e != hipSuccess)
             return e;
         if (p.num_splits > 1)
-            p.D <= 64 ? launch_merge<__bf16, 8>(p, s) : p.D <= 128 ? launch_merge<__bf16, 16>(p, s) : launch_merge<__bf16, 32>(p, s);
+            p.D <= 64 ? launch_merge<__bf16, 16>(p, s) : p.D <= 128 ? launch_merge<__bf16, 32>(p, s) : launch_merge<__bf16, 64>(p, s);
     } else {
         p.D <= 64 ? launch_f32<64, 16>(p, s) : p.D <= 128 ? launch_f32<128, 32>(p, s) : launch_f32<256, 64>(p, s);
     }

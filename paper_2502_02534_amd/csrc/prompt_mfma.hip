@@ -13,9 +13,8 @@
 // one barrier a tile.  The others (the causal edge, a prompt's ragged end) follow one by one with the mask;
 // wavefronts whose rows see nothing of such a tile skip it.
 //
-// Rounding: sums, statistics and accumulators are fp32.  The probabilities become bf16 as the second product's operand (2^-8 of a
-// term; the divisor is the sum of the unrounded ones), a part's result fp16 with a power-of-two scale a row (2^-11, and half the
-// traffic of fp32), the result bf16.
+// Rounding: sums, statistics and accumulators are fp32, and so is what a part hands on.  The probabilities become bf16 as the second
+// product's operand (2^-8 of a term; the divisor is the sum of the unrounded ones), the result bf16.
 //
 // Bound: the matrix pipe, and on long calls of real data its power.  64 and 8 heads of 128 channels, 16384 tokens: 3.97 to 4.11 ms, 1.07 to
 // 1.12 PFLOP/s of the products that the rows need, matrix pipe 58 % busy at 1.7 GHz (2.9 ms on zeros, where the clock stays up).  128 rows a
@@ -494,19 +493,26 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void prompt_mfma_ker
     const float l = l_run + __shfl_xor(l_run, 32);
     const float inv = l == 0.f ? 0.f : 1.f / l;
     __builtin_amdgcn_s_barrier();
-    char* const mine = lds + wave * 32 * S::kRow;
-    auto place = [&](int row, int piece) __attribute__((always_inline)) -> char* {
-        return mine + row * S::kRow + ((piece ^ (row & (S::kRow / 16 - 1))) << 4);
-    };
-    // Rows 0 .. 31 of the wavefront to `first` + out_row * `pitch`; `pack` makes two 16-bit values, of sums or as they are, `unpack`
-    // reads one.
-    auto store_rows = [&](auto pack, auto unpack, char* first, long long pitch) __attribute__((always_inline)) {
+    // Rows 0 .. 31 of the wavefront to `first` + out_row * `pitch`: a result's, in bf16, or a part's sums as they are, whose rows are twice as
+    // long and take the rings to their last byte.
+    auto store_rows = [&](auto sums_tag, char* first, long long pitch) __attribute__((always_inline)) {
+        constexpr bool SUMS = decltype(sums_tag)::value;
+        constexpr int kBytes = SUMS ? 2 * S::kRow : S::kRow, kPieces = kBytes / 16, kRowsAtOnce = 64 / kPieces;
+        char* const mine = lds + wave * 32 * kBytes;
+        auto place = [&](int row, int piece) __attribute__((always_inline)) -> char* {
+            return mine + row * kBytes + ((piece ^ (row & (kPieces - 1))) << 4);
+        };
 #pragma unroll
         for (int db = 0; db < S::kDB; ++db)
 #pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4)  // registers 4 q4 .. + 3 are channels 32 db + 8 q4 + 4 h .. + 3
-                *reinterpret_cast<uint2*>(place(col, 4 * db + q4) + 8 * h) =
-                    make_uint2(pack(o[db][4 * q4], o[db][4 * q4 + 1], true), pack(o[db][4 * q4 + 2], o[db][4 * q4 + 3], true));
+            for (int q4 = 0; q4 < 4; ++q4) {  // registers 4 q4 .. + 3 are channels 32 db + 8 q4 + 4 h .. + 3
+                const float x0 = o[db][4 * q4], x1 = o[db][4 * q4 + 1], x2 = o[db][4 * q4 + 2], x3 = o[db][4 * q4 + 3];
+                if constexpr (SUMS)
+                    *reinterpret_cast<float4*>(place(col, 8 * db + 2 * q4 + h)) = make_float4(x0, x1, x2, x3);
+                else
+                    *reinterpret_cast<uint2*>(place(col, 4 * db + q4) + 8 * h) =
+                        make_uint2(pack_bf16_rne(x0 * inv, x1 * inv), pack_bf16_rne(x2 * inv, x3 * inv));
+            }
         // rare: the values that were taken out of the tiles, to the rows that see them
         for (int w = 0; w < kOddWords; ++w)
             for (uint32_t bits = ntiles > 0 ? __builtin_amdgcn_readfirstlane(odd_words[w]) : 0u; bits != 0u; bits &= bits - 1u) {
@@ -520,50 +526,39 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void prompt_mfma_ker
                         continue;
                     for (int c = lane; c < head_bytes / 2; c += 64) {
                         const float value = __uint_as_float((uint32_t)v[c] << 16);
-                        uint16_t* const mine_at = reinterpret_cast<uint16_t*>(place(row, c >> 3)) + (c & 7);
-                        if (!(fabsf(value) < INFINITY))
-                            *mine_at = (uint16_t)pack(unpack(*mine_at) + value, 0.f, false);
+                        if (fabsf(value) < INFINITY)
+                            continue;
+                        if constexpr (SUMS) {
+                            reinterpret_cast<float*>(place(row, c >> 2))[c & 3] += value;
+                        } else {
+                            uint16_t* const at_c = reinterpret_cast<uint16_t*>(place(row, c >> 3)) + (c & 7);
+                            *at_c = (uint16_t)pack_bf16_rne(__uint_as_float((uint32_t)*at_c << 16) + value, 0.f);
+                        }
                     }
                 }
             }
-        const int to = row_ok ? (int)out_row : -1;
+        const int to = row_ok ? (int)out_row : -1, at_row = lane / kPieces, piece = lane % kPieces;
 #pragma unroll
-        for (int i = 0; i < S::kCopies; ++i) {
-            const int row = S::kRowsPerCopy * i + lane_row, dst = __shfl(to, row);
-            if (dst >= 0 && (FULL || lane_piece < head_pieces))
-                *reinterpret_cast<uint4*>(first + dst * pitch + lane_piece * 16) = *reinterpret_cast<const uint4*>(place(row, lane_piece));
+        for (int i = 0; i < 32 / kRowsAtOnce; ++i) {
+            const int row = kRowsAtOnce * i + at_row, dst = __shfl(to, row);
+            if (dst >= 0 && (FULL || piece < head_pieces * (SUMS ? 2 : 1)))
+                *reinterpret_cast<uint4*>(first + dst * pitch + piece * 16) = *reinterpret_cast<const uint4*>(place(row, piece));
         }
     };
     if (p.num_splits > 1) {
-        float top = 0.f;
-#pragma unroll
-        for (int db = 0; db < S::kDB; ++db)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float x = fabsf(o[db][i] * inv);
-                top = x < INFINITY ? fmaxf(top, x) : top;
-            }
-        top = fmaxf(top, __shfl_xor(top, 32));
-        // the largest power of two up to it, but none whose inverse overflows
-        const float scale = __uint_as_float(max(__float_as_uint(top) & 0x7f800000u, 0x01000000u)), unscale = 1.f / scale;
         if (h == 0 && row_ok) {
-            p.part_ml[out_row * p.num_splits + at.split] = make_float4(m_run, l, scale, 0.f);
+            p.part_ml[out_row * p.num_splits + at.split] = make_float4(m_run, l, 0.f, 0.f);
             if (at.split == 0)  // and the parts that this prompt does not have
                 for (int s = at.splits; s < p.num_splits; ++s)
-                    p.part_ml[out_row * p.num_splits + s] = make_float4(kNever, 0.f, 1.f, 0.f);
+                    p.part_ml[out_row * p.num_splits + s] = make_float4(kNever, 0.f, 0.f, 0.f);
         }
         if (t0 < t1)
-            store_rows([&](float x, float y, bool sums) __attribute__((always_inline)) {
-                const float f = sums ? inv * unscale : 1.f;
-                const __half2 v = __floats2half2_rn(x * f, y * f);
-                return *reinterpret_cast<const uint32_t*>(&v);
-            }, [](uint16_t x) __attribute__((always_inline)) { return __half2float(*reinterpret_cast<const __half*>(&x)); }, (char*)p.part_acc + (long long)at.split * head_bytes, (long long)p.num_splits * head_bytes);
+            store_rows(yes, (char*)p.part_acc + (long long)at.split * p.D * 4, (long long)p.num_splits * p.D * 4);
         return;
     }
     if (p.lse && h == 0 && row_ok)
         p.lse[out_row] = l == 0.f ? -INFINITY : m_run * kLn2 + logf(l);
-    store_rows([&](float x, float y, bool sums) __attribute__((always_inline)) { return sums ? pack_bf16_rne(x * inv, y * inv) : pack_bf16_rne(x, y); },
-               [](uint16_t x) __attribute__((always_inline)) { return __uint_as_float((uint32_t)x << 16); }, (char*)p.out, head_bytes);
+    store_rows(no, (char*)p.out, head_bytes);
 }
 
 template <int D, bool FULL> void launch(const PromptParams& p, hipStream_t s)

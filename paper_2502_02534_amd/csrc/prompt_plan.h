@@ -90,7 +90,7 @@ inline int make_prompt_plan(const spd_prompt_desc* d, int64_t total, int64_t max
     out->num_splits = (int)splits;
     out->split_tokens = (int)tokens;
     const size_t states = splits > 1 ? (size_t)total * d->num_q_heads * splits : 0;
-    out->acc_bytes = (states * d->head_dim * (d->dtype == SPD_BF16 ? 2 : 4) + 255) / 256 * 256;
+    out->acc_bytes = (states * d->head_dim * 4 + 255) / 256 * 256;
     out->ml_bytes = states * 4 * sizeof(float);
     return SPD_OK;
 }

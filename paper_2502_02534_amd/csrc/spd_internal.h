@@ -149,8 +149,7 @@ struct PromptParams {
     int num_splits;    // most parts that a prompt's tokens are cut into
     int split_tokens;  // fewest tokens of a part
     long long rows;    // total_queries * Hq
-    // Partial states, [rows][num_splits]: (m, l, scale), l = 0 where a part holds nothing, and the sums: fp32 as they are
-    // (scale 1), or (bf16) divided by l and by the scale, a power of two that brings the row into the range of fp16.
+    // Partial states, [rows][num_splits]: (m, l) in places of 16 bytes, l = 0 where a part holds nothing, and the sums in fp32.
     void* part_acc;
     float4* part_ml;
     void* out;
