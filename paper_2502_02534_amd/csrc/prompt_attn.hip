@@ -39,7 +39,7 @@ constexpr int kTileN = 32;      // tokens per tile
 constexpr int kThreads = 256;
 // Tiles that some row of a workgroup does not see whole: its 128 rows end at up to 128 tokens, and a prompt's end may be ragged.
 constexpr int kOddWords = 8;
-constexpr float kNever = -1e30f;  // reference maximum of a row that has seen nothing: finite, so that no exponent is inf - inf
+constexpr float kNever = -3.402823466e38f;  // reference maximum of a row that has seen nothing: finite, so that no exponent is inf - inf
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 {
@@ -142,7 +142,10 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void prompt_attn_f32_k
         fetch_pages(t0);
         request(t0);
     }
-    floatx4 qf[DP / 8];  // channels 8 u + 4 h .. + 3 of the lane's row
+    // Channels 8 u + 4 h .. + 3 of the lane's row, with the scale (one more rounding of 2^-24 a term): scores come out in base 2, and the
+    // highest of a row is the reference maximum to the last bit however large it is (a scale within the exponent's fma would leave
+    // the product's rounding, more than an exponent holds from 2^31 on).
+    floatx4 qf[DP / 8];
     {
         const float* q = (const float*)p.q + (long long)(q0 + token) * p.q_stride + (long long)head * p.D;
 #pragma unroll
@@ -150,7 +153,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void prompt_attn_f32_k
             floatx4 v = {0.f, 0.f, 0.f, 0.f};
             if (8 * u + 4 * h < p.D)
                 v = *reinterpret_cast<const floatx4*>(q + 8 * u + 4 * h);
-            qf[u] = v;
+            qf[u] = v * p.scale_log2;
         }
     }
 
@@ -201,7 +204,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void prompt_attn_f32_k
 #pragma unroll
             for (int i = 1; i < 16; ++i)
                 top = fmaxf(top, s[i]);
-            top = fmaxf(top, __shfl_xor(top, 32)) * p.scale_log2;
+            top = fmaxf(top, __shfl_xor(top, 32));
             // the reference maximum only has to bound the exponents: raised where the tile's is well above it
             if (__ballot(top > m + 10.f) != 0) {
                 const float m_new = fmaxf(m, top), corr = __builtin_amdgcn_exp2f(m - m_new);
@@ -218,7 +221,7 @@ __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void prompt_attn_f32_k
             float sum = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], p.scale_log2, -m));
+                s[i] = __builtin_amdgcn_exp2f(s[i] - m);
                 sum += s[i];
             }
             l += sum;

@@ -46,8 +46,11 @@ constexpr int kRing = 4;              // slots of K and of V: the tile in use an
 constexpr int kFragAhead = 4;         // LDS fragments in flight
 // Tiles that some row of a workgroup does not see whole: its 128 rows end at up to 128 tokens, and a prompt's end may be ragged.
 constexpr int kOddWords = 8;
-constexpr float kNever = -1e30f;      // reference maximum of a row that has seen nothing: finite, so that no exponent is inf - inf
+constexpr float kNever = -3.402823466e38f;  // reference maximum of a row that has seen nothing: finite, so that no exponent is inf - inf
 constexpr float kRaise = 1024.f;
+// Reference maxima from here on (in base 2) are too large for the exponents' fma: the product there is exact and the maximum rounded, and
+// the difference, up to 2^-24 of it, would go into the exponent.  Such rows take every tile's probabilities again, from rounded products.
+constexpr float kLarge = 16777216.f;
 
 template <int D> struct Shape {  // D: channels of a tile row
     static constexpr int kRow = 2 * D, kTile = kTileN * kRow;  // bytes
@@ -197,7 +200,7 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void prompt_mfma_ker
             }
     }
 
-    float m_run = kNever, l_run = 0.f;
+    float m_run = kNever, l_run = 0.f, sum_cap = kRaise;
     floatx16 o[S::kDB];
 #pragma unroll
     for (int db = 0; db < S::kDB; ++db)
@@ -315,14 +318,16 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void prompt_mfma_ker
         return psum;
     };
 
-    auto probabilities = [&](const floatx16& sc, bf16x8 (&pn)[2]) __attribute__((always_inline)) -> float {
+    auto probabilities = [&](auto rounded, const floatx16& sc, bf16x8 (&pn)[2]) __attribute__((always_inline)) -> float {
+#pragma clang fp contract(off)
         float psum = 0.f;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             float pv[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                pv[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[8 * u + e], p.scale_log2, -m_run));
+                const float x = sc[8 * u + e];
+                pv[e] = __builtin_amdgcn_exp2f(decltype(rounded)::value ? x * p.scale_log2 - m_run : __builtin_fmaf(x, p.scale_log2, -m_run));
                 psum += pv[e];
             }
             uint4 pu;
@@ -335,7 +340,7 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void prompt_mfma_ker
         return psum;
     };
     // The reference maximum only has to bound the exponents: it is raised where a lane's 16 probabilities add up to more
-    // than kRaise (none is above that otherwise: exact in fp32 and bf16 alike).  O holds every earlier tile by then.
+    // than kRaise (none is above that otherwise: exact in fp32 and bf16 alike), or where it is kLarge.  O holds every earlier tile by then.
     auto raise_maximum = [&](const floatx16& sc) __attribute__((always_inline)) -> float {
         float tmax = kNever;
 #pragma unroll
@@ -345,12 +350,13 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void prompt_mfma_ker
         const float m_up = fmaxf(m_run, tmax);
         const float corr = __builtin_amdgcn_exp2f(m_run - m_up);
         m_run = m_up;
+        sum_cap = fabsf(m_up) >= kLarge && m_up != kNever ? -1.f : kRaise;
         return corr;
     };
     auto take_sum = [&](float psum, const floatx16& sc, bf16x8 (&pn)[2]) __attribute__((always_inline)) {
-        if (__ballot(!(psum <= kRaise)) != 0) {
+        if (__ballot(!(psum <= sum_cap)) != 0) {
             const float corr = raise_maximum(sc);
-            psum = probabilities(sc, pn);
+            psum = probabilities(std::true_type{}, sc, pn);
             l_run *= corr;
 #pragma unroll
             for (int db = 0; db < S::kDB; ++db) {
@@ -477,7 +483,7 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void prompt_mfma_ker
                 for (int i = 0; i < 16; ++i)
                     sa[i] = 8 * (i >> 2) + (i & 3) <= end ? sa[i] : -INFINITY;
             }
-            take_sum(probabilities(sa, pa), sa, pa);
+            take_sum(probabilities(no, sa, pa), sa, pa);
         }
         if (masked) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
