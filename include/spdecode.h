@@ -546,7 +546,8 @@ typedef struct spd_penalties {
  *   x2 = x1 - frequency * c - presence * (c > 0)
  *   x3 = x2 + bias of i
  *   out = allowed ? x3 : -inf
- * in fp32.  Token ids outside 0 .. vocab - 1 are ignored.  A token listed twice among a row's biases gets
+ * in fp32, every step rounded once (a quotient below 2^-110 may be off by a unit in the last place).  Token ids outside
+ * 0 .. vocab - 1 are ignored.  A token listed twice among a row's biases gets
  * one of the two.
  *   logits     [rows, vocab] fp32 or bf16 (logits_dtype), rows row_stride elements apart
  *   out        float [rows, vocab], rows out_stride apart; may be logits itself (fp32, equal strides), else

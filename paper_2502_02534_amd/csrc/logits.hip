@@ -2,6 +2,7 @@
 // and the logits shaped by penalties, biases and a grammar mask.
 #include "spd_internal.h"
 
+#include <float.h>
 #include <type_traits>
 
 namespace spd {
@@ -60,8 +61,8 @@ __global__ __launch_bounds__(kMarkThreads) void mark_tokens_kernel(const int* to
 //
 // Bound: HBM, logits read and written once.  1024 rows of 128256 bf16 logits, histories up to 2048 by steps, 8 prompts' bits, 16 biases and
 // a grammar row each: 173 us, 4.6 TB/s (a cast of the same logits to fp32 136; histories row by row 163, none 150); 64 fp32 rows
-// 17.8 us, 3.7 TB/s: reading the history, then the table, is a chain that the first slices wait for.  48 to 64 registers: four
-// workgroups a CU (with 108, two: 198 us).
+// 17.8 us, 3.7 TB/s: reading the history, then the table, is a chain that the first slices wait for.  57 to 63 registers: four
+// workgroups a CU (with 108, two: 198 us); 77, three, with eight rounds of fp32.
 constexpr int kThreads = 512;
 constexpr int kTable = 2048;         // places
 constexpr int kEntries = 4;          // of the history, a thread: a history of kEntries * kThreads is read once
@@ -130,9 +131,14 @@ __global__ __launch_bounds__(kThreads) void penalize_kernel(LogitsParams p, int 
         return;
     const int lo = __builtin_amdgcn_readfirstlane((int)(unit % (unsigned)slices)) * slice_len, hi = min((int)p.vocab, lo + slice_len);
 
-    const float rep = p.repetition ? p.repetition[r] : 1.f, inv_rep = 1.f / rep;  // (a product for the quotient: half an ulp more)
+    // x / rep as x * (inv + rest), the reciprocal in two floats: rounded once, in five instructions with the product for x <= 0, where
+    // the division alone takes ten (1024 rows 190 us).  Exact so far as x * rest is, from |x| = 2^-110 on, and reciprocals are not subnormal.
+    const float rep = p.repetition ? p.repetition[r] : 1.f;
+    const bool repeats = rep != 1.f, usual_rep = rep >= 0x1p-60f && rep <= 0x1p60f;
+    const auto uniform = [](float x) { return __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(x))); };
+    const float inv = uniform(1.f / rep), rest = uniform(fmaf(-rep, inv, 1.f) * inv);
     const float freq = p.frequency ? p.frequency[r] : 0.f, pres = p.presence ? p.presence[r] : 0.f;
-    const long long prompt = !p.prompt_bits ? -1 : p.prompt_of_row ? p.prompt_of_row[r] : r;
+    const long long prompt = !p.prompt_bits || !repeats ? -1 : p.prompt_of_row ? p.prompt_of_row[r] : r;
     const long long grammar = !p.allowed_bits ? -1 : p.allowed_of_row ? p.allowed_of_row[r] : r;
     const uint32_t* seen_bits = p.prompt_bits + (prompt < 0 ? 0 : prompt) * p.prompt_stride;
     const uint32_t* allowed_bits = p.allowed_bits + (grammar < 0 ? 0 : grammar) * p.allowed_stride;
@@ -245,66 +251,82 @@ __global__ __launch_bounds__(kThreads) void penalize_kernel(LogitsParams p, int 
             each_bias([&](int id, int k) __attribute__((always_inline)) { bias[place(id)] = p.bias_values[k]; });
             __syncthreads();
         }
+        auto repeated = [&](auto by_product, float x) __attribute__((always_inline)) -> float {
+            if constexpr (decltype(by_product)::value)
+                return fmaf(x, x > 0.f ? inv : rep, __builtin_amdgcn_fmed3f(x, 0.f, FLT_MAX) * rest);  // (an infinite x stays one)
+            return x > 0.f ? x / rep : x * rep;
+        };
         // one that is listed: its count and bias
-        auto shape = [&](float x, bool seen, int k) __attribute__((always_inline)) -> float {
+        auto shape = [&](auto by_product, float x, bool seen, int k) __attribute__((always_inline)) -> float {
             const int at = before[k >> 5] + __popc(listed[k >> 5] & ((1u << (k & 31)) - 1u));
             const uint32_t c = counts[at];
-            if (c != 0u && !seen)
-                x *= x > 0.f ? inv_rep : rep;
+            if (c != 0u && !seen && repeats)
+                x = repeated(by_product, x);
             if (c != 0u)
                 x = x - freq * (float)c - pres;
             return x + bias[at];
         };
         uint32_t listed_words = any && 32 * lane < tile_len ? listed[tile0 / 32 + lane] : 0u;
         float* const to = out + s0 + tile0;
-        auto rounds = [&](auto full) __attribute__((always_inline)) {
+        auto round = [&](int u, const Four<BF16>& four, auto full, auto by_product) __attribute__((always_inline)) {
+            int at_lane = lane;
+            asm volatile("" : "+v"(at_lane), "+v"(listed_words), "+v"(seen_words), "+v"(allowed_words));
+            // the lane's four bits: of word 8 u + lane / 8, from bit 4 (lane % 8) on
+            const int from_lane = 8 * u + (at_lane >> 3), shift = 4 * (at_lane & 7), k = 256 * u + 4 * at_lane;
+            const uint32_t bits = any ? (uint32_t)__shfl((int)listed_words, from_lane) >> shift & 0xfu : 0u;
+            const uint32_t seen = prompt >= 0 ? (uint32_t)__shfl((int)seen_words, from_lane) >> shift & 0xfu : 0u;
+            const uint32_t allowed = grammar >= 0 ? (uint32_t)__shfl((int)allowed_words, from_lane) >> shift & 0xfu : 0xfu;
+            if (full || k < tile_len) {
+                float x[4];
 #pragma unroll
-            for (int u = 0; u < ROUNDS; ++u) {
-                int at_lane = lane;
-                asm volatile("" : "+v"(at_lane), "+v"(listed_words), "+v"(seen_words), "+v"(allowed_words));
-                // the lane's four bits: of word 8 u + lane / 8, from bit 4 (lane % 8) on
-                const int from_lane = 8 * u + (at_lane >> 3), shift = 4 * (at_lane & 7), k = 256 * u + 4 * at_lane;
-                const uint32_t bits = any ? (uint32_t)__shfl((int)listed_words, from_lane) >> shift & 0xfu : 0u;
-                const uint32_t seen = prompt >= 0 ? (uint32_t)__shfl((int)seen_words, from_lane) >> shift & 0xfu : 0u;
-                const uint32_t allowed = grammar >= 0 ? (uint32_t)__shfl((int)allowed_words, from_lane) >> shift & 0xfu : 0xfu;
-                if (full || k < tile_len) {
-                    float x[4];
+                for (int e = 0; e < 4; ++e)
+                    x[e] = four.get(e);
+                if (seen != 0u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float y = repeated(by_product, x[e]);
+                        x[e] = (seen >> e) & 1u ? y : x[e];
+                    }
+                if (bits != 0u)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        x[e] = raw[u].get(e);
-                    if (seen != 0u)
+                        if ((bits >> e) & 1u)
+                            x[e] = shape(by_product, x[e], (seen >> e) & 1u, tile0 + k + e);
+                if (allowed != 0xfu)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float y = x[e] * (x[e] > 0.f ? inv_rep : rep);
-                            x[e] = (seen >> e) & 1u ? y : x[e];
-                        }
-                    if (bits != 0u)
+                    for (int e = 0; e < 4; ++e)
+                        x[e] = (allowed >> e) & 1u ? x[e] : -INFINITY;
+                if (full || tile_len - k >= 4) {
+                    typedef float __attribute__((ext_vector_type(4), aligned(4))) any4;
+                    const any4 y = {x[0], x[1], x[2], x[3]};
+                    *reinterpret_cast<any4*>(to + k) = y;
+                } else {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if ((bits >> e) & 1u)
-                                x[e] = shape(x[e], (seen >> e) & 1u, tile0 + k + e);
-                    if (allowed != 0xfu)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            x[e] = (allowed >> e) & 1u ? x[e] : -INFINITY;
-                    if (full || tile_len - k >= 4) {
-                        typedef float __attribute__((ext_vector_type(4), aligned(4))) any4;
-                        const any4 y = {x[0], x[1], x[2], x[3]};
-                        *reinterpret_cast<any4*>(to + k) = y;
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 3; ++e)
-                            if (e < tile_len - k)
-                                to[k + e] = x[e];
-                    }
+                    for (int e = 0; e < 3; ++e)
+                        if (e < tile_len - k)
+                            to[k + e] = x[e];
                 }
-                __builtin_amdgcn_sched_barrier(0);
             }
+            __builtin_amdgcn_sched_barrier(0);
         };
-        if (tile_len == kTile)
-            rounds(std::true_type{});
-        else
-            rounds(std::false_type{});
+        if (!usual_rep) {  // (rare: its logits are read again, so that this copy of the code is short)
+#pragma unroll 1
+            for (int u = 0; u < ROUNDS; ++u) {
+                const int k = 256 * u + 4 * lane;
+                Four<BF16> four = {};
+                if (k < tile_len)
+                    four.load(from + k * (BF16 ? 2 : 4), min(4, tile_len - k));
+                round(u, four, std::false_type{}, std::false_type{});
+            }
+        } else if (tile_len == kTile) {
+#pragma unroll
+            for (int u = 0; u < ROUNDS; ++u)
+                round(u, raw[u], std::true_type{}, std::true_type{});
+        } else {
+#pragma unroll
+            for (int u = 0; u < ROUNDS; ++u)
+                round(u, raw[u], std::false_type{}, std::true_type{});
+        }
         s0 += len;
     }
 }
@@ -333,8 +355,8 @@ hipError_t launch_penalize_logits(const LogitsParams& p, hipStream_t s)
             hipLaunchKernelGGL((penalize_kernel<false, R>), grid, dim3(kThreads), 0, s, p, (int)slices);
     };
     // Rows of 128256 tokens, slices of 2 / 4 / 8 rounds.  fp32, histories of 128 to 1024: 1 row 8.4 / 8.4 / 11.6 us, 16 rows
-    // 9.5 / 10.4 / 12.8, 32 rows 16.6 / 14.4 / 16.2, 64 rows 20.7 / 19.1 / 19.9, 128 rows 34.7 / 31.6 / 29.1, 256 rows
-    // 80 / 62 / 65; bf16, histories up to 2048: 1024 rows 339 / 225 / 176.
+    // 9.5 / 10.4 / 12.8, 32 rows 16.6 / 14.4 / 16.2, 64 rows 20.7 / 19.1 / 19.9, of 4 / 8 rounds 96 rows 25.4 / 24.3, 128 rows 32.6 / 33.9, 256 rows
+    // 65 / 64.3, 1024 rows 211 / 203; bf16, histories up to 2048: 1024 rows 339 / 225 / 176.
     const long long tokens = p.rows * p.vocab;
     if (tokens >= 12000000)
         go(std::integral_constant<int, 8>{});
