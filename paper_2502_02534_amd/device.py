@@ -213,19 +213,22 @@ class DevicePrompts:
                      "the pools are [pages, kv_heads, 16, head_dim], contiguous")
         n = tables.lens.numel()
         _require(tables.page_size == 16, "the tables' pages have to be of 16 tokens")
-        _require(tables.slots is not None and tables.slots.numel() >= tokens, "the tables need a slot for every token")
+        _require(tokens == 0 or tables.slots is not None and tables.slots.numel() >= tokens, "the tables need a slot for every token")
         lists = {"lens": n, "new_indptr": n + 1, "page_indptr": n + 1, "page_indices": 0}
         if tables.packed_indptr is not None or tables.packed_lens is not None:
             _require(tables.packed_indptr is not None and tables.packed_lens is not None, "packed_indptr and packed_lens go together")
             lists.update(packed_indptr=n + 1, packed_lens=n)
         _require(all(getattr(tables, x).dtype == torch.int32 and getattr(tables, x).is_contiguous() and getattr(tables, x).numel() >= least
-                     for x, least in lists.items()) and tables.slots.dtype == torch.int64 and tables.slots.is_contiguous(),
+                     for x, least in lists.items()) and
+                 (tables.slots is None or tables.slots.dtype == torch.int64 and tables.slots.is_contiguous()),
                  "the tables are int32, the slots int64, contiguous, with an entry for every request")
         _require(_on_one_gpu(q, k, v, k_pool, v_pool, tables.slots, *(getattr(tables, x) for x in lists)),
                  "everything has to be on one GPU")
 
     def run(self, stream=None) -> None:
         t, tokens = self.tables, self.q.shape[0]
+        if tokens == 0:
+            return  # (tensors without elements have no address to hand on)
         B.write_prompt_kv(self.desc, self.k, self.v, t.slots, tokens, self.k_pool.shape[0], self.k_pool, self.v_pool, stream)
         starts, lens = (t.new_indptr, t.lens) if t.packed_indptr is None else (t.packed_indptr, t.packed_lens)
         B.prompt_attn(self.desc, self.q, self.k_pool, self.v_pool, starts, lens, t.page_indptr, t.page_indices, tokens,
