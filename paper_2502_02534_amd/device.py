@@ -243,6 +243,10 @@ def _check_penalties(sampler: DeviceSampler, raw, penalties: dict) -> None:
              "raw_logits need the shape of the sampler's float32 logits")
     rows, vocab = raw.shape
     _require(all(x[:1].is_contiguous() and (rows < 2 or x.stride(0) >= vocab) for x in (raw, to)), "a row of logits has to be contiguous")
+    (raw_first, raw_end), (to_first, to_end) = ((x.data_ptr(), x.data_ptr() + ((rows - 1) * x.stride(0) + vocab) * x.element_size())
+                                                for x in (raw, to))
+    _require(raw_first >= to_end or to_first >= raw_end,
+             "raw_logits must not share memory with the sampler's: every step shapes them anew")
     words = -(-vocab // 32)
     # type, entries at least
     lists = {"repetition": (torch.float32, rows), "frequency": (torch.float32, rows), "presence": (torch.float32, rows),

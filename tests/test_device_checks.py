@@ -223,3 +223,15 @@ def test_packed_counts_of_other_types_or_alone(dev):
     for kw in (dict(packed_indptr=i32(3), packed_lens=i32(3)), dict(packed_indptr=i32(4).long(), packed_lens=i32(3))):
         with pytest.raises(ValueError, match="int32"):
             _prompts(dev, tables=_tables(dev, **kw))
+
+
+def test_raw_logits_that_are_shaped_where_they_lie(dev):
+    """The second step would shape what the first one left."""
+    x = torch.zeros((ROWS, VOCAB))
+    wide = torch.zeros((ROWS, 2 * VOCAB))
+    both = torch.zeros((2 * ROWS, VOCAB))
+    for raw, to in ((x, x), (wide[:, :VOCAB], wide[:, 50:150]), (both[:ROWS], both[ROWS - 1:-1]), (x.view(torch.bfloat16)[:, :VOCAB], x)):
+        with pytest.raises(ValueError, match="share memory"):
+            _shape(dev, raw, to)
+    with pytest.raises(ValueError, match="one GPU"):
+        _shape(dev, both[:ROWS], both[ROWS:])
