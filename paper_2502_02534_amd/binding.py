@@ -144,6 +144,14 @@ def _bytes(t: Optional[torch.Tensor]) -> int:
 _cuda_ready = False
 
 
+def _forget_cuda() -> None:
+    global _cuda_ready
+    _cuda_ready = False
+
+
+os.register_at_fork(after_in_child=_forget_cuda)  # torch refuses a forked child that its parent's GPU state went into
+
+
 def _stream(stream) -> int:
     if stream is None:
         global _cuda_ready
