@@ -493,7 +493,7 @@ SPD_API int build_page_tables_packed(int64_t num_requests, int32_t page_size, co
 
 /*
  * Stores num_tokens rows of keys and values in the cache: token t goes to slot slot_map[t] (device,
- * int64).  Slots outside the pool are skipped; two tokens of one slot leave either's row.
+ * int64).  Slots outside the pool are skipped.  Tokens have slots of their own: two of one slot leave a row mixed of both.
  *   k, v            [num_tokens, Hkv, D], tokens desc->kv_stride apart
  *   k_pool, v_pool  page_size 16: [num_pages, Hkv, 16, D]; page_size 0: [num_pages, Hkv, D], a slot each
  * desc: dtype, num_kv_heads, head_dim, page_size, kv_stride.  Pointers 16-byte aligned.
