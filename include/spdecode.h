@@ -417,6 +417,8 @@ SPD_API size_t prompt_attn_workspace_size(const spd_prompt_desc *desc, int64_t t
  *   out = softmax(q K^T * scale) V over the tokens up to and including its position (causal), or over
  * all kv_lens[b] tokens.  A query that sees no token (n_b > kv_lens[b]) gets zeros, and -inf as its
  * log-sum-exp.  Nothing that a query does not see, whatever its value, enters its result.
+ * Sums and statistics are fp32; with bf16 the probabilities are rounded to bf16 on their way to the product with V (2^-8 of a
+ * term), and the result.
  *
  *   q              [total_queries, Hq, D], tokens q_stride apart; prompt b's start at query_indptr[b]
  *   contiguous KV  k, v [tokens, Hkv, D], tokens kv_stride apart; prompt b's start at kv_indptr[b]

@@ -60,8 +60,8 @@ __global__ __launch_bounds__(kMarkThreads) void mark_tokens_kernel(const int* to
 // tokens on their way before the table is begun, and takes a word of every bit row per lane, handed round with shuffles.
 //
 // Bound: HBM, logits read and written once.  1024 rows of 128256 bf16 logits, histories up to 2048 by steps, 8 prompts' bits, 16 biases and
-// a grammar row each: 173 us, 4.6 TB/s (a cast of the same logits to fp32 136; histories row by row 163, none 150); 64 fp32 rows
-// 17.8 us, 3.7 TB/s: reading the history, then the table, is a chain that the first slices wait for.  57 to 63 registers: four
+// a grammar row each: 176 us, 4.5 TB/s (a cast of the same logits to fp32 136; histories row by row 165, none 151); 64 fp32 rows
+// 18.1 us, 3.6 TB/s: reading the history, then the table, is a chain that the first slices wait for.  57 to 63 registers: four
 // workgroups a CU (with 108, two: 198 us); 77, three, with eight rounds of fp32.
 constexpr int kThreads = 512;
 constexpr int kTable = 2048;         // places
@@ -354,9 +354,11 @@ hipError_t launch_penalize_logits(const LogitsParams& p, hipStream_t s)
         else
             hipLaunchKernelGGL((penalize_kernel<false, R>), grid, dim3(kThreads), 0, s, p, (int)slices);
     };
-    // Rows of 128256 tokens, slices of 2 / 4 / 8 rounds.  fp32, histories of 128 to 1024: 1 row 8.4 / 8.4 / 11.6 us, 16 rows
-    // 9.5 / 10.4 / 12.8, 32 rows 16.6 / 14.4 / 16.2, 64 rows 20.7 / 19.1 / 19.9, of 4 / 8 rounds 96 rows 25.4 / 24.3, 128 rows 32.6 / 33.9, 256 rows
-    // 65 / 64.3, 1024 rows 211 / 203; bf16, histories up to 2048: 1024 rows 339 / 225 / 176.
+    // Rows of 128256 tokens, slices of 2 / 4 / 8 rounds.  fp32, histories of 128 to 1024: 1 row 9.0 / 9.4 / 12.5 us, 16 rows
+    // 9.7 / 10.8 / 13.8, 32 rows 15.0 / 15.1 / 17.2, 64 rows 20.8 / 19.6 / 21.0, 96 rows 27.5 / 25.5 / 24.4, 128 rows 34.3 / 30.8 / 32.9, of 4 / 8
+    // rounds 256 rows 65.0 / 64.3, 1024 rows 211 / 203; bf16, histories up to 2048: 1024 rows 339 / 225 / 176.  Rows of 32000 fp32 tokens: 64 rows
+    // 9.7 / 10.7 / 13.8, 1024 rows 75.6 / 64.6 / 67.6.  Rows shorter than a slice leave wavefronts without logits: 1024 rows of 4096 tokens
+    // 15.1 / 16.5 / 22.7, 8192 rows of 1024 60 / 64 / 94 (the rule takes 4).
     const long long tokens = p.rows * p.vocab;
     if (tokens >= 12000000)
         go(std::integral_constant<int, 8>{});

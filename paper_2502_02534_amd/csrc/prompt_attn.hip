@@ -15,10 +15,10 @@
 // added at the end to the rows that see them.
 //
 // Bound: the matrix pipe, 155 TFLOP/s for fp32 products.  The tile after the present one is on its way into registers
-// while its products run, and goes to the other half of LDS after them: one barrier a tile (two: 4096 tokens 697 us, one: 578).
-// 16 query and 4 KV heads, causal: 4096 tokens of 128 channels 578 us, 119 TFLOP/s of the products that the rows need (8192: 2.34 ms, 117),
-// 8192 of 64 1.21 ms, 114; 8 and 4 heads, 2000 of 256 243 us, 68 (one workgroup a CU: its LDS and registers hold no second).
-// Few rows: 256 tokens of 4 and 1 heads of 64 channels 9.0 us in 64 units of 32 tokens, and 3.6 for the launch that joins them.
+// while its products run, and goes to the other half of LDS after them: one barrier a tile (two: 4096 tokens 697 us, one: 582).
+// 16 query and 4 KV heads, causal: 4096 tokens of 128 channels 582 us, 118 TFLOP/s of the products that the rows need (8192: 2.36 ms, 117),
+// 8192 of 64 1.24 ms, 111; 8 and 4 heads, 2000 of 256 245 us, 67 (one workgroup a CU: its 134 KB of LDS leave no room for a second).
+// Few rows: 256 tokens of 4 and 1 heads of 64 channels 9.0 us in 64 units of 32 tokens, and 3.4 for the launch that joins them.
 #include "prompt_units.h"
 
 #include <type_traits>
@@ -397,8 +397,8 @@ template <int DP, int LANES> void launch_f32(const PromptParams& p, hipStream_t 
 {
     const dim3 grid((unsigned)((long long)p.tiles * p.num_splits * p.Hkv)), block(kThreads);
     // Two workgroups a CU, which the pairs of tiles and the length of parts count on (prompt_units.h): 64 channels alone would fit
-    // four, and then long units share a CU.  16 heads, 64 channels, with four / three / two a CU: 2 x 4096 tokens 788 / 689 / 657 us,
-    // 1 x 8192 1292 / 1185 / 1210.
+    // four, and then long units share a CU.  16 heads, 64 channels, with four / three / two a CU: 2 x 4096 tokens 654 / 606 / 634 us,
+    // 1 x 8192 1284 / 1182 / 1241 (three are ahead where there are neither pairs nor parts).
     constexpr int kSpareLds = DP == 64 ? 20480 : 0;
     if (p.page_size != 0)
         hipLaunchKernelGGL((prompt_attn_f32_kernel<DP, true>), grid, block, kSpareLds, s, p);

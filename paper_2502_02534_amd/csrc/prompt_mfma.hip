@@ -17,11 +17,11 @@
 // product's operand (2^-8 of a term; the divisor is the sum of the unrounded ones), the result bf16.
 //
 // Bound: the matrix pipe, and on long calls of real data its power.  64 and 8 heads of 128 channels, 16384 tokens: 3.97 to 4.11 ms, 1.07 to
-// 1.12 PFLOP/s of the products that the rows need, matrix pipe 58 % busy at 1.7 GHz (2.9 ms on zeros, where the clock stays up).  128 rows a
+// 1.12 PFLOP/s of the products that the rows need, matrix pipe 62 % busy at 1.7 GHz (2.9 ms on zeros, where the clock stays up).  128 rows a
 // workgroup against 256 (half the LDS traffic, one workgroup a CU): 16384 tokens 3.98 / 3.88 ms, 2 x 8192 of 64 channels 579 / 649 us,
-// 8 x 300..512 over 4k to 12k 545 / 603, 26 x 300..512 94 / 115.  Three prompts of 500 to 4001 tokens, 32 and 8 heads of 64: 108 us, 0.81
-// PFLOP/s, three workgroups a CU (with 212 registers, two: 117); 2 x 4096 of 256 channels 312 us, 0.88.  4 x 17..96 new tokens over
-// 2k to 8k paged ones: 40 us (85 MB), of which a unit's start is 4.3, a tile 1.0 with two units a CU, and the rows' way out 2.5.
+// 8 x 300..512 over 4k to 12k 545 / 603, 26 x 300..512 94 / 115.  Three prompts of 500 to 4001 tokens, 32 and 8 heads of 64: 107 us, 0.82
+// PFLOP/s, three workgroups a CU (with 212 registers, two: 117); 2 x 4096 of 256 channels 305 us, 0.90.  4 x 17..96 new tokens over
+// 2k to 8k paged ones: 40.5 us (87 MB read, 25 written), of which a unit's start is 4.3, a tile 1.0 with two units a CU, and the rows' way out 3.
 #include "attn_prefix_body.h"
 #include "prompt_units.h"
 

@@ -24,12 +24,12 @@ constexpr int kPromptPlaces = 512;     // workgroups that run at once
 constexpr int kPromptMaxSplits = 64;
 // Up to so many prompts, the units of all of them run in the order of their tokens, so that a launch ends with its shortest; with more,
 // prompt by prompt, so that those that run together read the same K and V.  Prompt by prompt / by length: 2 x 4096 fp32 tokens of 16 heads
-// of 64 channels 656 / 612 us; 32 and 8 bf16 heads of 64 channels, 3 x 500..4001 114.7 / 110.6, 3 x 2000 73.3 / 69.5, 24 x 300..1000 90.7 / 92.2;
+// of 64 channels 644 / 634 us; 32 and 8 bf16 heads of 64 channels, 3 x 500..4001 113.1 / 109.5, 3 x 2000 73.3 / 69.5, 24 x 300..1000 90.7 / 92.2;
 // of 128, 4 x 1000..4000 271 / 265, 8 x 2048 323 / 327, 26 x 300..512 85.7 / 98.8.
 constexpr int kPromptsByLength = 4;
 // Fewest tokens of a part: a tile of fp32 takes two to eight us, one of bf16 less than one, and a part costs its rows' states.
-// 256 tokens of 4 / 1 fp32 heads of 64 channels, at least 32 / 64 / 128 tokens: 14.2 / 16.5 / 20.9 us; 32 new tokens over 1024 of 32 / 8
-// bf16 heads, at least 64 / 96 / 128: 15.1 / 15.4 / 15.7, over 2048 17.1 / 16.7 / 16.0, over 4096 22.1 / 22.1 / 19.5.
+// 256 tokens of 4 / 1 fp32 heads of 64 channels, at least 32 / 64 / 128 tokens: 13.7 / 15.5 / 20.3 us; 32 new tokens over 1024 of 32 / 8
+// bf16 heads, at least 64 / 96 / 128: 15.2 / 15.1 / 15.9, over 2048 18.4 / 17.6 / 17.4, over 4096 24.1 / 23.9 / 20.1.
 inline int prompt_min_tokens(const spd_prompt_desc* d) { return d->dtype == SPD_BF16 ? 128 : 32; }
 
 inline int check_prompt_desc(const spd_prompt_desc* d, bool queries)
