@@ -242,6 +242,8 @@ def _check_penalties(sampler: DeviceSampler, raw, penalties: dict) -> None:
     _require(to.dtype == torch.float32 and raw.dim() == 2 and raw.shape == to.shape,
              "raw_logits need the shape of the sampler's float32 logits")
     rows, vocab = raw.shape
+    _require(sampler.tokens.dtype == torch.int32 and sampler.tokens.is_contiguous() and sampler.tokens.numel() == rows,
+             "the sampler needs an int32 token for every row")
     _require(all(x[:1].is_contiguous() and (rows < 2 or x.stride(0) >= vocab) for x in (raw, to)), "a row of logits has to be contiguous")
     (raw_first, raw_end), (to_first, to_end) = ((x.data_ptr(), x.data_ptr() + ((rows - 1) * x.stride(0) + vocab) * x.element_size())
                                                 for x in (raw, to))

@@ -235,3 +235,12 @@ def test_raw_logits_that_are_shaped_where_they_lie(dev):
             _shape(dev, raw, to)
     with pytest.raises(ValueError, match="one GPU"):
         _shape(dev, both[:ROWS], both[ROWS:])
+
+
+def test_a_sampler_without_a_token_for_every_row(dev):
+    """The record of its tokens is the rows' history."""
+    for tokens in (torch.full((ROWS - 1,), 5, dtype=torch.int32), torch.full((ROWS,), 5), torch.full((2 * ROWS,), 5, dtype=torch.int32)[::2]):
+        sampler = dev.DeviceSampler(torch.zeros((ROWS, VOCAB)), *(torch.zeros(ROWS) for _ in range(3)), tokens, torch.zeros(256))
+        q = torch.zeros((2, ROWS, 4, 8))
+        with pytest.raises(ValueError, match="token for every row"):
+            dev.DecodeLoop(None, sampler, q, q, q, torch.zeros((2, ROWS)), raw_logits=torch.zeros((ROWS, VOCAB)), penalties={})
