@@ -165,7 +165,9 @@ def build_tables(lens, free_pages, max_pages: int, max_tokens: int = 0, page_siz
         for x in (out.page_indptr, out.page_indices, out.lens, out.new_indptr, out.slots, out.free_end, out.packed_indptr, out.packed_lens):
             if x is not None and x.numel():
                 x.record_stream(torch.cuda.current_stream(dev))
-    args = (n, page_size, lens, held and held.lens, held and held.page_indptr, held and held.page_indices, free_pages,
+    # (a list without pages has no address; where nobody holds a page, none is read)
+    held_pages = held and (held.page_indices if held.page_indices.numel() else held.page_indptr)
+    args = (n, page_size, lens, held and held.lens, held and held.page_indptr, held_pages, free_pages,
             free_pages.numel(), free_begin, max_pages, max_tokens, out.page_indptr, out.page_indices, out.lens, out.new_indptr, out.slots,
             out.free_end)
     if max_tokens:
