@@ -562,6 +562,119 @@ SPD_API int penalize_logits(const void *logits, int32_t logits_dtype, int64_t ro
                             int64_t row_stride, const spd_penalties *penalties,
                             float *out, int64_t out_stride, void *stream);
 
+/* ---- what a step's two softmaxes say --------------------------------------------------------------
+ *
+ * The softmax over the vocabulary says how probable a token was, and what stood beside it (token_logprobs).  The softmax
+ * over the cached tokens says which of them are used: accumulate_kv_weights sums what every cached token got,
+ * select_kv_tokens picks those that stay, and compact_kv moves them together, so that a sample whose pages are full
+ * (append_suffix_kv leaves it unchanged) can go on, and a long prompt takes less room and time in every step.
+ */
+
+#define SPD_MAX_TOP_TOKENS 64
+
+/* Bytes of workspace token_logprobs needs (0 on invalid sizes). */
+SPD_API size_t token_logprobs_workspace_size(int64_t rows, int64_t vocab, int32_t num_top);
+
+/*
+ * Per row r, with x the row's logits, T its temperature, y = x / T and log p_i = y_i - log(sum_j exp(y_j)):
+ *   logprobs      float [rows]: log p of tokens[r]; -inf where tokens[r] is no token of the vocabulary
+ *   ranks         int32 [rows]: 1 + the number of tokens with a larger logit than tokens[r]; 0 where it is no token
+ *   entropy       float [rows]: - sum_i p_i log p_i
+ *   lse           float [rows]: log(sum_j exp(y_j)); log p of any other token i is y_i - lse
+ *   top_tokens    int32 [rows, num_top], top_logprobs float [rows, num_top]: the num_top tokens with the largest logits in
+ *                 descending order, the lower token first among equal ones, and their log p
+ *   temperature   float [rows], NULL = 1 everywhere; 0 (a row that is sampled greedily) counts as 1
+ *   tokens        int32 [rows] (sample_tokens' tokens_out, or the next tokens of a prompt)
+ *   logits        [rows, vocab] fp32 or bf16 (logits_dtype), rows row_stride elements apart
+ * Every output may be NULL; logprobs and ranks need tokens.  A logit of -inf has p = 0; a row of nothing else has lse and log p
+ * -inf and entropy 0.  Sums are fp32 at least.  num_top 0 .. min(vocab, SPD_MAX_TOP_TOKENS); vocab up to 2^30;
+ * (rows + 8) * ceil(vocab / 16384) up to 2^22.  rows 0 is a call that does nothing.  Returns spd_status.
+ */
+SPD_API int token_logprobs(const void *logits, int32_t logits_dtype, int64_t rows, int64_t vocab, int64_t row_stride,
+                           const float *temperature, const int32_t *tokens, int32_t num_top,
+                           float *logprobs, int32_t *ranks, float *entropy, float *lse,
+                           int32_t *top_tokens, float *top_logprobs,
+                           void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of workspace accumulate_kv_weights needs for these bounds (0 on an invalid desc). */
+SPD_API size_t accumulate_kv_weights_workspace_size(const spd_prompt_desc *desc, int64_t total_queries,
+                                                    int64_t max_query_len, int64_t max_kv_len);
+
+/*
+ * How much of the queries' attention every cached token got.  Sequence b (desc->num_prompts of them) has kv_lens[b] tokens
+ * of keys and n_b = query_indptr[b+1] - query_indptr[b] queries; with desc->causal they stand at its end, as in prompt_attn,
+ * and see what is not behind them, else each sees every token.  For every token t < kv_lens[b] and KV head j
+ *   weights_out[b, j, t] = decay * weights[b, j, t] + sum over queries i that see t and query heads h of j of
+ *                          exp(scale * q[i, h] . k[t, j] - lse[i, h])
+ * lse is the attention call's lse_out: a sample's covers prompt and suffix, so the weights of both add up to its query
+ * heads.  A query whose lse is -inf adds nothing.
+ *   one step's samples over their own tokens   query_indptr 0, 1, .. N, kv_lens = suffix_lens, the suffixes' table
+ *   the samples over the prompt they share     query_indptr = sample_indptr, kv_lens = prefix_lens, the prompts' table
+ *   a prompt's tokens over the prompt          prompt_attn's arguments, causal; or its last tokens' queries only
+ *   (in contiguous suffixes [N, max_suffix_len, Hkv, D], sample n starts at token n * max_suffix_len)
+ * q, k, query_indptr, kv_lens, kv_indptr, kv_page_indices, the strides, total_queries, max_query_len and max_kv_len as for
+ * prompt_attn; causal queries ahead of their sequence's first token see nothing.
+ *   lse          float [total_queries, Hq], natural log
+ *   weights      float [num_prompts, Hkv, weights_stride] or NULL (= 0); not read where decay is 0
+ *   weights_out  as weights, and may be weights itself, else must not overlap it.  Entries from kv_lens[b] on are neither
+ *                read nor written: where tokens are appended later, they have to hold 0 (compact_kv leaves them so).
+ *   weights_stride  at least max_kv_len
+ * Sums are fp32, in an order that depends on the bounds and lengths alone.  Returns spd_status.
+ */
+SPD_API int accumulate_kv_weights(const spd_prompt_desc *desc, const void *q, const void *k,
+                                  const int32_t *query_indptr, const int32_t *kv_lens,
+                                  const int32_t *kv_indptr, const int32_t *kv_page_indices,
+                                  const float *lse, int64_t total_queries, int64_t max_query_len, int64_t max_kv_len,
+                                  float decay, const float *weights, float *weights_out, int64_t weights_stride,
+                                  void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of workspace select_kv_tokens needs (0 on invalid sizes). */
+SPD_API size_t select_kv_tokens_workspace_size(int64_t num_seqs, int32_t num_heads, int64_t max_kv_len);
+
+/*
+ * Which tokens of a cache stay.  Of the n = kv_lens[b] tokens of sequence b, m = min(n, budgets[b]) stay for every
+ * KV head j: the last r = min(recent, m), the first f = min(sinks, m - r), and of those between the m - f - r with the
+ * largest weights[b, j, t], the lower t first among equal ones (a NaN weighs less than anything else).
+ *   source    int32 [num_seqs, num_heads, source_stride]: source[b, j, i] is the token that place i < m gets.  The last
+ *             r tokens keep their order at the end (place m - r + i gets token n - r + i).  Of the others, one at t < m - r
+ *             stays where it is, and the rest fill the places left before m - r in ascending order.  So source[b, j, i] >= i.
+ *             Entries from m on are not written.
+ *   new_lens  int32 [num_seqs]: m
+ *   weights   float [num_seqs, num_heads, weights_stride]
+ *   budgets   int32 [num_seqs] (negative ones count as 0), or NULL: max_new_len for all
+ *   max_kv_len, max_new_len  host-known upper bounds: longer lengths and larger budgets count as these
+ * max_kv_len up to 2^24.  Returns spd_status.
+ */
+SPD_API int select_kv_tokens(const float *weights, int64_t weights_stride, int64_t num_seqs, int32_t num_heads,
+                             const int32_t *kv_lens, int64_t max_kv_len,
+                             const int32_t *budgets, int64_t max_new_len, int32_t sinks, int32_t recent,
+                             int32_t *source, int64_t source_stride, int32_t *new_lens,
+                             void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Moves the tokens that stay: for every sequence b, KV head j and place i < new_lens[b], keys, values and weight of
+ * place i of (k_out, v_out, weights_out) become those of token source[b, j, i] of (k, v, weights).
+ *   source    entry (b, j, i) at source[b * source_seq_stride + j * source_head_stride + i] (a head stride of 0: one list for
+ *             all heads), source >= i; a place whose source is smaller, or lies past the sequence's table, is left as it is
+ *   new_lens  int32 [num_prompts]; max_new_len is a host-known upper bound, and larger ones count as it
+ *   kv_indptr, kv_page_indices, k, v          as for prompt_attn: where the sequences are
+ *   out_indptr, out_page_indices, k_out, v_out  where they go.  In place: the same four pointers, and no two sequences share a
+ *             page; else what is written must not overlap what is read, and places past a sequence's table are not
+ *             written.  Contiguous tokens are kv_stride apart in all four, and indptr holds num_prompts + 1 token starts.
+ *   weights, weights_out  float [num_prompts, Hkv, weights_stride], both or neither NULL; may be one array, else must not
+ *             overlap.  Entries of weights_out from new_lens[b] on are set to 0.  weights_stride is at least max_new_len;
+ *             sources from weights_stride on weigh 0.
+ *   lens_out  int32 [num_prompts] or NULL: gets new_lens (the decode call's suffix_lens, for one)
+ * Pages behind the new length stay in the sequence's table (room for what is appended next).
+ * desc: dtype, num_kv_heads, head_dim, num_prompts, page_size, kv_stride.  Pools 16-byte aligned.  Returns spd_status.
+ */
+SPD_API int compact_kv(const spd_prompt_desc *desc, const int32_t *source, int64_t source_seq_stride,
+                       int64_t source_head_stride, const int32_t *new_lens, int64_t max_new_len,
+                       const int32_t *kv_indptr, const int32_t *kv_page_indices, const void *k, const void *v,
+                       const int32_t *out_indptr, const int32_t *out_page_indices, void *k_out, void *v_out,
+                       const float *weights, float *weights_out, int64_t weights_stride,
+                       int32_t *lens_out, void *stream);
+
 /* Short description of a status code (static storage). */
 SPD_API const char *spd_status_string(int status);
 

@@ -123,6 +123,20 @@ def load() -> ctypes.CDLL:
     lib.mark_prompt_tokens.argtypes = [vp, vp, i64, i64, vp, i64, ctypes.c_int32, vp]
     lib.penalize_logits.restype = ctypes.c_int
     lib.penalize_logits.argtypes = [vp, ctypes.c_int32, i64, i64, i64, ctypes.POINTER(Penalties), vp, i64, vp]
+    lib.token_logprobs_workspace_size.restype = sz
+    lib.token_logprobs_workspace_size.argtypes = [i64, i64, ctypes.c_int32]
+    lib.token_logprobs.restype = ctypes.c_int
+    lib.token_logprobs.argtypes = [vp, ctypes.c_int32, i64, i64, i64, vp, vp, ctypes.c_int32] + [vp] * 7 + [sz, vp]
+    lib.accumulate_kv_weights_workspace_size.restype = sz
+    lib.accumulate_kv_weights_workspace_size.argtypes = [pp, i64, i64, i64]
+    lib.accumulate_kv_weights.restype = ctypes.c_int
+    lib.accumulate_kv_weights.argtypes = [pp] + [vp] * 7 + [i64, i64, i64, ctypes.c_float, vp, vp, i64, vp, sz, vp]
+    lib.select_kv_tokens_workspace_size.restype = sz
+    lib.select_kv_tokens_workspace_size.argtypes = [i64, ctypes.c_int32, i64]
+    lib.select_kv_tokens.restype = ctypes.c_int
+    lib.select_kv_tokens.argtypes = [vp, i64, i64, ctypes.c_int32, vp, i64, vp, i64, ctypes.c_int32, ctypes.c_int32, vp, i64, vp, vp, sz, vp]
+    lib.compact_kv.restype = ctypes.c_int
+    lib.compact_kv.argtypes = [pp, vp, i64, i64, vp, i64] + [vp] * 10 + [i64, vp, vp]
     _lib = lib
     return lib
 
@@ -399,3 +413,55 @@ def penalize_logits(logits, logits_dtype: int, rows: int, vocab: int, row_stride
                                 ctypes.byref(penalties), _ptr(out), int(out_stride), _stream(stream))
     if rc != SPD_OK:
         raise SpdError(rc, "penalize_logits")
+
+
+def token_logprobs_workspace_size(rows: int, vocab: int, num_top: int) -> int:
+    return int(load().token_logprobs_workspace_size(int(rows), int(vocab), int(num_top)))
+
+
+def token_logprobs(logits, logits_dtype: int, rows: int, vocab: int, row_stride: int, temperature, tokens, num_top: int, logprobs,
+                   ranks, entropy, lse, top_tokens, top_logprobs, workspace, stream=None) -> None:
+    rc = load().token_logprobs(_ptr(logits), int(logits_dtype), int(rows), int(vocab), int(row_stride), _ptr(temperature), _ptr(tokens),
+                               int(num_top), _ptr(logprobs), _ptr(ranks), _ptr(entropy), _ptr(lse), _ptr(top_tokens),
+                               _ptr(top_logprobs), _ptr(workspace), _bytes(workspace), _stream(stream))
+    if rc != SPD_OK:
+        raise SpdError(rc, "token_logprobs")
+
+
+def accumulate_kv_weights_workspace_size(desc: PromptDesc, total_queries: int, max_query_len: int, max_kv_len: int) -> int:
+    return int(load().accumulate_kv_weights_workspace_size(ctypes.byref(desc), int(total_queries), int(max_query_len), int(max_kv_len)))
+
+
+def accumulate_kv_weights(desc: PromptDesc, q, k, query_indptr, kv_lens, kv_indptr, kv_page_indices, lse, total_queries: int,
+                          max_query_len: int, max_kv_len: int, decay: float, weights, weights_out, weights_stride: int, workspace,
+                          stream=None) -> None:
+    rc = load().accumulate_kv_weights(
+        ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(query_indptr), _ptr(kv_lens), _ptr(kv_indptr), _ptr(kv_page_indices), _ptr(lse),
+        int(total_queries), int(max_query_len), int(max_kv_len), float(decay), _ptr(weights), _ptr(weights_out), int(weights_stride),
+        _ptr(workspace), _bytes(workspace), _stream(stream))
+    if rc != SPD_OK:
+        raise SpdError(rc, "accumulate_kv_weights")
+
+
+def select_kv_tokens_workspace_size(num_seqs: int, num_heads: int, max_kv_len: int) -> int:
+    return int(load().select_kv_tokens_workspace_size(int(num_seqs), int(num_heads), int(max_kv_len)))
+
+
+def select_kv_tokens(weights, weights_stride: int, num_seqs: int, num_heads: int, kv_lens, max_kv_len: int, budgets, max_new_len: int,
+                     sinks: int, recent: int, source, source_stride: int, new_lens, workspace, stream=None) -> None:
+    rc = load().select_kv_tokens(_ptr(weights), int(weights_stride), int(num_seqs), int(num_heads), _ptr(kv_lens), int(max_kv_len),
+                                 _ptr(budgets), int(max_new_len), int(sinks), int(recent), _ptr(source), int(source_stride),
+                                 _ptr(new_lens), _ptr(workspace), _bytes(workspace), _stream(stream))
+    if rc != SPD_OK:
+        raise SpdError(rc, "select_kv_tokens")
+
+
+def compact_kv(desc: PromptDesc, source, source_seq_stride: int, source_head_stride: int, new_lens, max_new_len: int, kv_indptr,
+               kv_page_indices, k, v, out_indptr, out_page_indices, k_out, v_out, weights, weights_out, weights_stride: int, lens_out,
+               stream=None) -> None:
+    rc = load().compact_kv(
+        ctypes.byref(desc), _ptr(source), int(source_seq_stride), int(source_head_stride), _ptr(new_lens), int(max_new_len),
+        _ptr(kv_indptr), _ptr(kv_page_indices), _ptr(k), _ptr(v), _ptr(out_indptr), _ptr(out_page_indices), _ptr(k_out), _ptr(v_out),
+        _ptr(weights), _ptr(weights_out), int(weights_stride), _ptr(lens_out), _stream(stream))
+    if rc != SPD_OK:
+        raise SpdError(rc, "compact_kv")

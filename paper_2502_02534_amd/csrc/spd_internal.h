@@ -211,6 +211,77 @@ struct LogitsParams {
     int max_tokens;
 };
 
+struct LogprobsParams {
+    const void* logits;
+    int bf16;
+    long long rows, vocab, stride;
+    const float* temperature;  // may be null
+    const int* tokens;         // may be null, as every output
+    int top;
+    float* logprobs;
+    int* ranks;
+    float* entropy;
+    float* lse;
+    int* top_tokens;
+    float* top_logprobs;
+    void* workspace;
+};
+
+// Attention weights of cached tokens (see kv_weights.hip).
+struct KvWeightsParams {
+    int dtype, Hq, Hkv, D, G, B, page_size, causal;
+    float scale_log2;  // sm_scale * log2(e)
+    const void* q;
+    const void* k;
+    long long q_stride, kv_stride;  // elements between tokens
+    const int* query_indptr;
+    const int* kv_lens;
+    const int* kv_indptr;
+    const int* pages;
+    const float* lse;
+    int max_query, max_kv;
+    float decay;
+    const float* weights;  // null: 0
+    float* weights_out;
+    long long stride;
+    int splits;   // parts of a sequence's query rows
+    float* part;  // [splits - 1][B][Hkv][max_kv]
+};
+
+struct SelectParams {
+    const float* weights;
+    long long stride, seqs;
+    int heads;
+    const int* lens;
+    int max_len;
+    const int* budgets;  // may be null
+    int max_new, sinks, recent;
+    int* source;
+    long long source_stride;
+    int* new_lens;
+};
+
+struct CompactParams {
+    const int* source;
+    long long seq_stride, head_stride;
+    const int* new_lens;
+    int max_new, B, Hkv, head_u4, page_size;  // head_u4: 16-byte pieces of one head's row
+    long long stride_u4;                      // pieces between contiguous tokens
+    const int* indptr;
+    const int* pages;
+    const void* k;
+    const void* v;
+    const int* out_indptr;
+    const int* out_pages;
+    void* k_out;
+    void* v_out;
+    const float* weights;  // may be null
+    float* weights_out;
+    long long weights_stride;
+    int* lens_out;  // may be null
+    int in_place;
+};
+
 // Index of the partial state of output row `row` (= n * Hq + h) in slot `slot`.
 __device__ __forceinline__ long long part_index(const AttnParams& p, long long row, int slot)
 {
@@ -256,6 +327,10 @@ hipError_t launch_kv_write(const KvWriteParams& p, hipStream_t s);
 hipError_t launch_mark_tokens(const int* tokens, const int* indptr, long long prompts, long long vocab, uint32_t* bits,
                               long long stride, bool accumulate, hipStream_t s);
 hipError_t launch_penalize_logits(const LogitsParams& p, hipStream_t s);
+hipError_t launch_token_logprobs(const LogprobsParams& p, hipStream_t s);
+hipError_t launch_kv_weights(const KvWeightsParams& p, hipStream_t s);
+hipError_t launch_select_kv(const SelectParams& p, hipStream_t s);
+hipError_t launch_compact_kv(const CompactParams& p, hipStream_t s);
 hipError_t launch_sampler(const SamplerParams& p, void* workspace, hipStream_t s);
 
 }  // namespace spd
