@@ -1,64 +1,608 @@
 // How much of the queries' attention every cached token got:
 //   w'[b, j, t] = decay w[b, j, t] + sum over the query rows (i, h) that see t of 2^(scale_log2 q . k_t - lse_log2)
-// One workgroup takes 64 tokens of one KV head and all query rows of their sequence, so a weight has one owner and its
-// sum one order.
+//
+// Rows are the (query, head of the group) pairs of a KV head.  The products are taken transposed, S^T = K Q^T: a lane of the
+// accumulator has one row's scores of several tokens, so the row's log-sum-exp is one number a lane, and a token's sum over
+// the rows stays in its register until the end, when the lanes' shares are added.  A weight has one owner (or one for each
+// part of the rows, which a second launch adds in order), so no sum depends on who comes first.
+//
+//   few rows (up to 32: one step's queries over a sample's own tokens): a wavefront keeps the rows' fragments in registers and streams
+//     the keys, the next tile's loads under way while it works on this one.  Bound: HBM, K read once.
+//   many rows (samples over their shared prompt, a prompt over itself): a wavefront keeps 64 tokens' keys in registers (32 in fp32),
+//     the rows pass by in blocks of 32: in bf16 through LDS, shared by the four wavefronts of a workgroup, with the
+//     exponentials of one block between the products of the next.  Bound: matrix pipe and vector ALU alike (16 products of 32 clocks
+//     against 32 fma, exponentials and additions a lane, 128 channels).
+//     Causal: the last rows, which every tile sees, come first, so that tiles that run together read the same rows.
+#include "prompt_plan.h"
 #include "spd_internal.h"
+
+#include <type_traits>
 
 namespace spd {
 namespace {
 
-constexpr int kThreads = 256, kTokens = 64;
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
 
-template <bool BF16> __device__ __forceinline__ float element(const void* x, long long at)
+constexpr int kWaves = 4;
+
+__device__ __forceinline__ bf16x8 as_bf16x8(const uint4& v) { return *reinterpret_cast<const bf16x8*>(&v); }
+__device__ __forceinline__ float part_of(const uint4& v, int e)
 {
-    if (BF16)
-        return __uint_as_float((unsigned)((const unsigned short*)x)[at] << 16);
-    return ((const float*)x)[at];
+    return __uint_as_float(e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w);
 }
 
-template <bool BF16> __global__ __launch_bounds__(kThreads) void kv_weights_kernel(KvWeightsParams p, int tiles)
+// -lse in base 2; a row that is not there, or saw nothing, has -inf: it adds 2^-inf = 0.
+__device__ __forceinline__ float exponent_of(float lse, bool there)
 {
-    __shared__ float sums[4][kTokens];
-    const int j = blockIdx.x % p.Hkv, tile = blockIdx.x / p.Hkv % tiles, b = blockIdx.x / p.Hkv / tiles;
-    const int L = min(p.kv_lens[b], p.max_kv), t0 = tile * kTokens;
-    if (t0 >= L)
+    return there && lse > -INFINITY ? -lse * kLog2e : there && lse != lse ? lse : -INFINITY;
+}
+
+// Sum over the 16 lanes of a lane row.
+template <int CTRL> __device__ __forceinline__ float add_dpp(float v)
+{
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float over_row(float v)
+{
+    return add_dpp<0x121>(add_dpp<0x122>(add_dpp<0x124>(add_dpp<0x128>(v))));  // rotations by 8, 4, 2, 1
+}
+
+// 16-byte piece `piece` of token t's key, KV head j; `head_pieces` of them, zeros behind.
+template <bool PAGED> struct Keys {
+    const uint4* base;
+    const int* pages;
+    long long head_at, token_pieces, page_pieces;
+    __device__ __forceinline__ Keys(const KvWeightsParams& p, int b, int j, int head_pieces)
+    {
+        const int first = p.kv_indptr[b];
+        const int per = p.dtype == 1 ? 8 : 4;
+        if (PAGED) {
+            base = (const uint4*)p.k;
+            pages = p.pages + first;
+            token_pieces = head_pieces;
+            page_pieces = (long long)p.Hkv * 16 * head_pieces;
+            head_at = (long long)j * 16 * head_pieces;
+        } else {
+            token_pieces = p.kv_stride / per;
+            base = (const uint4*)p.k + (long long)first * token_pieces;
+            pages = nullptr;
+            page_pieces = 0;
+            head_at = (long long)j * head_pieces;
+        }
+    }
+    __device__ __forceinline__ const uint4* row(int t) const
+    {
+        return PAGED ? base + (long long)pages[t >> 4] * page_pieces + head_at + (t & 15) * token_pieces : base + head_at + (long long)t * token_pieces;
+    }
+};
+
+// ---- few rows: the keys stream by --------------------------------------------------------------------------------
+
+// bf16: 16 x 16 x 32 products, step s takes pieces 4 s + g of a row (g = lane / 16); fp32: 16 x 16 x 4, piece 4 s + g's four elements
+// one after another.  Either way a lane's operand is 16-byte pieces of its row.
+template <bool BF16> __device__ __forceinline__ floatx4 product16(const uint4& k, const uint4& q, floatx4 c)
+{
+    if constexpr (BF16) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(k), as_bf16x8(q), c, 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(part_of(k, e), part_of(q, e), c, 0, 0, 0);
+        return c;
+    }
+}
+
+// P: 16-byte pieces of a padded head (D = 64, 128, 256 in bf16: 8, 16, 32); SUB: 16-token halves of a tile; NB: blocks of 16 rows.
+template <bool BF16, int P, int SUB, int NB, bool PAGED>
+__global__ __launch_bounds__(kWaves * 64) void kv_weights_few(KvWeightsParams p, int chunk, int chunks)
+{
+    constexpr int kSteps = P / 4, kTile = 16 * SUB;
+    const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
+    const int item = __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + (threadIdx.x >> 6));
+    // KV head fastest: the heads of a token lie beside each other
+    const int j = item % p.Hkv, rest = item / p.Hkv, b = rest % p.B, at = rest / p.B;
+    if (at >= chunks)
         return;
-    const int q0 = p.query_indptr[b], n = min(p.query_indptr[b + 1] - q0, p.max_query);
-    const int part = threadIdx.x >> 6, t = t0 + (threadIdx.x & 63), tk = min(t, L - 1), kv0 = p.kv_indptr[b];
-    const long long k_at = p.page_size ? (((long long)p.pages[kv0 + tk / 16] * p.Hkv + j) * 16 + tk % 16) * p.D
-                                       : (long long)(kv0 + tk) * p.kv_stride + (long long)j * p.D;
-    float sum = 0.f;
-    for (int r = part; r < n * p.G; r += 4) {
-        const int i = r / p.G, h = j * p.G + r % p.G;
-        const float lse = p.lse[(long long)(q0 + i) * p.Hq + h];
-        if (lse == -INFINITY || (p.causal && t > L - n + i))
+    const int L = min(p.kv_lens[b], p.max_kv), t0 = at * chunk, t1 = min(L, t0 + chunk);
+    if (t0 >= t1)
+        return;
+    const int q0 = p.query_indptr[b], n = max(min(p.query_indptr[b + 1] - q0, p.max_query), 0), rows = n * p.G;
+    const int head_pieces = p.D / (BF16 ? 8 : 4);
+    const Keys<PAGED> keys(p, b, j, head_pieces);
+
+    uint4 q[NB][kSteps];
+    float below[NB];  // -lse of the lane's row in base 2
+    int limit[NB];    // last token that it sees
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        const int r = nb * 16 + col, i = min(r, max(rows - 1, 0)) / p.G, h = j * p.G + min(r, max(rows - 1, 0)) % p.G;
+        const bool there = r < rows;
+        below[nb] = exponent_of(there ? p.lse[(long long)(q0 + i) * p.Hq + h] : 0.f, there);
+        limit[nb] = !there ? -1 : p.causal ? L - n + i : L;
+        const uint4* const from = (const uint4*)p.q + (long long)(q0 + i) * (p.q_stride / (BF16 ? 8 : 4)) + (long long)h * head_pieces;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            q[nb][s] = make_uint4(0u, 0u, 0u, 0u);
+            if (there && 4 * s + g < head_pieces)
+                q[nb][s] = from[4 * s + g];
+        }
+    }
+    // the lanes that store: 4 SUB of each lane row, token 16 (col / 4) + 4 g + col % 4 of the tile
+    const int mine = 16 * (col >> 2) + 4 * g + (col & 3);
+    const bool stores = col < 4 * SUB;
+    const long long out_at = ((long long)b * p.Hkv + j) * p.stride;
+    const auto load = [&](int tb, uint4 (&k)[SUB][kSteps], float& old) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+            const uint4* const row = keys.row(min(tb + 16 * u + col, t1 - 1));
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                k[u][s] = make_uint4(0u, 0u, 0u, 0u);
+                if (4 * s + g < head_pieces)
+                    k[u][s] = row[4 * s + g];
+            }
+        }
+        old = 0.f;
+        if (p.weights && stores && tb + mine < t1)
+            old = p.weights[out_at + tb + mine];
+    };
+    const auto work = [&](int tb, const uint4 (&k)[SUB][kSteps], float old) __attribute__((always_inline)) {
+        float total = 0.f;
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+            floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                floatx4 c = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s)
+                    c = product16<BF16>(k[u][s], q[nb][s], c);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(c[i], p.scale_log2, below[nb]));
+                    sum[i] += tb + 16 * u + 4 * g + i <= limit[nb] ? x : 0.f;  // (a row that is not there sees nothing)
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float all = over_row(sum[i]);
+                total = col == 4 * u + i ? all : total;
+            }
+        }
+        if (stores && tb + mine < t1)
+            p.weights_out[out_at + tb + mine] = p.weights ? __builtin_fmaf(p.decay, old, total) : total;
+    };
+    uint4 ka[SUB][kSteps], kb[SUB][kSteps];
+    float oa, ob;
+    load(t0, ka, oa);
+    for (int tb = t0; tb < t1; tb += 2 * kTile) {
+        if (tb + kTile < t1)
+            load(tb + kTile, kb, ob);
+        work(tb, ka, oa);
+        if (tb + kTile >= t1)
+            break;
+        if (tb + 2 * kTile < t1)
+            load(tb + 2 * kTile, ka, oa);
+        work(tb + kTile, kb, ob);
+    }
+}
+
+// ---- many rows -----------------------------------------------------------------------------------------------------
+
+// What a workgroup of the other kernels takes: `tokens` keys from t0 on of KV head j of sequence b, and the row blocks
+// first .. last - 1 of 32 rows that see any of them.
+struct Unit {
+    bool any;
+    int b, j, t0, L, q0, n, rows, first, last, split;
+};
+
+__device__ __forceinline__ Unit find_unit(const KvWeightsParams& p, int tokens, int tiles, int paired)
+{
+    Unit u;
+    const int j = blockIdx.x % p.Hkv;
+    int rest = blockIdx.x / p.Hkv;
+    const int units = tiles * p.B * p.splits;
+    if (paired && rest >= units / 2)  // all run at once, two a CU: a long one and a short one
+        rest = units - 1 - (rest - units / 2);
+    // causal tiles see the fewer rows the later they are: first tiles first
+    const int tile = rest / (p.B * p.splits), rem = rest % (p.B * p.splits);
+    u.j = j;
+    u.b = rem / p.splits;
+    u.split = rem % p.splits;
+    u.t0 = tile * tokens;
+    u.L = min(p.kv_lens[u.b], p.max_kv);
+    u.any = u.t0 < u.L;
+    if (!u.any)
+        return u;
+    u.q0 = p.query_indptr[u.b];
+    u.n = max(min(p.query_indptr[u.b + 1] - u.q0, p.max_query), 0);
+    u.rows = u.n * p.G;
+    const int hidden = p.causal ? min(max(u.t0 - (u.L - u.n), 0), u.n) * p.G : 0;  // rows that see nothing of the tile
+    const int lo = hidden / 32, hi = (u.rows + 31) / 32, per = (hi - lo + p.splits - 1) / p.splits;
+    u.first = lo + min(u.split * per, hi - lo);
+    u.last = min(u.first + per, hi);
+    return u;
+}
+
+// Sums of V values over the 32 lanes of a half: value c of the half's lane c afterwards (V = 16: lanes c and c + 16 alike).
+template <int V> __device__ __forceinline__ float over_columns(float (&v)[V])
+{
+    const int lane = threadIdx.x & 63;
+    int kept = V;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        if (V == 16 && o == 16) {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                v[i] += __shfl_xor(v[i], 16);
             continue;
-        const long long q_at = (long long)(q0 + i) * p.q_stride + (long long)h * p.D;
-        float s = 0.f;
-        for (int c = 0; c < p.D; ++c)
-            s = __builtin_fmaf(element<BF16>(p.q, q_at + c), element<BF16>(p.k, k_at + c), s);
-        sum += __builtin_amdgcn_exp2f(__builtin_fmaf(s, p.scale_log2, -lse * kLog2e));
+        }
+        kept >>= 1;
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            if (i < kept) {
+                const bool up = (lane & o) != 0;
+                const float give = up ? v[i] : v[i + kept], keep = up ? v[i + kept] : v[i];
+                v[i] = keep + __shfl_xor(give, o);
+            }
+        }
     }
-    sums[part][threadIdx.x & 63] = sum;
-    __syncthreads();
-    if (part == 0 && t < L) {
-        const long long at = ((long long)b * p.Hkv + j) * p.stride + t;
-        const float all = (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
-        p.weights_out[at] = p.weights ? __builtin_fmaf(p.decay, p.weights[at], all) : all;
+    return v[0];
+}
+
+// The unit's weights: value c of half h is token 32 (c / 16) + 8 (c % 16 / 4) + 4 h + c % 4 of the wavefront's.
+template <int V> __device__ __forceinline__ void store(const KvWeightsParams& p, const Unit& u, int tw, float (&v)[V])
+{
+    const int lane = threadIdx.x & 63, c = lane & (V - 1), h = lane >> 5;
+    const float total = over_columns(v);
+    const int t = tw + 32 * (c >> 4) + 8 * ((c & 15) >> 2) + 4 * h + (c & 3);
+    if (t >= u.L || (lane & 31) >= V)
+        return;
+    if (p.splits > 1) {
+        p.part[(((long long)u.split * p.B + u.b) * p.Hkv + u.j) * p.max_kv + t] = total;
+        return;
     }
+    const long long at = ((long long)u.b * p.Hkv + u.j) * p.stride + t;
+    p.weights_out[at] = p.weights ? __builtin_fmaf(p.decay, p.weights[at], total) : total;
+}
+
+// bf16.  D: channels of a padded head.
+template <int D> struct Shape {
+    static constexpr int kRow = 2 * D, kBlock = 32 * kRow, kPieces = D / 8, kSteps = D / 16, kCopies = kBlock / (kWaves * 64 * 16);
+    // Piece i of row r lies in slot i ^ swz(r), so that sixteen rows' equal pieces take all 64 banks.
+    static __device__ __forceinline__ int swz(int row)
+    {
+        if (D >= 128)
+            return ((row & 3) << 2) | ((row >> 2) & 3);
+        return (((row >> 1) & 1) << 2) | (((row >> 2) & 1) << 1) | ((row >> 3) & 1);
+    }
+};
+
+constexpr int kManyTokens = 64;  // of a wavefront
+
+template <int D, bool PAGED>
+__global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void kv_weights_many(KvWeightsParams p, int tiles, int paired)
+{
+    using S = Shape<D>;
+    __shared__ __align__(16) char lds[2 * S::kBlock];
+    const Unit u = find_unit(p, kWaves * kManyTokens, tiles, paired);
+    if (!u.any)
+        return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, h = lane >> 5;
+    const int tw = u.t0 + wave * kManyTokens, head_pieces = p.D / 8;
+    const int G = p.G;
+
+    // ---- rows: copied by all, two blocks ahead into registers, one ahead into LDS; (query, head) of a copy walk back 32 rows a time
+    int ci[S::kCopies], cg[S::kCopies];
+    const int back_i = 32 / G, back_g = 32 % G;
+    const int row_pieces = S::kPieces;
+#pragma unroll
+    for (int c = 0; c < S::kCopies; ++c) {
+        const int r = (u.last - 1) * 32 + (c * kWaves * 64 + tid) / row_pieces;
+        ci[c] = r / G;
+        cg[c] = r % G;
+    }
+    const int piece = tid % row_pieces;
+    const uint4* const q_base = (const uint4*)p.q + (long long)u.q0 * (p.q_stride / 8) + (long long)u.j * G * head_pieces + piece;
+    const bool has_piece = piece < head_pieces;
+    int to_copy = u.last - 1;
+    uint4 staged[2][S::kCopies];
+    const auto fetch = [&](uint4 (&v)[S::kCopies]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < S::kCopies; ++c) {
+            v[c] = make_uint4(0u, 0u, 0u, 0u);
+            if (to_copy >= u.first && has_piece)
+                v[c] = q_base[(long long)min(ci[c], u.n - 1) * (p.q_stride / 8) + (long long)cg[c] * head_pieces];
+            ci[c] -= back_i;
+            cg[c] -= back_g;
+            if (cg[c] < 0) {
+                cg[c] += G;
+                ci[c] -= 1;
+            }
+        }
+        --to_copy;
+    };
+    const auto put = [&](int slot, const uint4 (&v)[S::kCopies]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < S::kCopies; ++c) {
+            const int row = (c * kWaves * 64 + tid) / row_pieces;
+            *(uint4*)(lds + slot * S::kBlock + row * S::kRow + ((piece ^ S::swz(row)) << 4)) = v[c];
+        }
+    };
+    // the lane's own row: its log-sum-exp, and the last token that it sees
+    int li = ((u.last - 1) * 32 + col) / G, lg = ((u.last - 1) * 32 + col) % G;
+    const float* const lse_base = p.lse + (long long)u.q0 * p.Hq + (long long)u.j * G;
+    const auto next_lse = [&](bool more, float& lse, int& query) __attribute__((always_inline)) {
+        lse = 0.f;
+        query = li;
+        if (more && li < u.n)
+            lse = lse_base[(long long)li * p.Hq + lg];
+        li -= back_i;
+        lg -= back_g;
+        if (lg < 0) {
+            lg += G;
+            li -= 1;
+        }
+    };
+
+    const int blocks = u.last - u.first;
+    float sums[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+        sums[i] = 0.f;
+    if (blocks > 0) {
+        fetch(staged[0]);
+        fetch(staged[1]);
+        // ---- keys: A operand, row = token, channels 16 s + 8 h (tokens past the end repeat the last one)
+        uint4 k[2][S::kSteps];
+        {
+            const Keys<PAGED> keys(p, u.b, u.j, head_pieces);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const uint4* const row = keys.row(min(tw + 32 * x + col, u.L - 1));
+#pragma unroll
+                for (int s = 0; s < S::kSteps; ++s) {
+                    k[x][s] = make_uint4(0u, 0u, 0u, 0u);
+                    if (2 * s + h < head_pieces)
+                        k[x][s] = row[2 * s + h];
+                }
+            }
+        }
+        float lse_a, lse_b;
+        int query_a, query_b;
+        next_lse(true, lse_a, query_a);
+        put(0, staged[0]);
+        fetch(staged[0]);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        floatx16 sc[2][2];  // [block parity][half of the tokens]
+        float below = -INFINITY;
+        int limit = 0;
+        // Block i: its products into `now`, and between them the exponentials of the block before, `was` (MASK: of rows that do not see all tokens).
+        const auto block = [&](auto soft_tag, auto mask_tag, int i, floatx16 (&now)[2], const floatx16 (&was)[2], uint4 (&stage)[S::kCopies])
+            __attribute__((always_inline)) {
+            constexpr bool SOFT = decltype(soft_tag)::value, MASK = decltype(mask_tag)::value;
+            const int slot = i & 1;
+            next_lse(i + 1 < blocks, lse_b, query_b);
+            // what was fetched a block ago goes to the other slot, and its registers take the block after
+            const char* const from = lds + slot * S::kBlock + col * S::kRow;
+            uint4 f[2];
+            f[0] = *(const uint4*)(from + ((h ^ S::swz(col)) << 4));
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                now[0][e] = now[1][e] = 0.f;
+            constexpr int kPer = 32 / S::kSteps;
+#pragma unroll
+            for (int s = 0; s < S::kSteps; ++s) {
+                if (s + 1 < S::kSteps)
+                    f[(s + 1) & 1] = *(const uint4*)(from + (((2 * (s + 1) + h) ^ S::swz(col)) << 4));
+                now[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[0][s]), as_bf16x8(f[s & 1]), now[0], 0, 0, 0);
+                now[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[1][s]), as_bf16x8(f[s & 1]), now[1], 0, 0, 0);
+                if (SOFT) {
+#pragma unroll
+                    for (int x = 0; x < kPer; ++x) {
+                        const int v = s * kPer + x, e = v & 15;
+                        float w = __builtin_amdgcn_exp2f(__builtin_fmaf(was[v >> 4][e], p.scale_log2, below));
+                        if (MASK)
+                            w = tw + 32 * (v >> 4) + (e & 3) + 8 * (e >> 2) + 4 * h <= limit ? w : 0.f;
+                        sums[v] += w;
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (i + 1 < blocks) {
+                put(slot ^ 1, stage);
+                fetch(stage);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        };
+        const auto soft = [&](const floatx16 (&was)[2]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int v = 0; v < 32; ++v) {
+                const int e = v & 15;
+                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(was[v >> 4][e], p.scale_log2, below));
+                sums[v] += tw + 32 * (v >> 4) + (e & 3) + 8 * (e >> 2) + 4 * h <= limit ? w : 0.f;
+            }
+        };
+        // rows of the block before: whether all of them see all of this wavefront's tokens
+        const int hide = u.L - u.n;
+        const auto take = [&](int i) __attribute__((always_inline)) {
+            const bool there = (u.last - 1 - i) * 32 + col < u.rows;
+            below = exponent_of(lse_a, there);
+            limit = !there ? -1 : p.causal ? hide + query_a : u.L;
+        };
+        const auto whole = [&](int i) __attribute__((always_inline)) {
+            const int r = (u.last - 1 - i) * 32;
+            return r + 32 <= u.rows && (!p.causal || hide + r / G >= tw + kManyTokens - 1);
+        };
+        std::true_type yes;
+        std::false_type no;
+        block(no, no, 0, sc[0], sc[1], staged[1]);
+        take(0);
+        lse_a = lse_b;
+        query_a = query_b;
+        int i = 1;
+        const auto step = [&](int at, floatx16 (&now)[2], const floatx16 (&was)[2], uint4 (&stage)[S::kCopies]) __attribute__((always_inline)) {
+            if (whole(at - 1))
+                block(yes, no, at, now, was, stage);
+            else
+                block(yes, yes, at, now, was, stage);
+            take(at);
+            lse_a = lse_b;
+            query_a = query_b;
+        };
+#pragma unroll 1
+        for (; i + 1 < blocks; i += 2) {
+            step(i, sc[1], sc[0], staged[0]);
+            step(i + 1, sc[0], sc[1], staged[1]);
+        }
+        if (i < blocks) {
+            step(i, sc[1], sc[0], staged[0]);
+            soft(sc[1]);
+        } else {
+            soft(sc[0]);
+        }
+    }
+    store<32>(p, u, tw, sums);
+}
+
+// fp32: 32 tokens a wavefront, rows straight from memory (a product of fp32 takes 16 times as long).  P: 16-byte pieces of a padded head.
+template <int P, bool PAGED>
+__global__ __launch_bounds__(kWaves * 64, P <= 32 ? 2 : 1) void kv_weights_many_f32(KvWeightsParams p, int tiles, int paired)
+{
+    constexpr int kSteps = P / 2;
+    const Unit u = find_unit(p, kWaves * 32, tiles, paired);
+    if (!u.any)
+        return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, h = lane >> 5;
+    const int tw = u.t0 + wave * 32, head_pieces = p.D / 4, G = p.G;
+    if (tw >= u.L)
+        return;
+    uint4 k[kSteps];
+    const Keys<PAGED> keys(p, u.b, u.j, head_pieces);
+    const uint4* const row = keys.row(min(tw + col, u.L - 1));
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        k[s] = make_uint4(0u, 0u, 0u, 0u);
+        if (2 * s + h < head_pieces)
+            k[s] = row[2 * s + h];
+    }
+    float sums[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        sums[i] = 0.f;
+#pragma unroll 1
+    for (int at = u.last - 1; at >= u.first; --at) {
+        const int r = at * 32 + col, rc = min(r, u.rows - 1), i = rc / G, g = rc % G;
+        const bool there = r < u.rows;
+        const float below = exponent_of(p.lse[(long long)(u.q0 + i) * p.Hq + u.j * G + g], there);
+        const int limit = !there ? -1 : p.causal ? u.L - u.n + i : u.L;
+        const uint4* const q = (const uint4*)p.q + (long long)(u.q0 + i) * (p.q_stride / 4) + (long long)(u.j * G + g) * head_pieces;
+        floatx16 c;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            c[e] = 0.f;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            uint4 f = make_uint4(0u, 0u, 0u, 0u);
+            if (2 * s + h < head_pieces)
+                f = q[2 * s + h];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                c = __builtin_amdgcn_mfma_f32_32x32x2f32(part_of(k[s], e), part_of(f, e), c, 0, 0, 0);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(c[e], p.scale_log2, below));
+            sums[e] += tw + (e & 3) + 8 * (e >> 2) + 4 * h <= limit ? w : 0.f;
+        }
+    }
+    store<16>(p, u, tw, sums);
+}
+
+// Adds the parts of the rows in order.
+__global__ __launch_bounds__(256) void kv_weights_join(KvWeightsParams p)
+{
+    const int t = blockIdx.x * 256 + threadIdx.x, bj = blockIdx.y, b = bj / p.Hkv;
+    if (t >= min(p.kv_lens[b], p.max_kv))
+        return;
+    float total = 0.f;
+    for (int s = 0; s < p.splits; ++s)
+        total += p.part[((long long)s * p.B * p.Hkv + bj) * p.max_kv + t];
+    const long long at = (long long)bj * p.stride + t;
+    p.weights_out[at] = p.weights ? __builtin_fmaf(p.decay, p.weights[at], total) : total;
+}
+
+template <bool BF16, int P, int SUB, int NB> void few(const KvWeightsParams& p, hipStream_t s)
+{
+    // a wavefront's stretch of tokens: long ones keep its loads going, short ones fill the card
+    const long long pairs = (long long)p.B * p.Hkv;
+    int chunk = 256;
+    while (chunk > 16 * SUB && pairs * ((p.max_kv + chunk - 1) / chunk) < 4096)
+        chunk /= 2;
+    const int chunks = (p.max_kv + chunk - 1) / chunk;
+    const dim3 grid((unsigned)((pairs * chunks + kWaves - 1) / kWaves));
+    if (p.page_size)
+        hipLaunchKernelGGL((kv_weights_few<BF16, P, SUB, NB, true>), grid, dim3(kWaves * 64), 0, s, p, chunk, chunks);
+    else
+        hipLaunchKernelGGL((kv_weights_few<BF16, P, SUB, NB, false>), grid, dim3(kWaves * 64), 0, s, p, chunk, chunks);
 }
 
 }  // namespace
 
 hipError_t launch_kv_weights(const KvWeightsParams& p, hipStream_t s)
 {
-    const int tiles = (p.max_kv + kTokens - 1) / kTokens;
-    const dim3 grid((unsigned)((long long)tiles * p.Hkv * p.B));
-    if (p.dtype == 1)
-        hipLaunchKernelGGL((kv_weights_kernel<true>), grid, dim3(kThreads), 0, s, p, tiles);
-    else
-        hipLaunchKernelGGL((kv_weights_kernel<false>), grid, dim3(kThreads), 0, s, p, tiles);
-    return hipGetLastError();
+    const bool bf16 = p.dtype == 1;
+    const long long rows = (long long)p.max_query * p.G;
+    if (rows <= plan::kWeightsFewRows) {
+        const int pieces = p.D / (bf16 ? 8 : 4);
+        if (bf16) {
+            if (rows <= 16)
+                pieces <= 8 ? few<true, 8, 2, 1>(p, s) : pieces <= 16 ? few<true, 16, 2, 1>(p, s) : few<true, 32, 1, 1>(p, s);
+            else
+                pieces <= 8 ? few<true, 8, 2, 2>(p, s) : pieces <= 16 ? few<true, 16, 2, 2>(p, s) : few<true, 32, 1, 2>(p, s);
+        } else {
+            if (rows <= 16)
+                pieces <= 16 ? few<false, 16, 1, 1>(p, s) : pieces <= 32 ? few<false, 32, 1, 1>(p, s) : few<false, 64, 1, 1>(p, s);
+            else
+                pieces <= 16 ? few<false, 16, 1, 2>(p, s) : pieces <= 32 ? few<false, 32, 1, 2>(p, s) : few<false, 64, 1, 2>(p, s);
+        }
+        return hipGetLastError();
+    }
+    const int tokens = plan::weights_tile_tokens(bf16), tiles = (p.max_kv + tokens - 1) / tokens;
+    const long long units = (long long)tiles * p.B * p.splits;
+    const dim3 grid((unsigned)(units * p.Hkv)), block(kWaves * 64);
+    const int paired = p.causal && p.splits == 1 && units * p.Hkv > 256 && units * p.Hkv <= 512;
+#define SPD_MANY(K, W) \
+    if (p.page_size) \
+        hipLaunchKernelGGL((K<W, true>), grid, block, 0, s, p, tiles, paired); \
+    else \
+        hipLaunchKernelGGL((K<W, false>), grid, block, 0, s, p, tiles, paired)
+    if (bf16) {
+        if (p.D <= 64) {
+            SPD_MANY(kv_weights_many, 64);
+        } else if (p.D <= 128) {
+            SPD_MANY(kv_weights_many, 128);
+        } else {
+            SPD_MANY(kv_weights_many, 256);
+        }
+    } else {
+        if (p.D <= 64) {
+            SPD_MANY(kv_weights_many_f32, 16);
+        } else if (p.D <= 128) {
+            SPD_MANY(kv_weights_many_f32, 32);
+        } else {
+            SPD_MANY(kv_weights_many_f32, 64);
+        }
+    }
+#undef SPD_MANY
+    hipError_t rc = hipGetLastError();
+    if (rc == hipSuccess && p.splits > 1) {
+        hipLaunchKernelGGL(kv_weights_join, dim3((p.max_kv + 255) / 256, p.B * p.Hkv), dim3(256), 0, s, p);
+        rc = hipGetLastError();
+    }
+    return rc;
 }
 
 }  // namespace spd

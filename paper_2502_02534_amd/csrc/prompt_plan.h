@@ -95,5 +95,50 @@ inline int make_prompt_plan(const spd_prompt_desc* d, int64_t total, int64_t max
     return SPD_OK;
 }
 
+// ---- accumulate_kv_weights --------------------------------------------------------------------------------
+
+constexpr int kWeightsFewRows = 32;   // rows up to which a wavefront keeps them all and streams the keys
+constexpr int kWeightsMaxSplits = 32;
+
+inline int weights_tile_tokens(bool bf16) { return bf16 ? 256 : 128; }  // of a workgroup with many rows
+
+struct WeightsPlan {
+    int splits;         // parts of a sequence's rows
+    size_t part_bytes;  // their sums
+};
+
+inline int make_weights_plan(const spd_prompt_desc* d, int64_t total, int64_t max_query, int64_t max_kv, WeightsPlan* out)
+{
+    const int rc = check_prompt_desc(d, true);
+    if (rc != SPD_OK)
+        return rc;
+    if (total < 0 || max_query < 0 || max_kv < 0)
+        return SPD_EINVAL;
+    const int64_t most = 0x7fffffff, group = d->num_q_heads / d->num_kv_heads;
+    // row, token and workgroup numbers are 32-bit
+    if (total > most / d->num_q_heads || max_query > (1ll << 30) / group || max_kv > (1ll << 30))
+        return SPD_EUNSUPPORTED;
+    const int64_t pairs = (int64_t)d->num_prompts * d->num_kv_heads;
+    if (pairs > (1ll << 22) / ((max_kv + 63) / 64 + 1))
+        return SPD_EUNSUPPORTED;
+    out->splits = 1;
+    out->part_bytes = 0;
+    const int64_t rows = max_query * group, tokens = weights_tile_tokens(d->dtype == SPD_BF16);
+    if (rows <= kWeightsFewRows)
+        return SPD_OK;
+    // where the tiles leave CUs idle, the rows are cut into parts of four blocks at least, which another launch adds
+    const int64_t units = pairs * ((max_kv + tokens - 1) / tokens);
+    if (units > 0 && units <= 128) {
+        int64_t splits = 512 / units;
+        const int64_t useful = (rows + 127) / 128;
+        splits = splits < useful ? splits : useful;
+        splits = splits < kWeightsMaxSplits ? splits : kWeightsMaxSplits;
+        out->splits = (int)(splits > 1 ? splits : 1);
+    }
+    if (out->splits > 1)
+        out->part_bytes = (size_t)out->splits * pairs * max_kv * sizeof(float);
+    return SPD_OK;
+}
+
 }  // namespace plan
 }  // namespace spd

@@ -12,7 +12,6 @@ using namespace spd::plan;
 
 inline bool misaligned(const void* p, size_t a) { return ((uintptr_t)p % a) != 0; }
 
-constexpr int64_t kMostInt = 0x7fffffff;
 constexpr int64_t kMostBlocks = 1ll << 22;  // workgroups of up to 1024 threads: a launch counts its threads in 32 bits
 
 int check_logprobs(int64_t rows, int64_t vocab, int32_t num_top)
@@ -20,21 +19,6 @@ int check_logprobs(int64_t rows, int64_t vocab, int32_t num_top)
     if (rows < 0 || vocab <= 0 || num_top < 0 || num_top > vocab)
         return SPD_EINVAL;
     if (num_top > SPD_MAX_TOP_TOKENS || vocab > (1ll << 30) || rows > kMostBlocks / ((vocab + 16383) / 16384) - 8)
-        return SPD_EUNSUPPORTED;
-    return SPD_OK;
-}
-
-int check_weights(const spd_prompt_desc* d, int64_t total, int64_t max_query, int64_t max_kv)
-{
-    const int rc = check_prompt_desc(d, true);
-    if (rc != SPD_OK)
-        return rc;
-    if (total < 0 || max_query < 0 || max_kv < 0)
-        return SPD_EINVAL;
-    if (total > kMostInt / d->num_q_heads || max_query > (1ll << 30) || max_kv > (1ll << 30) ||
-        max_query * (d->num_q_heads / d->num_kv_heads) > (1ll << 30))
-        return SPD_EUNSUPPORTED;
-    if ((int64_t)d->num_prompts * d->num_kv_heads > kMostBlocks / ((max_kv + 63) / 64 + 1))
         return SPD_EUNSUPPORTED;
     return SPD_OK;
 }
@@ -101,7 +85,10 @@ int token_logprobs(const void* logits, int32_t logits_dtype, int64_t rows, int64
 size_t accumulate_kv_weights_workspace_size(const spd_prompt_desc* desc, int64_t total_queries, int64_t max_query_len,
                                             int64_t max_kv_len)
 {
-    return check_weights(desc, total_queries, max_query_len, max_kv_len) == SPD_OK ? 256 : 0;
+    WeightsPlan pl;
+    if (make_weights_plan(desc, total_queries, max_query_len, max_kv_len, &pl) != SPD_OK)
+        return 0;
+    return pl.part_bytes + 256;
 }
 
 int accumulate_kv_weights(const spd_prompt_desc* desc, const void* q, const void* k, const int32_t* query_indptr,
@@ -110,7 +97,8 @@ int accumulate_kv_weights(const spd_prompt_desc* desc, const void* q, const void
                           const float* weights, float* weights_out, int64_t weights_stride, void* workspace,
                           size_t workspace_bytes, void* stream)
 {
-    const int rc = check_weights(desc, total_queries, max_query_len, max_kv_len);
+    WeightsPlan pl;
+    const int rc = make_weights_plan(desc, total_queries, max_query_len, max_kv_len, &pl);
     if (rc != SPD_OK)
         return rc;
     if (!q || !k || !query_indptr || !kv_lens || !kv_indptr || !lse || !weights_out || (desc->page_size != 0 && !kv_page_indices))
@@ -123,8 +111,8 @@ int accumulate_kv_weights(const spd_prompt_desc* desc, const void* q, const void
     for (const void* x : four)
         if (misaligned(x, 4))
             return SPD_EINVAL;
-    (void)workspace;
-    (void)workspace_bytes;
+    if (pl.splits > 1 && (!workspace || misaligned(workspace, 256) || workspace_bytes < pl.part_bytes))
+        return SPD_EWORKSPACE;
     if (max_kv_len == 0)
         return SPD_OK;
     spd::KvWeightsParams p;
@@ -153,8 +141,8 @@ int accumulate_kv_weights(const spd_prompt_desc* desc, const void* q, const void
     p.weights = decay != 0.f ? weights : nullptr;
     p.weights_out = weights_out;
     p.stride = weights_stride;
-    p.splits = 1;
-    p.part = nullptr;
+    p.splits = pl.splits;
+    p.part = (float*)workspace;
     return spd::launch_kv_weights(p, (hipStream_t)stream) == hipSuccess ? SPD_OK : SPD_ELAUNCH;
 }
 
