@@ -244,8 +244,8 @@ template <int V> __device__ __forceinline__ float over_columns(float (&v)[V])
         for (int i = 0; i < V / 2; ++i) {
             if (i < kept) {
                 const bool up = (lane & o) != 0;
-                const float give = up ? v[i] : v[i + kept], keep = up ? v[i + kept] : v[i];
-                v[i] = keep + __shfl_xor(give, o);
+                const float lo = v[i] + 0.f, hi = v[i + kept] + 0.f;  // (values: a choice of places would be one of addresses)
+                v[i] = (up ? hi : lo) + __shfl_xor(up ? lo : hi, o);
             }
         }
     }
@@ -282,7 +282,10 @@ template <int D> struct Shape {
 
 constexpr int kManyTokens = 64;  // of a wavefront
 
-template <int D, bool PAGED>
+// A wavefront's tokens are two halves of 32.  While the products of one half's scores with a block of rows run, the other half's scores
+// (of the same block, or the one before) become weights, an element every few clocks of the matrix pipe; the rows' fragments
+// stay in registers for both halves, and the next block's take their place behind the last product that reads them.
+template <int D, bool FULL, bool EVEN>  // FULL: the heads have D channels, not fewer; EVEN: the group divides 32
 __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void kv_weights_many(KvWeightsParams p, int tiles, int paired)
 {
     using S = Shape<D>;
@@ -291,178 +294,179 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void kv_weights_many
     if (!u.any)
         return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, h = lane >> 5;
-    const int tw = u.t0 + wave * kManyTokens, head_pieces = p.D / 8;
-    const int G = p.G;
-
-    // ---- rows: copied by all, two blocks ahead into registers, one ahead into LDS; (query, head) of a copy walk back 32 rows a time
-    int ci[S::kCopies], cg[S::kCopies];
-    const int back_i = 32 / G, back_g = 32 % G;
-    const int row_pieces = S::kPieces;
-#pragma unroll
-    for (int c = 0; c < S::kCopies; ++c) {
-        const int r = (u.last - 1) * 32 + (c * kWaves * 64 + tid) / row_pieces;
-        ci[c] = r / G;
-        cg[c] = r % G;
-    }
-    const int piece = tid % row_pieces;
-    const uint4* const q_base = (const uint4*)p.q + (long long)u.q0 * (p.q_stride / 8) + (long long)u.j * G * head_pieces + piece;
-    const bool has_piece = piece < head_pieces;
-    int to_copy = u.last - 1;
-    uint4 staged[2][S::kCopies];
-    const auto fetch = [&](uint4 (&v)[S::kCopies]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int c = 0; c < S::kCopies; ++c) {
-            v[c] = make_uint4(0u, 0u, 0u, 0u);
-            if (to_copy >= u.first && has_piece)
-                v[c] = q_base[(long long)min(ci[c], u.n - 1) * (p.q_stride / 8) + (long long)cg[c] * head_pieces];
-            ci[c] -= back_i;
-            cg[c] -= back_g;
-            if (cg[c] < 0) {
-                cg[c] += G;
-                ci[c] -= 1;
-            }
-        }
-        --to_copy;
-    };
-    const auto put = [&](int slot, const uint4 (&v)[S::kCopies]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int c = 0; c < S::kCopies; ++c) {
-            const int row = (c * kWaves * 64 + tid) / row_pieces;
-            *(uint4*)(lds + slot * S::kBlock + row * S::kRow + ((piece ^ S::swz(row)) << 4)) = v[c];
-        }
-    };
-    // the lane's own row: its log-sum-exp, and the last token that it sees
-    int li = ((u.last - 1) * 32 + col) / G, lg = ((u.last - 1) * 32 + col) % G;
-    const float* const lse_base = p.lse + (long long)u.q0 * p.Hq + (long long)u.j * G;
-    const auto next_lse = [&](bool more, float& lse, int& query) __attribute__((always_inline)) {
-        lse = 0.f;
-        query = li;
-        if (more && li < u.n)
-            lse = lse_base[(long long)li * p.Hq + lg];
-        li -= back_i;
-        lg -= back_g;
-        if (lg < 0) {
-            lg += G;
-            li -= 1;
-        }
-    };
-
-    const int blocks = u.last - u.first;
+    const int tw = u.t0 + wave * kManyTokens, head_pieces = FULL ? S::kPieces : p.D / 8, G = p.G;
     float sums[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i)
         sums[i] = 0.f;
-    if (blocks > 0) {
-        fetch(staged[0]);
-        fetch(staged[1]);
+    if (u.first < u.last) {
+        // ---- rows, the last block first: from memory into registers two blocks ahead, into LDS one ahead.  A thread copies the same
+        // 16-byte piece of the same rows of every block; from block to block its row goes back by 32 (query, head) places.
+        const int back_i = 32 / G, back_g = 32 % G;
+        const long long q_pieces = p.q_stride / 8;
+        const int piece = tid % S::kPieces;
+        const bool has_piece = FULL || piece < head_pieces;
+        const uint4* const q_base = (const uint4*)p.q + (long long)u.q0 * q_pieces + (long long)u.j * G * head_pieces + (has_piece ? piece : 0);
+        const long long back = back_i * q_pieces + back_g * head_pieces, wrap = q_pieces - (long long)G * head_pieces;
+        const uint4* at_row[S::kCopies];
+        int at_g[S::kCopies];
+        uint4 staged[S::kCopies];
+        int fetched = u.last - 1;  // the block that at_row stands at
+#pragma unroll
+        for (int c = 0; c < S::kCopies; ++c) {
+            const int r = fetched * 32 + (c * kWaves * 64 + tid) / S::kPieces, i = r / G, g = r % G;
+            at_g[c] = g;
+            at_row[c] = q_base + i * q_pieces + (long long)g * head_pieces;
+            // (rows behind the last one repeat its query; nothing is added for them)
+            staged[c] = i < u.n ? *at_row[c] : q_base[(u.n - 1) * q_pieces + (long long)g * head_pieces];
+        }
+        const auto put = [&](int slot) __attribute__((always_inline)) {
+#pragma unroll
+            for (int c = 0; c < S::kCopies; ++c) {
+                const int row = (c * kWaves * 64 + tid) / S::kPieces;
+                const uint4 v = staged[c];
+                *(uint4*)(lds + slot * S::kBlock + row * S::kRow + ((piece ^ S::swz(row)) << 4)) =
+                    FULL ? v : make_uint4(has_piece ? v.x : 0u, has_piece ? v.y : 0u, has_piece ? v.z : 0u, has_piece ? v.w : 0u);
+            }
+        };
+        const float* lse_at;
+        int lse_g;
+        {
+            const int r = fetched * 32 + col, i = r / G;
+            lse_g = r % G;
+            lse_at = p.lse + ((long long)u.q0 + i) * p.Hq + u.j * G + lse_g;
+        }
+        const auto go_back = [&]() __attribute__((always_inline)) {  // (stands still at the first block)
+            const bool more = fetched > u.first;
+            fetched -= more ? 1 : 0;
+            const long long by = more ? back : 0;
+            const int by_g = more ? back_g : 0;
+#pragma unroll
+            for (int c = 0; c < S::kCopies; ++c) {
+                at_row[c] -= by;
+                if (!EVEN) {
+                    at_g[c] -= by_g;
+                    const bool under = at_g[c] < 0;
+                    at_g[c] += under ? G : 0;
+                    at_row[c] -= under ? wrap : 0;
+                }
+            }
+            lse_at -= more ? (long long)back_i * p.Hq + back_g : 0;
+            if (!EVEN) {
+                lse_g -= by_g;
+                const bool under = lse_g < 0;
+                lse_g += under ? G : 0;
+                lse_at -= under ? p.Hq - G : 0;
+            }
+        };
+        const auto fetch = [&]() __attribute__((always_inline)) {
+#pragma unroll
+            for (int c = 0; c < S::kCopies; ++c)
+                staged[c] = *at_row[c];
+        };
+        float lse_next = fetched * 32 + col < u.rows ? *lse_at : 0.f;  // of block `at` below
+        put(0);
+        go_back();
+        fetch();
         // ---- keys: A operand, row = token, channels 16 s + 8 h (tokens past the end repeat the last one)
         uint4 k[2][S::kSteps];
-        {
-            const Keys<PAGED> keys(p, u.b, u.j, head_pieces);
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const uint4* const row = keys.row(min(tw + 32 * x + col, u.L - 1));
-#pragma unroll
-                for (int s = 0; s < S::kSteps; ++s) {
-                    k[x][s] = make_uint4(0u, 0u, 0u, 0u);
-                    if (2 * s + h < head_pieces)
-                        k[x][s] = row[2 * s + h];
-                }
-            }
-        }
-        float lse_a, lse_b;
-        int query_a, query_b;
-        next_lse(true, lse_a, query_a);
-        put(0, staged[0]);
-        fetch(staged[0]);
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        floatx16 sc[2][2];  // [block parity][half of the tokens]
-        float below = -INFINITY;
-        int limit = 0;
-        // Block i: its products into `now`, and between them the exponentials of the block before, `was` (MASK: of rows that do not see all tokens).
-        const auto block = [&](auto soft_tag, auto mask_tag, int i, floatx16 (&now)[2], const floatx16 (&was)[2], uint4 (&stage)[S::kCopies])
-            __attribute__((always_inline)) {
-            constexpr bool SOFT = decltype(soft_tag)::value, MASK = decltype(mask_tag)::value;
-            const int slot = i & 1;
-            next_lse(i + 1 < blocks, lse_b, query_b);
-            // what was fetched a block ago goes to the other slot, and its registers take the block after
-            const char* const from = lds + slot * S::kBlock + col * S::kRow;
-            uint4 f[2];
-            f[0] = *(const uint4*)(from + ((h ^ S::swz(col)) << 4));
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                now[0][e] = now[1][e] = 0.f;
-            constexpr int kPer = 32 / S::kSteps;
+        for (int x = 0; x < 2; ++x) {
+            const int t = min(tw + 32 * x + col, u.L - 1);
+            const uint4* const row = p.page_size ? Keys<true>(p, u.b, u.j, head_pieces).row(t) : Keys<false>(p, u.b, u.j, head_pieces).row(t);
 #pragma unroll
             for (int s = 0; s < S::kSteps; ++s) {
-                if (s + 1 < S::kSteps)
-                    f[(s + 1) & 1] = *(const uint4*)(from + (((2 * (s + 1) + h) ^ S::swz(col)) << 4));
-                now[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[0][s]), as_bf16x8(f[s & 1]), now[0], 0, 0, 0);
-                now[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[1][s]), as_bf16x8(f[s & 1]), now[1], 0, 0, 0);
-                if (SOFT) {
+                k[x][s] = make_uint4(0u, 0u, 0u, 0u);
+                if (FULL || 2 * s + h < head_pieces)
+                    k[x][s] = row[2 * s + h];
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        uint4 f[S::kSteps];
+        const unsigned lds_row = (unsigned)(col * S::kRow + ((h ^ S::swz(col)) << 4));  // piece 2 s + h: the bits of 2 s turned in it
 #pragma unroll
-                    for (int x = 0; x < kPer; ++x) {
-                        const int v = s * kPer + x, e = v & 15;
-                        float w = __builtin_amdgcn_exp2f(__builtin_fmaf(was[v >> 4][e], p.scale_log2, below));
-                        if (MASK)
-                            w = tw + 32 * (v >> 4) + (e & 3) + 8 * (e >> 2) + 4 * h <= limit ? w : 0.f;
-                        sums[v] += w;
-                    }
-                }
+        for (int s = 0; s < S::kSteps; ++s)
+            f[s] = *(const uint4*)(lds + (lds_row ^ (32u * s)));
+        floatx16 sc[2];
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            sc[1][e] = 0.f;
+        float below_was = -INFINITY, below = -INFINITY;
+        int limit_was = 0, limit = 0;
+        const int hide = u.L - u.n;
+        // scores of half x become weights, element by element: exponent of e, exponential of e - 1, sum of e - 2
+        float ex[16];
+        const auto soft = [&](auto mask_tag, int x, int e, float b, int lim) __attribute__((always_inline)) {
+            constexpr bool MASK = decltype(mask_tag)::value;
+            if (e < 16)
+                ex[e] = __builtin_fmaf(sc[x][e], p.scale_log2, b);
+            if (e >= 1 && e < 17)
+                ex[e - 1] = __builtin_amdgcn_exp2f(ex[e - 1]);
+            if (e >= 2 && e < 18) {
+                const int d = e - 2;
+                float w = ex[d];
+                if (MASK)
+                    w = tw + 32 * x + (d & 3) + 8 * (d >> 2) + 4 * h <= lim ? w : 0.f;
+                sums[16 * x + d] += w;
+            }
+        };
+        const auto phase = [&](auto x_tag, auto mask_tag, int slot, float b, int lim) __attribute__((always_inline)) {
+            constexpr int X = decltype(x_tag)::value;
+            constexpr int kPer = (18 + S::kSteps - 1) / S::kSteps;
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                sc[X][e] = 0.f;
+#pragma unroll
+            for (int s = 0; s < S::kSteps; ++s) {
+                sc[X] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[X][s]), as_bf16x8(f[s]), sc[X], 0, 0, 0);
+                if (X == 1)
+                    f[s] = *(const uint4*)(lds + ((lds_row + slot * S::kBlock) ^ (32u * s)));
+#pragma unroll
+                for (int e = 0; e < kPer; ++e)
+                    soft(mask_tag, 1 - X, s * kPer + e, b, lim);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (i + 1 < blocks) {
-                put(slot ^ 1, stage);
-                fetch(stage);
-            }
+        };
+        const std::integral_constant<int, 0> lower{};
+        const std::integral_constant<int, 1> upper{};
+        const auto block = [&](auto mask_tag, int slot) __attribute__((always_inline)) {
+            const float lse = lse_next;
+            // the next block's rows go to LDS, and the loads of the one after start
+            put(slot);
+            lse_next = *lse_at;
+            go_back();
+            fetch();
+            __builtin_amdgcn_sched_barrier(0);
+            phase(lower, mask_tag, slot, below_was, limit_was);
+            below = exponent_of(lse, true);
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            phase(upper, mask_tag, slot, below, limit);
+            below_was = below;
         };
-        const auto soft = [&](const floatx16 (&was)[2]) __attribute__((always_inline)) {
-#pragma unroll
-            for (int v = 0; v < 32; ++v) {
-                const int e = v & 15;
-                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(was[v >> 4][e], p.scale_log2, below));
-                sums[v] += tw + 32 * (v >> 4) + (e & 3) + 8 * (e >> 2) + 4 * h <= limit ? w : 0.f;
-            }
-        };
-        // rows of the block before: whether all of them see all of this wavefront's tokens
-        const int hide = u.L - u.n;
-        const auto take = [&](int i) __attribute__((always_inline)) {
-            const bool there = (u.last - 1 - i) * 32 + col < u.rows;
-            below = exponent_of(lse_a, there);
-            limit = !there ? -1 : p.causal ? hide + query_a : u.L;
-        };
-        const auto whole = [&](int i) __attribute__((always_inline)) {
-            const int r = (u.last - 1 - i) * 32;
-            return r + 32 <= u.rows && (!p.causal || hide + r / G >= tw + kManyTokens - 1);
-        };
-        std::true_type yes;
-        std::false_type no;
-        block(no, no, 0, sc[0], sc[1], staged[1]);
-        take(0);
-        lse_a = lse_b;
-        query_a = query_b;
-        int i = 1;
-        const auto step = [&](int at, floatx16 (&now)[2], const floatx16 (&was)[2], uint4 (&stage)[S::kCopies]) __attribute__((always_inline)) {
-            if (whole(at - 1))
-                block(yes, no, at, now, was, stage);
-            else
-                block(yes, yes, at, now, was, stage);
-            take(at);
-            lse_a = lse_b;
-            query_a = query_b;
-        };
+        // blocks of which every row sees all of this wavefront's tokens
+        const int whole_first = p.causal ? (max(tw + kManyTokens - 1 - hide, 0) * G + 31) / 32 : 0, whole_last = u.rows / 32;
+        int slot = 1, at = u.last - 1;
 #pragma unroll 1
-        for (; i + 1 < blocks; i += 2) {
-            step(i, sc[1], sc[0], staged[0]);
-            step(i + 1, sc[0], sc[1], staged[1]);
+        while (at >= u.first) {  // (a loop of its own for either kind)
+#pragma unroll 1
+            for (; at >= u.first && (at < whole_first || at + 1 >= whole_last); --at) {
+                const int r = at * 32 + col;
+                limit = r >= u.rows ? -1 : p.causal ? hide + r / G : u.L;
+                limit_was = r + 32 >= u.rows ? -1 : p.causal ? hide + (r + 32) / G : u.L;
+                block(std::true_type{}, slot);
+                slot ^= 1;
+            }
+#pragma unroll 1
+            for (; at >= u.first && at >= whole_first && at + 1 < whole_last; --at) {
+                block(std::false_type{}, slot);
+                slot ^= 1;
+            }
         }
-        if (i < blocks) {
-            step(i, sc[1], sc[0], staged[0]);
-            soft(sc[1]);
-        } else {
-            soft(sc[0]);
-        }
+        const int r = u.first * 32 + col;
+        limit = r >= u.rows ? -1 : p.causal ? hide + r / G : u.L;
+#pragma unroll
+        for (int e = 0; e < 18; ++e)
+            soft(std::true_type{}, 1, e, below, limit);
     }
     store<32>(p, u, tw, sums);
 }
@@ -579,13 +583,23 @@ hipError_t launch_kv_weights(const KvWeightsParams& p, hipStream_t s)
         hipLaunchKernelGGL((K<W, true>), grid, block, 0, s, p, tiles, paired); \
     else \
         hipLaunchKernelGGL((K<W, false>), grid, block, 0, s, p, tiles, paired)
+    const bool even = 32 % p.G == 0;
+#define SPD_MANY_BF16(W) \
+    if (p.D == W && even) \
+        hipLaunchKernelGGL((kv_weights_many<W, true, true>), grid, block, 0, s, p, tiles, paired); \
+    else if (p.D == W) \
+        hipLaunchKernelGGL((kv_weights_many<W, true, false>), grid, block, 0, s, p, tiles, paired); \
+    else if (even) \
+        hipLaunchKernelGGL((kv_weights_many<W, false, true>), grid, block, 0, s, p, tiles, paired); \
+    else \
+        hipLaunchKernelGGL((kv_weights_many<W, false, false>), grid, block, 0, s, p, tiles, paired)
     if (bf16) {
         if (p.D <= 64) {
-            SPD_MANY(kv_weights_many, 64);
+            SPD_MANY_BF16(64);
         } else if (p.D <= 128) {
-            SPD_MANY(kv_weights_many, 128);
+            SPD_MANY_BF16(128);
         } else {
-            SPD_MANY(kv_weights_many, 256);
+            SPD_MANY_BF16(256);
         }
     } else {
         if (p.D <= 64) {
@@ -597,6 +611,7 @@ hipError_t launch_kv_weights(const KvWeightsParams& p, hipStream_t s)
         }
     }
 #undef SPD_MANY
+#undef SPD_MANY_BF16
     hipError_t rc = hipGetLastError();
     if (rc == hipSuccess && p.splits > 1) {
         hipLaunchKernelGGL(kv_weights_join, dim3((p.max_kv + 255) / 256, p.B * p.Hkv), dim3(256), 0, s, p);
