@@ -198,14 +198,11 @@ struct Unit {
     int b, j, t0, L, q0, n, rows, first, last, split;
 };
 
-__device__ __forceinline__ Unit find_unit(const KvWeightsParams& p, int tokens, int tiles, int paired)
+__device__ __forceinline__ Unit find_unit(const KvWeightsParams& p, int tokens)
 {
     Unit u;
     const int j = blockIdx.x % p.Hkv;
-    int rest = blockIdx.x / p.Hkv;
-    const int units = tiles * p.B * p.splits;
-    if (paired && rest >= units / 2)  // all run at once, two a CU: a long one and a short one
-        rest = units - 1 - (rest - units / 2);
+    const int rest = blockIdx.x / p.Hkv;
     // causal tiles see the fewer rows the later they are: first tiles first
     const int tile = rest / (p.B * p.splits), rem = rest % (p.B * p.splits);
     u.j = j;
@@ -286,11 +283,11 @@ constexpr int kManyTokens = 64;  // of a wavefront
 // (of the same block, or the one before) become weights, an element every few clocks of the matrix pipe; the rows' fragments
 // stay in registers for both halves, and the next block's take their place behind the last product that reads them.
 template <int D, bool FULL, bool EVEN>  // FULL: the heads have D channels, not fewer; EVEN: the group divides 32
-__global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void kv_weights_many(KvWeightsParams p, int tiles, int paired)
+__global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void kv_weights_many(KvWeightsParams p)
 {
     using S = Shape<D>;
     __shared__ __align__(16) char lds[2 * S::kBlock];
-    const Unit u = find_unit(p, kWaves * kManyTokens, tiles, paired);
+    const Unit u = find_unit(p, kWaves * kManyTokens);
     if (!u.any)
         return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, h = lane >> 5;
@@ -365,9 +362,6 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void kv_weights_many
                 staged[c] = *at_row[c];
         };
         float lse_next = fetched * 32 + col < u.rows ? *lse_at : 0.f;  // of block `at` below
-        put(0);
-        go_back();
-        fetch();
         // ---- keys: A operand, row = token, channels 16 s + 8 h (tokens past the end repeat the last one)
         uint4 k[2][S::kSteps];
 #pragma unroll
@@ -381,6 +375,9 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void kv_weights_many
                     k[x][s] = row[2 * s + h];
             }
         }
+        put(0);
+        go_back();
+        fetch();
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         uint4 f[S::kSteps];
         const unsigned lds_row = (unsigned)(col * S::kRow + ((h ^ S::swz(col)) << 4));  // piece 2 s + h: the bits of 2 s turned in it
@@ -410,9 +407,8 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void kv_weights_many
                 sums[16 * x + d] += w;
             }
         };
-        const auto phase = [&](auto x_tag, auto mask_tag, int slot, float b, int lim) __attribute__((always_inline)) {
+        const auto phase = [&](auto x_tag, auto mask_tag, int slot, float b, int lim, auto beside) __attribute__((always_inline)) {
             constexpr int X = decltype(x_tag)::value;
-            constexpr int kPer = (18 + S::kSteps - 1) / S::kSteps;
 #pragma unroll
             for (int e = 0; e < 16; ++e)
                 sc[X][e] = 0.f;
@@ -421,26 +417,29 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void kv_weights_many
                 sc[X] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[X][s]), as_bf16x8(f[s]), sc[X], 0, 0, 0);
                 if (X == 1)
                     f[s] = *(const uint4*)(lds + ((lds_row + slot * S::kBlock) ^ (32u * s)));
+                // (beside the first product the other half's last one still runs)
+                if (s == 0)
+                    beside();
+                else
 #pragma unroll
-                for (int e = 0; e < kPer; ++e)
-                    soft(mask_tag, 1 - X, s * kPer + e, b, lim);
+                    for (int e = (s - 1) * 18 / (S::kSteps - 1); e < s * 18 / (S::kSteps - 1); ++e)
+                        soft(mask_tag, 1 - X, e, b, lim);
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
         const std::integral_constant<int, 0> lower{};
         const std::integral_constant<int, 1> upper{};
         const auto block = [&](auto mask_tag, int slot) __attribute__((always_inline)) {
-            const float lse = lse_next;
             // the next block's rows go to LDS, and the loads of the one after start
-            put(slot);
-            lse_next = *lse_at;
-            go_back();
-            fetch();
-            __builtin_amdgcn_sched_barrier(0);
-            phase(lower, mask_tag, slot, below_was, limit_was);
-            below = exponent_of(lse, true);
+            phase(lower, mask_tag, slot, below_was, limit_was, [&]() __attribute__((always_inline)) {
+                below = exponent_of(lse_next, true);
+                put(slot);
+                lse_next = *lse_at;
+                go_back();
+                fetch();
+            });
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            phase(upper, mask_tag, slot, below, limit);
+            phase(upper, mask_tag, slot, below, limit, []() {});
             below_was = below;
         };
         // blocks of which every row sees all of this wavefront's tokens
@@ -473,10 +472,10 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void kv_weights_many
 
 // fp32: 32 tokens a wavefront, rows straight from memory (a product of fp32 takes 16 times as long).  P: 16-byte pieces of a padded head.
 template <int P, bool PAGED>
-__global__ __launch_bounds__(kWaves * 64, P <= 32 ? 2 : 1) void kv_weights_many_f32(KvWeightsParams p, int tiles, int paired)
+__global__ __launch_bounds__(kWaves * 64, P <= 32 ? 2 : 1) void kv_weights_many_f32(KvWeightsParams p)
 {
     constexpr int kSteps = P / 2;
-    const Unit u = find_unit(p, kWaves * 32, tiles, paired);
+    const Unit u = find_unit(p, kWaves * 32);
     if (!u.any)
         return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, h = lane >> 5;
@@ -577,22 +576,21 @@ hipError_t launch_kv_weights(const KvWeightsParams& p, hipStream_t s)
     const int tokens = plan::weights_tile_tokens(bf16), tiles = (p.max_kv + tokens - 1) / tokens;
     const long long units = (long long)tiles * p.B * p.splits;
     const dim3 grid((unsigned)(units * p.Hkv)), block(kWaves * 64);
-    const int paired = p.causal && p.splits == 1 && units * p.Hkv > 256 && units * p.Hkv <= 512;
 #define SPD_MANY(K, W) \
     if (p.page_size) \
-        hipLaunchKernelGGL((K<W, true>), grid, block, 0, s, p, tiles, paired); \
+        hipLaunchKernelGGL((K<W, true>), grid, block, 0, s, p); \
     else \
-        hipLaunchKernelGGL((K<W, false>), grid, block, 0, s, p, tiles, paired)
+        hipLaunchKernelGGL((K<W, false>), grid, block, 0, s, p)
     const bool even = 32 % p.G == 0;
 #define SPD_MANY_BF16(W) \
     if (p.D == W && even) \
-        hipLaunchKernelGGL((kv_weights_many<W, true, true>), grid, block, 0, s, p, tiles, paired); \
+        hipLaunchKernelGGL((kv_weights_many<W, true, true>), grid, block, 0, s, p); \
     else if (p.D == W) \
-        hipLaunchKernelGGL((kv_weights_many<W, true, false>), grid, block, 0, s, p, tiles, paired); \
+        hipLaunchKernelGGL((kv_weights_many<W, true, false>), grid, block, 0, s, p); \
     else if (even) \
-        hipLaunchKernelGGL((kv_weights_many<W, false, true>), grid, block, 0, s, p, tiles, paired); \
+        hipLaunchKernelGGL((kv_weights_many<W, false, true>), grid, block, 0, s, p); \
     else \
-        hipLaunchKernelGGL((kv_weights_many<W, false, false>), grid, block, 0, s, p, tiles, paired)
+        hipLaunchKernelGGL((kv_weights_many<W, false, false>), grid, block, 0, s, p)
     if (bf16) {
         if (p.D <= 64) {
             SPD_MANY_BF16(64);

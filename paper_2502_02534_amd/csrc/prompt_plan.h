@@ -102,6 +102,8 @@ constexpr int kWeightsMaxSplits = 32;
 
 inline int weights_tile_tokens(bool bf16) { return bf16 ? 256 : 128; }  // of a workgroup with many rows
 
+inline int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
+
 struct WeightsPlan {
     int splits;         // parts of a sequence's rows
     size_t part_bytes;  // their sums
@@ -126,14 +128,13 @@ inline int make_weights_plan(const spd_prompt_desc* d, int64_t total, int64_t ma
     const int64_t rows = max_query * group, tokens = weights_tile_tokens(d->dtype == SPD_BF16);
     if (rows <= kWeightsFewRows)
         return SPD_OK;
-    // where the tiles leave CUs idle, the rows are cut into parts of four blocks at least, which another launch adds
+    // The rows are cut into parts, which another launch adds, where the tiles leave CUs idle (512 workgroups run at once; parts of
+    // 128 rows at least), and where parts of 1024 rows and more even out what causal tiles have to do.
     const int64_t units = pairs * ((max_kv + tokens - 1) / tokens);
-    if (units > 0 && units <= 128) {
-        int64_t splits = 512 / units;
-        const int64_t useful = (rows + 127) / 128;
-        splits = splits < useful ? splits : useful;
-        splits = splits < kWeightsMaxSplits ? splits : kWeightsMaxSplits;
-        out->splits = (int)(splits > 1 ? splits : 1);
+    if (units > 0) {
+        const int64_t fill = least(512 / units, rows / 128), even = least(4096 / units, rows / 1024);
+        out->splits = (int)least(fill > even ? fill : even, kWeightsMaxSplits);
+        out->splits = out->splits > 1 ? out->splits : 1;
     }
     if (out->splits > 1)
         out->part_bytes = (size_t)out->splits * pairs * max_kv * sizeof(float);
