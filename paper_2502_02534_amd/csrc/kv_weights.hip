@@ -265,16 +265,10 @@ template <int V> __device__ __forceinline__ void store(const KvWeightsParams& p,
     p.weights_out[at] = p.weights ? __builtin_fmaf(p.decay, p.weights[at], total) : total;
 }
 
-// bf16.  D: channels of a padded head.
+// bf16.  D: channels of a padded head.  A row in LDS is 16 bytes longer than its channels, so that sixteen rows' equal pieces take all 64 banks.
 template <int D> struct Shape {
-    static constexpr int kRow = 2 * D, kBlock = 32 * kRow, kPieces = D / 8, kSteps = D / 16, kCopies = kBlock / (kWaves * 64 * 16);
-    // Piece i of row r lies in slot i ^ swz(r), so that sixteen rows' equal pieces take all 64 banks.
-    static __device__ __forceinline__ int swz(int row)
-    {
-        if (D >= 128)
-            return ((row & 3) << 2) | ((row >> 2) & 3);
-        return (((row >> 1) & 1) << 2) | (((row >> 2) & 1) << 1) | ((row >> 3) & 1);
-    }
+    static constexpr int kRow = 2 * D + 16, kBlock = 32 * kRow, kPieces = D / 8, kSteps = D / 16;
+    static constexpr int kCopyRows = kWaves * 64 / kPieces, kCopies = 32 / kCopyRows;
 };
 
 constexpr int kManyTokens = 64;  // of a wavefront
@@ -298,70 +292,68 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void kv_weights_many
         sums[i] = 0.f;
     if (u.first < u.last) {
         // ---- rows, the last block first: from memory into registers two blocks ahead, into LDS one ahead.  A thread copies the same
-        // 16-byte piece of the same rows of every block; from block to block its row goes back by 32 (query, head) places.
-        const int back_i = 32 / G, back_g = 32 % G;
-        const long long q_pieces = p.q_stride / 8;
-        const int piece = tid % S::kPieces;
+        // 16-byte piece of the same rows of every block.  Rows behind the last one repeat its query; nothing is added for them.
+        const long long q_bytes = p.q_stride * 2;
+        const int piece = tid % S::kPieces, copy_row = tid / S::kPieces, head_bytes = head_pieces * 16;
         const bool has_piece = FULL || piece < head_pieces;
-        const uint4* const q_base = (const uint4*)p.q + (long long)u.q0 * q_pieces + (long long)u.j * G * head_pieces + (has_piece ? piece : 0);
-        const long long back = back_i * q_pieces + back_g * head_pieces, wrap = q_pieces - (long long)G * head_pieces;
-        const uint4* at_row[S::kCopies];
-        int at_g[S::kCopies];
+        const char* const q_seq = (const char*)p.q + (long long)u.q0 * q_bytes + (long long)u.j * G * head_bytes;
+        const float* const lse_seq = p.lse + (long long)u.q0 * p.Hq + (long long)u.j * G;
+        const int piece_at = has_piece ? piece * 16 : 0;
         uint4 staged[S::kCopies];
-        int fetched = u.last - 1;  // the block that at_row stands at
+        const auto copy_any = [&](int block, int c) __attribute__((always_inline)) {  // of any block
+            const int r = block * 32 + c * S::kCopyRows + copy_row;
+            return *(const uint4*)(q_seq + min(r / G, u.n - 1) * q_bytes + r % G * head_bytes + piece_at);
+        };
+        const auto lse_any = [&](int block) __attribute__((always_inline)) {
+            const int r = block * 32 + col;
+            return lse_seq[(long long)min(r / G, u.n - 1) * p.Hq + r % G];
+        };
+        // EVEN: a whole block's rows lie as block 0's do, 32 / G queries a block apart (a sequence of less than a block has no other)
+        unsigned copy_at[S::kCopies], lse_off = 0;
+        if (EVEN) {
 #pragma unroll
-        for (int c = 0; c < S::kCopies; ++c) {
-            const int r = fetched * 32 + (c * kWaves * 64 + tid) / S::kPieces, i = r / G, g = r % G;
-            at_g[c] = g;
-            at_row[c] = q_base + i * q_pieces + (long long)g * head_pieces;
-            // (rows behind the last one repeat its query; nothing is added for them)
-            staged[c] = i < u.n ? *at_row[c] : q_base[(u.n - 1) * q_pieces + (long long)g * head_pieces];
+            for (int c = 0; c < S::kCopies; ++c) {
+                const int r = c * S::kCopyRows + copy_row;
+                copy_at[c] = (unsigned)(min(r / G, u.n - 1) * q_bytes + r % G * head_bytes + piece_at);
+            }
+            lse_off = (unsigned)(min(col / G, u.n - 1) * p.Hq + col % G) * 4u;
         }
+        const int block_queries = 32 / G;
+        int fetched = u.last - 1;
+        float lse_next = lse_any(fetched);
+#pragma unroll
+        for (int c = 0; c < S::kCopies; ++c)
+            staged[c] = copy_any(fetched, c);
+        const auto fetch = [&]() __attribute__((always_inline)) {  // the block before (block 0's where there is none: not used)
+            fetched = fetched > u.first ? fetched - 1 : 0;
+            if (EVEN) {
+                const char* const from = q_seq + (long long)fetched * block_queries * q_bytes;
+#pragma unroll
+                for (int c = 0; c < S::kCopies; ++c)
+                    staged[c] = *(const uint4*)(from + copy_at[c]);
+            } else {
+#pragma unroll
+                for (int c = 0; c < S::kCopies; ++c)
+                    staged[c] = copy_any(fetched, c);
+            }
+        };
+        int lse_block = fetched;
+        const auto fetch_lse = [&]() __attribute__((always_inline)) {
+            lse_block = lse_block > u.first ? lse_block - 1 : 0;
+            if (EVEN)
+                lse_next = *(const float*)((const char*)(lse_seq + (long long)lse_block * block_queries * p.Hq) + lse_off);
+            else
+                lse_next = lse_any(lse_block);
+        };
+        char* const lds_put = lds + copy_row * S::kRow + piece * 16;
         const auto put = [&](int slot) __attribute__((always_inline)) {
 #pragma unroll
             for (int c = 0; c < S::kCopies; ++c) {
-                const int row = (c * kWaves * 64 + tid) / S::kPieces;
                 const uint4 v = staged[c];
-                *(uint4*)(lds + slot * S::kBlock + row * S::kRow + ((piece ^ S::swz(row)) << 4)) =
+                *(uint4*)(lds_put + slot * S::kBlock + c * S::kCopyRows * S::kRow) =
                     FULL ? v : make_uint4(has_piece ? v.x : 0u, has_piece ? v.y : 0u, has_piece ? v.z : 0u, has_piece ? v.w : 0u);
             }
         };
-        const float* lse_at;
-        int lse_g;
-        {
-            const int r = fetched * 32 + col, i = r / G;
-            lse_g = r % G;
-            lse_at = p.lse + ((long long)u.q0 + i) * p.Hq + u.j * G + lse_g;
-        }
-        const auto go_back = [&]() __attribute__((always_inline)) {  // (stands still at the first block)
-            const bool more = fetched > u.first;
-            fetched -= more ? 1 : 0;
-            const long long by = more ? back : 0;
-            const int by_g = more ? back_g : 0;
-#pragma unroll
-            for (int c = 0; c < S::kCopies; ++c) {
-                at_row[c] -= by;
-                if (!EVEN) {
-                    at_g[c] -= by_g;
-                    const bool under = at_g[c] < 0;
-                    at_g[c] += under ? G : 0;
-                    at_row[c] -= under ? wrap : 0;
-                }
-            }
-            lse_at -= more ? (long long)back_i * p.Hq + back_g : 0;
-            if (!EVEN) {
-                lse_g -= by_g;
-                const bool under = lse_g < 0;
-                lse_g += under ? G : 0;
-                lse_at -= under ? p.Hq - G : 0;
-            }
-        };
-        const auto fetch = [&]() __attribute__((always_inline)) {
-#pragma unroll
-            for (int c = 0; c < S::kCopies; ++c)
-                staged[c] = *at_row[c];
-        };
-        float lse_next = fetched * 32 + col < u.rows ? *lse_at : 0.f;  // of block `at` below
         // ---- keys: A operand, row = token, channels 16 s + 8 h (tokens past the end repeat the last one)
         uint4 k[2][S::kSteps];
 #pragma unroll
@@ -376,14 +368,13 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void kv_weights_many
             }
         }
         put(0);
-        go_back();
         fetch();
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         uint4 f[S::kSteps];
-        const unsigned lds_row = (unsigned)(col * S::kRow + ((h ^ S::swz(col)) << 4));  // piece 2 s + h: the bits of 2 s turned in it
+        const char* const lds_row = lds + col * S::kRow + h * 16;
 #pragma unroll
         for (int s = 0; s < S::kSteps; ++s)
-            f[s] = *(const uint4*)(lds + (lds_row ^ (32u * s)));
+            f[s] = *(const uint4*)(lds_row + 32 * s);
         floatx16 sc[2];
 #pragma unroll
         for (int e = 0; e < 16; ++e)
@@ -416,11 +407,12 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void kv_weights_many
             for (int s = 0; s < S::kSteps; ++s) {
                 sc[X] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[X][s]), as_bf16x8(f[s]), sc[X], 0, 0, 0);
                 if (X == 1)
-                    f[s] = *(const uint4*)(lds + ((lds_row + slot * S::kBlock) ^ (32u * s)));
+                    f[s] = *(const uint4*)(lds_row + slot * S::kBlock + 32 * s);
                 // (beside the first product the other half's last one still runs)
-                if (s == 0)
+                if (s == 0) {
+                    __builtin_amdgcn_sched_barrier(0);
                     beside();
-                else
+                } else
 #pragma unroll
                     for (int e = (s - 1) * 18 / (S::kSteps - 1); e < s * 18 / (S::kSteps - 1); ++e)
                         soft(mask_tag, 1 - X, e, b, lim);
@@ -434,8 +426,7 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void kv_weights_many
             phase(lower, mask_tag, slot, below_was, limit_was, [&]() __attribute__((always_inline)) {
                 below = exponent_of(lse_next, true);
                 put(slot);
-                lse_next = *lse_at;
-                go_back();
+                fetch_lse();
                 fetch();
             });
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
