@@ -1,15 +1,43 @@
-// Log probabilities of given tokens, with rank, entropy and the most probable tokens: one workgroup a row.
+// Log probabilities of given tokens, with rank, entropy and the most probable tokens.
 //
-// With d_i = (x_i - max x) / T (no overflow, whatever the logits), Z = sum exp(d_i):
-//   log p_i = d_i - ln Z,  entropy = ln Z + sum exp(d_i) (-d_i) / Z  (both terms >= 0: nothing cancels)
+// With c = log2(e) / T, a reference r near the row's largest x c, and y_i = x_i c - r (one fma: a common shift of r by its own
+// rounding changes nothing), Z = sum 2^y_i, S = sum 2^y_i y_i:
+//   log p_i = ln2 (y_i - log2 Z),   entropy = ln2 (log2 Z - S / Z),   lse = ln2 (r + log2 Z)
+// Every thread has a reference of its own, raised only where a logit lies 2^24 above it; the threads' sums are brought to the
+// row's maximum at the end.  Where x c itself overflows (logits of the type's lowest value at a temperature below 1) the
+// row is summed again from y_i = (x_i - max) c.
+//
+// One pass over the row: a thread takes 8 logits at a time (a "chunk"), leaves the chunk's maximum in LDS, and adds its terms.
+// The most probable tokens then come from few chunks: of the threads' maxima the num_top-th largest is a value that at least
+// num_top logits reach; only chunks whose maximum is above it (and the first ones that equal it: ties go to the lower token) are read
+// again, and what they hold is ranked by counting.  Nothing is sorted, and no list depends on the order of arrival.
+//
+// A workgroup takes a slice of a row; with several slices a second launch joins them.
+#include "logprobs_plan.h"
 #include "spd_internal.h"
 
-#include <hip/hip_bfloat16.h>
+#include <type_traits>
 
 namespace spd {
 namespace {
 
-constexpr int kThreads = 256;
+using plan::kChunk;
+
+constexpr float kRaise = 24.f;      // how far above a thread's reference a logit may lie, in base 2
+constexpr float kFloor = -1000.f;   // y of a logit of -inf (2^-1000 = 0, and 0 * -1000 = 0)
+constexpr float kLowest = -3.402823466e38f;  // reference of a thread that has seen nothing above: finite, so that y is no inf - inf
+constexpr int kMostRead = 128;      // chunks that are read again
+
+// Larger logits first, then the lower token: whole numbers in that order, all different.  NaN counts as -inf.
+__device__ __forceinline__ unsigned value_key(float x)
+{
+    const unsigned u = __float_as_uint((x == x ? x : -INFINITY) + 0.f);  // (both zeros are one value)
+    return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+__device__ __forceinline__ float key_value(unsigned u)
+{
+    return __uint_as_float((u & 0x80000000u) ? (u & 0x7fffffffu) : ~u);
+}
 
 template <bool BF16> __device__ __forceinline__ float logit(const LogprobsParams& p, long long at)
 {
@@ -18,103 +46,506 @@ template <bool BF16> __device__ __forceinline__ float logit(const LogprobsParams
     return ((const float*)p.logits)[at];
 }
 
-// Larger logits first, then the lower token: whole numbers in that order, all different.
-__device__ __forceinline__ unsigned long long key_of(float x, unsigned i)
+// A chunk's 8 logits: of a whole one in 16-byte loads, else one by one (-inf outside the slice).
+template <bool BF16> struct Chunk {
+    uint4 v[BF16 ? 1 : 2];
+    __device__ __forceinline__ void load(const char* at)
+    {
+        v[0] = *(const uint4*)at;
+        if (!BF16)
+            v[BF16 ? 0 : 1] = *(const uint4*)(at + 16);
+    }
+    __device__ __forceinline__ void get(float (&x)[kChunk]) const
+    {
+        const unsigned w[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+        if (BF16) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[2 * i] = __uint_as_float(w[i] << 16);
+                x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+            }
+        } else {
+            const uint4 b = v[BF16 ? 0 : 1];
+            const unsigned u[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[i] = __uint_as_float(w[i]);
+                x[4 + i] = __uint_as_float(u[i]);
+            }
+        }
+    }
+};
+
+// The k-th largest of a wavefront's keys, S a lane: `floor` is it (exact: false), or a number that exactly k of them reach (exact: true).
+template <int S> __device__ __forceinline__ unsigned kth_key(const unsigned (&key)[S], int k, bool& exact)
 {
-    const unsigned u = __float_as_uint(x == 0.f ? 0.f : x);
-    return (unsigned long long)((u & 0x80000000u) ? ~u : (u | 0x80000000u)) << 32 | (0xffffffffu - i);
+    unsigned floor = 0u;
+    exact = false;
+    for (int bit = 31; bit >= 0 && !exact; --bit) {
+        const unsigned cand = floor | (1u << bit);
+        int count = 0;
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+            count += __popcll(__ballot(key[s] >= cand));
+        if (count >= k) {
+            floor = cand;
+            exact = count == k;
+        }
+    }
+    return floor;
 }
 
-__device__ __forceinline__ float logit_of(unsigned long long key)
+// The same of n keys; of(i): key i (LDS).
+template <class F> __device__ __forceinline__ unsigned kth_key(F of, int n, int k, bool& exact)
 {
-    const unsigned u = (unsigned)(key >> 32);
-    return __uint_as_float((u & 0x80000000u) ? (u & 0x7fffffffu) : ~u);
+    const int lane = threadIdx.x & 63;
+    unsigned floor = 0u;
+    exact = false;
+    for (int bit = 31; bit >= 0 && !exact; --bit) {
+        const unsigned cand = floor | (1u << bit);
+        int count = 0;
+        for (int i = 0; i < n; i += 64)
+            count += __popcll(__ballot(i + lane < n && of(i + lane) >= cand));
+        if (count >= k) {
+            floor = cand;
+            exact = count == k;
+        }
+    }
+    return floor;
 }
 
-template <class T, class F> __device__ T over_block(T v, T* lds, F join)
+__device__ __forceinline__ int lanes_below(unsigned long long mask)
 {
+    return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0u));
+}
+
+// State of a slice: its largest logit, the reference and the sums.
+struct State {
+    float m, r, z, s;
+};
+
+// The sums on reference r, no more than kRaise above which any of their terms lies.
+__device__ __forceinline__ void onto(State& a, float r)
+{
+    const float d = fmaxf(a.r - r, kFloor), f = __builtin_amdgcn_exp2f(d);
+    a.s = f * __builtin_fmaf(a.z, d, a.s);
+    a.z *= f;
+    a.r = r;
+}
+
+__device__ __forceinline__ bool overflows(float m, float c) { return m > -INFINITY && m < INFINITY && !(fabsf(m * c) < INFINITY); }
+
+// What a row's sums say of a logit x.
+__device__ __forceinline__ float log_p(const State& a, float log2_z, float c, float x)
+{
+    if (!(a.m > -INFINITY) || !(x > -INFINITY))
+        return -INFINITY;
+    const float y = overflows(a.m, c) ? (x - a.m) * c : __builtin_fmaf(x, c, -a.r);
+    if (!(y > -INFINITY))  // (too far below for base 2)
+        return (x - a.m) * (c * kLn2);
+    return (y - log2_z) * kLn2;
+}
+
+__device__ __forceinline__ void write_row(const LogprobsParams& p, long long row, const State& a, float c, bool known, float given, int above)
+{
+    const bool empty = !(a.m > -INFINITY);
+    const float log2_z = __builtin_amdgcn_logf(a.z);
+    if (p.logprobs)
+        p.logprobs[row] = known ? log_p(a, log2_z, c, given) : -INFINITY;
+    if (p.ranks)
+        p.ranks[row] = known ? above + 1 : 0;
+    if (p.entropy)
+        p.entropy[row] = empty ? 0.f : kLn2 * (log2_z - a.s / a.z);
+    if (p.lse)
+        p.lse[row] = empty ? -INFINITY : overflows(a.m, c) ? a.m * (c * kLn2) + kLn2 * log2_z : kLn2 * (a.r + log2_z);
+}
+
+__device__ __forceinline__ void write_top(const LogprobsParams& p, long long row, int at, unsigned long long key, const State& a, float log2_z, float c)
+{
+    if (p.top_tokens)
+        p.top_tokens[row * p.top + at] = (int)(0xffffffffu - (unsigned)key);
+    if (p.top_logprobs)
+        p.top_logprobs[row * p.top + at] = log_p(a, log2_z, c, key_value((unsigned)(key >> 32)));
+}
+
+__device__ __forceinline__ float scale_of(const LogprobsParams& p, long long row)
+{
+    const float t = p.temperature ? p.temperature[row] : 1.f;
+    return t > 0.f ? kLog2e / t : kLog2e;
+}
+
+// THREADS, STRIPES: a workgroup takes up to STRIPES times THREADS chunks.  PARTS: slices of rows, joined by another launch.
+template <bool BF16, int THREADS, int STRIPES, bool PARTS>
+__global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobsParams p, int slice, int slices)
+{
+    constexpr int kWaves = THREADS / 64, kAhead = STRIPES < 4 ? STRIPES : 4;
+    constexpr int kHits = (SPD_MAX_TOP_TOKENS - 1) * STRIPES + kWaves * SPD_MAX_TOP_TOKENS;
+    static_assert(THREADS * STRIPES <= 65536, "chunk numbers of 16 bits");
+    using Max = typename std::conditional<BF16, unsigned short, unsigned>::type;  // a chunk's maximum, all of its bits
+    __shared__ union {
+        Max maxima[THREADS * STRIPES];
+        unsigned long long found[kMostRead * kChunk];  // once the maxima are done with
+    } big;
+    __shared__ union {
+        unsigned thread_keys[THREADS];
+        unsigned short hits[kHits];  // once the threads' keys are
+    } lists;
+    __shared__ unsigned short read_again[kMostRead];
+    __shared__ State states[kWaves];
+    __shared__ int counts[kWaves], num_hits, num_found, num_read;
+    __shared__ unsigned threshold;
+    __shared__ bool threshold_exact;
+    auto& maxima = big.maxima;
+    auto& found = big.found;
+    auto& hits = lists.hits;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const long long row = PARTS ? blockIdx.x / slices : blockIdx.x;
+    const int part = PARTS ? blockIdx.x % slices : 0;
+    const int first = part * slice, len = min((int)p.vocab - first, slice);
+    const long long base = row * p.stride + first;
+    constexpr int kElt = BF16 ? 2 : 4;
+    // chunks start on 16 bytes: `ahead` places of the first one lie in front of the slice
+    const int ahead = (int)(((size_t)p.logits / kElt + (size_t)base) % (16 / kElt)), places = ahead + len;
+    const int chunks = (places + kChunk - 1) / kChunk;
+    const char* const from = (const char*)p.logits + (base - ahead) * kElt;
+    const float c = scale_of(p, row);
+    const int token = p.tokens ? p.tokens[row] : -1;
+    const bool known = token >= 0 && token < (int)p.vocab;
+    const float given = known ? logit<BF16>(p, row * p.stride + token) : INFINITY;
+
+    const auto whole = [&](int chunk) { return chunk * kChunk >= ahead && (chunk + 1) * kChunk <= places; };
+    const auto one_by_one = [&](int chunk, float (&x)[kChunk]) {
+#pragma unroll
+        for (int e = 0; e < kChunk; ++e) {
+            const int at = chunk * kChunk + e;
+            x[e] = -INFINITY;
+            if (at >= ahead && at < places)
+                x[e] = logit<BF16>(p, base - ahead + at);
+        }
+    };
+
+    State a = {-INFINITY, kLowest, 0.f, 0.f};
+    int above = 0;
+    const auto take = [&](int chunk, const float (&x)[kChunk]) __attribute__((always_inline)) {
+        float m = fmaxf(x[0], x[1]);
+#pragma unroll
+        for (int e = 2; e < kChunk; e += 2)
+            m = fmaxf(m, fmaxf(x[e], x[e + 1]));
+        if (p.top)
+            maxima[chunk] = (Max)(__float_as_uint(m) >> (BF16 ? 16 : 0));
+        a.m = fmaxf(a.m, m);
+        if (__any(m > given)) {
+#pragma unroll
+            for (int e = 0; e < kChunk; ++e)
+                above += __popcll(__ballot(x[e] > given));
+        }
+        const float r = fmaxf(m * c, kLowest);
+        if (!(r <= a.r + kRaise))
+            onto(a, r);
+        float w[kChunk], s = 0.f;
+#pragma unroll
+        for (int e = 0; e < kChunk; ++e) {
+            const float y = fmaxf(__builtin_fmaf(x[e], c, -a.r), kFloor);
+            w[e] = __builtin_amdgcn_exp2f(y);
+            s = __builtin_fmaf(w[e], y, s);
+        }
+        a.z += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+        a.s += s;
+    };
+    const int stripes = (chunks + THREADS - 1) / THREADS;
+    for (int s0 = 0; s0 < stripes; s0 += kAhead) {
+        Chunk<BF16> v[kAhead];
+        const bool inside = s0 * THREADS * kChunk >= ahead && (s0 + kAhead) * THREADS * kChunk <= places;
+        if (inside) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                v[i].load(from + (long long)((s0 + i) * THREADS + tid) * (kChunk * kElt));
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                float x[kChunk];
+                v[i].get(x);
+                take((s0 + i) * THREADS + tid, x);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int chunk = (s0 + i) * THREADS + tid;
+                if (whole(chunk))
+                    v[i].load(from + (long long)chunk * (kChunk * kElt));
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int chunk = (s0 + i) * THREADS + tid;
+                float x[kChunk];
+                if (whole(chunk))
+                    v[i].get(x);
+                else
+                    one_by_one(chunk, x);
+                if ((s0 + i) * THREADS < chunks)
+                    take(chunk, x);
+            }
+        }
+    }
+
+    // ---- sums over the workgroup, on the reference of the slice's maximum
+    const bool has = tid < chunks;  // (a thread without a chunk of its own has no maximum)
+    if (p.top)
+        lists.thread_keys[tid] = has ? value_key(a.m) : 0u;
+    float m = a.m;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1)
-        v = join(v, (T)__shfl_xor(v, o));
+        m = fmaxf(m, __shfl_xor(m, o));
+    if (lane == 0) {
+        states[wave].m = m;
+        counts[wave] = above;
+    }
+    if (tid == 0)
+        num_hits = num_found = 0;
     __syncthreads();
-    if ((threadIdx.x & 63) == 0)
-        lds[threadIdx.x >> 6] = v;
+    above = 0;
+    for (int w = 0; w < kWaves; ++w) {
+        m = fmaxf(m, states[w].m);
+        above += counts[w];
+    }
+    if (overflows(m, c)) {
+        a.z = a.s = 0.f;
+        for (int chunk = tid; chunk < chunks; chunk += THREADS) {
+            float x[kChunk];
+            one_by_one(chunk, x);
+            for (int e = 0; e < kChunk; ++e) {
+                const float y = fmaxf((x[e] - m) * c, kFloor), w = __builtin_amdgcn_exp2f(y);
+                a.z += w;
+                a.s = __builtin_fmaf(w, y, a.s);
+            }
+        }
+        a.r = m * c;
+    } else {
+        onto(a, fmaxf(m * c, kLowest));
+    }
+    a.m = m;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        a.z += __shfl_xor(a.z, o);
+        a.s += __shfl_xor(a.s, o);
+    }
+    if (lane == 0) {
+        states[wave].z = a.z;
+        states[wave].s = a.s;
+    }
+    // ---- a value that at least `top` logits of the slice reach
+    if (p.top && wave == 0) {
+        unsigned key[kWaves];
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w)
+            key[w] = lists.thread_keys[w * 64 + lane];
+        bool exact;
+        const unsigned t = kth_key(key, p.top, exact);
+        if (lane == 0) {
+            threshold = t;
+            threshold_exact = exact;
+        }
+    }
     __syncthreads();
-    v = lds[0];
-    for (int w = 1; w < kThreads / 64; ++w)
-        v = join(v, lds[w]);
-    return v;
+    a.z = a.s = 0.f;
+    for (int w = 0; w < kWaves; ++w) {
+        a.z += states[w].z;
+        a.s += states[w].s;
+    }
+    LogprobsPart* const out_part = (LogprobsPart*)p.workspace + (PARTS ? blockIdx.x : 0);
+    if (tid == 0) {
+        if (PARTS)
+            *out_part = {a.m, a.r, a.z, a.s, above, 0};
+        else
+            write_row(p, row, a, c, known, given, above);
+    }
+    if (p.top == 0)
+        return;
+
+    // ---- chunks above the threshold, and (unless exactly `top` maxima reach it) the first ones of every wavefront that equal it
+    const auto key_of = [&](int chunk) { return value_key(__uint_as_float((unsigned)maxima[chunk] << (BF16 ? 16 : 0))); };
+    const unsigned t = threshold;
+    const bool exact = threshold_exact;
+    int ties = 0;
+    for (int s = 0; s < stripes; ++s) {
+        const int chunk = s * THREADS + tid;
+        const unsigned key = chunk < chunks ? key_of(chunk) : 0u;
+        const bool over = exact ? key >= t : key > t;
+        const unsigned long long tied = __ballot(!exact && key == t && key != 0u);
+        const bool tie = (tied >> lane & 1) && ties + lanes_below(tied) < p.top;
+        ties += __popcll(tied);
+        if (over || tie) {
+            const int at = atomicAdd(&num_hits, 1);
+            hits[at] = (unsigned short)chunk;
+        }
+    }
+    __syncthreads();
+    const int n = num_hits;
+    if (n <= kMostRead) {
+        if (tid < n)
+            read_again[tid] = hits[tid];
+        if (tid == 0)
+            num_read = n;
+    } else if (wave == 0) {
+        // the same again among these: chunks above the top-th largest maximum, and of those that equal it the `top` lowest
+        bool fits;
+        const auto hit_key = [&](int i) { return key_of(hits[i]); };
+        const unsigned t2 = kth_key(hit_key, n, p.top, fits);
+        unsigned lowest = 0u;  // ~chunk from which on one that equals it is read
+        if (!fits) {
+            int equal = 0;
+            for (int i = 0; i < n; i += 64)
+                equal += __popcll(__ballot(i + lane < n && hit_key(i + lane) == t2));
+            bool ignored;
+            if (equal > p.top)
+                lowest = kth_key([&](int i) { return hit_key(i) == t2 ? ~(unsigned)hits[i] : 0u; }, n, p.top, ignored);
+        }
+        int all = 0;
+        for (int i = 0; i < n; i += 64) {
+            const unsigned chunk = i + lane < n ? hits[i + lane] : 0u, key = key_of((int)chunk);
+            const bool keep = i + lane < n && (fits ? key >= t2 : key > t2 || (key == t2 && ~chunk >= lowest));
+            const unsigned long long kept = __ballot(keep);
+            if (keep)
+                read_again[all + lanes_below(kept)] = (unsigned short)chunk;
+            all += __popcll(kept);
+        }
+        if (lane == 0)
+            num_read = all;
+    }
+    __syncthreads();
+    // ---- their logits, those that may be among the `top` largest, ranked by counting
+    const int elements = num_read * kChunk;
+    for (int i = tid; i < elements; i += THREADS) {
+        const int at = (int)read_again[i / kChunk] * kChunk + i % kChunk;
+        if (at >= ahead && at < places) {
+            const float x = logit<BF16>(p, base - ahead + at);
+            const unsigned key = value_key(x);
+            if (key >= t)
+                found[atomicAdd(&num_found, 1)] = (unsigned long long)key << 32 | (0xffffffffu - (unsigned)(first + at - ahead));
+        }
+    }
+    __syncthreads();
+    const float log2_z = __builtin_amdgcn_logf(a.z);
+    const int all = num_found;
+    for (int i = tid; i < all; i += THREADS) {
+        const unsigned long long key = found[i];
+        int rank = 0;
+        for (int q = 0; q < all; ++q)
+            rank += found[q] > key;
+        if (rank < p.top) {
+            if (PARTS)
+                ((unsigned long long*)((LogprobsPart*)p.workspace + p.rows * slices))[(long long)blockIdx.x * p.top + rank] = key;
+            else
+                write_top(p, row, rank, key, a, log2_z, c);
+        }
+    }
+    if (PARTS && tid == 0)
+        out_part->top = min(all, p.top);
 }
 
-template <bool BF16> __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobsParams p)
+// Joins a row's slices: sums on the reference of the row's maximum; the slices' sorted lists by their heads.
+template <bool BF16> __global__ __launch_bounds__(64) void logprobs_join(LogprobsParams p, int slices)
 {
-    __shared__ double lds_d[4];
-    __shared__ unsigned long long lds_k[4];
-    const long long row = blockIdx.x, base = row * p.stride;
-    const int vocab = (int)p.vocab;
+    const long long row = blockIdx.x;
+    const int lane = threadIdx.x;
+    const LogprobsPart* const parts = (const LogprobsPart*)p.workspace + row * slices;
+    const unsigned long long* const keys = (const unsigned long long*)((const LogprobsPart*)p.workspace + p.rows * slices) + row * slices * p.top;
+    const float c = scale_of(p, row);
     const int token = p.tokens ? p.tokens[row] : -1;
-    const bool known = token >= 0 && token < vocab;
-    const float given = known ? logit<BF16>(p, base + token) : 0.f;
-    const float t = p.temperature ? p.temperature[row] : 1.f;
-    const float inv_t = t > 0.f ? 1.f / t : 1.f;
+    const bool known = token >= 0 && token < (int)p.vocab;
+    const float given = known ? logit<BF16>(p, row * p.stride + token) : INFINITY;
     float m = -INFINITY;
     int above = 0;
-    for (int i = threadIdx.x; i < vocab; i += kThreads) {
-        const float x = logit<BF16>(p, base + i);
-        m = fmaxf(m, x);
-        above += x > given;
+    for (int i = lane; i < slices; i += 64) {
+        m = fmaxf(m, parts[i].m);
+        above += parts[i].above;
     }
-    m = (float)over_block<double>(m, lds_d, [](double a, double b) { return a > b ? a : b; });
-    above = (int)over_block<double>(above, lds_d, [](double a, double b) { return a + b; });
-    double z = 0., s = 0.;
-    if (m > -INFINITY)
-        for (int i = threadIdx.x; i < vocab; i += kThreads) {
-            const float d = (logit<BF16>(p, base + i) - m) * inv_t, e = expf(d);
-            z += e;
-            s += e > 0.f ? e * -d : 0.f;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        m = fmaxf(m, __shfl_xor(m, o));
+        above += __shfl_xor(above, o);
+    }
+    State a = {m, overflows(m, c) ? m * c : fmaxf(m * c, kLowest), 0.f, 0.f};
+    for (int i = lane; i < slices; i += 64) {
+        State b = {parts[i].m, parts[i].r, parts[i].z, parts[i].s};
+        if (overflows(m, c)) {  // (a slice whose own maximum does not overflow lies that far below)
+            b.r = overflows(b.m, c) ? (b.m - m) * c : kFloor;
+            onto(b, 0.f);
+        } else {
+            onto(b, a.r);
         }
-    z = over_block<double>(z, lds_d, [](double a, double b) { return a + b; });
-    s = over_block<double>(s, lds_d, [](double a, double b) { return a + b; });
-    const bool empty = !(m > -INFINITY);
-    const float log_z = empty ? 0.f : (float)log(z);
-    const auto log_p = [&](float x) { return empty ? -INFINITY : (x - m) * inv_t - log_z; };
-    if (threadIdx.x == 0) {
-        if (p.logprobs)
-            p.logprobs[row] = known ? log_p(given) : -INFINITY;
-        if (p.ranks)
-            p.ranks[row] = known ? above + 1 : 0;
-        if (p.entropy)
-            p.entropy[row] = empty ? 0.f : (float)(log(z) + s / z);
-        if (p.lse)
-            p.lse[row] = empty ? -INFINITY : m * inv_t + log_z;
+        a.z += b.z;
+        a.s += b.s;
     }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        a.z += __shfl_xor(a.z, o);
+        a.s += __shfl_xor(a.s, o);
+    }
+    if (lane == 0)
+        write_row(p, row, a, c, known, given, above);
+    if (p.top == 0)
+        return;
+    const float log2_z = __builtin_amdgcn_logf(a.z);
     unsigned long long last = ~0ull;
     for (int k = 0; k < p.top; ++k) {
-        unsigned long long best = 0;
-        for (int i = threadIdx.x; i < vocab; i += kThreads) {
-            const unsigned long long key = key_of(logit<BF16>(p, base + i), i);
-            if (key < last && key > best)
-                best = key;
+        // the largest key below the last one: every list's first that is
+        unsigned long long best = 0ull;
+        for (int i = lane; i < slices; i += 64) {
+            const int n = parts[i].top;
+            for (int e = 0; e < n; ++e) {
+                const unsigned long long key = keys[(long long)i * p.top + e];
+                if (key < last) {
+                    best = key > best ? key : best;
+                    break;
+                }
+            }
         }
-        last = over_block<unsigned long long>(best, lds_k, [](unsigned long long a, unsigned long long b) { return a > b ? a : b; });
-        if (threadIdx.x == 0) {
-            if (p.top_tokens)
-                p.top_tokens[row * p.top + k] = (int)(0xffffffffu - (unsigned)last);
-            if (p.top_logprobs)
-                p.top_logprobs[row * p.top + k] = log_p(logit_of(last));
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            const unsigned long long other = __shfl_xor(best, o);
+            best = other > best ? other : best;
         }
+        last = best;
+        if (lane == 0)
+            write_top(p, row, k, best, a, log2_z, c);
     }
+}
+
+template <bool BF16, int THREADS, int STRIPES> void run(const LogprobsParams& p, int slice, int slices, hipStream_t s)
+{
+    if (slices > 1)
+        hipLaunchKernelGGL((logprobs_kernel<BF16, THREADS, STRIPES, true>), dim3((unsigned)(p.rows * slices)), dim3(THREADS), 0, s, p, slice, slices);
+    else
+        hipLaunchKernelGGL((logprobs_kernel<BF16, THREADS, STRIPES, false>), dim3((unsigned)p.rows), dim3(THREADS), 0, s, p, slice, slices);
+}
+
+template <bool BF16> hipError_t run_all(const LogprobsParams& p, hipStream_t s)
+{
+    const plan::LogprobsPlan pl = plan::make_logprobs_plan(p.rows, p.vocab);
+    // (a slice that starts within 16 bytes has a chunk more)
+    const int chunks = (pl.slice + 2 * kChunk - 2) / kChunk;
+    if (pl.threads == 256)
+        chunks <= 256 * 4 ? run<BF16, 256, 4>(p, pl.slice, pl.slices, s) : run<BF16, 256, 8>(p, pl.slice, pl.slices, s);
+    else if (chunks <= 512 * 8)
+        run<BF16, 512, 8>(p, pl.slice, pl.slices, s);
+    else if (chunks <= 512 * 16)
+        run<BF16, 512, 16>(p, pl.slice, pl.slices, s);
+    else
+        run<BF16, 512, 32>(p, pl.slice, pl.slices, s);
+    hipError_t rc = hipGetLastError();
+    if (rc == hipSuccess && pl.slices > 1) {
+        hipLaunchKernelGGL((logprobs_join<BF16>), dim3((unsigned)p.rows), dim3(64), 0, s, p, pl.slices);
+        rc = hipGetLastError();
+    }
+    return rc;
 }
 
 }  // namespace
 
 hipError_t launch_token_logprobs(const LogprobsParams& p, hipStream_t s)
 {
-    if (p.bf16)
-        hipLaunchKernelGGL((logprobs_kernel<true>), dim3((unsigned)p.rows), dim3(kThreads), 0, s, p);
-    else
-        hipLaunchKernelGGL((logprobs_kernel<false>), dim3((unsigned)p.rows), dim3(kThreads), 0, s, p);
-    return hipGetLastError();
+    return p.bf16 ? run_all<true>(p, s) : run_all<false>(p, s);
 }
 
 }  // namespace spd

@@ -1,0 +1,46 @@
+// Launch planning of token_logprobs: host arithmetic only (no HIP, no allocation), so that it can also be compiled and
+// exercised on a machine without a GPU.
+#pragma once
+
+#include "../../include/spdecode.h"
+
+#include <stddef.h>
+#include <stdint.h>
+
+namespace spd {
+
+// What a slice of a row leaves for the launch that joins them.
+struct LogprobsPart {
+    float m, r, z, s;
+    int above, top;
+};
+
+namespace plan {
+
+constexpr int kChunk = 8;  // logits whose maximum is kept
+
+struct LogprobsPlan {
+    int threads, slice, slices;  // of a workgroup, logits of a slice, slices of a row
+};
+
+constexpr int kMostSlice = 131072 - kChunk;  // (32 chunks for each of 512 threads, one of them for a start within 16 bytes)
+
+inline LogprobsPlan make_logprobs_plan(int64_t rows, int64_t vocab)
+{
+    LogprobsPlan pl;
+    (void)rows;
+    pl.slices = (int)((vocab + kMostSlice - 1) / kMostSlice);
+    pl.slice = (int)((vocab + pl.slices - 1) / pl.slices);
+    pl.slice = (pl.slice + kChunk - 1) / kChunk * kChunk;  // (the bound is a multiple of a chunk)
+    pl.threads = pl.slice <= 8192 ? 256 : 512;
+    return pl;
+}
+
+inline size_t logprobs_workspace(int64_t rows, int64_t vocab, int top)
+{
+    const LogprobsPlan pl = make_logprobs_plan(rows, vocab);
+    return pl.slices > 1 ? (size_t)rows * pl.slices * (sizeof(LogprobsPart) + (size_t)top * 8) : 0;
+}
+
+}  // namespace plan
+}  // namespace spd

@@ -1,6 +1,7 @@
 // C ABI of what a step's two softmaxes say: token log probabilities, attention weights of cached tokens, their
 // selection and compaction.  Argument checks and launches.
 #include "../../include/spdecode.h"
+#include "logprobs_plan.h"
 #include "prompt_plan.h"
 #include "spd_internal.h"
 
@@ -38,7 +39,7 @@ extern "C" {
 
 size_t token_logprobs_workspace_size(int64_t rows, int64_t vocab, int32_t num_top)
 {
-    return check_logprobs(rows, vocab, num_top) == SPD_OK ? 256 : 0;
+    return check_logprobs(rows, vocab, num_top) == SPD_OK ? logprobs_workspace(rows, vocab, num_top) + 256 : 0;
 }
 
 int token_logprobs(const void* logits, int32_t logits_dtype, int64_t rows, int64_t vocab, int64_t row_stride,
@@ -59,10 +60,12 @@ int token_logprobs(const void* logits, int32_t logits_dtype, int64_t rows, int64
     for (const void* x : four)
         if (misaligned(x, 4))
             return SPD_EINVAL;
-    (void)workspace;
-    (void)workspace_bytes;
     if (rows == 0)
         return SPD_OK;
+    const int32_t tops = top_tokens || top_logprobs ? num_top : 0;
+    const size_t need = logprobs_workspace(rows, vocab, tops);
+    if (need > 0 && (!workspace || misaligned(workspace, 256) || workspace_bytes < need))
+        return SPD_EWORKSPACE;
     spd::LogprobsParams p;
     p.logits = logits;
     p.bf16 = logits_dtype == SPD_BF16;
@@ -71,7 +74,7 @@ int token_logprobs(const void* logits, int32_t logits_dtype, int64_t rows, int64
     p.stride = row_stride;
     p.temperature = temperature;
     p.tokens = tokens;
-    p.top = top_tokens || top_logprobs ? num_top : 0;
+    p.top = tops;
     p.logprobs = logprobs;
     p.ranks = ranks;
     p.entropy = entropy;
