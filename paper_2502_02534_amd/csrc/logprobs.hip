@@ -27,6 +27,7 @@ constexpr float kRaise = 24.f;      // how far above a thread's reference a logi
 constexpr float kFloor = -1000.f;   // y of a logit of -inf (2^-1000 = 0, and 0 * -1000 = 0)
 constexpr float kLowest = -3.402823466e38f;  // reference of a thread that has seen nothing above: finite, so that y is no inf - inf
 constexpr int kMostRead = 128;      // chunks that are read again
+constexpr int kJoinThreads = 256, kJoinKeys = 1024;
 
 // Larger logits first, then the lower token: whole numbers in that order, all different.  NaN counts as -inf.
 __device__ __forceinline__ unsigned value_key(float x)
@@ -79,9 +80,22 @@ template <bool BF16> struct Chunk {
 // The k-th largest of a wavefront's keys, S a lane: `floor` is it (exact: false), or a number that exactly k of them reach (exact: true).
 template <int S> __device__ __forceinline__ unsigned kth_key(const unsigned (&key)[S], int k, bool& exact)
 {
-    unsigned floor = 0u;
+    // leading bits that all keys have
+    const unsigned one = __builtin_amdgcn_readfirstlane(key[0]);
+    unsigned differ = 0u;
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+        differ |= key[s] ^ one;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1)
+        differ |= __shfl_xor(differ, o);
+    differ = __builtin_amdgcn_readfirstlane(differ);
     exact = false;
-    for (int bit = 31; bit >= 0 && !exact; --bit) {
+    if (differ == 0u)
+        return one;
+    const int top_bit = 31 - __clz((int)differ);
+    unsigned floor = one & ~((2u << top_bit) - 1u);
+    for (int bit = top_bit; bit >= 0 && !exact; --bit) {
         const unsigned cand = floor | (1u << bit);
         int count = 0;
 #pragma unroll
@@ -179,7 +193,9 @@ template <bool BF16, int THREADS, int STRIPES, bool PARTS>
 __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobsParams p, int slice, int slices)
 {
     constexpr int kWaves = THREADS / 64, kAhead = STRIPES < 4 ? STRIPES : 4;
-    constexpr int kHits = (SPD_MAX_TOP_TOKENS - 1) * STRIPES + kWaves * SPD_MAX_TOP_TOKENS;
+    constexpr int kHot = SPD_MAX_TOP_TOKENS + 8;  // threads up to which all of their chunks are looked through
+    // (otherwise fewer than `top` threads lie above the threshold, and every wavefront adds up to `top` chunks that equal it)
+    constexpr int kHits = kHot * STRIPES + kWaves * SPD_MAX_TOP_TOKENS;
     static_assert(THREADS * STRIPES <= 65536, "chunk numbers of 16 bits");
     using Max = typename std::conditional<BF16, unsigned short, unsigned>::type;  // a chunk's maximum, all of its bits
     __shared__ union {
@@ -192,9 +208,9 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobsParams p, int
     } lists;
     __shared__ unsigned short read_again[kMostRead];
     __shared__ State states[kWaves];
-    __shared__ int counts[kWaves], num_hits, num_found, num_read;
+    __shared__ int counts[kWaves], num_hot, num_hits, num_found, num_read;
+    __shared__ unsigned short hot_threads[kHot];
     __shared__ unsigned threshold;
-    __shared__ bool threshold_exact;
     auto& maxima = big.maxima;
     auto& found = big.found;
     auto& hits = lists.hits;
@@ -289,9 +305,9 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobsParams p, int
     }
 
     // ---- sums over the workgroup, on the reference of the slice's maximum
-    const bool has = tid < chunks;  // (a thread without a chunk of its own has no maximum)
+    const unsigned own_key = tid < chunks ? value_key(a.m) : 0u;  // (a thread without a chunk of its own has no maximum)
     if (p.top)
-        lists.thread_keys[tid] = has ? value_key(a.m) : 0u;
+        lists.thread_keys[tid] = own_key;
     float m = a.m;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1)
@@ -301,7 +317,7 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobsParams p, int
         counts[wave] = above;
     }
     if (tid == 0)
-        num_hits = num_found = 0;
+        num_hot = num_hits = num_found = 0;
     __syncthreads();
     above = 0;
     for (int w = 0; w < kWaves; ++w) {
@@ -341,10 +357,8 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobsParams p, int
             key[w] = lists.thread_keys[w * 64 + lane];
         bool exact;
         const unsigned t = kth_key(key, p.top, exact);
-        if (lane == 0) {
+        if (lane == 0)
             threshold = t;
-            threshold_exact = exact;
-        }
     }
     __syncthreads();
     a.z = a.s = 0.f;
@@ -362,21 +376,33 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobsParams p, int
     if (p.top == 0)
         return;
 
-    // ---- chunks above the threshold, and (unless exactly `top` maxima reach it) the first ones of every wavefront that equal it
+    // ---- chunks that reach the threshold.  Where few threads do, all of theirs that do; else (many that equal it) those above it and the
+    // first ones of every wavefront that equal it.
     const auto key_of = [&](int chunk) { return value_key(__uint_as_float((unsigned)maxima[chunk] << (BF16 ? 16 : 0))); };
     const unsigned t = threshold;
-    const bool exact = threshold_exact;
-    int ties = 0;
-    for (int s = 0; s < stripes; ++s) {
-        const int chunk = s * THREADS + tid;
-        const unsigned key = chunk < chunks ? key_of(chunk) : 0u;
-        const bool over = exact ? key >= t : key > t;
-        const unsigned long long tied = __ballot(!exact && key == t && key != 0u);
-        const bool tie = (tied >> lane & 1) && ties + lanes_below(tied) < p.top;
-        ties += __popcll(tied);
-        if (over || tie) {
-            const int at = atomicAdd(&num_hits, 1);
-            hits[at] = (unsigned short)chunk;
+    if (own_key >= t && own_key != 0u) {
+        const int at = atomicAdd(&num_hot, 1);
+        if (at < kHot)
+            hot_threads[at] = (unsigned short)tid;
+    }
+    __syncthreads();
+    if (num_hot <= kHot) {
+        const int items = num_hot * stripes;
+        for (int i = tid; i < items; i += THREADS) {
+            const int chunk = i / num_hot * THREADS + hot_threads[i % num_hot];
+            if (chunk < chunks && key_of(chunk) >= t)
+                hits[atomicAdd(&num_hits, 1)] = (unsigned short)chunk;
+        }
+    } else {
+        int ties = 0;
+        for (int s = 0; s < stripes; ++s) {
+            const int chunk = s * THREADS + tid;
+            const unsigned key = chunk < chunks ? key_of(chunk) : 0u;
+            const unsigned long long tied = __ballot(key == t && key != 0u);
+            const bool tie = (tied >> lane & 1) && ties + lanes_below(tied) < p.top;
+            ties += __popcll(tied);
+            if (key > t || tie)
+                hits[atomicAdd(&num_hits, 1)] = (unsigned short)chunk;
         }
     }
     __syncthreads();
@@ -444,10 +470,11 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobsParams p, int
 }
 
 // Joins a row's slices: sums on the reference of the row's maximum; the slices' sorted lists by their heads.
-template <bool BF16> __global__ __launch_bounds__(64) void logprobs_join(LogprobsParams p, int slices)
+template <bool BF16> __global__ __launch_bounds__(kJoinThreads) void logprobs_join(LogprobsParams p, int slices)
 {
+    __shared__ unsigned long long listed[kJoinKeys];
     const long long row = blockIdx.x;
-    const int lane = threadIdx.x;
+    const int lane = threadIdx.x & 63;  // (the sums are every wavefront's)
     const LogprobsPart* const parts = (const LogprobsPart*)p.workspace + row * slices;
     const unsigned long long* const keys = (const unsigned long long*)((const LogprobsPart*)p.workspace + p.rows * slices) + row * slices * p.top;
     const float c = scale_of(p, row);
@@ -482,16 +509,31 @@ template <bool BF16> __global__ __launch_bounds__(64) void logprobs_join(Logprob
         a.z += __shfl_xor(a.z, o);
         a.s += __shfl_xor(a.s, o);
     }
-    if (lane == 0)
+    if (threadIdx.x == 0)
         write_row(p, row, a, c, known, given, above);
     if (p.top == 0)
         return;
     const float log2_z = __builtin_amdgcn_logf(a.z);
+    if (slices * p.top <= kJoinKeys) {
+        // ranked by counting
+        for (int i = threadIdx.x; i < slices * p.top; i += kJoinThreads)
+            listed[i] = i % p.top < parts[i / p.top].top ? keys[i] : 0ull;
+        __syncthreads();
+        for (int i = threadIdx.x; i < slices * p.top; i += kJoinThreads) {
+            const unsigned long long key = listed[i];
+            int rank = 0;
+            for (int q = 0; q < slices * p.top; ++q)
+                rank += listed[q] > key;
+            if (key != 0ull && rank < p.top)
+                write_top(p, row, rank, key, a, log2_z, c);
+        }
+        return;
+    }
+    // the largest key below the last one, again and again: the first of every list that is
     unsigned long long last = ~0ull;
     for (int k = 0; k < p.top; ++k) {
-        // the largest key below the last one: every list's first that is
         unsigned long long best = 0ull;
-        for (int i = lane; i < slices; i += 64) {
+        for (int i = threadIdx.x; i < slices; i += kJoinThreads) {
             const int n = parts[i].top;
             for (int e = 0; e < n; ++e) {
                 const unsigned long long key = keys[(long long)i * p.top + e];
@@ -506,8 +548,14 @@ template <bool BF16> __global__ __launch_bounds__(64) void logprobs_join(Logprob
             const unsigned long long other = __shfl_xor(best, o);
             best = other > best ? other : best;
         }
-        last = best;
+        __syncthreads();
         if (lane == 0)
+            listed[threadIdx.x >> 6] = best;
+        __syncthreads();
+        for (int w = 0; w < kJoinThreads / 64; ++w)
+            best = listed[w] > best ? listed[w] : best;
+        last = best;
+        if (threadIdx.x == 0)
             write_top(p, row, k, best, a, log2_z, c);
     }
 }
@@ -535,7 +583,7 @@ template <bool BF16> hipError_t run_all(const LogprobsParams& p, hipStream_t s)
         run<BF16, 512, 32>(p, pl.slice, pl.slices, s);
     hipError_t rc = hipGetLastError();
     if (rc == hipSuccess && pl.slices > 1) {
-        hipLaunchKernelGGL((logprobs_join<BF16>), dim3((unsigned)p.rows), dim3(64), 0, s, p, pl.slices);
+        hipLaunchKernelGGL((logprobs_join<BF16>), dim3((unsigned)p.rows), dim3(kJoinThreads), 0, s, p, pl.slices);
         rc = hipGetLastError();
     }
     return rc;

@@ -28,8 +28,11 @@ constexpr int kMostSlice = 131072 - kChunk;  // (32 chunks for each of 512 threa
 inline LogprobsPlan make_logprobs_plan(int64_t rows, int64_t vocab)
 {
     LogprobsPlan pl;
-    (void)rows;
-    pl.slices = (int)((vocab + kMostSlice - 1) / kMostSlice);
+    // a workgroup a row, and slices where that leaves CUs idle
+    int64_t slices = rows > 0 && rows <= 128 ? 256 / rows : 1;
+    slices = slices < vocab / 16384 ? slices : vocab / 16384;
+    const int64_t fit = (vocab + kMostSlice - 1) / kMostSlice;
+    pl.slices = (int)(slices > fit ? slices : fit);
     pl.slice = (int)((vocab + pl.slices - 1) / pl.slices);
     pl.slice = (pl.slice + kChunk - 1) / kChunk * kChunk;  // (the bound is a multiple of a chunk)
     pl.threads = pl.slice <= 8192 ? 256 : 512;
