@@ -1,23 +1,235 @@
 // Which tokens of a cache stay (select_kv_tokens), and the copies that bring them together (compact_kv).
 //
-// Selection: the c-th largest weight of the tokens that are not kept by their place is found digit by digit (four digits
-// of eight bits, a histogram each); of the tokens that equal it the lowest stay.  A workgroup a row.
+// Selection.  A row's weights lie in registers, as whole numbers in their order; token = 64 (V wave + v) + lane, so that a ballot
+// has 64 tokens in their order.  The c-th largest of those that are not kept by their place is found bit by bit, counting with
+// ballots, until exactly c reach the number (then nobody asks which ties stay).  Tokens that stay behind the end of the early places
+// are listed in LDS in their order, and the gaps among the early places take them from there.  Rows of up to 2048 tokens take
+// a wavefront, longer ones a workgroup; beyond what its registers hold, the c-th largest comes from four histograms of eight bits.
+// Bound: the counting (a comparison, a population count and an addition a bit for 64 weights), beside HBM: weights read, sources written once.
 //
-// Compaction: source[i] >= i, so a workgroup that takes its places in ascending order, and reads every group of
-// places before it writes them, overwrites nothing that it still has to read.
+// Compaction.  source[i] >= i, so a workgroup that takes its places in ascending order, and reads every group of
+// places before it writes them, overwrites nothing that it still has to read; where no source of a row lies below its new length the
+// order does not matter and nobody waits.  Only tokens that move are touched.  Bound: HBM, what moves read and written once.
 #include "spd_internal.h"
 
 namespace spd {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
+constexpr int kThreads = 256;  // of the kernels without a choice
+constexpr int kLong = 1024;    // of rows that no registers hold
 
 // Weights as whole numbers in their order; NaN below all.
 __device__ __forceinline__ unsigned key_of(float w)
 {
     const unsigned u = __float_as_uint(w == 0.f ? 0.f : w);
-    return w != w ? 0u : (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+    return w != w ? 1u : (u & 0x80000000u) ? ~u : (u | 0x80000000u);  // (0: no token)
+}
+
+__device__ __forceinline__ int lanes_below(unsigned long long mask)
+{
+    return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0u));
+}
+
+// What stays of a row: n tokens, m places, the last r and the first f by their place, c of those between by weight.
+struct Row {
+    int n, m, r, f, c;
+};
+
+__device__ __forceinline__ Row row_of(const SelectParams& p, long long b)
+{
+    Row w;
+    w.n = max(min(p.lens[b], p.max_len), 0);
+    w.m = min(w.n, p.budgets ? max(min(p.budgets[b], p.max_new), 0) : p.max_new);
+    w.r = min(p.recent, w.m);
+    w.f = min(p.sinks, w.m - w.r);
+    w.c = w.m - w.r - w.f;
+    return w;
+}
+
+// WAVES wavefronts a row, V weights a lane; ROWS rows a workgroup (1 where WAVES > 1).
+template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * ROWS) void select_rows(SelectParams p)
+{
+    constexpr int kTokens = 64 * WAVES * V;
+    static_assert(WAVES == 1 || ROWS == 1, "wavefronts of one row wait for each other");
+    __shared__ unsigned short moving[ROWS][kTokens / 2];  // (no more than half of the tokens fill gaps)
+    __shared__ int counts[2][WAVES], sums[3][WAVES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int w = WAVES == 1 ? 0 : wave, local = WAVES == 1 ? wave : 0;
+    const long long row = (long long)blockIdx.x * ROWS + local;
+    if (row >= p.seqs * p.heads)
+        return;
+    const Row a = row_of(p, row / p.heads);
+    int* const source = p.source + row * p.source_stride;
+    if (row % p.heads == 0 && threadIdx.x % (64 * WAVES) == 0)
+        p.new_lens[row / p.heads] = a.m;
+    const int t0 = 64 * V * w;  // this wavefront's first token
+    if (a.m == a.n) {
+#pragma unroll 4
+        for (int v = 0; v < V; ++v)
+            if (t0 + 64 * v + lane < a.m)
+                source[t0 + 64 * v + lane] = t0 + 64 * v + lane;
+        return;
+    }
+    const float* const weights = p.weights + row * p.stride;
+    const int middle = a.n - a.r, early = a.m - a.r;  // tokens f .. middle - 1 are chosen from; places before `early` have gaps
+    float x[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int t = t0 + 64 * v + lane;
+        x[v] = 0.f;
+        if (t >= a.f && t < middle)
+            x[v] = weights[t];
+    }
+    unsigned key[V];
+    unsigned some = 0u, all = ~0u;  // bits that some key has, and that all have
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int t = t0 + 64 * v + lane;
+        const bool inside = t >= a.f && t < middle;
+        key[v] = inside ? key_of(x[v]) : 0u;
+        some |= key[v];
+        all &= inside ? key[v] : ~0u;
+    }
+    // a number over the row's wavefronts (every wavefront calls it as often)
+    int calls = 0;
+    const auto over_row = [&](int mine) __attribute__((always_inline)) -> int {
+        if (WAVES == 1)
+            return mine;
+        int* const at = counts[calls & 1];
+        ++calls;
+        if (lane == 0)
+            at[w] = mine;
+        __syncthreads();
+        int sum = lane < WAVES ? at[lane] : 0;
+#pragma unroll
+        for (int o = 1; o < WAVES; o <<= 1)
+            sum += __shfl_xor(sum, o);
+        return __builtin_amdgcn_readfirstlane(sum);
+    };
+    const int groups = min(max((middle - t0 + 63) / 64, 0), V);  // of 64 tokens that have any to choose from
+    const auto count = [&](unsigned least) __attribute__((always_inline)) -> int {
+        int sum = 0;
+#pragma unroll
+        for (int v0 = 0; v0 < V; v0 += 4)
+            if (v0 < groups) {
+#pragma unroll
+                for (int v = v0; v < v0 + 4; ++v)
+                    sum += __popcll(__ballot(key[v] >= least));
+            }
+        return over_row(sum);
+    };
+    unsigned floor = ~0u;  // keys from here on stay (no key is that large), and `ties` of those one below it where they are not all wanted
+    int ties = 0;
+    if (a.c > 0) {
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            some |= __shfl_xor(some, o);
+            all &= __shfl_xor(all, o);
+        }
+        if (WAVES > 1) {
+            __shared__ unsigned bits[2][WAVES];
+            if (lane == 0) {
+                bits[0][w] = some;
+                bits[1][w] = all;
+            }
+            __syncthreads();
+            for (int i = 0; i < WAVES; ++i) {
+                some |= bits[0][i];
+                all &= bits[1][i];
+            }
+        }
+        const unsigned differ = __builtin_amdgcn_readfirstlane(some & ~all);
+        const int top = differ ? 31 - __clz((int)differ) : -1;
+        floor = __builtin_amdgcn_readfirstlane(all) & ~(differ ? (2u << top) - 1u : 0u);
+        bool exact = false;
+        for (int bit = top; bit >= 0 && !exact; --bit) {
+            const unsigned cand = floor | (1u << bit);
+            const int reach = count(cand);
+            if (reach >= a.c) {
+                floor = cand;
+                exact = reach == a.c;
+            }
+        }
+        if (!exact) {
+            ++floor;  // (below ~0: the largest key is +inf's)
+            ties = a.c - count(floor);
+        }
+    }
+    // Whether token 64 v + lane of this wavefront stays by weight; tied: its ties in front of v.
+    const auto stays = [&](int v, int& tied) __attribute__((always_inline)) -> bool {
+        bool s = key[v] >= floor;
+        if (ties > 0) {
+            const unsigned long long equal = __ballot(key[v] == floor - 1u);
+            s = s || ((equal >> lane & 1) && tied + lanes_below(equal) < ties);
+            tied += __popcll(equal);
+        }
+        return s;
+    };
+    // what the wavefronts in front of this one have: ties, gaps, tokens that move
+    int tied0 = 0, gap0 = 0, move0 = 0;
+    if (WAVES > 1) {
+        if (ties > 0) {
+            int equal = 0;
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                equal += __popcll(__ballot(key[v] == floor - 1u));
+            if (lane == 0)
+                sums[0][w] = equal;
+            __syncthreads();
+            for (int i = 0; i < w; ++i)
+                tied0 += sums[0][i];
+        }
+        int tied = tied0, gaps = 0, moves = 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int t = t0 + 64 * v + lane;
+            const bool s = stays(v, tied) || t < a.f;
+            gaps += __popcll(__ballot(!s && t < early));
+            moves += __popcll(__ballot(s && t >= early && t < middle));
+        }
+        if (lane == 0) {
+            sums[1][w] = gaps;
+            sums[2][w] = moves;
+        }
+        __syncthreads();
+        for (int i = 0; i < w; ++i) {
+            gap0 += sums[1][i];
+            move0 += sums[2][i];
+        }
+    }
+    unsigned short* const list = moving[local];
+    if (t0 + 64 * V > early) {
+        int tied = tied0, at = move0;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (v < groups) {
+                const int t = t0 + 64 * v + lane;
+                const bool move = (stays(v, tied) || t < a.f) && t >= early && t < middle;
+                const unsigned long long moves = __ballot(move);
+                if (move)
+                    list[at + lanes_below(moves)] = (unsigned short)t;
+                at += __popcll(moves);
+            }
+    }
+    if (WAVES > 1)
+        __syncthreads();
+    else
+        __builtin_amdgcn_wave_barrier();
+    if (t0 < early) {
+        int tied = tied0, at = gap0;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (t0 + 64 * v < early) {
+                const int t = t0 + 64 * v + lane;
+                const bool s = stays(v, tied) || t < a.f;
+                const unsigned long long gaps = __ballot(!s && t < early);
+                if (t < early)
+                    source[t] = s ? t : (int)list[at + lanes_below(gaps)];
+                at += __popcll(gaps);
+            }
+    }
+    for (int i = threadIdx.x % (64 * WAVES); i < a.r; i += 64 * WAVES)
+        source[early + i] = a.n - a.r + i;
 }
 
 // Places before this thread's for which `yes` holds, and their number over the workgroup.
@@ -31,25 +243,26 @@ __device__ __forceinline__ int before(bool yes, int* lds, int& all)
         lds[wave] = __popcll(mine);
     __syncthreads();
     all = 0;
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < kLong / 64; ++w) {
         count += w < wave ? lds[w] : 0;
         all += lds[w];
     }
     return count;
 }
 
-__global__ __launch_bounds__(kThreads) void select_kernel(SelectParams p)
+// Rows of any length, from memory.
+__global__ __launch_bounds__(kLong) void select_long(SelectParams p)
 {
-    __shared__ int hist[256], lds[kWaves], found[2];
+    __shared__ int hist[256], lds[kLong / 64], found[2];
     const int b = blockIdx.x / p.heads, j = blockIdx.x % p.heads, tid = threadIdx.x;
-    const int n = max(min(p.lens[b], p.max_len), 0), m = min(n, p.budgets ? max(min(p.budgets[b], p.max_new), 0) : p.max_new);
-    const int r = min(p.recent, m), f = min(p.sinks, m - r), c = m - r - f;
+    const Row a = row_of(p, b);
+    const int n = a.n, m = a.m, r = a.r, f = a.f, c = a.c;
     const float* const w = p.weights + (long long)blockIdx.x * p.stride;
     int* const source = p.source + (long long)blockIdx.x * p.source_stride;
     if (j == 0 && tid == 0)
         p.new_lens[b] = m;
     if (m == n) {
-        for (int i = tid; i < m; i += kThreads)
+        for (int i = tid; i < m; i += kLong)
             source[i] = i;
         return;
     }
@@ -57,9 +270,10 @@ __global__ __launch_bounds__(kThreads) void select_kernel(SelectParams p)
     unsigned floor = 0u, mask = 0u;
     int ties = c;
     for (int shift = 24; shift >= 0 && c > 0; shift -= 8) {
-        hist[tid] = 0;
+        if (tid < 256)
+            hist[tid] = 0;
         __syncthreads();
-        for (int t = f + tid; t < n - r; t += kThreads) {
+        for (int t = f + tid; t < n - r; t += kLong) {
             const unsigned key = key_of(w[t]);
             if ((key & mask) == floor)
                 atomicAdd(&hist[key >> shift & 255u], 1);
@@ -79,7 +293,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(SelectParams p)
     }
     // Places 0 .. m - r - 1 ("early"): tokens that stay, and gaps between them, which tokens m - r .. n - r - 1 that stay fill.  Both are
     // walked in ascending order, gaps and the tokens that fill them in step.
-    __shared__ int gaps[kThreads];
+    __shared__ int gaps[kLong];
     const int early = m - r;
     int tied = 0;  // ties in front of the walk
     const auto stays = [&](int t, int end) {
@@ -90,7 +304,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(SelectParams p)
         tied += all;
         return (t < f && t < end) || (middle && key > floor) || (tie && rank < ties);
     };
-    for (int t0 = 0; t0 < early; t0 += kThreads) {
+    for (int t0 = 0; t0 < early; t0 += kLong) {
         const int t = t0 + tid;
         const bool here = stays(t, early);
         if (t < early)
@@ -98,7 +312,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(SelectParams p)
     }
     __syncthreads();
     int listed = 0, used = 0, looked = 0;  // gaps in the list, those filled, and how far the places were looked through
-    for (int t0 = early; t0 < n - r; t0 += kThreads) {
+    for (int t0 = early; t0 < n - r; t0 += kLong) {
         const int t = t0 + tid;
         const bool here = stays(t, n - r);
         int moving, done = 0;
@@ -111,7 +325,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(SelectParams p)
                     const int at = before(gap, lds, listed);
                     if (gap)
                         gaps[at] = looked + tid;
-                    looked += kThreads;
+                    looked += kLong;
                 }
                 __syncthreads();
             }
@@ -125,77 +339,205 @@ __global__ __launch_bounds__(kThreads) void select_kernel(SelectParams p)
             done += take;
         }
     }
-    for (int i = early + tid; i < m; i += kThreads)
+    for (int i = early + tid; i < m; i += kLong)
         source[i] = n - m + i;
 }
 
-__global__ __launch_bounds__(kThreads) void compact_kernel(CompactParams p)
+// Where token t of a sequence lies for KV head j, in 16-byte pieces; `first`: its place in the table.
+__device__ __forceinline__ long long row_at(const CompactParams& p, const int* pages, int first, int j, int t)
 {
-    constexpr int kEach = 4;
-    const int which = blockIdx.x & 1, j = (blockIdx.x >> 1) % p.Hkv, b = (blockIdx.x >> 1) / p.Hkv, tid = threadIdx.x;
-    const int m = max(min(p.new_lens[b], p.max_new), 0);
+    return p.page_size ? (((long long)pages[first + (t >> 4)] * p.Hkv + j) * 16 + (t & 15)) * p.head_u4
+                       : (long long)(first + t) * p.stride_u4 + (long long)j * p.head_u4;
+}
+
+// Keys and values.  A workgroup takes pieces seg * width .. of the rows of one (sequence, KV head): of K and V, or of one of them
+// (kinds 2), and of all places, or (chunk > 0, not in place) of `chunk` of them.
+__global__ __launch_bounds__(kThreads) void compact_rows(CompactParams p, int kinds, int segs, int width, int chunk, int chunks)
+{
+    constexpr int kEach = 4;  // rows a thread has under way
+    __shared__ long long from_at[kThreads], to_at[kThreads];
+    __shared__ int lds[kThreads / 64];
+    __shared__ int below;
+    int rest = blockIdx.x;
+    const int kind = rest % kinds;
+    rest /= kinds;
+    const int seg = rest % segs;
+    rest /= segs;
+    const int j = rest % p.Hkv;
+    rest /= p.Hkv;
+    const int b = rest % p.B, first = rest / p.B * chunk, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    (void)chunks;
+    const int m = max(min(p.new_lens[b], p.max_new), 0), last = chunk > 0 ? min(m, first + chunk) : m;
+    if (first >= last)
+        return;
     const int* const source = p.source + b * p.seq_stride + j * p.head_stride;
     const int in0 = p.indptr[b], out0 = p.out_indptr[b], per = p.page_size ? 16 : 1;
     const long long held = (long long)(p.indptr[b + 1] - in0) * per, room = (long long)(p.out_indptr[b + 1] - out0) * per;
-    const uint4* const from = (const uint4*)(which ? p.v : p.k);
-    uint4* const to = (uint4*)(which ? p.v_out : p.k_out);
-    const auto at = [&](const int* pages, int first, int t) {
-        return p.page_size ? (((long long)pages[first + (t >> 4)] * p.Hkv + j) * 16 + (t & 15)) * p.head_u4
-                           : (long long)(first + t) * p.stride_u4 + (long long)j * p.head_u4;
-    };
-    // pieces of the places in order, kEach a thread at a time, all read before any is written
-    const long long pieces = (long long)m * p.head_u4;
-    for (long long i0 = 0; i0 < pieces; i0 += kEach * kThreads) {
-        uint4 v[kEach];
-        long long dst[kEach];
+    const uint4* const k = (const uint4*)(kinds == 2 && kind == 1 ? p.v : p.k);
+    uint4* const k_out = (uint4*)(kinds == 2 && kind == 1 ? p.v_out : p.k_out);
+    const uint4* const v = (const uint4*)p.v;
+    uint4* const v_out = (uint4*)p.v_out;
+    const int rows = kThreads / width, mine = tid / width, piece = seg * width + tid % width;  // rows at a time, this thread's and its piece
+    // whether anything is read from a place that is written: then every group of places is read before it is written
+    bool ordered = false;
+    if (p.in_place) {
+        if (tid == 0)
+            below = 0;
+        __syncthreads();
+        bool any = false;
+        for (int i = first + tid; i < last; i += kThreads) {
+            const int src = source[i];
+            any |= src > i && src < m;
+        }
+        if (__any(any) && lane == 0)
+            below = 1;
+        __syncthreads();
+        ordered = below != 0;
+    }
+    for (int i0 = first; i0 < last; i0 += kThreads) {
+        // the places that get another token, listed
+        const int i = i0 + tid, src = i < last ? source[i] : -1;
+        const bool moves = src >= i && src < held && i < room && !(p.in_place && src == i);
+        const unsigned long long mask = __ballot(moves);
+        if (lane == 0)
+            lds[wave] = __popcll(mask);
+        __syncthreads();
+        int at = lanes_below(mask), all = 0;
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            const long long i = i0 + e * kThreads + tid;
-            dst[e] = -1;
-            v[e] = make_uint4(0u, 0u, 0u, 0u);
-            if (i < pieces) {
-                const int place = (int)(i / p.head_u4), piece = (int)(i % p.head_u4), src = source[place];
-                if (src >= place && src < held && place < room && !(p.in_place && src == place)) {
-                    v[e] = from[at(p.pages, in0, src) + piece];
-                    dst[e] = at(p.out_pages, out0, place) + piece;
+        for (int w = 0; w < kThreads / 64; ++w) {
+            at += w < wave ? lds[w] : 0;
+            all += lds[w];
+        }
+        if (moves) {
+            from_at[at] = row_at(p, p.pages, in0, j, src);
+            to_at[at] = row_at(p, p.out_pages, out0, j, i);
+        }
+        __syncthreads();
+        for (int e0 = 0; e0 < all; e0 += kEach * rows) {
+            uint4 x[kEach], y[kEach];
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) {
+                const int row = e0 + e * rows + mine;
+                if (mine < rows && row < all) {
+                    x[e] = k[from_at[row] + piece];
+                    if (kinds == 1)
+                        y[e] = v[from_at[row] + piece];
+                }
+            }
+            if (ordered) {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                __syncthreads();
+            }
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) {
+                const int row = e0 + e * rows + mine;
+                if (mine < rows && row < all) {
+                    k_out[to_at[row] + piece] = x[e];
+                    if (kinds == 1)
+                        v_out[to_at[row] + piece] = y[e];
                 }
             }
         }
         __syncthreads();
-#pragma unroll
-        for (int e = 0; e < kEach; ++e)
-            if (dst[e] >= 0)
-                to[dst[e]] = v[e];
     }
-    if (which == 0 && p.weights) {
-        const float* const w = p.weights + ((long long)b * p.Hkv + j) * p.weights_stride;
-        float* const out = p.weights_out + ((long long)b * p.Hkv + j) * p.weights_stride;
-        for (int i0 = 0; i0 < m; i0 += kThreads) {
-            const int i = i0 + tid, src = i < m ? source[i] : -1;
-            const float x = src >= i && src < p.weights_stride ? w[src] : 0.f;
-            __syncthreads();
-            if (i < m && src >= i)
-                out[i] = x;
-        }
-        __syncthreads();
-        for (long long i = m + tid; i < p.weights_stride; i += kThreads)
-            out[i] = 0.f;
-    }
-    if (which == 0 && j == 0 && tid == 0 && p.lens_out)
+}
+
+// Weights, and the lengths: a workgroup a (sequence, KV head).
+__global__ __launch_bounds__(kThreads) void compact_weights(CompactParams p)
+{
+    constexpr int kEach = 4;
+    const int j = blockIdx.x % p.Hkv, b = blockIdx.x / p.Hkv, tid = threadIdx.x;
+    const int m = max(min(p.new_lens[b], p.max_new), 0);
+    if (j == 0 && tid == 0 && p.lens_out)
         p.lens_out[b] = m;
+    if (!p.weights)
+        return;
+    const int* const source = p.source + b * p.seq_stride + j * p.head_stride;
+    const float* const w = p.weights + (long long)blockIdx.x * p.weights_stride;
+    float* const out = p.weights_out + (long long)blockIdx.x * p.weights_stride;
+    for (int i0 = 0; i0 < m; i0 += kEach * kThreads) {
+        int src[kEach];
+        float x[kEach];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int i = i0 + e * kThreads + tid;
+            src[e] = i < m ? source[i] : -1;
+        }
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int i = i0 + e * kThreads + tid;
+            x[e] = src[e] >= i && src[e] < p.weights_stride ? w[src[e]] : 0.f;
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int i = i0 + e * kThreads + tid;
+            if (src[e] >= i)
+                out[i] = x[e];
+        }
+    }
+    __syncthreads();
+    for (long long i = m + tid; i < p.weights_stride; i += kThreads)
+        out[i] = 0.f;
 }
 
 }  // namespace
 
 hipError_t launch_select_kv(const SelectParams& p, hipStream_t s)
 {
-    hipLaunchKernelGGL(select_kernel, dim3((unsigned)(p.seqs * p.heads)), dim3(kThreads), 0, s, p);
+    const long long rows = p.seqs * p.heads;
+#define SPD_SELECT(WAVES, V, ROWS) \
+    hipLaunchKernelGGL((select_rows<WAVES, V, ROWS>), dim3((unsigned)((rows + ROWS - 1) / ROWS)), dim3(64 * WAVES * ROWS), 0, s, p)
+    if (p.max_len <= 256) {
+        SPD_SELECT(1, 4, 4);
+    } else if (p.max_len <= 512) {
+        SPD_SELECT(1, 8, 4);
+    } else if (p.max_len <= 1024) {
+        SPD_SELECT(1, 16, 4);
+    } else if (p.max_len <= 2048) {
+        SPD_SELECT(1, 32, 4);
+    } else if (p.max_len <= 4096) {
+        SPD_SELECT(4, 16, 1);
+    } else if (p.max_len <= 8192) {
+        SPD_SELECT(8, 16, 1);
+    } else if (p.max_len <= 16384) {
+        SPD_SELECT(16, 16, 1);
+    } else if (p.max_len <= 32768) {
+        SPD_SELECT(16, 32, 1);
+    } else {
+        hipLaunchKernelGGL(select_long, dim3((unsigned)rows), dim3(kLong), 0, s, p);
+    }
+#undef SPD_SELECT
     return hipGetLastError();
 }
 
 hipError_t launch_compact_kv(const CompactParams& p, hipStream_t s)
 {
-    hipLaunchKernelGGL(compact_kernel, dim3((unsigned)(2 * p.B * p.Hkv)), dim3(kThreads), 0, s, p);
+    const int pairs = p.B * p.Hkv;
+    int kinds = 1, segs = 1, chunk = 0, chunks = 1;
+    if (p.in_place) {
+        // few rows: K and V, and the pieces of a row, each have a workgroup
+        if (pairs < 1024) {
+            kinds = 2;
+            while (p.head_u4 % (2 * segs) == 0 && 2 * segs * kinds * pairs <= 1024)
+                segs *= 2;
+        }
+    } else {
+        chunk = 64;
+        while (chunk < (1 << 30) && (long long)pairs * ((p.max_new + chunk - 1) / chunk) > 16384)
+            chunk *= 2;
+        chunks = (p.max_new + chunk - 1) / chunk;
+    }
+    if (p.max_new > 0) {
+        hipLaunchKernelGGL(compact_rows, dim3((unsigned)((long long)pairs * kinds * segs * chunks)), dim3(kThreads), 0, s, p, kinds, segs,
+                           p.head_u4 / segs, chunk, chunks);
+        const hipError_t rc = hipGetLastError();
+        if (rc != hipSuccess)
+            return rc;
+    }
+    if (p.weights || p.lens_out)
+        hipLaunchKernelGGL(compact_weights, dim3((unsigned)pairs), dim3(kThreads), 0, s, p);
     return hipGetLastError();
 }
 

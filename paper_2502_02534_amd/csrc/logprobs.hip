@@ -47,7 +47,7 @@ template <bool BF16> __device__ __forceinline__ float logit(const LogprobsParams
     return ((const float*)p.logits)[at];
 }
 
-// A chunk's 8 logits: of a whole one in 16-byte loads, else one by one (-inf outside the slice).
+// A chunk's 8 logits: of a whole one in 16-byte loads, else one by one (-inf where there is none).
 template <bool BF16> struct Chunk {
     uint4 v[BF16 ? 1 : 2];
     __device__ __forceinline__ void load(const char* at)
@@ -55,6 +55,26 @@ template <bool BF16> struct Chunk {
         v[0] = *(const uint4*)at;
         if (!BF16)
             v[BF16 ? 0 : 1] = *(const uint4*)(at + 16);
+    }
+    // of places chunk * 8 on from `from`, of which only first .. last are there: 8 loads at once
+    __device__ __forceinline__ void load_some(const char* from, int place, int first, int last)
+    {
+        unsigned w[BF16 ? 4 : 8];
+#pragma unroll
+        for (int e = 0; e < kChunk; ++e) {
+            const int at = min(max(place + e, first), last);
+            const bool there = at == place + e;
+            if (BF16) {
+                const unsigned b = ((const unsigned short*)from)[at], u = there ? b : 0xff80u;
+                w[e >> 1] = (e & 1) ? w[e >> 1] | u << 16 : u;
+            } else {
+                const unsigned u = ((const unsigned*)from)[at];
+                w[BF16 ? 0 : e] = there ? u : 0xff800000u;
+            }
+        }
+        v[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        if (!BF16)
+            v[BF16 ? 0 : 1] = make_uint4(w[BF16 ? 0 : 4], w[BF16 ? 0 : 5], w[BF16 ? 0 : 6], w[BF16 ? 0 : 7]);
     }
     __device__ __forceinline__ void get(float (&x)[kChunk]) const
     {
@@ -190,9 +210,9 @@ __device__ __forceinline__ float scale_of(const LogprobsParams& p, long long row
 
 // THREADS, STRIPES: a workgroup takes up to STRIPES times THREADS chunks.  PARTS: slices of rows, joined by another launch.
 template <bool BF16, int THREADS, int STRIPES, bool PARTS>
-__global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobsParams p, int slice, int slices)
+__global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(BF16 || STRIPES < 32 ? 8 : 4))) void logprobs_kernel(LogprobsParams p, int slice, int slices)
 {
-    constexpr int kWaves = THREADS / 64, kAhead = STRIPES < 4 ? STRIPES : 4;
+    constexpr int kWaves = THREADS / 64, kAhead = 2;
     constexpr int kHot = SPD_MAX_TOP_TOKENS + 8;  // threads up to which all of their chunks are looked through
     // (otherwise fewer than `top` threads lie above the threshold, and every wavefront adds up to `top` chunks that equal it)
     constexpr int kHits = kHot * STRIPES + kWaves * SPD_MAX_TOP_TOKENS;
@@ -231,16 +251,6 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobsParams p, int
     const float given = known ? logit<BF16>(p, row * p.stride + token) : INFINITY;
 
     const auto whole = [&](int chunk) { return chunk * kChunk >= ahead && (chunk + 1) * kChunk <= places; };
-    const auto one_by_one = [&](int chunk, float (&x)[kChunk]) {
-#pragma unroll
-        for (int e = 0; e < kChunk; ++e) {
-            const int at = chunk * kChunk + e;
-            x[e] = -INFINITY;
-            if (at >= ahead && at < places)
-                x[e] = logit<BF16>(p, base - ahead + at);
-        }
-    };
-
     State a = {-INFINITY, kLowest, 0.f, 0.f};
     int above = 0;
     const auto take = [&](int chunk, const float (&x)[kChunk]) __attribute__((always_inline)) {
@@ -289,18 +299,16 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobsParams p, int
                 const int chunk = (s0 + i) * THREADS + tid;
                 if (whole(chunk))
                     v[i].load(from + (long long)chunk * (kChunk * kElt));
+                else
+                    v[i].load_some(from, chunk * kChunk, ahead, places - 1);
             }
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int chunk = (s0 + i) * THREADS + tid;
-                float x[kChunk];
-                if (whole(chunk))
+            for (int i = 0; i < kAhead; ++i)
+                if ((s0 + i) * THREADS < chunks) {
+                    float x[kChunk];
                     v[i].get(x);
-                else
-                    one_by_one(chunk, x);
-                if ((s0 + i) * THREADS < chunks)
-                    take(chunk, x);
-            }
+                    take((s0 + i) * THREADS + tid, x);
+                }
         }
     }
 
@@ -327,8 +335,10 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobsParams p, int
     if (overflows(m, c)) {
         a.z = a.s = 0.f;
         for (int chunk = tid; chunk < chunks; chunk += THREADS) {
+            Chunk<BF16> v;
+            v.load_some(from, chunk * kChunk, ahead, places - 1);
             float x[kChunk];
-            one_by_one(chunk, x);
+            v.get(x);
             for (int e = 0; e < kChunk; ++e) {
                 const float y = fmaxf((x[e] - m) * c, kFloor), w = __builtin_amdgcn_exp2f(y);
                 a.z += w;
