@@ -50,9 +50,14 @@ __device__ __forceinline__ Row row_of(const SelectParams& p, long long b)
 template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * ROWS) void select_rows(SelectParams p)
 {
     constexpr int kTokens = 64 * WAVES * V;
+    constexpr int kBits = V < 16 ? 0 : WAVES == 1 ? 9 : 11;  // of the histogram
+    constexpr int kBins = 1 << kBits, kOwn = kBins / 64;      // and a lane's bins of it
     static_assert(WAVES == 1 || ROWS == 1, "wavefronts of one row wait for each other");
     __shared__ unsigned short moving[ROWS][kTokens / 2];  // (no more than half of the tokens fill gaps)
     __shared__ int counts[2][WAVES], sums[3][WAVES];
+    __shared__ __align__(16) int hist[kBits ? ROWS : 1][kBits ? kBins : 4];
+    __shared__ unsigned few[ROWS][64];
+    __shared__ int num_few[ROWS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int w = WAVES == 1 ? 0 : wave, local = WAVES == 1 ? wave : 0;
     const long long row = (long long)blockIdx.x * ROWS + local;
@@ -81,14 +86,14 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
             x[v] = weights[t];
     }
     unsigned key[V];
-    unsigned some = 0u, all = ~0u;  // bits that some key has, and that all have
+    unsigned lowest = ~0u, highest = 0u;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int t = t0 + 64 * v + lane;
         const bool inside = t >= a.f && t < middle;
         key[v] = inside ? key_of(x[v]) : 0u;
-        some |= key[v];
-        all &= inside ? key[v] : ~0u;
+        lowest = inside ? min(lowest, key[v]) : lowest;
+        highest = max(highest, key[v]);
     }
     // a number over the row's wavefronts (every wavefront calls it as often)
     int calls = 0;
@@ -123,25 +128,90 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
     if (a.c > 0) {
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) {
-            some |= __shfl_xor(some, o);
-            all &= __shfl_xor(all, o);
+            lowest = min(lowest, (unsigned)__shfl_xor(lowest, o));
+            highest = max(highest, (unsigned)__shfl_xor(highest, o));
+        }
+        if (kBits) {
+            int4* const own = (int4*)hist[local];
+            for (int i = threadIdx.x % (64 * WAVES); i < kBins / 4; i += 64 * WAVES)
+                own[i] = make_int4(0, 0, 0, 0);
+            if (threadIdx.x % (64 * WAVES) == 0)
+                num_few[local] = 0;
         }
         if (WAVES > 1) {
-            __shared__ unsigned bits[2][WAVES];
+            __shared__ unsigned ends[2][WAVES];
             if (lane == 0) {
-                bits[0][w] = some;
-                bits[1][w] = all;
+                ends[0][w] = lowest;
+                ends[1][w] = highest;
             }
             __syncthreads();
             for (int i = 0; i < WAVES; ++i) {
-                some |= bits[0][i];
-                all &= bits[1][i];
+                lowest = min(lowest, ends[0][i]);
+                highest = max(highest, ends[1][i]);
             }
         }
-        const unsigned differ = __builtin_amdgcn_readfirstlane(some & ~all);
-        const int top = differ ? 31 - __clz((int)differ) : -1;
-        floor = __builtin_amdgcn_readfirstlane(all) & ~(differ ? (2u << top) - 1u : 0u);
+        lowest = __builtin_amdgcn_readfirstlane(lowest);
+        highest = __builtin_amdgcn_readfirstlane(highest);
+        // from the lowest on: 1 and more
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            key[v] = key[v] ? key[v] - lowest + 1u : 0u;
+        int top = 31 - __clz((int)(highest - lowest + 1u));
+        floor = 0u;
         bool exact = false;
+        if (kBits && top >= kBits) {
+            // the first kBits bits from a histogram, and the others of the few keys that share them with the c-th largest
+            const int shift = top + 1 - kBits;
+            int* const bins = hist[local];
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (v < groups && key[v])
+                    atomicAdd(&bins[key[v] >> shift], 1);
+            if (WAVES > 1)
+                __syncthreads();
+            else
+                __builtin_amdgcn_wave_barrier();
+            int here = 0;
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i)
+                here += bins[lane * kOwn + i];
+            int from = here;  // keys of this lane's bins and of those above
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int y = __shfl_down(from, o);
+                from += lane + o < 64 ? y : 0;
+            }
+            const int owner = 63 - __clzll((long long)__ballot(from >= a.c));
+            int above = __builtin_amdgcn_readlane(from - here, owner), bin = owner * kOwn + kOwn - 1;
+            while (above + bins[bin] < a.c)
+                above += bins[bin--];
+            const int inside = __builtin_amdgcn_readfirstlane(bins[bin]);
+            above = __builtin_amdgcn_readfirstlane(above);
+            floor = (unsigned)__builtin_amdgcn_readfirstlane(bin) << shift;
+            exact = above + inside == a.c;
+            top = shift - 1;
+            if (!exact && inside <= 64) {
+                const unsigned shared = floor >> shift;
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    if (v < groups && key[v] >> shift == shared && key[v])
+                        few[local][atomicAdd(&num_few[local], 1)] = key[v];
+                if (WAVES > 1)
+                    __syncthreads();
+                else
+                    __builtin_amdgcn_wave_barrier();
+                const unsigned mine = lane < inside ? few[local][lane] : 0u;
+                for (int bit = top; bit >= 0 && !exact; --bit) {
+                    const unsigned cand = floor | (1u << bit);
+                    const int reach = above + __popcll(__ballot(mine >= cand));
+                    if (reach >= a.c) {
+                        floor = cand;
+                        exact = reach == a.c;
+                    }
+                }
+                top = -1;
+            }
+        }
         for (int bit = top; bit >= 0 && !exact; --bit) {
             const unsigned cand = floor | (1u << bit);
             const int reach = count(cand);
@@ -351,30 +421,29 @@ __device__ __forceinline__ long long row_at(const CompactParams& p, const int* p
 }
 
 // Keys and values.  A workgroup takes pieces seg * width .. of the rows of one (sequence, KV head): of K and V, or of one of them
-// (kinds 2), and of all places, or (chunk > 0, not in place) of `chunk` of them.
-__global__ __launch_bounds__(kThreads) void compact_rows(CompactParams p, int kinds, int segs, int width, int chunk, int chunks)
+// (KINDS 2), and of all places, or (chunk > 0, not in place) of `chunk` of them.
+template <int KINDS> __global__ __launch_bounds__(kThreads) void compact_rows(CompactParams p, int segs, int width, int chunk)
 {
-    constexpr int kEach = 4;  // rows a thread has under way
+    constexpr int kEach = KINDS == 1 ? 4 : 8;  // rows a thread has under way
     __shared__ long long from_at[kThreads], to_at[kThreads];
     __shared__ int lds[kThreads / 64];
     __shared__ int below;
     int rest = blockIdx.x;
-    const int kind = rest % kinds;
-    rest /= kinds;
+    const int kind = rest % KINDS;
+    rest /= KINDS;
     const int seg = rest % segs;
     rest /= segs;
     const int j = rest % p.Hkv;
     rest /= p.Hkv;
     const int b = rest % p.B, first = rest / p.B * chunk, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    (void)chunks;
     const int m = max(min(p.new_lens[b], p.max_new), 0), last = chunk > 0 ? min(m, first + chunk) : m;
     if (first >= last)
         return;
     const int* const source = p.source + b * p.seq_stride + j * p.head_stride;
     const int in0 = p.indptr[b], out0 = p.out_indptr[b], per = p.page_size ? 16 : 1;
     const long long held = (long long)(p.indptr[b + 1] - in0) * per, room = (long long)(p.out_indptr[b + 1] - out0) * per;
-    const uint4* const k = (const uint4*)(kinds == 2 && kind == 1 ? p.v : p.k);
-    uint4* const k_out = (uint4*)(kinds == 2 && kind == 1 ? p.v_out : p.k_out);
+    const uint4* const k = (const uint4*)(kind == 1 ? p.v : p.k);
+    uint4* const k_out = (uint4*)(kind == 1 ? p.v_out : p.k_out);
     const uint4* const v = (const uint4*)p.v;
     uint4* const v_out = (uint4*)p.v_out;
     const int rows = kThreads / width, mine = tid / width, piece = seg * width + tid % width;  // rows at a time, this thread's and its piece
@@ -415,14 +484,13 @@ __global__ __launch_bounds__(kThreads) void compact_rows(CompactParams p, int ki
         __syncthreads();
         for (int e0 = 0; e0 < all; e0 += kEach * rows) {
             uint4 x[kEach], y[kEach];
+            // (what has no row of its own repeats the last one)
 #pragma unroll
             for (int e = 0; e < kEach; ++e) {
-                const int row = e0 + e * rows + mine;
-                if (mine < rows && row < all) {
-                    x[e] = k[from_at[row] + piece];
-                    if (kinds == 1)
-                        y[e] = v[from_at[row] + piece];
-                }
+                const long long at_from = from_at[min(e0 + e * rows + mine, all - 1)] + piece;
+                x[e] = k[at_from];
+                if (KINDS == 1)
+                    y[e] = v[at_from];
             }
             if (ordered) {
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -433,7 +501,7 @@ __global__ __launch_bounds__(kThreads) void compact_rows(CompactParams p, int ki
                 const int row = e0 + e * rows + mine;
                 if (mine < rows && row < all) {
                     k_out[to_at[row] + piece] = x[e];
-                    if (kinds == 1)
+                    if (KINDS == 1)
                         v_out[to_at[row] + piece] = y[e];
                 }
             }
@@ -530,8 +598,11 @@ hipError_t launch_compact_kv(const CompactParams& p, hipStream_t s)
         chunks = (p.max_new + chunk - 1) / chunk;
     }
     if (p.max_new > 0) {
-        hipLaunchKernelGGL(compact_rows, dim3((unsigned)((long long)pairs * kinds * segs * chunks)), dim3(kThreads), 0, s, p, kinds, segs,
-                           p.head_u4 / segs, chunk, chunks);
+        const dim3 grid((unsigned)((long long)pairs * kinds * segs * chunks));
+        if (kinds == 1)
+            hipLaunchKernelGGL(compact_rows<1>, grid, dim3(kThreads), 0, s, p, segs, p.head_u4 / segs, chunk);
+        else
+            hipLaunchKernelGGL(compact_rows<2>, grid, dim3(kThreads), 0, s, p, segs, p.head_u4 / segs, chunk);
         const hipError_t rc = hipGetLastError();
         if (rc != hipSuccess)
             return rc;
