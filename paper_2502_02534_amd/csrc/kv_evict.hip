@@ -15,6 +15,8 @@
 namespace spd {
 namespace {
 
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
 constexpr int kThreads = 256;  // of the kernels without a choice
 constexpr int kLong = 1024;    // of rows that no registers hold
 
@@ -420,10 +422,54 @@ __device__ __forceinline__ long long row_at(const CompactParams& p, const int* p
                        : (long long)(first + t) * p.stride_u4 + (long long)j * p.head_u4;
 }
 
-// Keys and values.  A workgroup takes pieces seg * width .. of the rows of one (sequence, KV head): of K and V, or of one of them
-// (KINDS 2), and of all places, or (chunk > 0, not in place) of `chunk` of them.
-template <int KINDS> __global__ __launch_bounds__(kThreads) void compact_rows(CompactParams p, int segs, int width, int chunk)
+// Weights, and the lengths: a workgroup a (sequence, KV head).
+__device__ __forceinline__ void compact_weights(const CompactParams& p, int pair)
 {
+    constexpr int kEach = 4;
+    const int j = pair % p.Hkv, b = pair / p.Hkv, tid = threadIdx.x;
+    const int m = max(min(p.new_lens[b], p.max_new), 0);
+    if (j == 0 && tid == 0 && p.lens_out)
+        p.lens_out[b] = m;
+    if (!p.weights)
+        return;
+    const int* const source = p.source + b * p.seq_stride + j * p.head_stride;
+    const float* const w = p.weights + (long long)pair * p.weights_stride;
+    float* const out = p.weights_out + (long long)pair * p.weights_stride;
+    for (int i0 = 0; i0 < m; i0 += kEach * kThreads) {
+        int src[kEach];
+        float x[kEach];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int i = i0 + e * kThreads + tid;
+            src[e] = i < m ? source[i] : -1;
+        }
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int i = i0 + e * kThreads + tid;
+            x[e] = src[e] >= i && src[e] < p.weights_stride ? w[src[e]] : 0.f;
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int i = i0 + e * kThreads + tid;
+            if (src[e] >= i)
+                out[i] = x[e];
+        }
+    }
+    __syncthreads();
+    for (long long i = m + tid; i < p.weights_stride; i += kThreads)
+        out[i] = 0.f;
+}
+
+// Keys and values.  A workgroup takes pieces seg * width .. of the rows of one (sequence, KV head): of K and V, or of one of them
+// (KINDS 2), and of all places, or (chunk > 0, not in place) of `chunk` of them; the workgroups from weights_from on move the weights.
+template <int KINDS> __global__ __launch_bounds__(kThreads) void compact_rows(CompactParams p, int segs, int width, int chunk, int weights_from)
+{
+    if ((int)blockIdx.x >= weights_from) {
+        compact_weights(p, (int)blockIdx.x - weights_from);
+        return;
+    }
     constexpr int kEach = KINDS == 1 ? 4 : 8;  // rows a thread has under way
     __shared__ long long from_at[kThreads], to_at[kThreads];
     __shared__ int lds[kThreads / 64];
@@ -442,10 +488,10 @@ template <int KINDS> __global__ __launch_bounds__(kThreads) void compact_rows(Co
     const int* const source = p.source + b * p.seq_stride + j * p.head_stride;
     const int in0 = p.indptr[b], out0 = p.out_indptr[b], per = p.page_size ? 16 : 1;
     const long long held = (long long)(p.indptr[b + 1] - in0) * per, room = (long long)(p.out_indptr[b + 1] - out0) * per;
-    const uint4* const k = (const uint4*)(kind == 1 ? p.v : p.k);
-    uint4* const k_out = (uint4*)(kind == 1 ? p.v_out : p.k_out);
-    const uint4* const v = (const uint4*)p.v;
-    uint4* const v_out = (uint4*)p.v_out;
+    const u32x4* const k = (const u32x4*)(kind == 1 ? p.v : p.k);
+    u32x4* const k_out = (u32x4*)(kind == 1 ? p.v_out : p.k_out);
+    const u32x4* const v = (const u32x4*)p.v;
+    u32x4* const v_out = (u32x4*)p.v_out;
     const int rows = kThreads / width, mine = tid / width, piece = seg * width + tid % width;  // rows at a time, this thread's and its piece
     // whether anything is read from a place that is written: then every group of places is read before it is written
     bool ordered = false;
@@ -483,7 +529,7 @@ template <int KINDS> __global__ __launch_bounds__(kThreads) void compact_rows(Co
         }
         __syncthreads();
         for (int e0 = 0; e0 < all; e0 += kEach * rows) {
-            uint4 x[kEach], y[kEach];
+            u32x4 x[kEach], y[kEach];
             // (what has no row of its own repeats the last one)
 #pragma unroll
             for (int e = 0; e < kEach; ++e) {
@@ -508,46 +554,6 @@ template <int KINDS> __global__ __launch_bounds__(kThreads) void compact_rows(Co
         }
         __syncthreads();
     }
-}
-
-// Weights, and the lengths: a workgroup a (sequence, KV head).
-__global__ __launch_bounds__(kThreads) void compact_weights(CompactParams p)
-{
-    constexpr int kEach = 4;
-    const int j = blockIdx.x % p.Hkv, b = blockIdx.x / p.Hkv, tid = threadIdx.x;
-    const int m = max(min(p.new_lens[b], p.max_new), 0);
-    if (j == 0 && tid == 0 && p.lens_out)
-        p.lens_out[b] = m;
-    if (!p.weights)
-        return;
-    const int* const source = p.source + b * p.seq_stride + j * p.head_stride;
-    const float* const w = p.weights + (long long)blockIdx.x * p.weights_stride;
-    float* const out = p.weights_out + (long long)blockIdx.x * p.weights_stride;
-    for (int i0 = 0; i0 < m; i0 += kEach * kThreads) {
-        int src[kEach];
-        float x[kEach];
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            const int i = i0 + e * kThreads + tid;
-            src[e] = i < m ? source[i] : -1;
-        }
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            const int i = i0 + e * kThreads + tid;
-            x[e] = src[e] >= i && src[e] < p.weights_stride ? w[src[e]] : 0.f;
-        }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            const int i = i0 + e * kThreads + tid;
-            if (src[e] >= i)
-                out[i] = x[e];
-        }
-    }
-    __syncthreads();
-    for (long long i = m + tid; i < p.weights_stride; i += kThreads)
-        out[i] = 0.f;
 }
 
 }  // namespace
@@ -597,18 +603,13 @@ hipError_t launch_compact_kv(const CompactParams& p, hipStream_t s)
             chunk *= 2;
         chunks = (p.max_new + chunk - 1) / chunk;
     }
-    if (p.max_new > 0) {
-        const dim3 grid((unsigned)((long long)pairs * kinds * segs * chunks));
-        if (kinds == 1)
-            hipLaunchKernelGGL(compact_rows<1>, grid, dim3(kThreads), 0, s, p, segs, p.head_u4 / segs, chunk);
-        else
-            hipLaunchKernelGGL(compact_rows<2>, grid, dim3(kThreads), 0, s, p, segs, p.head_u4 / segs, chunk);
-        const hipError_t rc = hipGetLastError();
-        if (rc != hipSuccess)
-            return rc;
-    }
-    if (p.weights || p.lens_out)
-        hipLaunchKernelGGL(compact_weights, dim3((unsigned)pairs), dim3(kThreads), 0, s, p);
+    const int copies = p.max_new > 0 ? pairs * kinds * segs * chunks : 0, others = p.weights || p.lens_out ? pairs : 0;
+    if (copies + others == 0)
+        return hipSuccess;
+    if (kinds == 1)
+        hipLaunchKernelGGL(compact_rows<1>, dim3((unsigned)(copies + others)), dim3(kThreads), 0, s, p, segs, p.head_u4 / segs, chunk, copies);
+    else
+        hipLaunchKernelGGL(compact_rows<2>, dim3((unsigned)(copies + others)), dim3(kThreads), 0, s, p, segs, p.head_u4 / segs, chunk, copies);
     return hipGetLastError();
 }
 
