@@ -274,6 +274,85 @@ def _check_penalties(sampler: DeviceSampler, raw, penalties: dict) -> None:
     _require(_on_one_gpu(raw, to, *penalties.values()), "everything has to be on one GPU")
 
 
+class DeviceLogprobs:
+    """How probable given tokens are under their rows' logits, and what stood beside them.  logits: [rows, vocab], fp32 or bf16 (a row
+    contiguous); tokens: int32 [rows] on the device, read when `run` is called (a sampler's `tokens`, or a prompt's next ones);
+    temperature: float [rows] (a sampler's: 0 counts as 1) or None.  `run` fills logprobs, ranks, entropy, lse [rows] and top_tokens,
+    top_logprobs [rows, num_top]."""
+
+    def __init__(self, logits, tokens, temperature=None, num_top: int = 0):
+        _require(logits.dtype in (torch.bfloat16, torch.float32) and logits.dim() == 2, "logits are bfloat16 or float32 [rows, vocab]")
+        rows, vocab = logits.shape
+        _require(logits[:1].is_contiguous() and (rows < 2 or logits.stride(0) >= vocab), "a row of logits has to be contiguous")
+        _require(tokens.dtype == torch.int32 and tokens.is_contiguous() and tokens.numel() == rows, "tokens are int32, one for every row")
+        _require(temperature is None or temperature.dtype == torch.float32 and temperature.is_contiguous() and temperature.numel() == rows,
+                 "temperature is float32, one for every row")
+        _require(0 <= num_top <= min(vocab, 64), "num_top is 0 to 64, and no more than the vocabulary")
+        _require(_on_one_gpu(logits, tokens, temperature), "everything has to be on one GPU")
+        self.logits, self.tokens, self.temperature, self.num_top = logits, tokens, temperature, num_top
+        empty = lambda *n, t=torch.float32: torch.empty(n, dtype=t, device=logits.device)  # noqa: E731
+        self.logprobs, self.entropy, self.lse = empty(rows), empty(rows), empty(rows)
+        self.ranks = empty(rows, t=torch.int32)
+        self.top_tokens, self.top_logprobs = empty(rows, num_top, t=torch.int32), empty(rows, num_top)
+        self.workspace = empty(max(B.token_logprobs_workspace_size(rows, vocab, num_top), 256), t=torch.uint8)
+
+    def run(self, stream=None) -> None:
+        rows, vocab = self.logits.shape
+        if rows == 0:
+            return  # (tensors without elements have no address to hand on)
+        top = (self.top_tokens, self.top_logprobs) if self.num_top else (None, None)
+        B.token_logprobs(self.logits, B.SPD_BF16 if self.logits.dtype == torch.bfloat16 else B.SPD_F32, rows, vocab,
+                         self.logits.stride(0) if rows > 1 else vocab, self.temperature, self.tokens, self.num_top, self.logprobs,
+                         self.ranks, self.entropy, self.lse, *top, self.workspace, stream)
+
+
+class DeviceEviction:
+    """Keeps the private suffixes of a decode call within bounds.  `accumulate`, after the attention of every step, adds what each
+    cached token got to its weight (`decay` times what it had); `evict`, when the suffixes are full or before, leaves the `budget` tokens
+    of every sample and KV head that weigh most, the first `sinks` and the last `recent` among them, in the front of the sample's own
+    slots or pages, and sets suffix_lens.  Weights belong to tokens: they move with them, and a token appended starts from 0.  Where
+    suffixes are set back by anything else, `reset` forgets all weights.  The calls launch kernels only and can be captured."""
+
+    def __init__(self, attn: DeviceAttn, budget: int, sinks: int = 4, recent: int = 32, decay: float = 1.0):
+        n, hq, d = attn.q.shape
+        hkv, room = attn.desc.num_kv_heads, attn.max_suffix_len
+        _require(0 < budget <= room, "the budget is 1 to max_suffix_len tokens")
+        _require(sinks >= 0 and recent >= 0, "sinks and recent are counts")
+        _require(attn.lse is not None, "the decode call has to leave its log-sum-exps")
+        dev = attn.q.device
+        self.attn, self.budget, self.sinks, self.recent, self.decay = attn, budget, sinks, recent, decay
+        self.desc = B.make_prompt_desc(dtype=attn.desc.dtype, num_q_heads=hq, num_kv_heads=hkv, head_dim=d, num_prompts=n,
+                                       page_size=attn.desc.page_size, causal=False, sm_scale=attn.desc.sm_scale)
+        self.one_each = torch.arange(n + 1, dtype=torch.int32, device=dev)
+        if attn.desc.page_size:
+            self.starts = attn.suffix_page_indptr
+        else:
+            _require(n * room < 2 ** 31, "contiguous suffixes of 2^31 tokens and more have no 32-bit starts")
+            self.starts = self.one_each * room
+        self.weights = torch.zeros((n, hkv, room), dtype=torch.float32, device=dev)
+        self.source = torch.empty((n, hkv, budget), dtype=torch.int32, device=dev)
+        self.new_lens = torch.empty(n, dtype=torch.int32, device=dev)
+        size = max(B.accumulate_kv_weights_workspace_size(self.desc, n, 1, room), B.select_kv_tokens_workspace_size(n, hkv, room), 256)
+        self.workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+
+    def reset(self) -> None:
+        self.weights.zero_()
+
+    def accumulate(self, stream=None) -> None:
+        a = self.attn
+        B.accumulate_kv_weights(self.desc, a.q, a.k_suffix, self.one_each, a.suffix_lens, self.starts, a.suffix_page_indices, a.lse,
+                                a.q.shape[0], 1, a.max_suffix_len, self.decay, self.weights, self.weights, self.weights.stride(1),
+                                self.workspace, stream)
+
+    def evict(self, stream=None) -> None:
+        a, (n, hkv, room) = self.attn, self.weights.shape
+        B.select_kv_tokens(self.weights, room, n, hkv, a.suffix_lens, room, None, self.budget, self.sinks, self.recent, self.source,
+                           self.budget, self.new_lens, self.workspace, stream)
+        B.compact_kv(self.desc, self.source, self.source.stride(0), self.source.stride(1), self.new_lens, self.budget, self.starts,
+                     a.suffix_page_indices, a.k_suffix, a.v_suffix, self.starts, a.suffix_page_indices, a.k_suffix, a.v_suffix,
+                     self.weights, self.weights, room, a.suffix_lens, stream)
+
+
 class DecodeLoop:
     """A loop of decode steps on the device: append the step's K/V (synthetic: there are no
     weights), attention, sampling; lengths, finished flags and the step counter live on the
@@ -286,18 +365,27 @@ class DecodeLoop:
     drawn before it).  How many there are follows the step counter: a loop whose counter is set back starts
     from none, whatever its record still holds.
 
+    With `logprobs` (a DeviceLogprobs of the sampler's `tokens`) every step says how probable what it drew was:
+    logprobs_steps, ranks_steps, entropy_steps [steps, rows] and top_tokens_steps, top_logprobs_steps [steps, rows, num_top].  With
+    `eviction` (a DeviceEviction of `attn`) every step's attention adds to the weights of the tokens it looked at; `eviction.evict()`
+    between two steps, before the suffixes are full, makes room (a full suffix takes no new token); lens_steps has what the next step finds.
+
     Per-step inputs are rows of tensors indexed by the device-side step counter:
       q_steps [steps, N, Hq, D], k_steps / v_steps [steps, N, Hkv, D], u_steps [steps, rows].
     The logits are the same every step (only the uniforms change); `tokens_steps`, `out_steps`
     and `lens_steps` record every step's results for checking."""
 
     def __init__(self, attn: DeviceAttn, sampler: DeviceSampler, q_steps, k_steps, v_steps, u_steps,
-                 end_token: int = -1, one_launch: bool = True, raw_logits=None, penalties: Optional[dict] = None):
+                 end_token: int = -1, one_launch: bool = True, raw_logits=None, penalties: Optional[dict] = None,
+                 logprobs: Optional[DeviceLogprobs] = None, eviction: Optional[DeviceEviction] = None):
         if (raw_logits is None) != (penalties is None) or (penalties is not None and not one_launch):
             raise ValueError("raw_logits and penalties go together, and need one_launch")
         if penalties is not None:
             _check_penalties(sampler, raw_logits, penalties)
+        _require(logprobs is None or logprobs.tokens is sampler.tokens, "logprobs have to be those of the sampler's tokens")
+        _require(eviction is None or eviction.attn is attn, "eviction has to be that of this attention call")
         self.attn, self.sampler = attn, sampler
+        self.logprobs, self.eviction = logprobs, eviction
         self.one_launch = one_launch
         self.q_steps, self.k_steps, self.v_steps, self.u_steps = q_steps, k_steps, v_steps, u_steps
         self.steps = q_steps.shape[0]
@@ -316,15 +404,22 @@ class DecodeLoop:
         self._select = B.make_row_copies([(q_steps, attn.q, nbytes(attn.q)), (k_steps, self.k_cur, nbytes(self.k_cur)),
                                           (v_steps, self.v_cur, nbytes(self.v_cur)),
                                           (u_steps, sampler.uniforms, nbytes(sampler.uniforms))])
+        said = []  # what the log probabilities' call leaves, and where every step's goes
+        if logprobs is not None:
+            for name in ("logprobs", "ranks", "entropy") + (("top_tokens", "top_logprobs") if logprobs.num_top else ()):
+                x = getattr(logprobs, name)
+                steps = torch.zeros((self.steps,) + tuple(x.shape), dtype=x.dtype, device=dev)
+                setattr(self, name + "_steps", steps)
+                said.append((x, steps, nbytes(x)))
         self._record = B.make_row_copies([(sampler.tokens, self.tokens_steps, nbytes(sampler.tokens)),
                                           (attn.out, self.out_steps, nbytes(attn.out)),
-                                          (attn.suffix_lens, self.lens_steps, nbytes(attn.suffix_lens))])
+                                          (attn.suffix_lens, self.lens_steps, nbytes(attn.suffix_lens))] + said)
         # one launch per step: the lengths are recorded by the append itself, K and V rows are read
         # straight from the step tensors
         self._select_qu = B.make_row_copies([(q_steps, attn.q, nbytes(attn.q)),
                                              (u_steps, sampler.uniforms, nbytes(sampler.uniforms))])
         self._record_to = B.make_row_copies([(sampler.tokens, self.tokens_steps, nbytes(sampler.tokens)),
-                                             (attn.out, self.out_steps, nbytes(attn.out))])
+                                             (attn.out, self.out_steps, nbytes(attn.out))] + said)
         self.raw_logits, self.penalties = raw_logits, None
         if penalties is not None:
             # one more step input: step t's history is the record's first t rows (steps past the last repeat its inputs,
@@ -343,6 +438,16 @@ class DecodeLoop:
         B.penalize_logits(raw, B.SPD_BF16 if raw.dtype == torch.bfloat16 else B.SPD_F32, raw.shape[0], raw.shape[1], raw.stride(0),
                           self.penalties, s.logits, s.logits.stride(0))
 
+    def _attend(self) -> None:
+        self.attn.run()
+        if self.eviction is not None:
+            self.eviction.accumulate()
+
+    def _sample(self) -> None:
+        self.sampler.run()
+        if self.logprobs is not None:
+            self.logprobs.run()
+
     def one_step(self) -> None:
         """Enqueues one decode step on the current stream (capturable: kernel launches only).  With
         `one_launch` the results of a step are recorded by the next step's advance call, those of
@@ -353,17 +458,17 @@ class DecodeLoop:
                                   self.v_steps, a.k_suffix, a.v_suffix, a.suffix_lens, a.suffix_page_indptr,
                                   a.suffix_page_indices, a.max_suffix_len, s.tokens, self.end_token, self.finished,
                                   self.lens_steps)
-            a.run()
+            self._attend()
             if self.penalties is not None:
                 self._shape_logits()
-            s.run()
+            self._sample()
             return
         B.decode_step_select(self.step, self.steps, self._select)
         B.append_suffix_kv(a.desc, self.k_cur, self.v_cur, a.k_suffix, a.v_suffix, a.suffix_lens,
                            a.suffix_page_indptr, a.suffix_page_indices, a.max_suffix_len,
                            s.tokens, self.end_token, self.finished)
-        a.run()
-        s.run()
+        self._attend()
+        self._sample()
         B.decode_step_record(self.step, self.steps, self._record)
 
     def flush(self) -> None:
