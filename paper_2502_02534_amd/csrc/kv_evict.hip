@@ -53,11 +53,13 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
 {
     constexpr int kTokens = 64 * WAVES * V;
     constexpr int kBits = V < 16 ? 0 : WAVES == 1 ? 9 : 11;  // of the histogram
-    constexpr int kBins = 1 << kBits, kOwn = kBins / 64;      // and a lane's bins of it
+    constexpr int kBins = 1 << kBits, kOwn = kBins < 64 ? 1 : kBins / 64;  // and a lane's bins of it, with a place between two lanes' (bank conflicts)
+    constexpr int kPlaces = (kBins + 64 + 3) / 4 * 4;
+    const auto place = [](int bin) { return bin + bin / kOwn; };
     static_assert(WAVES == 1 || ROWS == 1, "wavefronts of one row wait for each other");
     __shared__ unsigned short moving[ROWS][kTokens / 2];  // (no more than half of the tokens fill gaps)
     __shared__ int counts[2][WAVES], sums[3][WAVES];
-    __shared__ __align__(16) int hist[kBits ? ROWS : 1][kBits ? kBins : 4];
+    __shared__ __align__(16) int hist[kBits ? ROWS : 1][kBits ? kPlaces : 4];
     __shared__ unsigned few[ROWS][64];
     __shared__ int num_few[ROWS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -135,7 +137,7 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
         }
         if (kBits) {
             int4* const own = (int4*)hist[local];
-            for (int i = threadIdx.x % (64 * WAVES); i < kBins / 4; i += 64 * WAVES)
+            for (int i = threadIdx.x % (64 * WAVES); i < kPlaces / 4; i += 64 * WAVES)
                 own[i] = make_int4(0, 0, 0, 0);
             if (threadIdx.x % (64 * WAVES) == 0)
                 num_few[local] = 0;
@@ -168,28 +170,52 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
 #pragma unroll
             for (int v = 0; v < V; ++v)
                 if (v < groups && key[v])
-                    atomicAdd(&bins[key[v] >> shift], 1);
+                    atomicAdd(&bins[place((int)(key[v] >> shift))], 1);
             if (WAVES > 1)
                 __syncthreads();
             else
                 __builtin_amdgcn_wave_barrier();
-            int here = 0;
+            // the bin of the c-th largest, how many lie above it and in it
+            int bin = 0, above = 0, inside = 0;
+            if (w == 0) {
+                int here = 0;
 #pragma unroll
-            for (int i = 0; i < kOwn; ++i)
-                here += bins[lane * kOwn + i];
-            int from = here;  // keys of this lane's bins and of those above
+                for (int i = 0; i < kOwn; ++i)
+                    here += bins[place(lane * kOwn + i)];
+                int from = here;  // keys of this lane's bins and of those above
 #pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int y = __shfl_down(from, o);
-                from += lane + o < 64 ? y : 0;
+                for (int o = 1; o < 64; o <<= 1) {
+                    const int y = __shfl_down(from, o);
+                    from += lane + o < 64 ? y : 0;
+                }
+                const int owner = 63 - __clzll((long long)__ballot(from >= a.c));
+                const int over = __builtin_amdgcn_readlane(from - here, owner);
+                // the owner's bins, a lane each, from the last one down
+                const int mine = lane < kOwn ? bins[place(owner * kOwn + kOwn - 1 - lane)] : 0;
+                int upto = mine;
+#pragma unroll
+                for (int o = 1; o < kOwn; o <<= 1) {
+                    const int y = __shfl_up(upto, o);
+                    upto += lane >= o ? y : 0;
+                }
+                const int at = __ffsll((unsigned long long)__ballot(lane < kOwn && over + upto >= a.c)) - 1;
+                bin = owner * kOwn + kOwn - 1 - at;
+                inside = __builtin_amdgcn_readlane(mine, at);
+                above = over + __builtin_amdgcn_readlane(upto - mine, at);
             }
-            const int owner = 63 - __clzll((long long)__ballot(from >= a.c));
-            int above = __builtin_amdgcn_readlane(from - here, owner), bin = owner * kOwn + kOwn - 1;
-            while (above + bins[bin] < a.c)
-                above += bins[bin--];
-            const int inside = __builtin_amdgcn_readfirstlane(bins[bin]);
-            above = __builtin_amdgcn_readfirstlane(above);
-            floor = (unsigned)__builtin_amdgcn_readfirstlane(bin) << shift;
+            if (WAVES > 1) {
+                __shared__ int chosen[3];
+                if (threadIdx.x == 0) {
+                    chosen[0] = bin;
+                    chosen[1] = above;
+                    chosen[2] = inside;
+                }
+                __syncthreads();
+                bin = __builtin_amdgcn_readfirstlane(chosen[0]);
+                above = __builtin_amdgcn_readfirstlane(chosen[1]);
+                inside = __builtin_amdgcn_readfirstlane(chosen[2]);
+            }
+            floor = (unsigned)bin << shift;
             exact = above + inside == a.c;
             top = shift - 1;
             if (!exact && inside <= 64) {

@@ -7,7 +7,9 @@
 // part of the rows, which a second launch adds in order), so no sum depends on who comes first.
 //
 //   few rows (up to 32: one step's queries over a sample's own tokens): a wavefront keeps the rows' fragments in registers and streams
-//     the keys, the next tile's loads under way while it works on this one.  Bound: HBM, K read once.
+//     the keys: whole lines, marked as used once, the next tile's under way while it works on this one, which goes through LDS of the
+//     wavefront's own to the lanes that multiply it.  Bound: HBM, K read once (1024 samples of up to 2048 paged tokens, 8 heads of 128
+//     channels, 2.2 GB: 387 us, 5.7 TB/s; without the products the same; loads in the products' order 449).
 //   many rows (samples over their shared prompt, a prompt over itself): a wavefront keeps 64 tokens' keys in registers (32 in fp32),
 //     the rows pass by in blocks of 32: in bf16 through LDS, shared by the four wavefronts of a workgroup, with the
 //     exponentials of one block between the products of the next.  Bound: matrix pipe and vector ALU alike (16 products of 32 clocks
@@ -26,6 +28,10 @@ typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4;
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
 
 constexpr int kWaves = 4;
+// Wavefronts of a workgroup where each works by itself.  Where pages lie anywhere, workgroups of one spread the heads of a page over the chip:
+// 1024 samples of up to 2048 paged tokens, 8 heads of 128 channels, 1 / 2 / 4 / 8 of them 387 / 438 / 454 / 405 us (contiguous, up to 1024
+// tokens: 203 / 192 / 192 / 199), 256 samples of 64 channels 55 / 60 / 61 / 60.
+constexpr int few_waves(bool paged) { return paged ? 1 : 4; }
 
 __device__ __forceinline__ bf16x8 as_bf16x8(const uint4& v) { return *reinterpret_cast<const bf16x8*>(&v); }
 __device__ __forceinline__ float part_of(const uint4& v, int e)
@@ -96,11 +102,12 @@ template <bool BF16> __device__ __forceinline__ floatx4 product16(const uint4& k
 
 // P: 16-byte pieces of a padded head (D = 64, 128, 256 in bf16: 8, 16, 32); SUB: 16-token halves of a tile; NB: blocks of 16 rows.
 template <bool BF16, int P, int SUB, int NB, bool PAGED>
-__global__ __launch_bounds__(kWaves * 64) void kv_weights_few(KvWeightsParams p, int chunk, int chunks)
+__global__ __launch_bounds__(few_waves(PAGED) * 64) void kv_weights_few(KvWeightsParams p, int chunk, int chunks)
 {
-    constexpr int kSteps = P / 4, kTile = 16 * SUB;
+    constexpr int kSteps = P / 4, kTile = 16 * SUB, kLoads = kTile * P / 64, kPitch = P + 1, kFewWaves = few_waves(PAGED);  // (a piece between rows: bank conflicts)
+    __shared__ uint4 lds[kFewWaves][kTile * kPitch];
     const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
-    const int item = __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + (threadIdx.x >> 6));
+    const int item = __builtin_amdgcn_readfirstlane(blockIdx.x * kFewWaves + (threadIdx.x >> 6));
     // KV head fastest: the heads of a token lie beside each other
     const int j = item % p.Hkv, rest = item / p.Hkv, b = rest % p.B, at = rest / p.B;
     if (at >= chunks)
@@ -133,23 +140,47 @@ __global__ __launch_bounds__(kWaves * 64) void kv_weights_few(KvWeightsParams p,
     const int mine = 16 * (col >> 2) + 4 * g + (col & 3);
     const bool stores = col < 4 * SUB;
     const long long out_at = ((long long)b * p.Hkv + j) * p.stride;
-    const auto load = [&](int tb, uint4 (&k)[SUB][kSteps], float& old) __attribute__((always_inline)) {
+    // A tile's rows are loaded as they lie, P pieces one after another (whole lines, used once), and get to the lanes that multiply them
+    // through LDS of the wavefront's own.
+    uint4* const mine_lds = lds[threadIdx.x >> 6];
+    const int in_row = lane % P, in_tile = lane / P;  // piece and first row of a lane's loads
+    const bool has_piece = in_row < head_pieces;
+    // (tiles start with a page; its number is fetched a tile ahead of its rows)
+    const int last_page = (t1 - 1) >> 4;
+    int next_page[SUB];
+    const auto fetch_pages = [&](int tb) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < SUB; ++u) {
-            const uint4* const row = keys.row(min(tb + 16 * u + col, t1 - 1));
+        for (int u = 0; u < SUB; ++u)
+            next_page[u] = PAGED ? keys.pages[min((tb >> 4) + u, last_page)] : 0;
+    };
+    const auto load = [&](int tb, uint4 (&k)[kLoads], float& old) __attribute__((always_inline)) {
+        typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                k[u][s] = make_uint4(0u, 0u, 0u, 0u);
-                if (4 * s + g < head_pieces)
-                    k[u][s] = row[4 * s + g];
-            }
+        for (int i = 0; i < kLoads; ++i) {
+            const int t = min(tb + i * (64 / P) + in_tile, t1 - 1);
+            const uint4* const row = PAGED ? keys.base + next_page[i * (64 / P) / 16] * keys.page_pieces + keys.head_at + (t & 15) * keys.token_pieces
+                                           : keys.row(t);
+            const u32x4 v = __builtin_nontemporal_load((const u32x4*)(row + (has_piece ? in_row : 0)));
+            k[i] = has_piece ? make_uint4(v[0], v[1], v[2], v[3]) : make_uint4(0u, 0u, 0u, 0u);
         }
+        fetch_pages(tb + kTile);
         old = 0.f;
         if (p.weights && stores && tb + mine < t1)
             old = p.weights[out_at + tb + mine];
     };
-    const auto work = [&](int tb, const uint4 (&k)[SUB][kSteps], float old) __attribute__((always_inline)) {
+    const auto work = [&](int tb, const uint4 (&loaded)[kLoads], float old) __attribute__((always_inline)) {
         float total = 0.f;
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            mine_lds[(i * (64 / P) + in_tile) * kPitch + in_row] = loaded[i];
+        __builtin_amdgcn_wave_barrier();
+        uint4 k[SUB][kSteps];
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s)
+                k[u][s] = mine_lds[(16 * u + col) * kPitch + 4 * s + g];
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
             floatx4 sum = {0.f, 0.f, 0.f, 0.f};
@@ -174,8 +205,9 @@ __global__ __launch_bounds__(kWaves * 64) void kv_weights_few(KvWeightsParams p,
         if (stores && tb + mine < t1)
             p.weights_out[out_at + tb + mine] = p.weights ? __builtin_fmaf(p.decay, old, total) : total;
     };
-    uint4 ka[SUB][kSteps], kb[SUB][kSteps];
+    uint4 ka[kLoads], kb[kLoads];
     float oa, ob;
+    fetch_pages(t0);
     load(t0, ka, oa);
     for (int tb = t0; tb < t1; tb += 2 * kTile) {
         if (tb + kTile < t1)
@@ -536,11 +568,12 @@ template <bool BF16, int P, int SUB, int NB> void few(const KvWeightsParams& p, 
     while (chunk > 16 * SUB && pairs * ((p.max_kv + chunk - 1) / chunk) < 4096)
         chunk /= 2;
     const int chunks = (p.max_kv + chunk - 1) / chunk;
-    const dim3 grid((unsigned)((pairs * chunks + kWaves - 1) / kWaves));
+    const int waves = few_waves(p.page_size != 0);
+    const dim3 grid((unsigned)((pairs * chunks + waves - 1) / waves)), block(waves * 64);
     if (p.page_size)
-        hipLaunchKernelGGL((kv_weights_few<BF16, P, SUB, NB, true>), grid, dim3(kWaves * 64), 0, s, p, chunk, chunks);
+        hipLaunchKernelGGL((kv_weights_few<BF16, P, SUB, NB, true>), grid, block, 0, s, p, chunk, chunks);
     else
-        hipLaunchKernelGGL((kv_weights_few<BF16, P, SUB, NB, false>), grid, dim3(kWaves * 64), 0, s, p, chunk, chunks);
+        hipLaunchKernelGGL((kv_weights_few<BF16, P, SUB, NB, false>), grid, block, 0, s, p, chunk, chunks);
 }
 
 }  // namespace
