@@ -23,8 +23,8 @@ constexpr int kLong = 1024;    // of rows that no registers hold
 // Weights as whole numbers in their order; NaN below all.
 __device__ __forceinline__ unsigned key_of(float w)
 {
-    const unsigned u = __float_as_uint(w == 0.f ? 0.f : w);
-    return w != w ? 1u : (u & 0x80000000u) ? ~u : (u | 0x80000000u);  // (0: no token)
+    const int u = __float_as_int(w + 0.f);  // (both zeros are one value)
+    return w != w ? 1u : (unsigned)(u ^ (u >> 31 | (int)0x80000000));  // (0: no token)
 }
 
 __device__ __forceinline__ int lanes_below(unsigned long long mask)
@@ -81,23 +81,34 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
     }
     const float* const weights = p.weights + row * p.stride;
     const int middle = a.n - a.r, early = a.m - a.r;  // tokens f .. middle - 1 are chosen from; places before `early` have gaps
+    // (four groups of 64 tokens at a time, as far as there are any)
     float x[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int t = t0 + 64 * v + lane;
-        x[v] = 0.f;
-        if (t >= a.f && t < middle)
-            x[v] = weights[t];
-    }
-    unsigned key[V];
-    unsigned lowest = ~0u, highest = 0u;
+    for (int v0 = 0; v0 < V; v0 += 4)
+        if (t0 + 64 * v0 < middle) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int t = t0 + 64 * v + lane;
-        const bool inside = t >= a.f && t < middle;
-        key[v] = inside ? key_of(x[v]) : 0u;
-        lowest = inside ? min(lowest, key[v]) : lowest;
-        highest = max(highest, key[v]);
+            for (int v = v0; v < v0 + 4; ++v) {
+                const int t = t0 + 64 * v + lane;
+                x[v] = weights[min(max(t, a.f), middle - 1)];
+            }
+        }
+    unsigned key[V];
+    unsigned lowest = ~0u, highest = 0u;  // (less one)
+#pragma unroll
+    for (int v0 = 0; v0 < V; v0 += 4) {
+        if (t0 + 64 * v0 < middle) {
+#pragma unroll
+            for (int v = v0; v < v0 + 4; ++v) {
+                const int t = t0 + 64 * v + lane;
+                key[v] = t >= a.f && t < middle ? key_of(x[v]) : 0u;
+                lowest = min(lowest, key[v] - 1u);
+                highest = max(highest, key[v]);
+            }
+        } else {
+#pragma unroll
+            for (int v = v0; v < v0 + 4; ++v)
+                key[v] = 0u;
+        }
     }
     // a number over the row's wavefronts (every wavefront calls it as often)
     int calls = 0;
@@ -156,21 +167,21 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
         }
         lowest = __builtin_amdgcn_readfirstlane(lowest);
         highest = __builtin_amdgcn_readfirstlane(highest);
-        // from the lowest on: 1 and more
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            key[v] = key[v] ? key[v] - lowest + 1u : 0u;
-        int top = 31 - __clz((int)(highest - lowest + 1u));
-        floor = 0u;
+        floor = lowest + 1u;
+        int top = highest != floor ? 31 - __clz((int)(highest - floor)) : -1;
         bool exact = false;
         if (kBits && top >= kBits) {
             // the first kBits bits from a histogram, and the others of the few keys that share them with the c-th largest
             const int shift = top + 1 - kBits;
             int* const bins = hist[local];
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (v < groups && key[v])
-                    atomicAdd(&bins[place((int)(key[v] >> shift))], 1);
+            for (int v0 = 0; v0 < V; v0 += 4)
+                if (v0 < groups) {
+#pragma unroll
+                    for (int v = v0; v < v0 + 4; ++v)
+                        if (key[v])
+                            atomicAdd(&bins[place((int)((key[v] - floor) >> shift))], 1);
+                }
             if (WAVES > 1)
                 __syncthreads();
             else
@@ -215,23 +226,26 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
                 above = __builtin_amdgcn_readfirstlane(chosen[1]);
                 inside = __builtin_amdgcn_readfirstlane(chosen[2]);
             }
-            floor = (unsigned)bin << shift;
+            floor += (unsigned)bin << shift;
             exact = above + inside == a.c;
             top = shift - 1;
             if (!exact && inside <= 64) {
-                const unsigned shared = floor >> shift;
 #pragma unroll
-                for (int v = 0; v < V; ++v)
-                    if (v < groups && key[v] >> shift == shared && key[v])
-                        few[local][atomicAdd(&num_few[local], 1)] = key[v];
+                for (int v0 = 0; v0 < V; v0 += 4)
+                    if (v0 < groups) {
+#pragma unroll
+                        for (int v = v0; v < v0 + 4; ++v)
+                            if ((key[v] - floor) >> shift == 0u)
+                                few[local][atomicAdd(&num_few[local], 1)] = key[v];
+                    }
                 if (WAVES > 1)
                     __syncthreads();
                 else
                     __builtin_amdgcn_wave_barrier();
                 const unsigned mine = lane < inside ? few[local][lane] : 0u;
                 for (int bit = top; bit >= 0 && !exact; --bit) {
-                    const unsigned cand = floor | (1u << bit);
-                    const int reach = above + __popcll(__ballot(mine >= cand));
+                    const unsigned cand = floor + (1u << bit);
+                    const int reach = cand > floor ? above + __popcll(__ballot(mine >= cand)) : 0;
                     if (reach >= a.c) {
                         floor = cand;
                         exact = reach == a.c;
@@ -241,9 +255,9 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
             }
         }
         for (int bit = top; bit >= 0 && !exact; --bit) {
-            const unsigned cand = floor | (1u << bit);
+            const unsigned cand = floor + (1u << bit);
             const int reach = count(cand);
-            if (reach >= a.c) {
+            if (cand > floor && reach >= a.c) {
                 floor = cand;
                 exact = reach == a.c;
             }
@@ -279,12 +293,16 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
         }
         int tied = tied0, gaps = 0, moves = 0;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int t = t0 + 64 * v + lane;
-            const bool s = stays(v, tied) || t < a.f;
-            gaps += __popcll(__ballot(!s && t < early));
-            moves += __popcll(__ballot(s && t >= early && t < middle));
-        }
+        for (int v0 = 0; v0 < V; v0 += 4)
+            if (v0 < groups || t0 + 64 * v0 < early) {
+#pragma unroll
+                for (int v = v0; v < v0 + 4; ++v) {
+                    const int t = t0 + 64 * v + lane;
+                    const bool s = stays(v, tied) || t < a.f;
+                    gaps += __popcll(__ballot(!s && t < early));
+                    moves += __popcll(__ballot(s && t >= early && t < middle));
+                }
+            }
         if (lane == 0) {
             sums[1][w] = gaps;
             sums[2][w] = moves;
@@ -300,7 +318,7 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
         int tied = tied0, at = move0;
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            if (v < groups) {
+            if (v < groups && (t0 + 64 * v + 63 >= early || ties > 0)) {
                 const int t = t0 + 64 * v + lane;
                 const bool move = (stays(v, tied) || t < a.f) && t >= early && t < middle;
                 const unsigned long long moves = __ballot(move);
