@@ -97,8 +97,8 @@ template <bool BF16> struct Chunk {
     }
 };
 
-// The k-th largest of a wavefront's keys, S a lane: `floor` is it (exact: false), or a number that exactly k of them reach (exact: true).
-template <int S> __device__ __forceinline__ unsigned kth_key(const unsigned (&key)[S], int k, bool& exact)
+// A number that at least k of a wavefront's keys, S a lane, reach, and no more than `most` where there is one; else the k-th largest.
+template <int S> __device__ __forceinline__ unsigned threshold_key(const unsigned (&key)[S], int k, int most)
 {
     // leading bits that all keys have
     const unsigned one = __builtin_amdgcn_readfirstlane(key[0]);
@@ -110,12 +110,11 @@ template <int S> __device__ __forceinline__ unsigned kth_key(const unsigned (&ke
     for (int o = 32; o > 0; o >>= 1)
         differ |= __shfl_xor(differ, o);
     differ = __builtin_amdgcn_readfirstlane(differ);
-    exact = false;
     if (differ == 0u)
         return one;
     const int top_bit = 31 - __clz((int)differ);
     unsigned floor = one & ~((2u << top_bit) - 1u);
-    for (int bit = top_bit; bit >= 0 && !exact; --bit) {
+    for (int bit = top_bit; bit >= 0; --bit) {
         const unsigned cand = floor | (1u << bit);
         int count = 0;
 #pragma unroll
@@ -123,13 +122,14 @@ template <int S> __device__ __forceinline__ unsigned kth_key(const unsigned (&ke
             count += __popcll(__ballot(key[s] >= cand));
         if (count >= k) {
             floor = cand;
-            exact = count == k;
+            if (count <= most)
+                break;
         }
     }
     return floor;
 }
 
-// The same of n keys; of(i): key i (LDS).
+// The k-th largest of n keys, of(i) each (LDS): it (exact: false), or a number that exactly k of them reach (exact: true).
 template <class F> __device__ __forceinline__ unsigned kth_key(F of, int n, int k, bool& exact)
 {
     const int lane = threadIdx.x & 63;
@@ -365,8 +365,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(BF16 ||
 #pragma unroll
         for (int w = 0; w < kWaves; ++w)
             key[w] = lists.thread_keys[w * 64 + lane];
-        bool exact;
-        const unsigned t = kth_key(key, p.top, exact);
+        const unsigned t = threshold_key(key, p.top, min(p.top + p.top / 2 + 2, kHot));
         if (lane == 0)
             threshold = t;
     }
