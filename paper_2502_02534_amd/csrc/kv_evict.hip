@@ -185,7 +185,7 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
             if (WAVES > 1)
                 __syncthreads();
             else
-                __builtin_amdgcn_wave_barrier();
+                wave_sync();
             // the bin of the c-th largest, how many lie above it and in it
             int bin = 0, above = 0, inside = 0;
             if (w == 0) {
@@ -241,7 +241,7 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
                 if (WAVES > 1)
                     __syncthreads();
                 else
-                    __builtin_amdgcn_wave_barrier();
+                    wave_sync();
                 const unsigned mine = lane < inside ? few[local][lane] : 0u;
                 for (int bit = top; bit >= 0 && !exact; --bit) {
                     const unsigned cand = floor + (1u << bit);
@@ -330,7 +330,7 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
     if (WAVES > 1)
         __syncthreads();
     else
-        __builtin_amdgcn_wave_barrier();
+        wave_sync();
     if (t0 < early) {
         int tied = tied0, at = gap0;
 #pragma unroll

@@ -170,11 +170,11 @@ __global__ __launch_bounds__(few_waves(PAGED) * 64) void kv_weights_few(KvWeight
     };
     const auto work = [&](int tb, const uint4 (&loaded)[kLoads], float old) __attribute__((always_inline)) {
         float total = 0.f;
-        __builtin_amdgcn_wave_barrier();
+        wave_sync();
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
             mine_lds[(i * (64 / P) + in_tile) * kPitch + in_row] = loaded[i];
-        __builtin_amdgcn_wave_barrier();
+        wave_sync();
         uint4 k[SUB][kSteps];
 #pragma unroll
         for (int u = 0; u < SUB; ++u)

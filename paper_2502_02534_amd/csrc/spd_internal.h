@@ -282,6 +282,14 @@ struct CompactParams {
     int in_place;
 };
 
+// What a wavefront's lanes wrote to LDS is there for its other lanes (they run in step: no instruction, only an order for the compiler).
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
 // Index of the partial state of output row `row` (= n * Hq + h) in slot `slot`.
 __device__ __forceinline__ long long part_index(const AttnParams& p, long long row, int slot)
 {

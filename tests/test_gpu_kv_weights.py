@@ -134,6 +134,30 @@ def test_prompts_and_their_last_tokens(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hq,hkv", [(17, 1), (33, 1), (48, 1), (64, 2), (64, 1), (7, 1)])
+def test_large_and_odd_groups(dtype, hq, hkv):
+    """Groups that fill, split and overlap blocks of 16 and 32 rows, with one query and a few."""
+    Problem(dtype, hq, hkv, 64, [1] * 5, [0, 40, 17, 129, 300], page=16, elsewhere=3.0).check()
+    Problem(dtype, hq, hkv, 64, [3, 11], [150, 30], causal=True, seed=1).check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("g", [1, 3, 4])
+def test_parts_of_the_rows(dtype, g):
+    """Long prompts, whose rows are cut into parts, some of them empty, causal and not, beside one without queries."""
+    Problem(dtype, 2 * g, 2, 64, [1100 // g, 0, 3, 260], [1100 // g, 50, 300, 260], causal=True, seed=g).check()
+    Problem(dtype, g, 1, 64, [900 // g], [20], seed=g).check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_last_queries_of_the_last_row(dtype):
+    """The queries end where their tensor does, in the middle of a block."""
+    for n in (9, 17, 40):
+        Problem(dtype, 4, 1, 128, [n], [64]).check()
+        Problem(dtype, 12, 1, 128, [n], [64], causal=True).check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_more_queries_than_tokens(dtype):
     """Causal queries ahead of the first token see nothing; their lse is -inf."""
     Problem(dtype, 4, 2, 64, [40, 9], [25, 3], causal=True).check()
