@@ -515,7 +515,8 @@ template <int KINDS> __global__ __launch_bounds__(kThreads) void compact_rows(Co
         return;
     }
     constexpr int kEach = KINDS == 1 ? 4 : 8;  // rows a thread has under way
-    __shared__ long long from_at[kThreads], to_at[kThreads];
+    constexpr int kPlaces = 4 * kThreads;  // looked at in one go
+    __shared__ long long from_at[kPlaces], to_at[kPlaces];
     __shared__ int lds[kThreads / 64];
     __shared__ int below;
     int rest = blockIdx.x;
@@ -553,24 +554,44 @@ template <int KINDS> __global__ __launch_bounds__(kThreads) void compact_rows(Co
         __syncthreads();
         ordered = below != 0;
     }
-    for (int i0 = first; i0 < last; i0 += kThreads) {
-        // the places that get another token, listed
-        const int i = i0 + tid, src = i < last ? source[i] : -1;
-        const bool moves = src >= i && src < held && i < room && !(p.in_place && src == i);
-        const unsigned long long mask = __ballot(moves);
-        if (lane == 0)
-            lds[wave] = __popcll(mask);
+    for (int i0 = first; i0 < last; i0 += kPlaces) {
+        // the places that get another token, listed in ascending order: a thread looks at kPlaces / kThreads in a row
+        constexpr int kOwn = kPlaces / kThreads;
+        int src[kOwn], mine_moves = 0;
+        bool moves[kOwn];
+#pragma unroll
+        for (int o = 0; o < kOwn; ++o) {
+            const int i = i0 + tid * kOwn + o;
+            src[o] = i < last ? source[i] : -1;
+        }
+#pragma unroll
+        for (int o = 0; o < kOwn; ++o) {
+            const int i = i0 + tid * kOwn + o;
+            moves[o] = src[o] >= i && src[o] < held && i < room && !(p.in_place && src[o] == i);
+            mine_moves += moves[o];
+        }
+        int upto = mine_moves;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(upto, o);
+            upto += lane >= o ? y : 0;
+        }
+        if (lane == 63)
+            lds[wave] = upto;
         __syncthreads();
-        int at = lanes_below(mask), all = 0;
+        int at = upto - mine_moves, all = 0;
 #pragma unroll
         for (int w = 0; w < kThreads / 64; ++w) {
             at += w < wave ? lds[w] : 0;
             all += lds[w];
         }
-        if (moves) {
-            from_at[at] = row_at(p, p.pages, in0, j, src);
-            to_at[at] = row_at(p, p.out_pages, out0, j, i);
-        }
+#pragma unroll
+        for (int o = 0; o < kOwn; ++o)
+            if (moves[o]) {
+                from_at[at] = row_at(p, p.pages, in0, j, src[o]);
+                to_at[at] = row_at(p, p.out_pages, out0, j, i0 + tid * kOwn + o);
+                ++at;
+            }
         __syncthreads();
         for (int e0 = 0; e0 < all; e0 += kEach * rows) {
             u32x4 x[kEach], y[kEach];

@@ -493,55 +493,96 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void kv_weights_many
     store<32>(p, u, tw, sums);
 }
 
-// fp32: 32 tokens a wavefront, rows straight from memory (a product of fp32 takes 16 times as long).  P: 16-byte pieces of a padded head.
-template <int P, bool PAGED>
+// fp32: 32 tokens a wavefront; the rows go through LDS as in bf16, a block ahead (a product of fp32 takes 16 times as long).
+// P: 16-byte pieces of a padded head.
+template <int P>
 __global__ __launch_bounds__(kWaves * 64, P <= 32 ? 2 : 1) void kv_weights_many_f32(KvWeightsParams p)
 {
-    constexpr int kSteps = P / 2;
+    constexpr int kSteps = P / 2, kPitch = P + 1, kCopies = 32 * P / (kWaves * 64);
+    static_assert(32 * P % (kWaves * 64) == 0 && P % 2 == 0, "whole copies, and rows that end in another bank");
+    __shared__ uint4 lds[2][32 * kPitch];
     const Unit u = find_unit(p, kWaves * 32);
     if (!u.any)
         return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, h = lane >> 5;
     const int tw = u.t0 + wave * 32, head_pieces = p.D / 4, G = p.G;
-    if (tw >= u.L)
-        return;
-    uint4 k[kSteps];
-    const Keys<PAGED> keys(p, u.b, u.j, head_pieces);
-    const uint4* const row = keys.row(min(tw + col, u.L - 1));
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-        k[s] = make_uint4(0u, 0u, 0u, 0u);
-        if (2 * s + h < head_pieces)
-            k[s] = row[2 * s + h];
-    }
     float sums[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i)
         sums[i] = 0.f;
-#pragma unroll 1
-    for (int at = u.last - 1; at >= u.first; --at) {
-        const int r = at * 32 + col, rc = min(r, u.rows - 1), i = rc / G, g = rc % G;
-        const bool there = r < u.rows;
-        const float below = exponent_of(p.lse[(long long)(u.q0 + i) * p.Hq + u.j * G + g], there);
-        const int limit = !there ? -1 : p.causal ? u.L - u.n + i : u.L;
-        const uint4* const q = (const uint4*)p.q + (long long)(u.q0 + i) * (p.q_stride / 4) + (long long)(u.j * G + g) * head_pieces;
-        floatx16 c;
+    if (u.first < u.last) {
+        const uint4* const q_seq = (const uint4*)p.q + (long long)u.q0 * (p.q_stride / 4) + (long long)u.j * G * head_pieces;
+        uint4 staged[kCopies];
+        const auto fetch = [&](int at) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-            c[e] = 0.f;
+            for (int c = 0; c < kCopies; ++c) {
+                const int x = c * kWaves * 64 + tid, r = min(at * 32 + x / P, u.rows - 1), piece = x % P;
+                staged[c] = make_uint4(0u, 0u, 0u, 0u);
+                if (piece < head_pieces)
+                    staged[c] = q_seq[r / G * (p.q_stride / 4) + r % G * head_pieces + piece];
+            }
+        };
+        const auto put = [&](int slot) __attribute__((always_inline)) {
+#pragma unroll
+            for (int c = 0; c < kCopies; ++c) {
+                const int x = c * kWaves * 64 + tid;
+                lds[slot][x / P * kPitch + x % P] = staged[c];
+            }
+        };
+        float lse;
+        int query;
+        const auto fetch_lse = [&](int at) __attribute__((always_inline)) {
+            const int r = min(at * 32 + col, u.rows - 1);
+            query = r / G;
+            lse = p.lse[(long long)(u.q0 + query) * p.Hq + u.j * G + r % G];
+        };
+        fetch(u.last - 1);
+        fetch_lse(u.last - 1);
+        uint4 k[kSteps];
+        const int tk = min(tw + col, u.L - 1);
+        const uint4* const row = p.page_size ? Keys<true>(p, u.b, u.j, head_pieces).row(tk) : Keys<false>(p, u.b, u.j, head_pieces).row(tk);
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-            uint4 f = make_uint4(0u, 0u, 0u, 0u);
+            k[s] = make_uint4(0u, 0u, 0u, 0u);
             if (2 * s + h < head_pieces)
-                f = q[2 * s + h];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                c = __builtin_amdgcn_mfma_f32_32x32x2f32(part_of(k[s], e), part_of(f, e), c, 0, 0, 0);
+                k[s] = row[2 * s + h];
         }
+        put(0);
+        // (causal: blocks that see none of this wavefront's tokens are only copied)
+        const int first = tw >= u.L ? u.last : p.causal ? min(max(tw - (u.L - u.n), 0), u.n) * G / 32 : 0;
+        int slot = 0;
+#pragma unroll 1
+        for (int at = u.last - 1; at >= u.first; --at) {
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            const bool there = at * 32 + col < u.rows;
+            const float below = exponent_of(lse, there);
+            const int limit = !there ? -1 : p.causal ? u.L - u.n + query : u.L;
+            if (at > u.first) {
+                fetch(at - 1);
+                fetch_lse(at - 1);
+            }
+            if (at >= first) {
+                floatx16 c;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(c[e], p.scale_log2, below));
-            sums[e] += tw + (e & 3) + 8 * (e >> 2) + 4 * h <= limit ? w : 0.f;
+                for (int e = 0; e < 16; ++e)
+                    c[e] = 0.f;
+                const uint4* const from = &lds[slot][col * kPitch + h];
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) {
+                    const uint4 f = from[2 * s];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        c = __builtin_amdgcn_mfma_f32_32x32x2f32(part_of(k[s], e), part_of(f, e), c, 0, 0, 0);
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(c[e], p.scale_log2, below));
+                    sums[e] += tw + (e & 3) + 8 * (e >> 2) + 4 * h <= limit ? w : 0.f;
+                }
+            }
+            slot ^= 1;
+            if (at > u.first)
+                put(slot);
         }
     }
     store<16>(p, u, tw, sums);
@@ -600,11 +641,6 @@ hipError_t launch_kv_weights(const KvWeightsParams& p, hipStream_t s)
     const int tokens = plan::weights_tile_tokens(bf16), tiles = (p.max_kv + tokens - 1) / tokens;
     const long long units = (long long)tiles * p.B * p.splits;
     const dim3 grid((unsigned)(units * p.Hkv)), block(kWaves * 64);
-#define SPD_MANY(K, W) \
-    if (p.page_size) \
-        hipLaunchKernelGGL((K<W, true>), grid, block, 0, s, p); \
-    else \
-        hipLaunchKernelGGL((K<W, false>), grid, block, 0, s, p)
     const bool even = 32 % p.G == 0;
 #define SPD_MANY_BF16(W) \
     if (p.D == W && even) \
@@ -625,14 +661,17 @@ hipError_t launch_kv_weights(const KvWeightsParams& p, hipStream_t s)
         }
     } else {
         if (p.D <= 64) {
-            SPD_MANY(kv_weights_many_f32, 16);
+            hipLaunchKernelGGL(kv_weights_many_f32<16>, grid, block, 0, s, p);
+        } else if (p.D <= 96) {
+            hipLaunchKernelGGL(kv_weights_many_f32<24>, grid, block, 0, s, p);
         } else if (p.D <= 128) {
-            SPD_MANY(kv_weights_many_f32, 32);
+            hipLaunchKernelGGL(kv_weights_many_f32<32>, grid, block, 0, s, p);
+        } else if (p.D <= 192) {
+            hipLaunchKernelGGL(kv_weights_many_f32<48>, grid, block, 0, s, p);
         } else {
-            SPD_MANY(kv_weights_many_f32, 64);
+            hipLaunchKernelGGL(kv_weights_many_f32<64>, grid, block, 0, s, p);
         }
     }
-#undef SPD_MANY
 #undef SPD_MANY_BF16
     hipError_t rc = hipGetLastError();
     if (rc == hipSuccess && p.splits > 1) {

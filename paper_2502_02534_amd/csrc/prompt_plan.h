@@ -129,10 +129,10 @@ inline int make_weights_plan(const spd_prompt_desc* d, int64_t total, int64_t ma
     if (rows <= kWeightsFewRows)
         return SPD_OK;
     // The rows are cut into parts, which another launch adds, where the tiles leave CUs idle (512 workgroups run at once; parts of
-    // 128 rows at least), and where parts of 1024 rows and more even out what causal tiles have to do.
+    // 128 rows at least, 32 in fp32, whose blocks of 32 take 16 times as long), and where parts of 1024 rows and more even out what causal tiles have to do.
     const int64_t units = pairs * ((max_kv + tokens - 1) / tokens);
     if (units > 0) {
-        const int64_t fill = units <= 128 ? least(512 / units, rows / 128) : 1, even = least(4096 / units, rows / 1024);
+        const int64_t fill = units <= 128 ? least(512 / units, rows / (d->dtype == SPD_BF16 ? 128 : 32)) : 1, even = least(4096 / units, rows / 1024);
         out->splits = (int)least(fill > even ? fill : even, kWeightsMaxSplits);
         out->splits = out->splits > 1 ? out->splits : 1;
     }
