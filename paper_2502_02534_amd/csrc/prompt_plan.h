@@ -128,11 +128,12 @@ inline int make_weights_plan(const spd_prompt_desc* d, int64_t total, int64_t ma
     const int64_t rows = max_query * group, tokens = weights_tile_tokens(d->dtype == SPD_BF16);
     if (rows <= kWeightsFewRows)
         return SPD_OK;
-    // The rows are cut into parts, which another launch adds, where the tiles leave CUs idle (512 workgroups run at once; parts of
-    // 128 rows at least, 32 in fp32, whose blocks of 32 take 16 times as long), and where parts of 1024 rows and more even out what causal tiles have to do.
+    // The rows are cut into parts, which another launch adds, where the tiles leave CUs idle, and where parts of 1024 rows and more even
+    // out what causal tiles have to do.  A block of 32 rows takes 0.5 us, in fp32 1 to 4: there parts may be as short as one.
     const int64_t units = pairs * ((max_kv + tokens - 1) / tokens);
     if (units > 0) {
-        const int64_t fill = units <= 128 ? least(512 / units, rows / (d->dtype == SPD_BF16 ? 128 : 32)) : 1, even = least(4096 / units, rows / 1024);
+        const int64_t fill = d->dtype != SPD_BF16 ? least(2048 / units, rows / 32) : units <= 128 ? least(512 / units, rows / 128) : 1;
+        const int64_t even = least(4096 / units, rows / 1024);
         out->splits = (int)least(fill > even ? fill : even, kWeightsMaxSplits);
         out->splits = out->splits > 1 ? out->splits : 1;
     }
