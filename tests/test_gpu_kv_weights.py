@@ -150,6 +150,22 @@ def test_parts_of_the_rows(dtype, g):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [64, 72, 128])
+@pytest.mark.parametrize("causal", [False, True])
+def test_windows_of_many_sequences(dtype, d, causal):
+    """Some dozens of rows over many sequences, with and without pages: none, one and several tiles of tokens, rows that end in a block."""
+    queries = [(7 * i) % 41 for i in range(18)]
+    kv = [max((97 * i) % 700, 0) for i in range(18)]
+    Problem(dtype, 6, 2, d, queries, kv, page=16 if causal else 0, causal=causal, seed=d, elsewhere=0.0 if causal else 2.0).check()
+
+
+def test_one_window_over_a_long_cache():
+    """More tokens than a workgroup's wavefronts take at once, and shared samples over them."""
+    Problem("bf16", 4, 1, 64, [60], [9000], page=16, causal=True).check()
+    Problem("bf16", 4, 4, 128, [40, 33], [5000, 3100]).check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_last_queries_of_the_last_row(dtype):
     """The queries end where their tensor does, in the middle of a block."""
     for n in (9, 17, 40):
