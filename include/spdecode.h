@@ -12,7 +12,8 @@
  *   2. temperature sampling of the next token from the logits.
  *
  * This library provides those two operations, and what stands before them: page tables, the prompts'
- * own attention and KV writes, penalties on the logits.  The decode attention is computed
+ * own attention and KV writes, penalties on the logits; and what a step says: log probabilities, attention weights
+ * of cached tokens, and their eviction.  The decode attention is computed
  * as a cascade: one pass treats all samples' queries of a KV head as a dense tile
  * against the shared prefix (so the prefix is read once, not once per sample), a
  * second pass streams each sample's private suffix, and the two partial softmax

@@ -10,11 +10,17 @@
 //     the keys: whole lines, marked as used once, the next tile's under way while it works on this one, which goes through LDS of the
 //     wavefront's own to the lanes that multiply it.  Bound: HBM, K read once (1024 samples of up to 2048 paged tokens, 8 heads of 128
 //     channels, 2.2 GB: 387 us, 5.7 TB/s; without the products the same; loads in the products' order 449).
-//   many rows (samples over their shared prompt, a prompt over itself): a wavefront keeps 64 tokens' keys in registers (32 in fp32),
-//     the rows pass by in blocks of 32: in bf16 through LDS, shared by the four wavefronts of a workgroup, with the
-//     exponentials of one block between the products of the next.  Bound: matrix pipe and vector ALU alike (16 products of 32 clocks
-//     against 32 fma, exponentials and additions a lane, 128 channels).
-//     Causal: the last rows, which every tile sees, come first, so that tiles that run together read the same rows.
+//   many rows (samples over their shared prompt, a prompt over itself): a wavefront keeps 64 tokens' keys in registers (32 in fp32), and
+//     the rows pass by in blocks of 32 through LDS, shared by a workgroup's four wavefronts; in bf16 the exponentials of one half of the
+//     tokens run between the products of the other.  Bound: matrix pipe and vector ALU together, and the clock that their power leaves:
+//     a block takes 16 products of 32 clocks beside 32 fma, exponentials and additions a lane (128 channels).  16384 tokens of 64 / 8 heads
+//     2.20 ms: 1.0 PFLOP/s of the products that the rows need, matrix pipe 56 % busy, 1.83 GHz; 4096 fp32 tokens of 16 / 4 heads of 64
+//     channels 175 us (98 TFLOP/s).
+//     Causal: the last rows, which every tile sees, come first, and first tiles, which see most, are launched first.  Rows in eight parts
+//     instead of one, which even out the tiles' work: 2.65 -> 2.28 ms; parts of the same rows for every tile, which keep them in the L2
+//     (7.5 GB fetched otherwise), win 3 % there and lose 5 to 70 % on shorter prompts, whose parts are then half empty.
+//     64 samples over a prompt of 8192, 32 / 8 heads: 11.1 us, latency (a chain of loads, eight blocks, the sums over the lanes).  All rows in
+//     LDS at once, and wavefronts that walk several tiles without a barrier: 12.4, and 80 against 84 for 8 x 64 queries over 1k to 16k tokens.
 #include "prompt_plan.h"
 #include "spd_internal.h"
 

@@ -12,7 +12,13 @@
 // num_top logits reach; only chunks whose maximum is above it (and the first ones that equal it: ties go to the lower token) are read
 // again, and what they hold is ranked by counting.  Nothing is sorted, and no list depends on the order of arrival.
 //
-// A workgroup takes a slice of a row; with several slices a second launch joins them.
+// A workgroup takes a row, or (up to 128 rows) a slice of one, which a second launch joins.
+//
+// Rounding: exponents, terms and a thread's sums are fp32 (up to 32 chunks one after another, each added as a tree), and so is the join.
+// Bound: HBM.  1024 rows of 128256 bf16 logits with 5 alternatives 55.5 us (4.7 TB/s; without any 53), 500 fp32 rows with 20 50.7 (5.1),
+// 2000 unaligned rows of 50257 45.5 (4.4).  64 fp32 rows of 128256 with 20 alternatives 16.3: slices 12 (a chain of loads, sums, threshold,
+// second look) and the join 4.7; one workgroup a row 21.8, two slices 18.5, eight instead of four 18.1.  Two stripes of chunks ahead against four: 55.7 / 56.4
+// and 45.9 / 48.7.  Four rows of 1024: 5.8, latency.
 #include "logprobs_plan.h"
 #include "spd_internal.h"
 
