@@ -644,7 +644,7 @@ SPD_API size_t select_kv_tokens_workspace_size(int64_t num_seqs, int32_t num_hea
  *   weights   float [num_seqs, num_heads, weights_stride]
  *   budgets   int32 [num_seqs] (negative ones count as 0), or NULL: max_new_len for all
  *   max_kv_len, max_new_len  host-known upper bounds: longer lengths and larger budgets count as these
- * max_kv_len up to 2^24.  Returns spd_status.
+ * max_kv_len up to 2^24, num_seqs * num_heads below 2^22.  Returns spd_status.
  */
 SPD_API int select_kv_tokens(const float *weights, int64_t weights_stride, int64_t num_seqs, int32_t num_heads,
                              const int32_t *kv_lens, int64_t max_kv_len,

@@ -28,7 +28,7 @@ int check_select(int64_t seqs, int32_t heads, int64_t max_kv)
 {
     if (seqs <= 0 || heads <= 0 || max_kv < 0)
         return SPD_EINVAL;
-    if (max_kv > (1 << 24) || seqs > kMostBlocks / heads)
+    if (max_kv > (1 << 24) || seqs > (kMostBlocks - 1) / heads)
         return SPD_EUNSUPPORTED;
     return SPD_OK;
 }
