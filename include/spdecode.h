@@ -640,7 +640,7 @@ SPD_API size_t select_kv_tokens_workspace_size(int64_t num_seqs, int32_t num_hea
  *             r tokens keep their order at the end (place m - r + i gets token n - r + i).  Of the others, one at t < m - r
  *             stays where it is, and the rest fill the places left before m - r in ascending order.  So source[b, j, i] >= i.
  *             Entries from m on are not written.
- *   new_lens  int32 [num_seqs]: m
+ *   new_lens  int32 [num_seqs]: m; not kv_lens itself, which every KV head still reads (compact_kv's lens_out may be)
  *   weights   float [num_seqs, num_heads, weights_stride]
  *   budgets   int32 [num_seqs] (negative ones count as 0), or NULL: max_new_len for all
  *   max_kv_len, max_new_len  host-known upper bounds: longer lengths and larger budgets count as these

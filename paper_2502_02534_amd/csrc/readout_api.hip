@@ -166,6 +166,8 @@ int select_kv_tokens(const float* weights, int64_t weights_stride, int64_t num_s
         return rc;
     if (!weights || !kv_lens || !source || !new_lens || max_new_len < 0 || sinks < 0 || recent < 0)
         return SPD_EINVAL;
+    if (new_lens == kv_lens)  // (written by a sequence's first head, read by all)
+        return SPD_EINVAL;
     if (max_new_len > max_kv_len)
         max_new_len = max_kv_len;
     if (weights_stride < max_kv_len || source_stride < max_new_len)

@@ -26,3 +26,9 @@ def test_a_launch_counts_its_threads_in_32_bits(B):
     """2^22 rows of 1024 threads are one thread too many."""
     assert _select(B, seqs=1 << 22, heads=1) == EUNSUPPORTED and _select(B, seqs=1 << 21, heads=2) == EUNSUPPORTED
     assert B.select_kv_tokens_workspace_size(1 << 22, 1, 40000) == 0 and B.select_kv_tokens_workspace_size((1 << 22) - 1, 1, 40000) > 0
+
+
+@pytest.mark.parametrize("heads", [2, 8])
+def test_new_lengths_do_not_replace_those_still_read(B, heads):
+    """A sequence's first head writes its new length while the others still read the old one."""
+    assert _select(B, heads=heads, lens=P, new=P) == EINVAL
