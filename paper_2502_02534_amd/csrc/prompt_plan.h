@@ -128,11 +128,18 @@ inline int make_weights_plan(const spd_prompt_desc* d, int64_t total, int64_t ma
     const int64_t rows = max_query * group, tokens = weights_tile_tokens(d->dtype == SPD_BF16);
     if (rows <= kWeightsFewRows)
         return SPD_OK;
-    // The rows are cut into parts, which another launch adds, where the tiles leave CUs idle, and where parts of 1024 rows and more even
-    // out what causal tiles have to do.  A block of 32 rows takes 0.5 us, in fp32 1 to 4: there parts may be as short as one.
+    // The rows are cut into parts, which another launch adds (3 us and more), where the tiles that there are (total_queries says how many
+    // of the longest sequence's each has) leave CUs idle, and where parts of 1024 rows and more even out what causal tiles have to do.  A block of
+    // 32 rows takes 0.5 us: parts of at least 4 of them where three quarters of the places are idle, else 20 (512 queries over 4096 more
+    // tokens, 32 / 8 heads: 34.8 us, whole 43.8; 256 over 8192: two parts 25.7, whole 24.1).  In fp32 a block takes 1 to 4 us, and parts may be as short as one.
+    // 4 sequences of 373 to 2642 tokens, 4 / 2 heads: 25.2 us, by the longest alone 30.3; 4 fp32 ones of 456 to 2914, 60.4 and 71.2.
     const int64_t units = pairs * ((max_kv + tokens - 1) / tokens);
     if (units > 0) {
-        const int64_t fill = d->dtype != SPD_BF16 ? least(2048 / units, rows / 32) : units <= 128 ? least(512 / units, rows / 128) : 1;
+        const int64_t every = d->num_prompts * max_query, there = total < every ? units * total / every : units;
+        const int64_t live = there > units / 4 ? there : units / 4 + 1;  // (no more than a guess, and workspace is for all)
+        const int64_t places = d->head_dim <= 128 ? 512 : 256;  // two workgroups a CU, or one
+        const int64_t fill = d->dtype != SPD_BF16 ? least(2048 / live, rows / 32)
+                             : 2 * live <= places ? least(places / live, rows / (4 * live <= places ? 128 : 640)) : 1;
         const int64_t even = least(4096 / units, rows / 1024);
         out->splits = (int)least(fill > even ? fill : even, kWeightsMaxSplits);
         out->splits = out->splits > 1 ? out->splits : 1;

@@ -245,7 +245,7 @@ struct KvWeightsParams {
     float* weights_out;
     long long stride;
     int splits;   // parts of a sequence's query rows
-    float* part;  // [splits - 1][B][Hkv][max_kv]
+    float* part;  // [splits][B][Hkv][max_kv]
 };
 
 struct SelectParams {
