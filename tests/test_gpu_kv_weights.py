@@ -317,3 +317,15 @@ def test_far_keys():
         desc = B.make_prompt_desc(dtype=B.SPD_BF16, num_q_heads=4, num_kv_heads=hkv, head_dim=d, num_prompts=1, page_size=page, causal=False)
         B.accumulate_kv_weights(desc, q, pool, i32([0, 2]), i32([n]), starts, table, lse, 2, 2, n, 0.0, None, out, n, ws)
         assert bool(((out[0].double() - want).abs() <= 3e-5 * want).all()), page
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("queries,kv,causal", [([700, 3, 1, 0], [700, 3, 1, 2], True), ([2, 400, 30], [900, 400, 31], True), ([300, 1], [40, 1500], False)])
+@pytest.mark.parametrize("spare", [0, 2000])
+def test_one_long_sequence_among_short_ones(dtype, queries, kv, causal, spare):
+    """The parts are made for the queries that there are, or (`spare`: total_queries is more than the sequences have) for each
+    sequence's most: the short ones' parts are empty, or one row block's share."""
+    from paper_2502_02534_amd import binding as B
+    p = Problem(dtype, 4, 2, 64, queries, kv, causal=causal, spare=spare, seed=91)
+    assert B.accumulate_kv_weights_workspace_size(p.desc, p.total, p.max_query, p.max_kv) > 256  # (parts)
+    p.check()
