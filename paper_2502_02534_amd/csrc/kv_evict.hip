@@ -36,6 +36,45 @@ __device__ __forceinline__ int lanes_below(unsigned long long mask)
     return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0u));
 }
 
+// The lowest n of 64 bits.
+__device__ __forceinline__ unsigned long long lowest_bits(int n)
+{
+    return n >= 64 ? ~0ull : (1ull << max(n, 0)) - 1ull;
+}
+
+// Over the 16 lanes of a lane row (rotations by 8, 4, 2, 1; shifts by 1, 2, 4, 8 with zeros behind).
+template <int CTRL> __device__ __forceinline__ unsigned dpp(unsigned x)
+{
+    return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
+}
+template <class F> __device__ __forceinline__ unsigned over_row(unsigned x, F f)
+{
+    x = f(x, dpp<0x128>(x));
+    x = f(x, dpp<0x124>(x));
+    x = f(x, dpp<0x122>(x));
+    return f(x, dpp<0x121>(x));
+}
+template <class F> __device__ __forceinline__ unsigned over_wave(unsigned x, F f)
+{
+    x = over_row(x, f);
+    const auto of = [&](int lane) { return (unsigned)__builtin_amdgcn_readlane((int)x, lane); };
+    return f(f(of(0), of(16)), f(of(32), of(48)));
+}
+// Sum of the lanes up to this one, of lanes 0 .. 31.
+__device__ __forceinline__ unsigned up_to_lane(unsigned x)
+{
+    x += dpp<0x111>(x);
+    x += dpp<0x112>(x);
+    x += dpp<0x114>(x);
+    x += dpp<0x118>(x);
+    const unsigned first = (unsigned)__builtin_amdgcn_readlane((int)x, 15);
+    return x + ((threadIdx.x & 16) ? first : 0u);
+}
+__device__ __forceinline__ unsigned long long lane_bits(unsigned long long x, int lane)
+{
+    return (unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)x, lane);
+}
+
 // What stays of a row: n tokens, m places, the last r and the first f by their place, c of those between by weight.
 struct Row {
     int n, m, r, f, c;
@@ -58,11 +97,11 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
     constexpr int kTokens = 64 * WAVES * V;
     constexpr int kBits = V < 16 ? 0 : WAVES == 1 ? 9 : 11;  // of the histogram
     constexpr int kBins = 1 << kBits, kOwn = kBins < 64 ? 1 : kBins / 64;  // and a lane's bins of it, with a place between two lanes' (bank conflicts)
-    constexpr int kPlaces = (kBins + 64 + 3) / 4 * 4;
+    constexpr int kPlaces = (kBins + 65 + 3) / 4 * 4;
     const auto place = [](int bin) { return bin + bin / kOwn; };
     static_assert(WAVES == 1 || ROWS == 1, "wavefronts of one row wait for each other");
     __shared__ unsigned short moving[ROWS][kTokens / 2];  // (no more than half of the tokens fill gaps)
-    __shared__ int counts[2][WAVES], sums[3][WAVES];
+    __shared__ int counts[2][WAVES], sums[2][WAVES];
     __shared__ __align__(16) int hist[kBits ? ROWS : 1][kBits ? kPlaces : 4];
     __shared__ unsigned few[ROWS][64];
     __shared__ int num_few[ROWS];
@@ -103,8 +142,7 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
         if (t0 + 64 * v0 < middle) {
 #pragma unroll
             for (int v = v0; v < v0 + 4; ++v) {
-                const int t = t0 + 64 * v + lane;
-                key[v] = t >= a.f && t < middle ? key_of(x[v]) : 0u;
+                key[v] = (unsigned)(t0 + 64 * v + lane - a.f) < (unsigned)(middle - a.f) ? key_of(x[v]) : 0u;
                 lowest = min(lowest, key[v] - 1u);
                 highest = max(highest, key[v]);
             }
@@ -116,7 +154,7 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
     }
     // a number over the row's wavefronts (every wavefront calls it as often)
     int calls = 0;
-    const auto over_row = [&](int mine) __attribute__((always_inline)) -> int {
+    const auto over_waves = [&](int mine) __attribute__((always_inline)) -> int {
         if (WAVES == 1)
             return mine;
         int* const at = counts[calls & 1];
@@ -124,11 +162,7 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
         if (lane == 0)
             at[w] = mine;
         __syncthreads();
-        int sum = lane < WAVES ? at[lane] : 0;
-#pragma unroll
-        for (int o = 1; o < WAVES; o <<= 1)
-            sum += __shfl_xor(sum, o);
-        return __builtin_amdgcn_readfirstlane(sum);
+        return __builtin_amdgcn_readfirstlane((int)over_row((lane & 15) < WAVES ? (unsigned)at[lane % WAVES] : 0u, [](unsigned x, unsigned y) { return x + y; }));
     };
     const int groups = min(max((middle - t0 + 63) / 64, 0), V);  // of 64 tokens that have any to choose from
     const auto count = [&](unsigned least) __attribute__((always_inline)) -> int {
@@ -140,16 +174,13 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
                 for (int v = v0; v < v0 + 4; ++v)
                     sum += __popcll(__ballot(key[v] >= least));
             }
-        return over_row(sum);
+        return over_waves(sum);
     };
     unsigned floor = ~0u;  // keys from here on stay (no key is that large), and `ties` of those one below it where they are not all wanted
     int ties = 0;
     if (a.c > 0) {
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-            lowest = min(lowest, (unsigned)__shfl_xor(lowest, o));
-            highest = max(highest, (unsigned)__shfl_xor(highest, o));
-        }
+        lowest = over_wave(lowest, [](unsigned x, unsigned y) { return min(x, y); });
+        highest = over_wave(highest, [](unsigned x, unsigned y) { return max(x, y); });
         if (kBits) {
             int4* const own = (int4*)hist[local];
             for (int i = threadIdx.x % (64 * WAVES); i < kPlaces / 4; i += 64 * WAVES)
@@ -164,10 +195,8 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
                 ends[1][w] = highest;
             }
             __syncthreads();
-            for (int i = 0; i < WAVES; ++i) {
-                lowest = min(lowest, ends[0][i]);
-                highest = max(highest, ends[1][i]);
-            }
+            lowest = over_row(ends[0][lane % WAVES], [](unsigned x, unsigned y) { return min(x, y); });
+            highest = over_row(ends[1][lane % WAVES], [](unsigned x, unsigned y) { return max(x, y); });
         }
         lowest = __builtin_amdgcn_readfirstlane(lowest);
         highest = __builtin_amdgcn_readfirstlane(highest);
@@ -183,8 +212,7 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
                 if (v0 < groups) {
 #pragma unroll
                     for (int v = v0; v < v0 + 4; ++v)
-                        if (key[v])
-                            atomicAdd(&bins[place((int)((key[v] - floor) >> shift))], 1);
+                        atomicAdd(&bins[place(key[v] ? (int)((key[v] - floor) >> shift) : kBins)], 1);  // (no token: the bin behind)
                 }
             if (WAVES > 1)
                 __syncthreads();
@@ -258,95 +286,85 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
                 top = -1;
             }
         }
-        for (int bit = top; bit >= 0 && !exact; --bit) {
-            const unsigned cand = floor + (1u << bit);
+        // (one more look at the end: how many lie above the c-th)
+        for (int bit = top; bit >= -1 && !exact; --bit) {
+            const unsigned cand = floor + (bit >= 0 ? 1u << bit : 1u);  // (below ~0: the largest key is +inf's)
             const int reach = count(cand);
-            if (cand > floor && reach >= a.c) {
+            if (bit < 0) {
+                floor = cand;
+                ties = a.c - reach;
+            } else if (cand > floor && reach >= a.c) {
                 floor = cand;
                 exact = reach == a.c;
             }
         }
-        if (!exact) {
-            ++floor;  // (below ~0: the largest key is +inf's)
-            ties = a.c - count(floor);
-        }
     }
-    // Whether token 64 v + lane of this wavefront stays by weight; tied: its ties in front of v.
-    const auto stays = [&](int v, int& tied) __attribute__((always_inline)) -> bool {
-        bool s = key[v] >= floor;
-        if (ties > 0) {
-            const unsigned long long equal = __ballot(key[v] == floor - 1u);
-            s = s || ((equal >> lane & 1) && tied + lanes_below(equal) < ties);
-            tied += __popcll(equal);
-        }
-        return s;
-    };
-    // what the wavefronts in front of this one have: ties, gaps, tokens that move
-    int tied0 = 0, gap0 = 0, move0 = 0;
-    if (WAVES > 1) {
-        if (ties > 0) {
-            int equal = 0;
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                equal += __popcll(__ballot(key[v] == floor - 1u));
-            if (lane == 0)
-                sums[0][w] = equal;
-            __syncthreads();
-            for (int i = 0; i < w; ++i)
-                tied0 += sums[0][i];
-        }
-        int tied = tied0, gaps = 0, moves = 0;
+    // Which of tokens 64 v .. 64 v + 63 of this wavefront stay are 64 bits of lane v: all groups are counted at once, and loops walk those that
+    // have something to do.
+    const auto reach = [&](auto yes) __attribute__((always_inline)) -> unsigned long long {
+        int lo = 0, hi = 0;
 #pragma unroll
         for (int v0 = 0; v0 < V; v0 += 4)
-            if (v0 < groups || t0 + 64 * v0 < early) {
+            if (v0 < groups) {
 #pragma unroll
                 for (int v = v0; v < v0 + 4; ++v) {
-                    const int t = t0 + 64 * v + lane;
-                    const bool s = stays(v, tied) || t < a.f;
-                    gaps += __popcll(__ballot(!s && t < early));
-                    moves += __popcll(__ballot(s && t >= early && t < middle));
+                    const unsigned long long m = __ballot(yes(key[v]));
+                    lo = lane == v ? (int)m : lo;
+                    hi = lane == v ? (int)(m >> 32) : hi;
                 }
             }
-        if (lane == 0) {
-            sums[1][w] = gaps;
-            sums[2][w] = moves;
-        }
+        return (unsigned long long)(unsigned)hi << 32 | (unsigned)lo;
+    };
+    const auto add = [](unsigned x, unsigned y) { return x + y; };
+    // sum over the wavefronts in front of this one
+    const auto in_front = [&](unsigned mine, int* at) __attribute__((always_inline)) -> unsigned {
+        if (WAVES == 1)
+            return 0u;
+        if (lane == 0)
+            at[w] = (int)mine;
         __syncthreads();
-        for (int i = 0; i < w; ++i) {
-            gap0 += sums[1][i];
-            move0 += sums[2][i];
+        return (unsigned)__builtin_amdgcn_readfirstlane((int)over_row(lane < w ? (unsigned)at[lane] : 0u, add));
+    };
+    unsigned long long kept = reach([&](unsigned k) { return k >= floor; });
+    if (ties > 0) {  // the first `ties` of those that equal the c-th
+        const unsigned long long equal = reach([&](unsigned k) { return k == floor - 1u; });
+        const int here = __popcll(equal), upto = (int)up_to_lane((unsigned)here);
+        const int wanted = ties - (int)in_front((unsigned)__builtin_amdgcn_readlane(upto, 31), sums[0]) - (upto - here);
+        kept |= wanted >= here ? equal : 0ull;
+        const unsigned long long part = __ballot(wanted > 0 && wanted < here);  // (a group at most)
+        if (part != 0ull) {
+            const int v = __ffsll(part) - 1, some = __builtin_amdgcn_readlane(wanted, v);
+            const unsigned long long of = lane_bits(equal, v), first = __ballot((of >> lane & 1) && lanes_below(of) < some);
+            kept |= lane == v ? first : 0ull;
         }
     }
+    const int base = t0 + 64 * lane;
+    const unsigned long long places = lane < V ? lowest_bits(early - base) : 0ull;
+    kept |= lane < V ? lowest_bits(a.f - base) : 0ull;
+    const unsigned long long gaps = ~kept & places, moves = kept & ~places;
+    // (16 bits each: no more than half of the tokens move)
+    const unsigned both = (unsigned)__popcll(gaps) << 16 | (unsigned)__popcll(moves), upto = up_to_lane(both);
+    const unsigned before = upto - both + in_front((unsigned)__builtin_amdgcn_readlane((int)upto, 31), sums[1]);
     unsigned short* const list = moving[local];
-    if (t0 + 64 * V > early) {
-        int tied = tied0, at = move0;
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (v < groups && (t0 + 64 * v + 63 >= early || ties > 0)) {
-                const int t = t0 + 64 * v + lane;
-                const bool move = (stays(v, tied) || t < a.f) && t >= early && t < middle;
-                const unsigned long long moves = __ballot(move);
-                if (move)
-                    list[at + lanes_below(moves)] = (unsigned short)t;
-                at += __popcll(moves);
-            }
+    for (unsigned long long todo = __ballot(moves != 0ull); todo != 0ull; todo &= todo - 1ull) {
+        const int v = __ffsll(todo) - 1;
+        const unsigned long long some = lane_bits(moves, v);
+        if (__builtin_amdgcn_inverse_ballot_w64(some))
+            list[(__builtin_amdgcn_readlane((int)before, v) & 0xffff) + lanes_below(some)] = (unsigned short)(t0 + 64 * v + lane);
     }
     if (WAVES > 1)
         __syncthreads();
     else
         wave_sync();
-    if (t0 < early) {
-        int tied = tied0, at = gap0;
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (t0 + 64 * v < early) {
-                const int t = t0 + 64 * v + lane;
-                const bool s = stays(v, tied) || t < a.f;
-                const unsigned long long gaps = __ballot(!s && t < early);
-                if (t < early)
-                    source[t] = s ? t : (int)list[at + lanes_below(gaps)];
-                at += __popcll(gaps);
-            }
+#pragma unroll 4
+    for (int v = 0; v < min((early - t0 + 63) / 64, V); ++v) {
+        const int t = t0 + 64 * v + lane;
+        const unsigned long long some = lane_bits(gaps, v);
+        int from = t;
+        if (__builtin_amdgcn_inverse_ballot_w64(some))
+            from = (int)list[((unsigned)__builtin_amdgcn_readlane((int)before, v) >> 16) + lanes_below(some)];
+        if (t < early)
+            source[t] = from;
     }
     for (int i = threadIdx.x % (64 * WAVES); i < a.r; i += 64 * WAVES)
         source[early + i] = a.n - a.r + i;
