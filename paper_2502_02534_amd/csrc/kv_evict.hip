@@ -104,7 +104,7 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
     __shared__ int counts[2][WAVES], sums[2][WAVES];
     __shared__ __align__(16) int hist[kBits ? ROWS : 1][kBits ? kPlaces : 4];
     __shared__ unsigned few[ROWS][64];
-    __shared__ int num_few[ROWS];
+    __shared__ int num_few;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int w = WAVES == 1 ? 0 : wave, local = WAVES == 1 ? wave : 0;
     const long long row = (long long)blockIdx.x * ROWS + local;
@@ -185,8 +185,8 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
             int4* const own = (int4*)hist[local];
             for (int i = threadIdx.x % (64 * WAVES); i < kPlaces / 4; i += 64 * WAVES)
                 own[i] = make_int4(0, 0, 0, 0);
-            if (threadIdx.x % (64 * WAVES) == 0)
-                num_few[local] = 0;
+            if (WAVES > 1 && threadIdx.x == 0)
+                num_few = 0;
         }
         if (WAVES > 1) {
             __shared__ unsigned ends[2][WAVES];
@@ -262,13 +262,25 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
             exact = above + inside == a.c;
             top = shift - 1;
             if (!exact && inside <= 64) {
+                int listed = 0;
 #pragma unroll
                 for (int v0 = 0; v0 < V; v0 += 4)
                     if (v0 < groups) {
 #pragma unroll
-                        for (int v = v0; v < v0 + 4; ++v)
-                            if ((key[v] - floor) >> shift == 0u)
-                                few[local][atomicAdd(&num_few[local], 1)] = key[v];
+                        for (int v = v0; v < v0 + 4; ++v) {
+                            const bool hit = (key[v] - floor) >> shift == 0u;
+                            if (WAVES > 1) {
+                                if (hit)
+                                    few[local][atomicAdd(&num_few, 1)] = key[v];
+                                continue;
+                            }
+                            const unsigned long long some = __ballot(hit);
+                            if (some != 0ull) {
+                                if (hit)
+                                    few[local][listed + lanes_below(some)] = key[v];
+                                listed += __popcll(some);
+                            }
+                        }
                     }
                 if (WAVES > 1)
                     __syncthreads();
@@ -352,19 +364,34 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
         if (__builtin_amdgcn_inverse_ballot_w64(some))
             list[(__builtin_amdgcn_readlane((int)before, v) & 0xffff) + lanes_below(some)] = (unsigned short)(t0 + 64 * v + lane);
     }
-    if (WAVES > 1)
-        __syncthreads();
-    else
-        wave_sync();
-#pragma unroll 4
-    for (int v = 0; v < min((early - t0 + 63) / 64, V); ++v) {
-        const int t = t0 + 64 * v + lane;
-        const unsigned long long some = lane_bits(gaps, v);
+    const auto fill = [&](int t, unsigned long long some, int at) __attribute__((always_inline)) {
         int from = t;
         if (__builtin_amdgcn_inverse_ballot_w64(some))
-            from = (int)list[((unsigned)__builtin_amdgcn_readlane((int)before, v) >> 16) + lanes_below(some)];
+            from = (int)list[at + lanes_below(some)];
         if (t < early)
             source[t] = from;
+    };
+    if (WAVES == 1) {
+        wave_sync();
+#pragma unroll 4
+        for (int v = 0; v < (early + 63) / 64; ++v)
+            fill(64 * v + lane, lane_bits(gaps, v), (int)((unsigned)__builtin_amdgcn_readlane((int)before, v) >> 16));
+    } else {
+        // (by all wavefronts, not only those that have the early places)
+        __shared__ unsigned long long gaps_of[WAVES == 1 ? 1 : WAVES * V];
+        __shared__ unsigned before_of[WAVES == 1 ? 1 : WAVES * V];
+        if (lane < V) {
+            gaps_of[w * V + lane] = gaps;
+            before_of[w * V + lane] = before >> 16;
+        }
+        __syncthreads();
+#pragma unroll 2
+        for (int v = w; v < (early + 63) / 64; v += WAVES) {
+            const unsigned long long some = gaps_of[v];
+            fill(64 * v + lane, (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(some >> 32)) << 32 |
+                                    (unsigned)__builtin_amdgcn_readfirstlane((int)some),
+                 __builtin_amdgcn_readfirstlane((int)before_of[v]));
+        }
     }
     for (int i = threadIdx.x % (64 * WAVES); i < a.r; i += 64 * WAVES)
         source[early + i] = a.n - a.r + i;
