@@ -556,7 +556,7 @@ __device__ __forceinline__ void compact_weights(const CompactParams& p, int pair
 }
 
 // Keys and values.  A workgroup takes pieces seg * width .. of the rows of one (sequence, KV head): of K and V, or of one of them
-// (KINDS 2), and of all places, or (chunk > 0, not in place) of `chunk` of them; the workgroups from weights_from on move the weights.
+// (KINDS 2), and of all places, or (chunk > 0) of `chunk` of them; the workgroups from weights_from on move the weights.
 template <int KINDS> __global__ __launch_bounds__(kThreads) void compact_rows(CompactParams p, int segs, int width, int chunk, int weights_from)
 {
     if ((int)blockIdx.x >= weights_from) {
@@ -576,7 +576,8 @@ template <int KINDS> __global__ __launch_bounds__(kThreads) void compact_rows(Co
     const int j = rest % p.Hkv;
     rest /= p.Hkv;
     const int b = rest % p.B, first = rest / p.B * chunk, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int m = max(min(p.new_lens[b], p.max_new), 0), last = chunk > 0 ? min(m, first + chunk) : m;
+    const int m = max(min(p.new_lens[b], p.max_new), 0);
+    int last = chunk > 0 ? min(m, first + chunk) : m;
     if (first >= last)
         return;
     const int* const source = p.source + b * p.seq_stride + j * p.head_stride;
@@ -587,14 +588,16 @@ template <int KINDS> __global__ __launch_bounds__(kThreads) void compact_rows(Co
     const u32x4* const v = (const u32x4*)p.v;
     u32x4* const v_out = (u32x4*)p.v_out;
     const int rows = kThreads / width, mine = tid / width, piece = seg * width + tid % width;  // rows at a time, this thread's and its piece
-    // whether anything is read from a place that is written: then every group of places is read before it is written
+    // whether anything is read from a place that is written: then one workgroup takes all places, and reads every group of them before
+    // it writes them
     bool ordered = false;
     if (p.in_place) {
         if (tid == 0)
             below = 0;
         __syncthreads();
         bool any = false;
-        for (int i = first + tid; i < last; i += kThreads) {
+#pragma unroll 4
+        for (int i = tid; i < m; i += kThreads) {
             const int src = source[i];
             any |= src > i && src < m;
         }
@@ -602,6 +605,11 @@ template <int KINDS> __global__ __launch_bounds__(kThreads) void compact_rows(Co
             below = 1;
         __syncthreads();
         ordered = below != 0;
+        if (ordered && chunk > 0) {
+            if (first > 0)
+                return;
+            last = m;
+        }
     }
     for (int i0 = first; i0 < last; i0 += kPlaces) {
         // the places that get another token, listed in ascending order: a thread looks at kPlaces / kThreads in a row
@@ -705,10 +713,14 @@ hipError_t launch_compact_kv(const CompactParams& p, hipStream_t s)
     const int pairs = p.B * p.Hkv;
     int kinds = 1, segs = 1, chunk = 0, chunks = 1;
     if (p.in_place) {
-        // few rows: K and V, and the pieces of a row, each have a workgroup
+        // few rows: K and V, stretches of places, and where there are still few the pieces of a row, each have a workgroup
         if (pairs < 1024) {
             kinds = 2;
-            while (p.head_u4 % (2 * segs) == 0 && 2 * segs * kinds * pairs <= 1024)
+            chunk = 256;
+            while (chunk < (1 << 30) && (long long)pairs * kinds * ((p.max_new + chunk - 1) / chunk) > 2048)
+                chunk *= 2;
+            chunks = (p.max_new + chunk - 1) / chunk;
+            while (p.head_u4 % (2 * segs) == 0 && 2 * segs * kinds * pairs * chunks <= 1024)
                 segs *= 2;
         }
     } else {

@@ -342,3 +342,27 @@ def test_far_pages():
                  i32([12]), 12, starts, table, k, v, starts, table, k, v, None, None, 0, None)
     for x, y in ((k, kw), (v, vw)):
         assert torch.equal(x[table.long()].transpose(1, 2).reshape(48, 64)[:12], y[s])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("page", [0, 16])
+@pytest.mark.parametrize("budget,recent", [(1500, 0), (1023, 64), (1500, 1490), (2890, 20)])
+def test_long_rows_in_place(dtype, page, budget, recent):
+    """Few long rows: some whose gaps are filled from behind the new length, in any order, beside some that read places which others
+    write."""
+    c = Cache(dtype, 2, 64, [3000, 2900, 1024, 40, 0], page, seed=budget)
+    s = lists(c, budget, 4, recent)
+    k, v, w = run_compact(c, c, s)
+    ek, ev, ew = expected(c, c, s, c.weights, c.weights)
+    assert same(k, ek) and same(v, ev) and torch.equal(w, ew)
+
+
+@pytest.mark.parametrize("length", [2040, 5000, 32768])
+def test_signs_infinities_and_missing_weights_together(length):
+    """A row's lowest key and its highest lie as far apart as any two, beside places that hold no token."""
+    x = draw(2, 2, length, length, "signed")
+    x[0, :, 7::11], x[0, 0, 5::13] = float("nan"), float("-inf")
+    x[1, 0, 3::17] = float("inf")
+    x[1, 1] = torch.randint(0, 3, (length,), generator=torch.Generator().manual_seed(1)).float() - 1.0
+    for budget in (length // 20, length // 2, length - 70):
+        check_select(x, [length, length - 333], [budget] * 2, 4, 60)
