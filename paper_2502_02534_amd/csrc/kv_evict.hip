@@ -724,7 +724,9 @@ hipError_t launch_compact_kv(const CompactParams& p, hipStream_t s)
                 segs *= 2;
         }
     } else {
-        chunk = 64;
+        // a stretch is one trip of loads and stores (in stretches of 64, K and V together 7 % more)
+        kinds = 2;
+        chunk = 128;
         while (chunk < (1 << 30) && (long long)pairs * ((p.max_new + chunk - 1) / chunk) > 16384)
             chunk *= 2;
         chunks = (p.max_new + chunk - 1) / chunk;
