@@ -97,7 +97,7 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
     constexpr int kTokens = 64 * WAVES * V;
     constexpr int kBits = V < 16 ? 0 : WAVES == 1 ? 9 : 11;  // of the histogram
     constexpr int kBins = 1 << kBits, kOwn = kBins < 64 ? 1 : kBins / 64;  // and a lane's bins of it, with a place between two lanes' (bank conflicts)
-    constexpr int kPlaces = (kBins + 65 + 3) / 4 * 4;
+    constexpr int kPlaces = kBins + 128;
     const auto place = [](int bin) { return bin + bin / kOwn; };
     static_assert(WAVES == 1 || ROWS == 1, "wavefronts of one row wait for each other");
     __shared__ unsigned short moving[ROWS][kTokens / 2];  // (no more than half of the tokens fill gaps)
@@ -212,7 +212,7 @@ template <int WAVES, int V, int ROWS> __global__ __launch_bounds__(64 * WAVES * 
                 if (v0 < groups) {
 #pragma unroll
                     for (int v = v0; v < v0 + 4; ++v)
-                        atomicAdd(&bins[place(key[v] ? (int)((key[v] - floor) >> shift) : kBins)], 1);  // (no token: the bin behind)
+                        atomicAdd(&bins[key[v] ? place((int)((key[v] - floor) >> shift)) : kBins + 64 + lane], 1);  // (no token: a bin behind, of the lane's own)
                 }
             if (WAVES > 1)
                 __syncthreads();
