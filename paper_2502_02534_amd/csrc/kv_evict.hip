@@ -3,17 +3,19 @@
 // Selection.  A row's weights lie in registers, as whole numbers in their order; token = 64 (V wave + v) + lane, so that a ballot
 // has 64 tokens in their order.  The c-th largest of those that are not kept by their place: a histogram in LDS of the first 9 or 11
 // bits above the lowest, then the others, bit by bit, of the few keys that share them, until exactly c reach the number (then nobody
-// asks which ties stay).  Tokens that stay behind the end of the early places are listed in LDS in their order, and the gaps
-// among the early places take them from there.  Rows of up to 2048 tokens take a wavefront, longer ones a workgroup; beyond what its
+// asks which ties stay).  From there on a group of 64 tokens is 64 bits of one lane: gaps among the early places and tokens that move are counted
+// for all groups at once, the tokens that move are listed in LDS in their order, and the gaps take them from there, in loops over the groups that
+// have any (in straight lines from the ballots, group by group: 15.6 us instead of 10.6 for 8 rows of 16384).  Rows of up to 2048 tokens take a wavefront, longer ones a workgroup; beyond what its
 // registers hold (32768), the c-th largest comes from four histograms over memory.
-// Bound: the vector ALU and one round of wavefronts: 8192 rows of up to 2048 weights 24.3 us (59 MB; bit by bit from the first on 37), 8 rows of
-// 16384 15.5 (bit by bit 25; 8 wavefronts instead of 16 20).
+// Bound: issue, of the vector and the scalar unit alike, and one round of wavefronts: 8192 rows of up to 2048 weights 22 to 23 us (59 MB; bit by bit
+// from the first on 37), 8 rows of 16384 10.6, 16 of 32768 15.7.
 //
 // Compaction.  source[i] >= i, so a workgroup that takes its places in ascending order, and reads every group of
 // places before it writes them, overwrites nothing that it still has to read; where no source of a row lies below its new length the
-// order does not matter and nobody waits.  Only tokens that move are touched.  Bound: HBM, what moves read and written once: 1024 samples
+// order does not matter, nobody waits, and few long rows are cut into stretches of places.  Only tokens that move are touched.  Bound: HBM, what moves read and written once: 1024 samples
 // of up to 2048 tokens, 8 heads of 128 bf16 channels, down to 1024: 312 us (1.44 GB, 4.6 TB/s); 8 prompts of 1k to 16k down to a quarter, into
-// other pages, 42 (148 MB).  Places listed 1024 at a time against 256: 29 rows of up to 10k places 43 / 64, the two above 312 / 310 and 43 / 42.
+// other pages, 42 (148 MB), in place 32 (one workgroup for every piece of a row instead of stretches 65); 29 fp32 rows of up to 10k down to three
+// quarters 19 (54).
 #include "spd_internal.h"
 
 namespace spd {
@@ -713,7 +715,8 @@ hipError_t launch_compact_kv(const CompactParams& p, hipStream_t s)
     const int pairs = p.B * p.Hkv;
     int kinds = 1, segs = 1, chunk = 0, chunks = 1;
     if (p.in_place) {
-        // few rows: K and V, stretches of places, and where there are still few the pieces of a row, each have a workgroup
+        // few rows: K and V, stretches of places, and where there are still few the pieces of a row, each have a workgroup.  Every one
+        // looks through its row's list first: 512 rows of 2032 places of which few move 14.4 us, in twice as many workgroups 19.8, in one a row and kind 14.1.
         if (pairs < 1024) {
             kinds = 2;
             chunk = 256;

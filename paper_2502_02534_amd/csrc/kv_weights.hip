@@ -15,7 +15,7 @@
 //     tokens run between the products of the other.  Bound: matrix pipe and vector ALU together, and the clock that their power leaves:
 //     a block takes 16 products of 32 clocks beside 32 fma, exponentials and additions a lane (128 channels).  16384 tokens of 64 / 8 heads
 //     2.20 ms: 1.0 PFLOP/s of the products that the rows need, matrix pipe 56 % busy, 1.83 GHz; 4096 fp32 tokens of 16 / 4 heads of 64
-//     channels 175 us (98 TFLOP/s).
+//     channels 171 us (100 TFLOP/s).
 //     Causal: the last rows, which every tile sees, come first, and first tiles, which see most, are launched first.  Rows in eight parts
 //     instead of one, which even out the tiles' work: 2.65 -> 2.28 ms; parts of the same rows for every tile, which keep them in the L2
 //     (7.5 GB fetched otherwise), win 3 % there and lose 5 to 70 % on shorter prompts, whose parts are then half empty.
