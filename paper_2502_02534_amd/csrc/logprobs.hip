@@ -1,11 +1,12 @@
 // Log probabilities of given tokens, with rank, entropy and the most probable tokens.
 //
-// With c = log2(e) / T, a reference r near the row's largest x c, and y_i = x_i c - r (one fma: a common shift of r by its own
-// rounding changes nothing), Z = sum 2^y_i, S = sum 2^y_i y_i:
-//   log p_i = ln2 (y_i - log2 Z),   entropy = ln2 (log2 Z - S / Z),   lse = ln2 (r + log2 Z)
+// With c = log2(e) / T, a reference r near the row's largest x c, and y_i = x_i c - r (one fma, so that r's own rounding shifts all y_i
+// alike), Z = sum 2^y_i, S = sum 2^y_i y_i:
+//   log p_i = ln2 (y_i - log2 Z),   entropy = ln2 (log2 Z - S / Z),   lse = max / T + ln2 (log2 Z - y of the maximum)
 // Every thread has a reference of its own, raised only where a logit lies 2^24 above it; the threads' sums are brought to the
-// row's maximum at the end.  Where x c itself overflows (logits of the type's lowest value at a temperature below 1) the
-// row is summed again from y_i = (x_i - max) c.
+// row's maximum at the end.  The shift is half a unit in the last place of r: harmless below 2^20 (1/16), beyond what 2^y holds from 2^32
+// on.  So no reference starts or goes below -2^20 (what lies far below it adds nothing to a row whose maximum does not), and a row, or
+// slice, whose maximum is 2^20 from zero or more is summed again from y_i = (x_i - max) c.
 //
 // One pass over the row: a thread takes 8 logits at a time (a "chunk"), leaves the chunk's maximum in LDS, and adds its terms.
 // The most probable tokens then come from few chunks: of the threads' maxima the num_top-th largest is a value that at least
@@ -31,7 +32,8 @@ using plan::kChunk;
 
 constexpr float kRaise = 24.f;      // how far above a thread's reference a logit may lie, in base 2
 constexpr float kFloor = -1000.f;   // y of a logit of -inf (2^-1000 = 0, and 0 * -1000 = 0)
-constexpr float kLowest = -3.402823466e38f;  // reference of a thread that has seen nothing above: finite, so that y is no inf - inf
+constexpr float kFar = 1048576.f;   // from here on max c is rounded too far for a reference
+constexpr float kLowest = -kFar;    // reference of a thread that has seen nothing above
 constexpr int kMostRead = 128;      // chunks that are read again
 constexpr int kJoinThreads = 256, kJoinKeys = 1024;
 
@@ -159,7 +161,7 @@ __device__ __forceinline__ int lanes_below(unsigned long long mask)
     return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0u));
 }
 
-// State of a slice: its largest logit, the reference and the sums.
+// State of a slice: its largest logit, the reference and the sums; where the logit is far from zero, it is the reference.
 struct State {
     float m, r, z, s;
 };
@@ -173,45 +175,66 @@ __device__ __forceinline__ void onto(State& a, float r)
     a.r = r;
 }
 
-__device__ __forceinline__ bool overflows(float m, float c) { return m > -INFINITY && m < INFINITY && !(fabsf(m * c) < INFINITY); }
+__device__ __forceinline__ bool is_far(float m, float c) { return m > -INFINITY && m < INFINITY && !(fabsf(m * c) < kFar); }
+
+// Exponent of x.
+__device__ __forceinline__ float exponent(const State& a, float c, float x)
+{
+    return is_far(a.m, c) ? (x - a.m) * c : __builtin_fmaf(x, c, -a.r);
+}
+
+// How far a slice's reference lies above that of its row.
+__device__ __forceinline__ float step_of(const State& b, const State& row, float c)
+{
+    if (!(b.m > -INFINITY))
+        return kFloor;  // (nothing in it)
+    if (is_far(row.m, c))
+        return is_far(b.m, c) ? (b.m - row.m) * c : __builtin_fmaf(-row.m, c, b.r);
+    return is_far(b.m, c) ? __builtin_fmaf(b.m, c, -row.r) : b.r - row.r;
+}
+
+// T, and log2(e) / T.
+struct Scale {
+    float t, c;
+};
 
 // What a row's sums say of a logit x.
-__device__ __forceinline__ float log_p(const State& a, float log2_z, float c, float x)
+__device__ __forceinline__ float log_p(const State& a, float log2_z, const Scale& by, float x)
 {
     if (!(a.m > -INFINITY) || !(x > -INFINITY))
         return -INFINITY;
-    const float y = overflows(a.m, c) ? (x - a.m) * c : __builtin_fmaf(x, c, -a.r);
+    const float y = exponent(a, by.c, x);
     if (!(y > -INFINITY))  // (too far below for base 2)
-        return (x - a.m) * (c * kLn2);
+        return (x - a.m) / by.t;
     return (y - log2_z) * kLn2;
 }
 
-__device__ __forceinline__ void write_row(const LogprobsParams& p, long long row, const State& a, float c, bool known, float given, int above)
+__device__ __forceinline__ void write_row(const LogprobsParams& p, long long row, const State& a, const Scale& by, bool known, float given, int above)
 {
     const bool empty = !(a.m > -INFINITY);
     const float log2_z = __builtin_amdgcn_logf(a.z);
     if (p.logprobs)
-        p.logprobs[row] = known ? log_p(a, log2_z, c, given) : -INFINITY;
+        p.logprobs[row] = known ? log_p(a, log2_z, by, given) : -INFINITY;
     if (p.ranks)
         p.ranks[row] = known ? above + 1 : 0;
     if (p.entropy)
         p.entropy[row] = empty ? 0.f : kLn2 * (log2_z - a.s / a.z);
     if (p.lse)
-        p.lse[row] = empty ? -INFINITY : overflows(a.m, c) ? a.m * (c * kLn2) + kLn2 * log2_z : kLn2 * (a.r + log2_z);
+        p.lse[row] = empty ? -INFINITY : a.m / by.t + kLn2 * (log2_z - exponent(a, by.c, a.m));
 }
 
-__device__ __forceinline__ void write_top(const LogprobsParams& p, long long row, int at, unsigned long long key, const State& a, float log2_z, float c)
+__device__ __forceinline__ void write_top(const LogprobsParams& p, long long row, int at, unsigned long long key, const State& a, float log2_z, const Scale& by)
 {
     if (p.top_tokens)
         p.top_tokens[row * p.top + at] = (int)(0xffffffffu - (unsigned)key);
     if (p.top_logprobs)
-        p.top_logprobs[row * p.top + at] = log_p(a, log2_z, c, key_value((unsigned)(key >> 32)));
+        p.top_logprobs[row * p.top + at] = log_p(a, log2_z, by, key_value((unsigned)(key >> 32)));
 }
 
-__device__ __forceinline__ float scale_of(const LogprobsParams& p, long long row)
+__device__ __forceinline__ Scale scale_of(const LogprobsParams& p, long long row)
 {
-    const float t = p.temperature ? p.temperature[row] : 1.f;
-    return t > 0.f ? kLog2e / t : kLog2e;
+    const float given = p.temperature ? p.temperature[row] : 1.f, t = given > 0.f ? given : 1.f;
+    return {t, kLog2e / t};
 }
 
 // THREADS, STRIPES: a workgroup takes up to STRIPES times THREADS chunks.  PARTS: slices of rows, joined by another launch.
@@ -251,7 +274,8 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(BF16 ||
     const int ahead = (int)(((size_t)p.logits / kElt + (size_t)base) % (16 / kElt)), places = ahead + len;
     const int chunks = (places + kChunk - 1) / kChunk;
     const char* const from = (const char*)p.logits + (base - ahead) * kElt;
-    const float c = scale_of(p, row);
+    const Scale by = scale_of(p, row);
+    const float c = by.c;
     const int token = p.tokens ? p.tokens[row] : -1;
     const bool known = token >= 0 && token < (int)p.vocab;
     const float given = known ? logit<BF16>(p, row * p.stride + token) : INFINITY;
@@ -338,7 +362,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(BF16 ||
         m = fmaxf(m, states[w].m);
         above += counts[w];
     }
-    if (overflows(m, c)) {
+    if (is_far(m, c)) {
         a.z = a.s = 0.f;
         for (int chunk = tid; chunk < chunks; chunk += THREADS) {
             Chunk<BF16> v;
@@ -351,7 +375,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(BF16 ||
                 a.s = __builtin_fmaf(w, y, a.s);
             }
         }
-        a.r = m * c;
+        a.r = 0.f;
     } else {
         onto(a, fmaxf(m * c, kLowest));
     }
@@ -386,7 +410,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(BF16 ||
         if (PARTS)
             *out_part = {a.m, a.r, a.z, a.s, above, 0};
         else
-            write_row(p, row, a, c, known, given, above);
+            write_row(p, row, a, by, known, given, above);
     }
     if (p.top == 0)
         return;
@@ -477,7 +501,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(BF16 ||
             if (PARTS)
                 ((unsigned long long*)((LogprobsPart*)p.workspace + p.rows * slices))[(long long)blockIdx.x * p.top + rank] = key;
             else
-                write_top(p, row, rank, key, a, log2_z, c);
+                write_top(p, row, rank, key, a, log2_z, by);
         }
     }
     if (PARTS && tid == 0)
@@ -492,7 +516,8 @@ template <bool BF16> __global__ __launch_bounds__(kJoinThreads) void logprobs_jo
     const int lane = threadIdx.x & 63;  // (the sums are every wavefront's)
     const LogprobsPart* const parts = (const LogprobsPart*)p.workspace + row * slices;
     const unsigned long long* const keys = (const unsigned long long*)((const LogprobsPart*)p.workspace + p.rows * slices) + row * slices * p.top;
-    const float c = scale_of(p, row);
+    const Scale by = scale_of(p, row);
+    const float c = by.c;
     const int token = p.tokens ? p.tokens[row] : -1;
     const bool known = token >= 0 && token < (int)p.vocab;
     const float given = known ? logit<BF16>(p, row * p.stride + token) : INFINITY;
@@ -507,15 +532,11 @@ template <bool BF16> __global__ __launch_bounds__(kJoinThreads) void logprobs_jo
         m = fmaxf(m, __shfl_xor(m, o));
         above += __shfl_xor(above, o);
     }
-    State a = {m, overflows(m, c) ? m * c : fmaxf(m * c, kLowest), 0.f, 0.f};
+    State a = {m, is_far(m, c) ? 0.f : fmaxf(m * c, kLowest), 0.f, 0.f};
     for (int i = lane; i < slices; i += 64) {
         State b = {parts[i].m, parts[i].r, parts[i].z, parts[i].s};
-        if (overflows(m, c)) {  // (a slice whose own maximum does not overflow lies that far below)
-            b.r = overflows(b.m, c) ? (b.m - m) * c : kFloor;
-            onto(b, 0.f);
-        } else {
-            onto(b, a.r);
-        }
+        b.r = step_of(b, a, c);
+        onto(b, 0.f);
         a.z += b.z;
         a.s += b.s;
     }
@@ -525,7 +546,7 @@ template <bool BF16> __global__ __launch_bounds__(kJoinThreads) void logprobs_jo
         a.s += __shfl_xor(a.s, o);
     }
     if (threadIdx.x == 0)
-        write_row(p, row, a, c, known, given, above);
+        write_row(p, row, a, by, known, given, above);
     if (p.top == 0)
         return;
     const float log2_z = __builtin_amdgcn_logf(a.z);
@@ -540,7 +561,7 @@ template <bool BF16> __global__ __launch_bounds__(kJoinThreads) void logprobs_jo
             for (int q = 0; q < slices * p.top; ++q)
                 rank += listed[q] > key;
             if (key != 0ull && rank < p.top)
-                write_top(p, row, rank, key, a, log2_z, c);
+                write_top(p, row, rank, key, a, log2_z, by);
         }
         return;
     }
@@ -571,7 +592,7 @@ template <bool BF16> __global__ __launch_bounds__(kJoinThreads) void logprobs_jo
             best = listed[w] > best ? listed[w] : best;
         last = best;
         if (threadIdx.x == 0)
-            write_top(p, row, k, best, a, log2_z, c);
+            write_top(p, row, k, best, a, log2_z, by);
     }
 }
 
