@@ -33,6 +33,7 @@ using plan::kChunk;
 constexpr float kRaise = 24.f;      // how far above a thread's reference a logit may lie, in base 2
 constexpr float kFloor = -1000.f;   // y of a logit of -inf (2^-1000 = 0, and 0 * -1000 = 0)
 constexpr float kFar = 1048576.f;   // from here on max c is rounded too far for a reference
+constexpr float kMost = 3.402823466e38f;
 constexpr float kLowest = -kFar;    // reference of a thread that has seen nothing above
 constexpr int kMostRead = 128;      // chunks that are read again
 constexpr int kJoinThreads = 256, kJoinKeys = 1024;
@@ -234,7 +235,7 @@ __device__ __forceinline__ void write_top(const LogprobsParams& p, long long row
 __device__ __forceinline__ Scale scale_of(const LogprobsParams& p, long long row)
 {
     const float given = p.temperature ? p.temperature[row] : 1.f, t = given > 0.f ? given : 1.f;
-    return {t, kLog2e / t};
+    return {t, fminf(kLog2e / t, kMost)};  // (0 times it is 0)
 }
 
 // THREADS, STRIPES: a workgroup takes up to STRIPES times THREADS chunks.  PARTS: slices of rows, joined by another launch.
