@@ -587,8 +587,8 @@ SPD_API size_t token_logprobs_workspace_size(int64_t rows, int64_t vocab, int32_
  *   temperature   float [rows], NULL = 1 everywhere; 0 (a row that is sampled greedily) counts as 1
  *   tokens        int32 [rows] (sample_tokens' tokens_out, or the next tokens of a prompt)
  *   logits        [rows, vocab] fp32 or bf16 (logits_dtype), rows row_stride elements apart
- * Every output may be NULL; logprobs and ranks need tokens.  A logit of -inf has p = 0; a row of nothing else has lse and log p
- * -inf and entropy 0.  Sums are fp32 at least.  num_top 0 .. min(vocab, SPD_MAX_TOP_TOKENS); vocab up to 2^30;
+ * Every output may be NULL; logprobs and ranks need tokens.  A logit of -inf has p = 0, and a NaN counts as one; a row of nothing else
+ * has lse and log p -inf and entropy 0.  What a row with a logit of +inf gets is unspecified.  Sums are fp32 at least.  num_top 0 .. min(vocab, SPD_MAX_TOP_TOKENS); vocab up to 2^30;
  * (rows + 8) * ceil(vocab / 16384) up to 2^22.  rows 0 is a call that does nothing.  Returns spd_status.
  */
 SPD_API int token_logprobs(const void *logits, int32_t logits_dtype, int64_t rows, int64_t vocab, int64_t row_stride,

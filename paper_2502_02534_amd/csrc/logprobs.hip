@@ -279,7 +279,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(BF16 ||
     const float c = by.c;
     const int token = p.tokens ? p.tokens[row] : -1;
     const bool known = token >= 0 && token < (int)p.vocab;
-    const float given = known ? logit<BF16>(p, row * p.stride + token) : INFINITY;
+    const float given = known ? fmaxf(logit<BF16>(p, row * p.stride + token), -INFINITY) : INFINITY;  // (a NaN counts as -inf)
 
     const auto whole = [&](int chunk) { return chunk * kChunk >= ahead && (chunk + 1) * kChunk <= places; };
     State a = {-INFINITY, kLowest, 0.f, 0.f};
@@ -521,7 +521,7 @@ template <bool BF16> __global__ __launch_bounds__(kJoinThreads) void logprobs_jo
     const float c = by.c;
     const int token = p.tokens ? p.tokens[row] : -1;
     const bool known = token >= 0 && token < (int)p.vocab;
-    const float given = known ? logit<BF16>(p, row * p.stride + token) : INFINITY;
+    const float given = known ? fmaxf(logit<BF16>(p, row * p.stride + token), -INFINITY) : INFINITY;  // (a NaN counts as -inf)
     float m = -INFINITY;
     int above = 0;
     for (int i = lane; i < slices; i += 64) {
