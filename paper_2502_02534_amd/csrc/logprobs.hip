@@ -3,8 +3,8 @@
 // With c = log2(e) / T, a reference r near the row's largest x c, and y_i = x_i c - r (one fma, so that r's own rounding shifts all y_i
 // alike), Z = sum 2^y_i, S = sum 2^y_i y_i:
 //   log p_i = ln2 (y_i - log2 Z),   entropy = ln2 (log2 Z - S / Z),   lse = max / T + ln2 (log2 Z - y of the maximum)
-// Every thread has a reference of its own, raised only where a logit lies 2^24 above it; the threads' sums are brought to the
-// row's maximum at the end.  The shift is half a unit in the last place of r: harmless below 2^20 (1/16), beyond what 2^y holds from 2^32
+// Every thread has a reference of its own, its largest logit so far (one that lags behind by up to 2^24 made S of numbers up to 24 times as large,
+// and the entropy of a peaked row off by 2e-6; the times are equal); the threads' sums are brought to the row's maximum at the end.  The shift is half a unit in the last place of r: harmless below 2^20 (1/16), beyond what 2^y holds from 2^32
 // on.  So no reference starts or goes below -2^20 (what lies far below it adds nothing to a row whose maximum does not), and a row, or
 // slice, whose maximum is 2^20 from zero or more is summed again from y_i = (x_i - max) c.
 //
@@ -30,7 +30,6 @@ namespace {
 
 using plan::kChunk;
 
-constexpr float kRaise = 24.f;      // how far above a thread's reference a logit may lie, in base 2
 constexpr float kFloor = -1000.f;   // y of a logit of -inf (2^-1000 = 0, and 0 * -1000 = 0)
 constexpr float kFar = 1048576.f;   // from here on max c is rounded too far for a reference
 constexpr float kMost = 3.402823466e38f;
@@ -167,7 +166,7 @@ struct State {
     float m, r, z, s;
 };
 
-// The sums on reference r, no more than kRaise above which any of their terms lies.
+// The sums on reference r, not below their own.
 __device__ __forceinline__ void onto(State& a, float r)
 {
     const float d = fmaxf(a.r - r, kFloor), f = __builtin_amdgcn_exp2f(d);
@@ -298,7 +297,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(BF16 ||
                 above += __popcll(__ballot(x[e] > given));
         }
         const float r = fmaxf(m * c, kLowest);
-        if (!(r <= a.r + kRaise))
+        if (r > a.r)
             onto(a, r);
         float w[kChunk], s = 0.f;
 #pragma unroll
