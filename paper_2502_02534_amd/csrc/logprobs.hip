@@ -406,14 +406,13 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(BF16 ||
         a.s += states[w].s;
     }
     LogprobsPart* const out_part = (LogprobsPart*)p.workspace + (PARTS ? blockIdx.x : 0);
-    if (tid == 0) {
-        if (PARTS)
-            *out_part = {a.m, a.r, a.z, a.s, above, 0};
-        else
+    if (PARTS && tid == 0)
+        *out_part = {a.m, a.r, a.z, a.s, above, 0};
+    if (p.top == 0) {
+        if (!PARTS && tid == 0)
             write_row(p, row, a, by, known, given, above);
-    }
-    if (p.top == 0)
         return;
+    }
 
     // ---- chunks that reach the threshold.  Where few threads do, all of theirs that do; else (many that equal it) those above it and the
     // first ones of every wavefront that equal it.
@@ -490,6 +489,8 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(BF16 ||
         }
     }
     __syncthreads();
+    if (!PARTS && tid == THREADS - 1)  // (beside the first wavefronts' last work)
+        write_row(p, row, a, by, known, given, above);
     const float log2_z = __builtin_amdgcn_logf(a.z);
     const int all = num_found;
     for (int i = tid; i < all; i += THREADS) {
@@ -545,7 +546,7 @@ template <bool BF16> __global__ __launch_bounds__(kJoinThreads) void logprobs_jo
         a.z += __shfl_xor(a.z, o);
         a.s += __shfl_xor(a.s, o);
     }
-    if (threadIdx.x == 0)
+    if (threadIdx.x == kJoinThreads - 1)  // (the first wavefronts have the lists)
         write_row(p, row, a, by, known, given, above);
     if (p.top == 0)
         return;
