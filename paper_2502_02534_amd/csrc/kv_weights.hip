@@ -1,5 +1,7 @@
 // How much of the queries' attention every cached token got:
-//   w'[b, j, t] = decay w[b, j, t] + sum over the query rows (i, h) that see t of 2^(scale_log2 q . k_t - lse_log2)
+//   w'[b, j, t] = decay w[b, j, t] + sum over the query rows (i, h) that see t of 2^(scale_log2 q . k_t - lse_log2) f
+// f, next to 1, takes back what lse_log2 = lse log2(e) loses by its rounding to 24 bits: one error for all of a row's tokens, 5e-7 of them at an lse
+// of 10.  The sums multiply by it as they add.
 //
 // Rows are the (query, head of the group) pairs of a KV head.  The products are taken transposed, S^T = K Q^T: a lane of the
 // accumulator has one row's scores of several tokens, so the row's log-sum-exp is one number a lane, and a token's sum over
@@ -9,13 +11,13 @@
 //   few rows (up to 32: one step's queries over a sample's own tokens): a wavefront keeps the rows' fragments in registers and streams
 //     the keys: whole lines, marked as used once, the next tile's under way while it works on this one, which goes through LDS of the
 //     wavefront's own to the lanes that multiply it.  Bound: HBM, K read once (1024 samples of up to 2048 paged tokens, 8 heads of 128
-//     channels, 2.2 GB: 387 us, 5.7 TB/s; without the products the same; loads in the products' order 449).
+//     channels, 2.2 GB: 376 us, 5.9 TB/s; loads in the products' order 449 where these took 387).
 //   many rows (samples over their shared prompt, a prompt over itself): a wavefront keeps 64 tokens' keys in registers (32 in fp32), and
 //     the rows pass by in blocks of 32 through LDS, shared by a workgroup's four wavefronts; in bf16 the exponentials of one half of the
 //     tokens run between the products of the other.  Bound: matrix pipe and vector ALU together, and the clock that their power leaves:
-//     a block takes 16 products of 32 clocks beside 32 fma, exponentials and additions a lane (128 channels).  16384 tokens of 64 / 8 heads
-//     2.20 ms: 1.0 PFLOP/s of the products that the rows need, matrix pipe 56 % busy, 1.83 GHz; 4096 fp32 tokens of 16 / 4 heads of 64
-//     channels 171 us (100 TFLOP/s).
+//     a block takes 16 products of 32 clocks beside 32 exponentials and 64 fma a lane (128 channels).  16384 tokens of 64 / 8 heads
+//     2.22 ms: 1.0 PFLOP/s of the products that the rows need, matrix pipe 56 % busy, 1.83 GHz; 4096 fp32 tokens of 16 / 4 heads of 64
+//     channels 172 us (100 TFLOP/s).
 //     Causal: the last rows, which every tile sees, come first, and first tiles, which see most, are launched first.  Rows in eight parts
 //     instead of one, which even out the tiles' work: 2.65 -> 2.28 ms; parts of the same rows for every tile, which keep them in the L2
 //     (7.5 GB fetched otherwise), win 3 % there and lose 5 to 70 % on shorter prompts, whose parts are then half empty.
@@ -35,8 +37,8 @@ typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
 
 constexpr int kWaves = 4;
 // Wavefronts of a workgroup where each works by itself.  Where pages lie anywhere, workgroups of one spread the heads of a page over the chip:
-// 1024 samples of up to 2048 paged tokens, 8 heads of 128 channels, 1 / 2 / 4 / 8 of them 387 / 438 / 454 / 405 us (contiguous, up to 1024
-// tokens: 203 / 192 / 192 / 199), 256 samples of 64 channels 55 / 60 / 61 / 60.
+// 1024 samples of up to 2048 paged tokens, 8 heads of 128 channels, 1 / 2 / 4 / 8 of them 376 / 378 / 380 / 388 us, 64 samples 26.7 / 28.3 / 30.4 / 30.5
+// (contiguous, 1024 of up to 1024 tokens: 200 / 191 / 188 / 195).
 constexpr int few_waves(bool paged) { return paged ? 1 : 4; }
 
 __device__ __forceinline__ bf16x8 as_bf16x8(const uint4& v) { return *reinterpret_cast<const bf16x8*>(&v); }
@@ -45,10 +47,20 @@ __device__ __forceinline__ float part_of(const uint4& v, int e)
     return __uint_as_float(e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w);
 }
 
-// -lse in base 2; a row that is not there, or saw nothing, has -inf: it adds 2^-inf = 0.
-__device__ __forceinline__ float exponent_of(float lse, bool there)
+// What a row's lse does to its terms: an exponent, -lse in base 2, and the factor that its rounding needs.  A row that is not there, or saw
+// nothing, has -inf: it adds 2^-inf = 0.
+struct Shift {
+    float below = -INFINITY, by = 1.f;
+};
+__device__ __forceinline__ Shift shift_of(float lse, bool there)
 {
-    return there && lse > -INFINITY ? -lse * kLog2e : there && lse != lse ? lse : -INFINITY;
+    constexpr float kLog2eRest = 1.92596299e-8f;  // log2(e) - kLog2e
+    const float x = lse * kLog2e, lost = __builtin_fmaf(lse, kLog2eRest, __builtin_fmaf(lse, kLog2e, -x));
+    Shift s;
+    s.below = !there || lse == -INFINITY ? -INFINITY : -x;
+    // (an lse of 2^23 and more has no last place that means anything, and an infinite one loses NaN)
+    s.by = __builtin_amdgcn_fmed3f(__builtin_fmaf(lost, -kLn2, 1.f), 0.5f, 2.f);
+    return s;
 }
 
 // Sum over the 16 lanes of a lane row.
@@ -114,8 +126,9 @@ __global__ __launch_bounds__(few_waves(PAGED) * 64) void kv_weights_few(KvWeight
     __shared__ uint4 lds[kFewWaves][kTile * kPitch];
     const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
     const int item = __builtin_amdgcn_readfirstlane(blockIdx.x * kFewWaves + (threadIdx.x >> 6));
-    // KV head fastest: the heads of a token lie beside each other
-    const int j = item % p.Hkv, rest = item / p.Hkv, b = rest % p.B, at = rest / p.B;
+    // KV head fastest: the heads of a token lie beside each other.  The later a stretch, the fewer sequences have it: each starts three sequences on, or a
+    // CU would get the long ones again and again (64 paged sequences of up to 2048 tokens 29.3 us, so 26.7; 512 189.8 and 187.4)
+    const int j = item % p.Hkv, rest = item / p.Hkv, at = rest / p.B, b = (int)((rest + 3ll * at) % p.B);
     if (at >= chunks)
         return;
     const int L = min(p.kv_lens[b], p.max_kv), t0 = at * chunk, t1 = min(L, t0 + chunk);
@@ -126,13 +139,13 @@ __global__ __launch_bounds__(few_waves(PAGED) * 64) void kv_weights_few(KvWeight
     const Keys<PAGED> keys(p, b, j, head_pieces);
 
     uint4 q[NB][kSteps];
-    float below[NB];  // -lse of the lane's row in base 2
+    Shift shift[NB];  // of the lane's row
     int limit[NB];    // last token that it sees
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
         const int r = nb * 16 + col, i = min(r, max(rows - 1, 0)) / p.G, h = j * p.G + min(r, max(rows - 1, 0)) % p.G;
         const bool there = r < rows;
-        below[nb] = exponent_of(there ? p.lse[(long long)(q0 + i) * p.Hq + h] : 0.f, there);
+        shift[nb] = shift_of(there ? p.lse[(long long)(q0 + i) * p.Hq + h] : 0.f, there);
         limit[nb] = !there ? -1 : p.causal ? L - n + i : L;
         const uint4* const from = (const uint4*)p.q + (long long)(q0 + i) * (p.q_stride / (BF16 ? 8 : 4)) + (long long)h * head_pieces;
 #pragma unroll
@@ -151,35 +164,42 @@ __global__ __launch_bounds__(few_waves(PAGED) * 64) void kv_weights_few(KvWeight
     uint4* const mine_lds = lds[threadIdx.x >> 6];
     const int in_row = lane % P, in_tile = lane / P;  // piece and first row of a lane's loads
     const bool has_piece = in_row < head_pieces;
-    // (tiles start with a page; its number is fetched a tile ahead of its rows)
+    // (tiles start with a page; its number is fetched a tile ahead of its rows, into lanes: a scalar would be waited for at once)
     const int last_page = (t1 - 1) >> 4;
-    int next_page[SUB];
+    int next_page[SUB], any_lane = 0;
+    asm("" : "+v"(any_lane));
     const auto fetch_pages = [&](int tb) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
-            next_page[u] = PAGED ? keys.pages[min((tb >> 4) + u, last_page)] : 0;
+            next_page[u] = PAGED ? keys.pages[min((tb >> 4) + u, last_page) + any_lane] : 0;
     };
     const auto load = [&](int tb, uint4 (&k)[kLoads], float& old) __attribute__((always_inline)) {
         typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+        int page[SUB];
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+            page[u] = next_page[u];
+        fetch_pages(tb + kTile);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int t = min(tb + i * (64 / P) + in_tile, t1 - 1);
-            const uint4* const row = PAGED ? keys.base + next_page[i * (64 / P) / 16] * keys.page_pieces + keys.head_at + (t & 15) * keys.token_pieces
+            const uint4* const row = PAGED ? keys.base + page[i * (64 / P) / 16] * keys.page_pieces + keys.head_at + (t & 15) * keys.token_pieces
                                            : keys.row(t);
             const u32x4 v = __builtin_nontemporal_load((const u32x4*)(row + (has_piece ? in_row : 0)));
-            k[i] = has_piece ? make_uint4(v[0], v[1], v[2], v[3]) : make_uint4(0u, 0u, 0u, 0u);
+            k[i] = make_uint4(v[0], v[1], v[2], v[3]);
         }
-        fetch_pages(tb + kTile);
         old = 0.f;
-        if (p.weights && stores && tb + mine < t1)
-            old = p.weights[out_at + tb + mine];
+        if (p.weights)
+            old = p.weights[out_at + min(tb + mine, t1 - 1)];
     };
     const auto work = [&](int tb, const uint4 (&loaded)[kLoads], float old) __attribute__((always_inline)) {
         float total = 0.f;
         wave_sync();
+        if (has_piece) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-            mine_lds[(i * (64 / P) + in_tile) * kPitch + in_row] = loaded[i];
+            for (int i = 0; i < kLoads; ++i)
+                mine_lds[(i * (64 / P) + in_tile) * kPitch + in_row] = loaded[i];
+        }
         wave_sync();
         uint4 k[SUB][kSteps];
 #pragma unroll
@@ -198,8 +218,8 @@ __global__ __launch_bounds__(few_waves(PAGED) * 64) void kv_weights_few(KvWeight
                     c = product16<BF16>(k[u][s], q[nb][s], c);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(c[i], p.scale_log2, below[nb]));
-                    sum[i] += tb + 16 * u + 4 * g + i <= limit[nb] ? x : 0.f;  // (a row that is not there sees nothing)
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(c[i], p.scale_log2, shift[nb].below));
+                    sum[i] = __builtin_fmaf(tb + 16 * u + 4 * g + i <= limit[nb] ? x : 0.f, shift[nb].by, sum[i]);  // (a row that is not there sees nothing)
                 }
             }
 #pragma unroll
@@ -208,22 +228,33 @@ __global__ __launch_bounds__(few_waves(PAGED) * 64) void kv_weights_few(KvWeight
                 total = col == 4 * u + i ? all : total;
             }
         }
+        total = p.weights ? __builtin_fmaf(p.decay, old, total) : total;
         if (stores && tb + mine < t1)
-            p.weights_out[out_at + tb + mine] = p.weights ? __builtin_fmaf(p.decay, old, total) : total;
+            p.weights_out[out_at + tb + mine] = total;
     };
+    if (!has_piece) {  // (zeros behind a head's channels, once)
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            mine_lds[(i * (64 / P) + in_tile) * kPitch + in_row] = make_uint4(0u, 0u, 0u, 0u);
+    }
     uint4 ka[kLoads], kb[kLoads];
     float oa, ob;
     fetch_pages(t0);
     load(t0, ka, oa);
-    for (int tb = t0; tb < t1; tb += 2 * kTile) {
-        if (tb + kTile < t1)
-            load(tb + kTile, kb, ob);
+    // (no branch around a load in the loop: after one, all loads that may be under way would be waited for)
+    int tb = t0;
+    for (; tb + 2 * kTile < t1; tb += 2 * kTile) {
+        load(tb + kTile, kb, ob);
         work(tb, ka, oa);
-        if (tb + kTile >= t1)
-            break;
-        if (tb + 2 * kTile < t1)
-            load(tb + 2 * kTile, ka, oa);
+        load(tb + 2 * kTile, ka, oa);
         work(tb + kTile, kb, ob);
+    }
+    if (tb + kTile < t1) {
+        load(tb + kTile, kb, ob);
+        work(tb, ka, oa);
+        work(tb + kTile, kb, ob);
+    } else {
+        work(tb, ka, oa);
     }
 }
 
@@ -417,15 +448,16 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void kv_weights_many
 #pragma unroll
         for (int e = 0; e < 16; ++e)
             sc[1][e] = 0.f;
-        float below_was = -INFINITY, below = -INFINITY;
+        Shift shift_was, shift;
+        float lse = 0.f;
         int limit_was = 0, limit = 0;
         const int hide = u.L - u.n;
         // scores of half x become weights, element by element: exponent of e, exponential of e - 1, sum of e - 2
         float ex[16];
-        const auto soft = [&](auto mask_tag, int x, int e, float b, int lim) __attribute__((always_inline)) {
+        const auto soft = [&](auto mask_tag, int x, int e, const Shift& b, int lim) __attribute__((always_inline)) {
             constexpr bool MASK = decltype(mask_tag)::value;
             if (e < 16)
-                ex[e] = __builtin_fmaf(sc[x][e], p.scale_log2, b);
+                ex[e] = __builtin_fmaf(sc[x][e], p.scale_log2, b.below);
             if (e >= 1 && e < 17)
                 ex[e - 1] = __builtin_amdgcn_exp2f(ex[e - 1]);
             if (e >= 2 && e < 18) {
@@ -433,10 +465,10 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void kv_weights_many
                 float w = ex[d];
                 if (MASK)
                     w = tw + 32 * x + (d & 3) + 8 * (d >> 2) + 4 * h <= lim ? w : 0.f;
-                sums[16 * x + d] += w;
+                sums[16 * x + d] = __builtin_fmaf(w, b.by, sums[16 * x + d]);
             }
         };
-        const auto phase = [&](auto x_tag, auto mask_tag, int slot, float b, int lim, auto beside) __attribute__((always_inline)) {
+        const auto phase = [&](auto x_tag, auto mask_tag, int slot, const Shift& b, int lim, auto beside) __attribute__((always_inline)) {
             constexpr int X = decltype(x_tag)::value;
 #pragma unroll
             for (int e = 0; e < 16; ++e)
@@ -461,15 +493,15 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void kv_weights_many
         const std::integral_constant<int, 1> upper{};
         const auto block = [&](auto mask_tag, int slot) __attribute__((always_inline)) {
             // the next block's rows go to LDS, and the loads of the one after start
-            phase(lower, mask_tag, slot, below_was, limit_was, [&]() __attribute__((always_inline)) {
-                below = exponent_of(lse_next, true);
+            phase(lower, mask_tag, slot, shift_was, limit_was, [&]() __attribute__((always_inline)) {
+                lse = lse_next;
                 put(slot);
                 fetch_lse();
                 fetch();
             });
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            phase(upper, mask_tag, slot, below, limit, []() {});
-            below_was = below;
+            phase(upper, mask_tag, slot, shift, limit, [&]() __attribute__((always_inline)) { shift = shift_of(lse, true); });
+            shift_was = shift;
         };
         // blocks of which every row sees all of this wavefront's tokens
         const int whole_first = p.causal ? (max(tw + kManyTokens - 1 - hide, 0) * G + 31) / 32 : 0, whole_last = u.rows / 32;
@@ -494,7 +526,7 @@ __global__ __launch_bounds__(kWaves * 64, D <= 128 ? 2 : 1) void kv_weights_many
         limit = r >= u.rows ? -1 : p.causal ? hide + r / G : u.L;
 #pragma unroll
         for (int e = 0; e < 18; ++e)
-            soft(std::true_type{}, 1, e, below, limit);
+            soft(std::true_type{}, 1, e, shift, limit);
     }
     store<32>(p, u, tw, sums);
 }
@@ -561,7 +593,7 @@ __global__ __launch_bounds__(kWaves * 64, P <= 32 ? 2 : 1) void kv_weights_many_
         for (int at = u.last - 1; at >= u.first; --at) {
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
             const bool there = at * 32 + col < u.rows;
-            const float below = exponent_of(lse, there);
+            const Shift shift = shift_of(lse, there);
             const int limit = !there ? -1 : p.causal ? u.L - u.n + query : u.L;
             if (at > u.first) {
                 fetch(at - 1);
@@ -582,8 +614,8 @@ __global__ __launch_bounds__(kWaves * 64, P <= 32 ? 2 : 1) void kv_weights_many_
                 }
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(c[e], p.scale_log2, below));
-                    sums[e] += tw + (e & 3) + 8 * (e >> 2) + 4 * h <= limit ? w : 0.f;
+                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(c[e], p.scale_log2, shift.below));
+                    sums[e] = __builtin_fmaf(tw + (e & 3) + 8 * (e >> 2) + 4 * h <= limit ? w : 0.f, shift.by, sums[e]);
                 }
             }
             slot ^= 1;
