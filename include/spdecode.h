@@ -656,7 +656,7 @@ SPD_API int select_kv_tokens(const float *weights, int64_t weights_stride, int64
  * Moves the tokens that stay: for every sequence b, KV head j and place i < new_lens[b], keys, values and weight of
  * place i of (k_out, v_out, weights_out) become those of token source[b, j, i] of (k, v, weights).
  *   source    entry (b, j, i) at source[b * source_seq_stride + j * source_head_stride + i] (a head stride of 0: one list for
- *             all heads), source >= i; a place whose source is smaller, or lies past the sequence's table, is left as it is
+ *             all heads), source >= i; a place whose source is smaller, or lies past the sequence's table, is left as it is, weight and all
  *   new_lens  int32 [num_prompts]; max_new_len is a host-known upper bound, and larger ones count as it
  *   kv_indptr, kv_page_indices, k, v          as for prompt_attn: where the sequences are
  *   out_indptr, out_page_indices, k_out, v_out  where they go.  In place: the same four pointers, and no two sequences share a
@@ -664,7 +664,7 @@ SPD_API int select_kv_tokens(const float *weights, int64_t weights_stride, int64
  *             written.  Contiguous tokens are kv_stride apart in all four, and indptr holds num_prompts + 1 token starts.
  *   weights, weights_out  float [num_prompts, Hkv, weights_stride], both or neither NULL; may be one array, else must not
  *             overlap.  Entries of weights_out from new_lens[b] on are set to 0.  weights_stride is at least max_new_len;
- *             sources from weights_stride on weigh 0.
+ *             sources from weights_stride on weigh 0, also those that no table has.
  *   lens_out  int32 [num_prompts] or NULL: gets new_lens (the decode call's suffix_lens, for one)
  * Pages behind the new length stay in the sequence's table (room for what is appended next).
  * desc: dtype, num_kv_heads, head_dim, num_prompts, page_size, kv_stride.  Pools 16-byte aligned.  Returns spd_status.

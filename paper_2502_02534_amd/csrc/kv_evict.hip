@@ -510,6 +510,17 @@ __global__ __launch_bounds__(kLong) void select_long(SelectParams p)
         source[i] = n - m + i;
 }
 
+// A sequence's places in both tables: the first ones, and how many tokens they hold.
+struct Places {
+    int in0, out0;
+    long long held, room;
+};
+__device__ __forceinline__ Places places_of(const CompactParams& p, int b)
+{
+    const int in0 = p.indptr[b], out0 = p.out_indptr[b], per = p.page_size ? 16 : 1;
+    return {in0, out0, (long long)(p.indptr[b + 1] - in0) * per, (long long)(p.out_indptr[b + 1] - out0) * per};
+}
+
 // Where token t of a sequence lies for KV head j, in 16-byte pieces; `first`: its place in the table.
 __device__ __forceinline__ long long row_at(const CompactParams& p, const int* pages, int first, int j, int t)
 {
@@ -523,33 +534,36 @@ __device__ __forceinline__ void compact_weights(const CompactParams& p, int pair
     constexpr int kEach = 4;
     const int j = pair % p.Hkv, b = pair / p.Hkv, tid = threadIdx.x;
     const int m = max(min(p.new_lens[b], p.max_new), 0);
+    // (places and sources past their tables stay as they are; a source past the row of weights weighs 0.  All read ahead of the first store)
+    const Places at = places_of(p, b);
     if (j == 0 && tid == 0 && p.lens_out)
         p.lens_out[b] = m;
     if (!p.weights)
         return;
     const int* const source = p.source + b * p.seq_stride + j * p.head_stride;
+    const int last = (int)min(at.room, (long long)m), stride = (int)p.weights_stride;
+    const int held = (int)min(at.held, (long long)stride);
     const float* const w = p.weights + (long long)pair * p.weights_stride;
     float* const out = p.weights_out + (long long)pair * p.weights_stride;
-    for (int i0 = 0; i0 < m; i0 += kEach * kThreads) {
+    for (int i0 = 0; i0 < last; i0 += kEach * kThreads) {
         int src[kEach];
         float x[kEach];
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
             const int i = i0 + e * kThreads + tid;
-            src[e] = i < m ? source[i] : -1;
+            src[e] = source[min(i, last - 1)];
         }
+        // (what is not asked for reads another place: no branch, and all loads at once)
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            const int i = i0 + e * kThreads + tid;
-            x[e] = src[e] >= i && src[e] < p.weights_stride ? w[src[e]] : 0.f;
-        }
+        for (int e = 0; e < kEach; ++e)
+            x[e] = w[min(max(src[e], 0), stride - 1)];
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
             const int i = i0 + e * kThreads + tid;
-            if (src[e] >= i)
-                out[i] = x[e];
+            if (i < last && src[e] >= i && (src[e] < held || src[e] >= stride))
+                out[i] = src[e] < stride ? x[e] : 0.f;
         }
     }
     __syncthreads();
@@ -583,8 +597,7 @@ template <int KINDS> __global__ __launch_bounds__(kThreads) void compact_rows(Co
     if (first >= last)
         return;
     const int* const source = p.source + b * p.seq_stride + j * p.head_stride;
-    const int in0 = p.indptr[b], out0 = p.out_indptr[b], per = p.page_size ? 16 : 1;
-    const long long held = (long long)(p.indptr[b + 1] - in0) * per, room = (long long)(p.out_indptr[b + 1] - out0) * per;
+    const auto [in0, out0, held, room] = places_of(p, b);
     const u32x4* const k = (const u32x4*)(kind == 1 ? p.v : p.k);
     u32x4* const k_out = (u32x4*)(kind == 1 ? p.v_out : p.k_out);
     const u32x4* const v = (const u32x4*)p.v;
