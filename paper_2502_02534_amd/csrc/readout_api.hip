@@ -224,7 +224,8 @@ int compact_kv(const spd_prompt_desc* desc, const int32_t* source, int64_t sourc
         if (misaligned(x, 4))
             return SPD_EINVAL;
     // In place all of it, or none: what would be half of either cannot be what the caller wants.
-    const bool same_k = k == k_out, same_v = v == v_out, same_table = kv_indptr == out_indptr && kv_page_indices == out_page_indices;
+    const bool same_k = k == k_out, same_v = v == v_out;
+    const bool same_table = kv_indptr == out_indptr && (desc->page_size == 0 || kv_page_indices == out_page_indices);
     if (k_out == v_out || (same_table && same_k != same_v))
         return SPD_EINVAL;
     spd::CompactParams p;
