@@ -572,6 +572,7 @@ SPD_API int penalize_logits(const void *logits, int32_t logits_dtype, int64_t ro
  */
 
 #define SPD_MAX_TOP_TOKENS 64
+#define SPD_MAX_COMPACT_ROWS 65536
 
 /* Bytes of workspace token_logprobs needs (0 on invalid sizes). */
 SPD_API size_t token_logprobs_workspace_size(int64_t rows, int64_t vocab, int32_t num_top);
@@ -620,7 +621,8 @@ SPD_API size_t accumulate_kv_weights_workspace_size(const spd_prompt_desc *desc,
  *   weights_out  as weights, and may be weights itself, else must not overlap it.  Entries from kv_lens[b] on are neither
  *                read nor written: where tokens are appended later, they have to hold 0 (compact_kv leaves them so).
  *   weights_stride  at least max_kv_len
- * Sums are fp32, in an order that depends on the bounds and lengths alone.  Returns spd_status.
+ * Sums are fp32, in an order that depends on the bounds and lengths alone.  max_kv_len up to 2^30, total_queries * Hq below 2^31, max_query_len *
+ * Hq / Hkv up to 2^30, num_prompts * Hkv * (ceil(max_kv_len / 64) + 1) up to 2^22, weights_stride up to 2^31.  Returns spd_status.
  */
 SPD_API int accumulate_kv_weights(const spd_prompt_desc *desc, const void *q, const void *k,
                                   const int32_t *query_indptr, const int32_t *kv_lens,
@@ -667,7 +669,8 @@ SPD_API int select_kv_tokens(const float *weights, int64_t weights_stride, int64
  *             sources from weights_stride on weigh 0, also those that no table has.
  *   lens_out  int32 [num_prompts] or NULL: gets new_lens (the decode call's suffix_lens, for one)
  * Pages behind the new length stay in the sequence's table (room for what is appended next).
- * desc: dtype, num_kv_heads, head_dim, num_prompts, page_size, kv_stride.  Pools 16-byte aligned.  Returns spd_status.
+ * desc: dtype, num_kv_heads, head_dim, num_prompts, page_size, kv_stride.  Pools 16-byte aligned.  num_prompts * Hkv up to
+ * SPD_MAX_COMPACT_ROWS, max_new_len and weights_stride up to 2^30.  Returns spd_status.
  */
 SPD_API int compact_kv(const spd_prompt_desc *desc, const int32_t *source, int64_t source_seq_stride,
                        int64_t source_head_stride, const int32_t *new_lens, int64_t max_new_len,

@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libspdecode.so")
 
 SPD_OK = 0
 SPD_F32, SPD_BF16 = 0, 1
+SPD_MAX_COMPACT_ROWS = 65536
 STAGE_PREFIX, STAGE_SUFFIX, STAGE_MERGE = 1, 2, 4
 
 _lib = None

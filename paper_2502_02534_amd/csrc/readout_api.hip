@@ -213,7 +213,7 @@ int compact_kv(const spd_prompt_desc* desc, const int32_t* source, int64_t sourc
     if ((source_head_stride != 0 && source_head_stride < max_new_len) || (source_seq_stride != 0 && source_seq_stride < max_new_len))
         return SPD_EINVAL;
     if (max_new_len > (1ll << 30) || weights_stride > (1ll << 30) ||
-        (int64_t)desc->num_prompts * desc->num_kv_heads > kMostBlocks / 64)
+        (int64_t)desc->num_prompts * desc->num_kv_heads > SPD_MAX_COMPACT_ROWS)
         return SPD_EUNSUPPORTED;
     const void* pools[] = {k, v, k_out, v_out};
     for (const void* x : pools)

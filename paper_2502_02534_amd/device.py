@@ -289,12 +289,14 @@ class DeviceLogprobs:
                  "temperature is float32, one for every row")
         _require(0 <= num_top <= min(vocab, 64), "num_top is 0 to 64, and no more than the vocabulary")
         _require(_on_one_gpu(logits, tokens, temperature), "everything has to be on one GPU")
+        size = B.token_logprobs_workspace_size(rows, vocab, num_top)
+        _require(rows == 0 or size > 0, "these are more than token_logprobs takes, or rows of no logits")
         self.logits, self.tokens, self.temperature, self.num_top = logits, tokens, temperature, num_top
         empty = lambda *n, t=torch.float32: torch.empty(n, dtype=t, device=logits.device)  # noqa: E731
         self.logprobs, self.entropy, self.lse = empty(rows), empty(rows), empty(rows)
         self.ranks = empty(rows, t=torch.int32)
         self.top_tokens, self.top_logprobs = empty(rows, num_top, t=torch.int32), empty(rows, num_top)
-        self.workspace = empty(max(B.token_logprobs_workspace_size(rows, vocab, num_top), 256), t=torch.uint8)
+        self.workspace = empty(max(size, 256), t=torch.uint8)
 
     def run(self, stream=None) -> None:
         rows, vocab = self.logits.shape
@@ -323,6 +325,8 @@ class DeviceEviction:
         self.attn, self.budget, self.sinks, self.recent, self.decay = attn, budget, sinks, recent, decay
         self.desc = B.make_prompt_desc(dtype=attn.desc.dtype, num_q_heads=hq, num_kv_heads=hkv, head_dim=d, num_prompts=n,
                                        page_size=attn.desc.page_size, causal=False, sm_scale=attn.desc.sm_scale)
+        sizes = (B.accumulate_kv_weights_workspace_size(self.desc, n, 1, room), B.select_kv_tokens_workspace_size(n, hkv, room))
+        _require(min(sizes) > 0 and n * hkv <= B.SPD_MAX_COMPACT_ROWS, "these are more than accumulate_kv_weights, select_kv_tokens or compact_kv takes")
         self.one_each = torch.arange(n + 1, dtype=torch.int32, device=dev)
         if attn.desc.page_size:
             self.starts = attn.suffix_page_indptr
@@ -332,8 +336,7 @@ class DeviceEviction:
         self.weights = torch.zeros((n, hkv, room), dtype=torch.float32, device=dev)
         self.source = torch.empty((n, hkv, budget), dtype=torch.int32, device=dev)
         self.new_lens = torch.empty(n, dtype=torch.int32, device=dev)
-        size = max(B.accumulate_kv_weights_workspace_size(self.desc, n, 1, room), B.select_kv_tokens_workspace_size(n, hkv, room), 256)
-        self.workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+        self.workspace = torch.empty(max(sizes), dtype=torch.uint8, device=dev)
 
     def reset(self) -> None:
         self.weights.zero_()
