@@ -574,7 +574,7 @@ SPD_API int penalize_logits(const void *logits, int32_t logits_dtype, int64_t ro
 #define SPD_MAX_TOP_TOKENS 64
 #define SPD_MAX_COMPACT_ROWS 65536
 
-/* Bytes of workspace token_logprobs needs (0 on invalid sizes). */
+/* Bytes of workspace token_logprobs needs for so many rows, logits and alternatives or fewer (0 on invalid sizes). */
 SPD_API size_t token_logprobs_workspace_size(int64_t rows, int64_t vocab, int32_t num_top);
 
 /*
@@ -598,7 +598,7 @@ SPD_API int token_logprobs(const void *logits, int32_t logits_dtype, int64_t row
                            int32_t *top_tokens, float *top_logprobs,
                            void *workspace, size_t workspace_bytes, void *stream);
 
-/* Bytes of workspace accumulate_kv_weights needs for these bounds (0 on an invalid desc). */
+/* Bytes of workspace accumulate_kv_weights needs for these bounds or smaller ones, and as many prompts or fewer (0 on an invalid desc). */
 SPD_API size_t accumulate_kv_weights_workspace_size(const spd_prompt_desc *desc, int64_t total_queries,
                                                     int64_t max_query_len, int64_t max_kv_len);
 

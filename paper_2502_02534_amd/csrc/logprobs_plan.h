@@ -45,5 +45,13 @@ inline size_t logprobs_workspace(int64_t rows, int64_t vocab, int top)
     return pl.slices > 1 ? (size_t)rows * pl.slices * (sizeof(LogprobsPart) + (size_t)top * 8) : 0;
 }
 
+// What no call of at most so many rows, logits and alternatives passes: few rows are cut into up to 256 slices in all, others as far as a slice holds.
+inline size_t logprobs_workspace_of_any(int64_t rows, int64_t vocab, int top)
+{
+    const int64_t few = (rows < 128 ? rows : 128) * (vocab / 16384), fit = (vocab + kMostSlice - 1) / kMostSlice;
+    const int64_t cut = vocab / 16384 > 1 ? (few < 256 ? few : 256) : 0, long_rows = fit > 1 ? rows * fit : 0;
+    return (size_t)(cut > long_rows ? cut : long_rows) * (sizeof(LogprobsPart) + (size_t)top * 8);
+}
+
 }  // namespace plan
 }  // namespace spd

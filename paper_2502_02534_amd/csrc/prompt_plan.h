@@ -105,8 +105,9 @@ inline int weights_tile_tokens(bool bf16) { return bf16 ? 256 : 128; }  // of a 
 inline int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
 
 struct WeightsPlan {
-    int splits;         // parts of a sequence's rows
-    size_t part_bytes;  // their sums
+    int splits;              // parts of a sequence's rows
+    size_t part_bytes;       // their sums
+    size_t most_part_bytes;  // those of any call with no larger bounds and no more sequences or queries
 };
 
 inline int make_weights_plan(const spd_prompt_desc* d, int64_t total, int64_t max_query, int64_t max_kv, WeightsPlan* out)
@@ -116,18 +117,22 @@ inline int make_weights_plan(const spd_prompt_desc* d, int64_t total, int64_t ma
         return rc;
     if (total < 0 || max_query < 0 || max_kv < 0)
         return SPD_EINVAL;
-    const int64_t most = 0x7fffffff, group = d->num_q_heads / d->num_kv_heads;
+    const int64_t numbers = 0x7fffffff, group = d->num_q_heads / d->num_kv_heads;
     // row, token and workgroup numbers are 32-bit
-    if (total > most / d->num_q_heads || max_query > (1ll << 30) / group || max_kv > (1ll << 30))
+    if (total > numbers / d->num_q_heads || max_query > (1ll << 30) / group || max_kv > (1ll << 30))
         return SPD_EUNSUPPORTED;
     const int64_t pairs = (int64_t)d->num_prompts * d->num_kv_heads;
     if (pairs > (1ll << 22) / ((max_kv + 63) / 64 + 1))
         return SPD_EUNSUPPORTED;
     out->splits = 1;
-    out->part_bytes = 0;
+    out->part_bytes = out->most_part_bytes = 0;
     const int64_t rows = max_query * group, tokens = weights_tile_tokens(d->dtype == SPD_BF16);
     if (rows <= kWeightsFewRows)
         return SPD_OK;
+    // (fewer queries or tokens may be cut into more parts, but parts times tiles stay below 4096 in bf16 and 8192 in fp32: 2^20 sums either way)
+    const int64_t most = least(rows / (d->dtype == SPD_BF16 ? 128 : 32), kWeightsMaxSplits);
+    if (most > 1)
+        out->most_part_bytes = (size_t)least(most * pairs * max_kv, 1ll << 20) * sizeof(float);
     // The rows are cut into parts, which another launch adds (3 us and more), where the tiles that there are (total_queries says how many
     // of the longest sequence's each has) leave CUs idle, and where parts of 1024 rows and more even out what causal tiles have to do.  A block of
     // 32 rows takes 0.5 us: parts of at least 4 of them where three quarters of the places are idle, else 20 (512 queries over 4096 more

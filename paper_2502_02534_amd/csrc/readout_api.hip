@@ -39,7 +39,7 @@ extern "C" {
 
 size_t token_logprobs_workspace_size(int64_t rows, int64_t vocab, int32_t num_top)
 {
-    return check_logprobs(rows, vocab, num_top) == SPD_OK ? logprobs_workspace(rows, vocab, num_top) + 256 : 0;
+    return check_logprobs(rows, vocab, num_top) == SPD_OK ? logprobs_workspace_of_any(rows, vocab, num_top) + 256 : 0;
 }
 
 int token_logprobs(const void* logits, int32_t logits_dtype, int64_t rows, int64_t vocab, int64_t row_stride,
@@ -91,7 +91,7 @@ size_t accumulate_kv_weights_workspace_size(const spd_prompt_desc* desc, int64_t
     WeightsPlan pl;
     if (make_weights_plan(desc, total_queries, max_query_len, max_kv_len, &pl) != SPD_OK)
         return 0;
-    return pl.part_bytes + 256;
+    return pl.most_part_bytes + 256;
 }
 
 int accumulate_kv_weights(const spd_prompt_desc* desc, const void* q, const void* k, const int32_t* query_indptr,
