@@ -608,13 +608,11 @@ template <bool BF16, int THREADS, int STRIPES> void run(const LogprobsParams& p,
 template <bool BF16> hipError_t run_all(const LogprobsParams& p, hipStream_t s)
 {
     const plan::LogprobsPlan pl = plan::make_logprobs_plan(p.rows, p.vocab);
-    // (a slice that starts within 16 bytes has a chunk more)
-    const int chunks = (pl.slice + 2 * kChunk - 2) / kChunk;
     if (pl.threads == 256)
-        chunks <= 256 * 4 ? run<BF16, 256, 4>(p, pl.slice, pl.slices, s) : run<BF16, 256, 8>(p, pl.slice, pl.slices, s);
-    else if (chunks <= 512 * 8)
+        pl.stripes == 4 ? run<BF16, 256, 4>(p, pl.slice, pl.slices, s) : run<BF16, 256, 8>(p, pl.slice, pl.slices, s);
+    else if (pl.stripes == 8)
         run<BF16, 512, 8>(p, pl.slice, pl.slices, s);
-    else if (chunks <= 512 * 16)
+    else if (pl.stripes == 16)
         run<BF16, 512, 16>(p, pl.slice, pl.slices, s);
     else
         run<BF16, 512, 32>(p, pl.slice, pl.slices, s);

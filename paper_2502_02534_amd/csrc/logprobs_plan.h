@@ -20,7 +20,7 @@ namespace plan {
 constexpr int kChunk = 8;  // logits whose maximum is kept
 
 struct LogprobsPlan {
-    int threads, slice, slices;  // of a workgroup, logits of a slice, slices of a row
+    int threads, stripes, slice, slices;  // of a workgroup, chunks of its threads at most, logits of a slice, slices of a row
 };
 
 constexpr int kMostSlice = 131072 - kChunk;  // (32 chunks for each of 512 threads, one of them for a start within 16 bytes)
@@ -36,6 +36,8 @@ inline LogprobsPlan make_logprobs_plan(int64_t rows, int64_t vocab)
     pl.slice = (int)((vocab + pl.slices - 1) / pl.slices);
     pl.slice = (pl.slice + kChunk - 1) / kChunk * kChunk;  // (the bound is a multiple of a chunk)
     pl.threads = pl.slice <= 8192 ? 256 : 512;
+    const int chunks = (pl.slice + 2 * kChunk - 2) / kChunk;  // (a slice that starts within 16 bytes has one more)
+    pl.stripes = pl.threads == 256 ? (chunks <= 256 * 4 ? 4 : 8) : chunks <= 512 * 8 ? 8 : chunks <= 512 * 16 ? 16 : 32;
     return pl;
 }
 
