@@ -1,7 +1,8 @@
 // How much of the queries' attention every cached token got:
 //   w'[b, j, t] = decay w[b, j, t] + sum over the query rows (i, h) that see t of 2^(scale_log2 q . k_t - lse_log2) f
 // f, next to 1, takes back what lse_log2 = lse log2(e) loses by its rounding to 24 bits: one error for all of a row's tokens, 5e-7 of them at an lse
-// of 10.  The sums multiply by it as they add.
+// of 10.  The sums multiply by it as they add.  The scale's own rounding, up to 6e-8 of a score, is taken back where few rows wait for memory; beside
+// many rows' products the instruction for it would cost 7 to 12 %.
 //
 // Rows are the (query, head of the group) pairs of a KV head.  The products are taken transposed, S^T = K Q^T: a lane of the
 // accumulator has one row's scores of several tokens, so the row's log-sum-exp is one number a lane, and a token's sum over
@@ -218,7 +219,7 @@ __global__ __launch_bounds__(few_waves(PAGED) * 64) void kv_weights_few(KvWeight
                     c = product16<BF16>(k[u][s], q[nb][s], c);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(c[i], p.scale_log2, shift[nb].below));
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(c[i], p.scale_rest, __builtin_fmaf(c[i], p.scale_log2, shift[nb].below)));
                     sum[i] = __builtin_fmaf(tb + 16 * u + 4 * g + i <= limit[nb] ? x : 0.f, shift[nb].by, sum[i]);  // (a row that is not there sees nothing)
                 }
             }

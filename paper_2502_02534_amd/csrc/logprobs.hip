@@ -3,10 +3,11 @@
 // With c = log2(e) / T, a reference r near the row's largest x c, and y_i = x_i c - r (one fma, so that r's own rounding shifts all y_i
 // alike), Z = sum 2^y_i, S = sum 2^y_i y_i:
 //   log p_i = ln2 (y_i - log2 Z),   entropy = ln2 (log2 Z - S / Z),   lse = max / T + ln2 (log2 Z - y of the maximum)
-// Every thread has a reference of its own, its largest logit so far (one that lags behind by up to 2^24 made S of numbers up to 24 times as large,
-// and the entropy of a peaked row off by 2e-6; the times are equal); the threads' sums are brought to the row's maximum at the end.  The shift is half a unit in the last place of r: harmless below 2^20 (1/16), beyond what 2^y holds from 2^32
-// on.  So no reference starts or goes below -2^20 (what lies far below it adds nothing to a row whose maximum does not), and a row, or
-// slice, whose maximum is 2^20 from zero or more is summed again from y_i = (x_i - max) c.
+// Every thread has a reference of its own, its largest logit so far (one that lags behind by up to 2^24 made S of numbers up to 24 times as
+// large, and the entropy of a peaked row off by 2e-6; the times are equal); the threads' sums are brought to the row's maximum at the end.
+// The shift is half a unit in the last place of r: harmless below 2^20 (1/16), more than 2^y holds from 2^32 on.  So no reference starts or
+// goes below -2^20 (what lies far below it adds nothing to a row whose maximum does not), and a row, or slice, whose maximum is 2^20 from
+// zero or more is summed again from y_i = (x_i - max) c.
 //
 // One pass over the row: a thread takes 8 logits at a time (a "chunk"), leaves the chunk's maximum in LDS, and adds its terms.
 // The most probable tokens then come from few chunks: of the threads' maxima the num_top-th largest is a value that at least

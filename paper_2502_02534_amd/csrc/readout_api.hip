@@ -127,8 +127,9 @@ int accumulate_kv_weights(const spd_prompt_desc* desc, const void* q, const void
     p.B = desc->num_prompts;
     p.page_size = desc->page_size;
     p.causal = desc->causal != 0;
-    const float scale = desc->sm_scale > 0.f ? desc->sm_scale : 1.f / sqrtf((float)p.D);
-    p.scale_log2 = scale * spd::kLog2e;
+    const double scale = (desc->sm_scale > 0.f ? (double)desc->sm_scale : 1.0 / sqrt((double)p.D)) * 1.4426950408889634;
+    p.scale_log2 = (float)scale;
+    p.scale_rest = (float)(scale - (double)p.scale_log2);
     p.q = q;
     p.k = k;
     p.q_stride = desc->q_stride != 0 ? desc->q_stride : (long long)p.Hq * p.D;

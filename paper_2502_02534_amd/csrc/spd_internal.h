@@ -230,7 +230,7 @@ struct LogprobsParams {
 // Attention weights of cached tokens (see kv_weights.hip).
 struct KvWeightsParams {
     int dtype, Hq, Hkv, D, G, B, page_size, causal;
-    float scale_log2;  // sm_scale * log2(e)
+    float scale_log2, scale_rest;  // sm_scale * log2(e), and what that lost by its rounding
     const void* q;
     const void* k;
     long long q_stride, kv_stride;  // elements between tokens
