@@ -631,7 +631,7 @@ SPD_API int accumulate_kv_weights(const spd_prompt_desc *desc, const void *q, co
                                   float decay, const float *weights, float *weights_out, int64_t weights_stride,
                                   void *workspace, size_t workspace_bytes, void *stream);
 
-/* Bytes of workspace select_kv_tokens needs (0 on invalid sizes). */
+/* Bytes of workspace select_kv_tokens needs (0 on invalid sizes).  Its kernels use none so far, and NULL is taken. */
 SPD_API size_t select_kv_tokens_workspace_size(int64_t num_seqs, int32_t num_heads, int64_t max_kv_len);
 
 /*
