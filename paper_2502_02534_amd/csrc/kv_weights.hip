@@ -219,7 +219,9 @@ __global__ __launch_bounds__(few_waves(PAGED) * 64) void kv_weights_few(KvWeight
                     c = product16<BF16>(k[u][s], q[nb][s], c);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(c[i], p.scale_rest, __builtin_fmaf(c[i], p.scale_log2, shift[nb].below)));
+                    // (an infinite score stays what it is)
+                    const float rest = __builtin_amdgcn_fmed3f(c[i], -3.402823466e38f, 3.402823466e38f) * p.scale_rest;
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(c[i], p.scale_log2, shift[nb].below) + rest);
                     sum[i] = __builtin_fmaf(tb + 16 * u + 4 * g + i <= limit[nb] ? x : 0.f, shift[nb].by, sum[i]);  // (a row that is not there sees nothing)
                 }
             }
