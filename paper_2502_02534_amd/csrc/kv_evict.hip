@@ -533,9 +533,10 @@ __device__ __forceinline__ void compact_weights(const CompactParams& p, int pair
 {
     constexpr int kEach = 4;
     const int j = pair % p.Hkv, b = pair / p.Hkv, tid = threadIdx.x;
-    const int m = max(min(p.new_lens[b], p.max_new), 0);
-    // (places and sources past their tables stay as they are; a source past the row of weights weighs 0.  All read ahead of the first store)
+    // (places and sources past their tables stay as they are; a source past the row of weights weighs 0.  All read at once, ahead of the first store)
+    const int new_len = p.new_lens[b];
     const Places at = places_of(p, b);
+    const int m = max(min(new_len, p.max_new), 0);
     if (j == 0 && tid == 0 && p.lens_out)
         p.lens_out[b] = m;
     if (!p.weights)

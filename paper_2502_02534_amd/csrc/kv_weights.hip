@@ -119,8 +119,9 @@ template <bool BF16> __device__ __forceinline__ floatx4 product16(const uint4& k
     }
 }
 
-// P: 16-byte pieces of a padded head (D = 64, 128, 256 in bf16: 8, 16, 32); SUB: 16-token halves of a tile; NB: blocks of 16 rows.
-template <bool BF16, int P, int SUB, int NB, bool PAGED>
+// P: 16-byte pieces of a padded head (D = 64, 128, 256 in bf16: 8, 16, 32); SUB: 16-token halves of a tile; NB: blocks of 16 rows; ONE: a stretch
+// is one tile: no second one's registers (20 sequences of up to 640 tokens, 8 heads of 256 channels 8.5 -> 7.0 us).
+template <bool BF16, int P, int SUB, int NB, bool PAGED, bool ONE>
 __global__ __launch_bounds__(few_waves(PAGED) * 64) void kv_weights_few(KvWeightsParams p, int chunk, int chunks)
 {
     constexpr int kSteps = P / 4, kTile = 16 * SUB, kLoads = kTile * P / 64, kPitch = P + 1, kFewWaves = few_waves(PAGED);  // (a piece between rows: bank conflicts)
@@ -129,7 +130,10 @@ __global__ __launch_bounds__(few_waves(PAGED) * 64) void kv_weights_few(KvWeight
     const int item = __builtin_amdgcn_readfirstlane(blockIdx.x * kFewWaves + (threadIdx.x >> 6));
     // KV head fastest: the heads of a token lie beside each other.  The later a stretch, the fewer sequences have it: each starts three sequences on, or a
     // CU would get the long ones again and again (64 paged sequences of up to 2048 tokens 29.3 us, so 26.7; 512 189.8 and 187.4)
-    const int j = item % p.Hkv, rest = item / p.Hkv, at = rest / p.B, b = (int)((rest + 3ll * at) % p.B);
+    const int j = item % p.Hkv, rest = item / p.Hkv, at = rest / p.B;
+    int b = rest - at * p.B + 3 * at;
+    if (b >= p.B)
+        b = b < 2 * p.B ? b - p.B : b % p.B;
     if (at >= chunks)
         return;
     const int L = min(p.kv_lens[b], p.max_kv), t0 = at * chunk, t1 = min(L, t0 + chunk);
@@ -165,14 +169,14 @@ __global__ __launch_bounds__(few_waves(PAGED) * 64) void kv_weights_few(KvWeight
     uint4* const mine_lds = lds[threadIdx.x >> 6];
     const int in_row = lane % P, in_tile = lane / P;  // piece and first row of a lane's loads
     const bool has_piece = in_row < head_pieces;
-    // (tiles start with a page; its number is fetched a tile ahead of its rows, into lanes: a scalar would be waited for at once)
+    // (tiles start with a page; its number is fetched a tile ahead of its rows, beside loads into lanes: a scalar would be waited for at once)
     const int last_page = (t1 - 1) >> 4;
     int next_page[SUB], any_lane = 0;
     asm("" : "+v"(any_lane));
-    const auto fetch_pages = [&](int tb) __attribute__((always_inline)) {
+    const auto fetch_pages = [&](int tb, int lane_zero) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
-            next_page[u] = PAGED ? keys.pages[min((tb >> 4) + u, last_page) + any_lane] : 0;
+            next_page[u] = PAGED ? keys.pages[min((tb >> 4) + u, last_page) + lane_zero] : 0;
     };
     const auto load = [&](int tb, uint4 (&k)[kLoads], float& old) __attribute__((always_inline)) {
         typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
@@ -180,7 +184,8 @@ __global__ __launch_bounds__(few_waves(PAGED) * 64) void kv_weights_few(KvWeight
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
             page[u] = next_page[u];
-        fetch_pages(tb + kTile);
+        if (!ONE)
+            fetch_pages(tb + kTile, any_lane);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int t = min(tb + i * (64 / P) + in_tile, t1 - 1);
@@ -242,8 +247,12 @@ __global__ __launch_bounds__(few_waves(PAGED) * 64) void kv_weights_few(KvWeight
     }
     uint4 ka[kLoads], kb[kLoads];
     float oa, ob;
-    fetch_pages(t0);
+    fetch_pages(t0, 0);
     load(t0, ka, oa);
+    if constexpr (ONE) {
+        work(t0, ka, oa);
+        return;
+    }
     // (no branch around a load in the loop: after one, all loads that may be under way would be waited for)
     int tb = t0;
     for (; tb + 2 * kTile < t1; tb += 2 * kTile) {
@@ -661,10 +670,15 @@ template <bool BF16, int P, int SUB, int NB> void few(const KvWeightsParams& p, 
     const int chunks = (p.max_kv + chunk - 1) / chunk;
     const int waves = few_waves(p.page_size != 0);
     const dim3 grid((unsigned)((pairs * chunks + waves - 1) / waves)), block(waves * 64);
-    if (p.page_size)
-        hipLaunchKernelGGL((kv_weights_few<BF16, P, SUB, NB, true>), grid, block, 0, s, p, chunk, chunks);
+    const bool one = chunk == 16 * SUB;
+    if (p.page_size && one)
+        hipLaunchKernelGGL((kv_weights_few<BF16, P, SUB, NB, true, true>), grid, block, 0, s, p, chunk, chunks);
+    else if (p.page_size)
+        hipLaunchKernelGGL((kv_weights_few<BF16, P, SUB, NB, true, false>), grid, block, 0, s, p, chunk, chunks);
+    else if (one)
+        hipLaunchKernelGGL((kv_weights_few<BF16, P, SUB, NB, false, true>), grid, block, 0, s, p, chunk, chunks);
     else
-        hipLaunchKernelGGL((kv_weights_few<BF16, P, SUB, NB, false>), grid, block, 0, s, p, chunk, chunks);
+        hipLaunchKernelGGL((kv_weights_few<BF16, P, SUB, NB, false, false>), grid, block, 0, s, p, chunk, chunks);
 }
 
 }  // namespace
